@@ -295,6 +295,116 @@ mt_status mt_get_kernel_times(const char** names, double* total_ms, int32_t* lau
 mt_status mt_bucket_noalloc(const int32_t* model_ids, int32_t n, int32_t n_models, int32_t* counts_out,
                             int32_t* offsets_out, int32_t* perm_out, int32_t* inv_out, void* stream);
 
+/* ------------------------------------------------------------------------------------------------------------------
+ * Operators of language-model tenants.  (The paper's tenants upload DNNs of standard layers, Sec. 3.1; a language model
+ * adds layers that look back at earlier tokens.)  What a worker needs to run such tenants token by token: attention over
+ * a prompt, a cache of keys and values held in 4 bits with the attention that reads it, products of a mixed batch of
+ * tokens with the tenants' 4-bit weights, and the probability of the tokens that come out.
+ *
+ * They need mt_init (else MT_ERR_NOT_INIT) but no registered model: every array is the caller's.  Unless marked "host",
+ * pointers are device memory of the context's device.  Each call only enqueues kernels on `stream` and returns; arrays
+ * must stay valid, and unchanged where they are inputs, until the stream has passed the call.  mt_kv_attention and
+ * mt_token_logprobs use scratch that the library keeps PER STREAM, so calls on different streams may overlap; the
+ * first call on a stream, and one that needs more than any before, allocates it (that call may synchronise; make it
+ * before a stream capture).  At most 64 streams may use them (then MT_ERR_OOM).  Scratch goes away with mt_shutdown.
+ * All of them may be captured into CUDA graphs; replays of graphs that were captured on ONE stream must not overlap.
+ *
+ * Refusals: MT_ERR_INVALID_ARG null pointer, negative size, unknown type, misaligned pointer; MT_ERR_UNSUPPORTED a
+ * size or stride outside what the kernels take; nothing is enqueued then.  A count of zero is a no-op.  What only the
+ * device can see (an id, page, slot, length or offset out of range) never faults: the rows concerned are NaN (or left
+ * out, where rows are written to a cache), and the sticky status of mt_get_async_status is MT_ERR_BAD_MODEL_ID (ids) or
+ * MT_ERR_INVALID_ARG, with the smallest index concerned. */
+typedef enum { MT_BF16 = 0, MT_FP32 = 1 } mt_dtype;
+
+/* Attention over whole prompts, causal, packed one behind the other: sequence s is rows offsets[s] .. offsets[s+1]-1.
+ *   o[i][h] = sum over j <= i of the same sequence of softmax_j(scale * q[i][h] . k[j][h / g]) v[j][h / g],
+ * g = q_heads / kv_heads.  q [n_tokens][q_heads][head_dim], k and v [n_tokens][kv_heads][head_dim], bf16, each with its own
+ * strides (elements) between tokens and heads and head_dim contiguous, so the three may be slices of one projection's
+ * output; out bf16, contiguous [n_tokens][q_heads][head_dim], must not overlap the inputs.  offsets: int32 [n_seqs + 1], not decreasing,
+ * between 0 and n_tokens; rows outside every sequence are not written.  A sequence that breaks this is not computed (its
+ * rows, where it has any, are left as they were; sticky status, index of the sequence).  Scores and sums are fp32; the
+ * probabilities are rounded to bf16 before they meet v.  A masked position never shows: infinities and NaN in k or v of
+ * later tokens or other sequences leave an output as it is.
+ * Limits: head_dim 64 or 128; q_heads a multiple of kv_heads; pointers 16-byte aligned; strides multiples of 8, a head
+ * stride of at least head_dim, a token stride of at least head_dim, each below 2^36. */
+typedef struct {
+    int32_t n_tokens, n_seqs, q_heads, kv_heads, head_dim;
+    float scale;
+    int64_t q_token_stride, q_head_stride, k_token_stride, k_head_stride, v_token_stride, v_head_stride;
+} mt_prompt_desc;
+mt_status mt_prompt_attention(const mt_prompt_desc* desc_host, const void* q, const void* k, const void* v,
+                              const int32_t* offsets, void* out, void* stream);
+
+/* A cache of keys and values in pages of page_tokens tokens.  A row (one token, one head) is head_dim codes of 4 bits and
+ * two bf16, scale and bias: element d is code[d] * scale + bias.
+ *   k_codes, v_codes    uint8 [n_pages][kv_heads][page_tokens][head_dim / 2], even d in the low nibble; 16-byte aligned
+ *   k_params, v_params  bf16  [n_pages][kv_heads][page_tokens][2]: scale, bias; 16-byte aligned
+ * Limits: head_dim 64 or 128; page_tokens 16, 32, 64, 128 or 256. */
+typedef struct {
+    int32_t n_pages, page_tokens, kv_heads, head_dim;
+    void *k_codes, *k_params, *v_codes, *v_params;
+} mt_kv_cache;
+
+/* Rounds the rows of n tokens to 4 bits and writes token i to slot slots[i] = page * page_tokens + place (int64).
+ * bias = the row's least element, scale = (largest - least) / 15 rounded to bf16, code = the nearest of the sixteen levels
+ * (ties to even).  A row with an infinity or NaN, or whose spread passes fp32, reads back as NaN.  k and v: bf16
+ * [n][kv_heads][head_dim] with strides (elements, multiples of 8) between tokens and heads, 16-byte aligned.  A slot of -1 leaves its
+ * token out; any other slot outside the cache does too and sets the sticky status.  Two tokens of one call must not name the
+ * same slot. */
+mt_status mt_kv_append(const mt_kv_cache* cache_host, const void* k, int64_t k_token_stride, int64_t k_head_stride,
+                       const void* v, int64_t v_token_stride, int64_t v_head_stride, const int64_t* slots, int32_t n,
+                       void* stream);
+
+/* The values of n slots, rounded to bf16: k_out and v_out [n][kv_heads][head_dim], contiguous (what a prompt that goes on from cached tokens, or a move to
+ * another cache, needs).  A slot of -1 gives zeros; any other slot outside the cache gives NaN and sets the sticky status. */
+mt_status mt_kv_read(const mt_kv_cache* cache_host, const int64_t* slots, int32_t n, void* k_out, void* v_out, void* stream);
+
+/* Attention of ONE new token per sequence over its cached tokens:
+ *   out[s][h] = sum over j < lengths[s] of softmax_j(scale * q[s][h] . K[j][h / g]) V[j][h / g],
+ * token j of sequence s in page tables[s][j / page_tokens], place j % page_tokens.  tables int32 [n_seqs][table_width], entries past a
+ * sequence's last page are not read; lengths int32 [n_seqs].  A sequence without tokens gives zeros.  A length below zero or
+ * beyond table_width pages, or a page outside the cache, gives NaN rows and the sticky status.  q bf16
+ * [n_seqs][q_heads][head_dim] with strides (elements, multiples of 8), 16-byte aligned; out bf16, contiguous.
+ * Codes meet the products as whole numbers (exact in bf16), scales and biases are applied in fp32; probabilities times the
+ * value's scale are rounded to bf16 before they meet the codes.
+ * Limits: q_heads = g * kv_heads with g at most 16; n_seqs * kv_heads below 2^20. */
+mt_status mt_kv_attention(const mt_kv_cache* cache_host, const void* q, int64_t q_seq_stride, int64_t q_head_stride,
+                          const int32_t* tables, int32_t table_width, const int32_t* lengths, int32_t n_seqs,
+                          int32_t q_heads, float scale, void* out, void* stream);
+
+/* A linear layer of several tenants with 4-bit weights: tenant t's weight is (code - 8) * scale, codes uint8
+ * [out_features][in_features / 2] (even inputs in the low nibble), one bf16 scale per `group` inputs of a row
+ * ([out_features][in_features / group]).  mt_quant_pack lays codes [tenants][..] and scales [tenants][..] out in the kernel's
+ * order, once; `packed` takes tenants * mt_quant_packed_bytes bytes, 16-byte aligned, and holds all that mt_quant_linear reads.
+ * Limits: in_features a multiple of 64 and of group; group 32, 64 or a larger multiple of 64. */
+typedef struct {
+    int32_t tenants, in_features, out_features, group;
+    const void* packed;
+    const float* bias;     /* [tenants][out_features], or NULL */
+} mt_quant_bank;
+mt_status mt_quant_packed_bytes(int32_t in_features, int32_t out_features, int32_t group, size_t* bytes_out);
+mt_status mt_quant_pack(const uint8_t* codes, const void* scales, int32_t tenants, int32_t in_features,
+                        int32_t out_features, int32_t group, void* packed, void* stream);
+
+/* y[i] = weight[ids[i]] x[i] + bias[ids[i]] for a mixed batch of n rows.  x bf16, rows x_stride elements apart (a multiple
+ * of 8), 16-byte aligned; y bf16 or fp32 by y_dtype, rows y_stride elements apart.  Products and sums are fp32, codes enter as whole numbers.  An id outside
+ * [0, tenants) gives a NaN row and the sticky status.  Any n; made for the few rows of a token step (each distinct tenant's weights are read once
+ * per 64 of its rows, at most 256 rows a launch). */
+mt_status mt_quant_linear(const mt_quant_bank* bank_host, const void* x, int64_t x_stride, const int32_t* ids, int32_t n,
+                          void* y, int64_t y_stride, int32_t y_dtype, void* stream);
+
+/* For n rows of `vocab` logits (bf16 or fp32 by dtype, row_stride elements apart, any alignment of whole elements):
+ *   logprobs[i]        log of the softmax at tokens[i]; NaN if that is outside [0, vocab)
+ *   entropies[i]       - sum p log p, in nats
+ *   top_ids[i][0..top-1], top_logprobs[i][..]   the likeliest tokens, best first, equal logits by the lower index
+ * A logit of minus infinity has probability zero: it adds nothing and is no alternative; where fewer than `top` remain, the
+ * places left over hold id -1 and minus infinity.  A row without a distribution (nothing but minus infinity, or a NaN
+ * or plus infinity in it) gives NaN, and ids -1.  Sums are fp32.  entropies may be NULL; top_ids and top_logprobs may be NULL if
+ * top is 0.  Limits: top at most 32; vocab below 2^30. */
+mt_status mt_token_logprobs(const void* logits, int32_t dtype, int64_t row_stride, int32_t n, int32_t vocab,
+                            const int32_t* tokens, int32_t top, float* logprobs, float* entropies, int32_t* top_ids,
+                            float* top_logprobs, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -24,7 +24,9 @@ EXPORTS = ["mt_init", "mt_shutdown", "mt_register_model", "mt_infer", "mt_infer_
            "mt_get_async_status", "mt_status_string", "mt_debug_last_bucketing", "mt_set_kernel_timing",
            "mt_get_kernel_times", "mt_bucket_noalloc", "mt_debug_wait_timeout", "mt_debug_launch_count", "mt_debug_set_option", "mt_debug_empty_launches", "mt_debug_item_cost",
            "mt_debug_schedule_balance", "mt_set_cache_bytes", "mt_prefetch", "mt_get_cache_stats", "mt_cache_sim_create",
-           "mt_cache_sim_access", "mt_cache_sim_release", "mt_cache_sim_stats", "mt_cache_sim_destroy", "mt_output_elems", "mt_input_elems"]
+           "mt_cache_sim_access", "mt_cache_sim_release", "mt_cache_sim_stats", "mt_cache_sim_destroy", "mt_output_elems", "mt_input_elems",
+           "mt_prompt_attention", "mt_kv_append", "mt_kv_read", "mt_kv_attention", "mt_quant_packed_bytes", "mt_quant_pack",
+           "mt_quant_linear", "mt_token_logprobs"]
 
 
 class MtError(RuntimeError):
@@ -45,6 +47,23 @@ class LayerDesc(ctypes.Structure):
     _fields_ = [("kind", ctypes.c_int32), ("in_ch", ctypes.c_int32), ("out_ch", ctypes.c_int32),
                 ("h", ctypes.c_int32), ("w", ctypes.c_int32), ("relu", ctypes.c_int32), ("residual", ctypes.c_int32),
                 ("weight", ctypes.c_void_p), ("bias", ctypes.c_void_p)]
+
+
+class PromptDesc(ctypes.Structure):
+    _fields_ = [(k, ctypes.c_int32) for k in ("n_tokens", "n_seqs", "q_heads", "kv_heads", "head_dim")] + \
+               [("scale", ctypes.c_float)] + \
+               [(k, ctypes.c_int64) for k in ("q_token_stride", "q_head_stride", "k_token_stride", "k_head_stride",
+                                              "v_token_stride", "v_head_stride")]
+
+
+class KvCacheDesc(ctypes.Structure):
+    _fields_ = [(k, ctypes.c_int32) for k in ("n_pages", "page_tokens", "kv_heads", "head_dim")] + \
+               [(k, ctypes.c_void_p) for k in ("k_codes", "k_params", "v_codes", "v_params")]
+
+
+class QuantBankDesc(ctypes.Structure):
+    _fields_ = [(k, ctypes.c_int32) for k in ("tenants", "in_features", "out_features", "group")] + \
+               [(k, ctypes.c_void_p) for k in ("packed", "bias")]
 
 
 _lib = None
@@ -90,6 +109,15 @@ def lib() -> ctypes.CDLL:
         l.mt_cache_sim_destroy.argtypes = [vp]
         l.mt_debug_item_cost.argtypes = [i32, i32, i32, ctypes.POINTER(ctypes.c_double)]
         l.mt_debug_schedule_balance.argtypes = [i32, ctypes.POINTER(ctypes.c_double), ctypes.POINTER(i32), ctypes.POINTER(i32)]
+        i64, f32 = ctypes.c_int64, ctypes.c_float
+        l.mt_prompt_attention.argtypes = [vp] * 7
+        l.mt_kv_append.argtypes = [vp, vp, i64, i64, vp, i64, i64, vp, i32, vp]
+        l.mt_kv_read.argtypes = [vp, vp, i32, vp, vp, vp]
+        l.mt_kv_attention.argtypes = [vp, vp, i64, i64, vp, i32, vp, i32, i32, f32, vp, vp]
+        l.mt_quant_packed_bytes.argtypes = [i32, i32, i32, ctypes.POINTER(ctypes.c_size_t)]
+        l.mt_quant_pack.argtypes = [vp, vp, i32, i32, i32, i32, vp, vp]
+        l.mt_quant_linear.argtypes = [vp, vp, i64, vp, i32, vp, i64, i32, vp]
+        l.mt_token_logprobs.argtypes = [vp, i32, i64, i32, i32, vp, i32, vp, vp, vp, vp, vp]
         for name in EXPORTS:
             if name != "mt_status_string":
                 getattr(l, name).restype = ctypes.c_int
@@ -309,3 +337,169 @@ def mt_bucket_noalloc(model_ids, n: int, n_models: int, counts_out, offsets_out,
     Calls that overlap on the GPU share that scratch and race."""
     _check(lib().mt_bucket_noalloc(_ptr(model_ids), int(n), int(n_models), _ptr(counts_out), _ptr(offsets_out),
                                    _ptr(perm_out), _ptr(inv_out), _stream_handle(stream)), "mt_bucket_noalloc")
+
+
+# ------------------------------------------------------------------------------------------------
+# Operators of language-model tenants.  These take torch tensors on the context's device and read sizes and strides from
+# them; a tensor of another type, shape or place is refused here (MT_ERR_INVALID_ARG), sizes are judged by the library.
+# ------------------------------------------------------------------------------------------------
+def _need(ok: bool, where: str) -> None:
+    if not ok:
+        raise MtError(1, where)
+
+
+def mt_prompt_attention(q, k, v, offsets, out, scale: Optional[float] = None, stream=None) -> None:
+    """Causal attention over packed prompts: q bf16 [n, q_heads, dim], k and v [n, kv_heads, dim] (any token and head strides),
+    offsets int32 [sequences + 1], out bf16 [n, q_heads, dim] contiguous.  scale: 1 / sqrt(dim) if None."""
+    where = "mt_prompt_attention"
+    import torch
+    bf16 = torch.bfloat16
+    n, hq, d = q.shape
+    qs, ks, vs = q.stride(), k.stride(), v.stride()
+    _need(q.dtype == bf16 and k.dtype == bf16 and v.dtype == bf16 and out.dtype == bf16 and offsets.dtype == torch.int32 and
+          q.is_cuda and k.is_cuda and v.is_cuda and out.is_cuda and offsets.is_cuda and k.shape == v.shape and
+          k.shape[0] == n and k.shape[2] == d and out.shape == q.shape and out.is_contiguous() and offsets.is_contiguous() and
+          offsets.dim() == 1 and offsets.shape[0] > 0 and (n == 0 or (qs[2] == 1 and ks[2] == 1 and vs[2] == 1)), where)
+    desc = PromptDesc(n, offsets.shape[0] - 1, hq, k.shape[1], d, d ** -0.5 if scale is None else scale, qs[0], qs[1], ks[0], ks[1],
+                      vs[0], vs[1])
+    _check(lib().mt_prompt_attention(ctypes.byref(desc), q.data_ptr(), k.data_ptr(), v.data_ptr(), offsets.data_ptr(), out.data_ptr(),
+                                     _stream_handle(stream)), where)
+
+
+class KvCache:
+    """The caller's tensors as one 4-bit cache: codes uint8 [pages, kv_heads, page_tokens, dim / 2], params bf16
+    [pages, kv_heads, page_tokens, 2] (scale, bias), contiguous.  Keeps them alive; allocates nothing."""
+
+    def __init__(self, k_codes, k_params, v_codes, v_params):
+        import torch
+        pages, heads, page, half = k_codes.shape
+        for c, p in ((k_codes, k_params), (v_codes, v_params)):
+            _need(c.dtype == torch.uint8 and p.dtype == torch.bfloat16 and c.is_cuda and p.is_cuda and c.is_contiguous() and
+                  p.is_contiguous() and tuple(c.shape) == (pages, heads, page, half) and tuple(p.shape) == (pages, heads, page, 2), "KvCache")
+        self.tensors = (k_codes, k_params, v_codes, v_params)
+        self.heads, self.dim = heads, 2 * half
+        self.desc = KvCacheDesc(pages, page, heads, 2 * half, *[x.data_ptr() for x in self.tensors])
+        self.ref = ctypes.byref(self.desc)
+
+    @classmethod
+    def empty(cls, n_pages: int, page_tokens: int, kv_heads: int, head_dim: int, device="cuda"):
+        """A new cache of zeros."""
+        import torch
+        t = []
+        for _ in range(2):
+            t.append(torch.zeros((n_pages, kv_heads, page_tokens, head_dim // 2), dtype=torch.uint8, device=device))
+            t.append(torch.zeros((n_pages, kv_heads, page_tokens, 2), dtype=torch.bfloat16, device=device))
+        return cls(*t)
+
+
+def mt_kv_append(cache: KvCache, k, v, slots, stream=None) -> None:
+    """Round k and v, bf16 [n, kv_heads, dim] (any token and head strides), to 4 bits and write token i to slot slots[i] (int64 [n])."""
+    where = "mt_kv_append"
+    import torch
+    n, (ks, vs) = k.shape[0], (k.stride(), v.stride())
+    _need(k.dtype == torch.bfloat16 and v.dtype == torch.bfloat16 and slots.dtype == torch.int64 and k.is_cuda and v.is_cuda and
+          slots.is_cuda and k.shape == v.shape and tuple(k.shape[1:]) == (cache.heads, cache.dim) and slots.shape == (n,) and
+          slots.is_contiguous() and (n == 0 or (ks[2] == 1 and vs[2] == 1)), where)
+    _check(lib().mt_kv_append(cache.ref, k.data_ptr(), ks[0], ks[1], v.data_ptr(), vs[0], vs[1], slots.data_ptr(), n,
+                              _stream_handle(stream)), where)
+
+
+def mt_kv_read(cache: KvCache, slots, k_out, v_out, stream=None) -> None:
+    """The cached values of slots (int64 [n]) as bf16 [n, kv_heads, dim]."""
+    where = "mt_kv_read"
+    import torch
+    n = slots.shape[0]
+    shape = (n, cache.heads, cache.dim)
+    _need(k_out.dtype == torch.bfloat16 and v_out.dtype == torch.bfloat16 and slots.dtype == torch.int64 and slots.dim() == 1 and
+          k_out.is_cuda and v_out.is_cuda and slots.is_cuda and k_out.shape == shape and v_out.shape == shape and
+          k_out.is_contiguous() and v_out.is_contiguous() and slots.is_contiguous(), where)
+    _check(lib().mt_kv_read(cache.ref, slots.data_ptr(), n, k_out.data_ptr(), v_out.data_ptr(), _stream_handle(stream)), where)
+
+
+def mt_kv_attention(cache: KvCache, q, tables, lengths, out, scale: Optional[float] = None, stream=None) -> None:
+    """One new token per sequence over its cached tokens: q bf16 [sequences, q_heads, dim] (any strides), tables int32
+    [sequences, width], lengths int32 [sequences], out bf16 like q, contiguous.  scale: 1 / sqrt(dim) if None."""
+    where = "mt_kv_attention"
+    import torch
+    n, hq, d = q.shape
+    qs = q.stride()
+    _need(q.dtype == torch.bfloat16 and out.dtype == torch.bfloat16 and tables.dtype == torch.int32 and lengths.dtype == torch.int32 and
+          q.is_cuda and out.is_cuda and tables.is_cuda and lengths.is_cuda and d == cache.dim and out.shape == q.shape and
+          tables.dim() == 2 and tables.shape[0] == n and lengths.shape == (n,) and out.is_contiguous() and
+          tables.is_contiguous() and lengths.is_contiguous() and (n == 0 or qs[2] == 1), where)
+    _check(lib().mt_kv_attention(cache.ref, q.data_ptr(), qs[0], qs[1], tables.data_ptr(), tables.shape[1], lengths.data_ptr(), n, hq,
+                                 d ** -0.5 if scale is None else scale, out.data_ptr(), _stream_handle(stream)), where)
+
+
+def mt_quant_packed_bytes(in_features: int, out_features: int, group: int) -> int:
+    """Bytes of one tenant's packed weights (host code only; needs no GPU)."""
+    b = ctypes.c_size_t(0)
+    _check(lib().mt_quant_packed_bytes(int(in_features), int(out_features), int(group), ctypes.byref(b)), "mt_quant_packed_bytes")
+    return int(b.value)
+
+
+def mt_quant_pack(codes, scales, packed, stream=None) -> None:
+    """codes uint8 [tenants, out, in / 2], scales bf16 [tenants, out, in / group] -> packed uint8 [tenants, mt_quant_packed_bytes]."""
+    where = "mt_quant_pack"
+    import torch
+    _need(codes.dtype == torch.uint8 and scales.dtype == torch.bfloat16 and packed.dtype == torch.uint8 and codes.is_cuda and
+          scales.is_cuda and packed.is_cuda and codes.dim() == 3 and scales.dim() == 3 and codes.shape[:2] == scales.shape[:2] and
+          codes.is_contiguous() and scales.is_contiguous() and packed.is_contiguous() and scales.shape[2] > 0 and
+          2 * codes.shape[2] % scales.shape[2] == 0, where)
+    t, n, half = codes.shape
+    group = 2 * half // scales.shape[2]
+    _need(packed.numel() >= t * mt_quant_packed_bytes(2 * half, n, group), where)
+    _check(lib().mt_quant_pack(codes.data_ptr(), scales.data_ptr(), t, 2 * half, n, group, packed.data_ptr(), _stream_handle(stream)), where)
+
+
+class QuantBank:
+    """The packed 4-bit weights of several tenants' layer, with an optional fp32 bias [tenants, out]."""
+
+    def __init__(self, codes, scales, bias=None, stream=None):
+        import torch
+        t, n, half = codes.shape
+        k = 2 * half
+        _need(scales.dim() == 3 and scales.shape[2] > 0 and k % scales.shape[2] == 0, "QuantBank")
+        group = k // scales.shape[2]
+        if bias is not None:
+            _need(bias.dtype == torch.float32 and bias.is_cuda and bias.is_contiguous() and tuple(bias.shape) == (t, n), "QuantBank")
+        self.packed = torch.empty((t, mt_quant_packed_bytes(k, n, group)), dtype=torch.uint8, device=codes.device)
+        mt_quant_pack(codes, scales, self.packed, stream)
+        self.bias, self.in_features, self.out_features = bias, k, n
+        self.desc = QuantBankDesc(t, k, n, group, self.packed.data_ptr(), _ptr(bias))
+        self.ref = ctypes.byref(self.desc)
+
+
+def mt_quant_linear(x, ids, bank: QuantBank, y, stream=None) -> None:
+    """y[i] = weight[ids[i]] x[i] + bias[ids[i]]: x bf16 [n, in] (any row stride), ids int32 [n], y bf16 or fp32 [n, out]."""
+    where = "mt_quant_linear"
+    import torch
+    n, k = x.shape
+    yt = y.dtype
+    _need(x.dtype == torch.bfloat16 and ids.dtype == torch.int32 and (yt == torch.bfloat16 or yt == torch.float32) and x.is_cuda and
+          ids.is_cuda and y.is_cuda and k == bank.in_features and tuple(y.shape) == (n, bank.out_features) and ids.shape == (n,) and
+          ids.is_contiguous() and (n == 0 or (x.stride(1) == 1 and (y.stride(1) == 1 or bank.out_features == 1))), where)
+    _check(lib().mt_quant_linear(bank.ref, x.data_ptr(), x.stride(0), ids.data_ptr(), n, y.data_ptr(), y.stride(0),
+                                 1 if yt == torch.float32 else 0, _stream_handle(stream)), where)
+
+
+def mt_token_logprobs(logits, tokens, logprobs, entropies=None, top_ids=None, top_logprobs=None, stream=None) -> None:
+    """logits bf16 or fp32 [n, vocab] (any row stride), tokens int32 [n] -> logprobs fp32 [n], entropies fp32 [n] (or None),
+    top_ids int32 [n, top] and top_logprobs fp32 [n, top] (or None)."""
+    where = "mt_token_logprobs"
+    import torch
+    n, vocab = logits.shape
+    f32, top = torch.float32, 0
+    ok = (logits.dtype == torch.bfloat16 or logits.dtype == f32) and tokens.dtype == torch.int32 and logprobs.dtype == f32 and \
+        logits.is_cuda and tokens.is_cuda and logprobs.is_cuda and tokens.shape == (n,) and logprobs.shape == (n,) and \
+        tokens.is_contiguous() and logprobs.is_contiguous() and (n == 0 or vocab <= 1 or logits.stride(1) == 1)
+    if entropies is not None:
+        ok = ok and entropies.dtype == f32 and entropies.is_cuda and entropies.shape == (n,) and entropies.is_contiguous()
+    if top_ids is not None or top_logprobs is not None:
+        ok = ok and top_ids is not None and top_logprobs is not None and top_ids.dtype == torch.int32 and top_logprobs.dtype == f32 and \
+            top_ids.is_cuda and top_logprobs.is_cuda and top_ids.dim() == 2 and top_ids.shape[0] == n and \
+            top_ids.shape == top_logprobs.shape and top_ids.is_contiguous() and top_logprobs.is_contiguous()
+        top = top_ids.shape[1] if ok else 0
+    _need(ok, where)
+    _check(lib().mt_token_logprobs(logits.data_ptr(), 1 if logits.dtype == f32 else 0, logits.stride(0), n, vocab, tokens.data_ptr(), top,
+                                   logprobs.data_ptr(), _ptr(entropies), _ptr(top_ids), _ptr(top_logprobs), _stream_handle(stream)), where)

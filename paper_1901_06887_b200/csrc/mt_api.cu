@@ -24,10 +24,6 @@ namespace {
 
 using namespace mt;
 
-typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
-                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
-                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
 // kind is the EXECUTOR's kind: a pointwise conv (MT_CONV1X1 at the interface) is a dense layer over the pixels of the
 // request's image, i.e. MT_DENSE with hw = H * W matrix rows per request (hw = 1 for a fully-connected layer).
 struct HostLayer {
@@ -267,6 +263,7 @@ mt_status do_init(int device, int max_models, int /*max_batch*/) {
     CU_OK(configure_grouped_gemm_pair());
     CU_OK(configure_fused_mlp());
     CU_OK(configure_grouped_conv_pair());
+    CU_OK(configure_operators());
     g.T = 0;
     g.live = 0;
     for (int l = 0; l < MT_MAX_LAYERS; ++l) g.n_residual[l] = 0;
@@ -1186,6 +1183,18 @@ mt_status register_async(const mt_layer_desc* layers, const std::vector<HostLaye
 
 }  // namespace
 
+namespace mt {
+mt_status op_begin(std::unique_lock<std::mutex>* lk, OpContext* out) {
+    *lk = std::unique_lock<std::mutex>(g_mu);
+    if (!g.init) return MT_ERR_NOT_INIT;
+    CU_OK(cudaSetDevice(g.device));
+    out->sm_count = g.sm_count;
+    out->status = g.d_status;
+    out->encode = g.encode;
+    return MT_OK;
+}
+}  // namespace mt
+
 extern "C" {
 
 mt_status mt_init(int32_t device, int32_t max_models, int32_t max_batch) {
@@ -1198,6 +1207,7 @@ mt_status mt_shutdown(void) {
     if (!g.init) return MT_OK;
     cudaSetDevice(g.device);
     cudaDeviceSynchronize();
+    op_free_scratch();
     for (HostModel& m : g.models) {
         if (m.dev_block) { cudaFree(m.dev_block); m.dev_block = nullptr; }
         if (m.host_image) { cudaFreeHost(m.host_image); m.host_image = nullptr; }

@@ -5,6 +5,10 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <mutex>
+
+#include "../../include/mt.h"
+
 namespace mt {
 
 // Launch with programmatic stream serialization: the kernel may start while its predecessor in the stream is
@@ -24,6 +28,23 @@ inline cudaError_t launch_pdl(void (*kernel)(KArgs...), dim3 grid, dim3 block, s
 
 struct ModelDev;
 struct WorkItem;
+
+typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
+                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
+                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+// What the operators of language-model tenants (lm_api.cu) take from the context.  op_begin locks the library's mutex into
+// *lk, makes the context's device current and fills *out, or says MT_ERR_NOT_INIT.
+struct OpContext {
+    int sm_count;
+    int32_t* status;
+    EncodeTiledFn encode;
+};
+mt_status op_begin(std::unique_lock<std::mutex>* lk, OpContext* out);
+// Frees the operators' per-stream scratch (mt_shutdown, device idle, mutex held).
+void op_free_scratch();
+// Sets the kernels' function attributes (mt_init).
+cudaError_t configure_operators();
 
 // Dealing of a layer's work items to the CTAs (or CTA pairs) of a persistent launch: rounds of `grid` consecutive
 // items, forwards in even rounds and backwards in odd ones.  The list is laid out heaviest items first, so a plain
