@@ -2,15 +2,20 @@
 //
 // Mathematics.  For one sequence and one key/value head, with the g query heads that share it as columns:
 //   S = K q (tokens x heads), p = exp(S - m), o = sum p v / sum p, one pass with a running maximum m per head.
-// K and V rows are code * scale + bias.  The codes enter the matrix instructions as the exact bf16 numbers 16 + code (four bits
-// put in the top of a mantissa: one shift and one and-or per two codes, no conversion), and everything else is applied in
-// fp32 outside:
-//   S    = scale_k (sum_d (16 + code) q_d) + (bias_k - 16 scale_k) sum_d q_d
-//   o    = sum P (16 + code) - 24 sum P + sum p (8 scale_v + bias_v),   P = bf16(p scale_v)
-// P is the only rounding on the way; subtracting 24 times the ROUNDED P leaves its error relative to the centred codes
-// (code - 8), not to 16 + code.
+// K and V rows are code * scale + bias.  The codes go into integer matrix instructions (u8 times s8, exact 32-bit sums) as they stand:
+// four codes cost one mask, or a shift and a mask, where a floating type takes two instructions for every two codes.  The other
+// operand is rounded to whole numbers and cut into two signed bytes:
+//   q' = 256 q1 + q2, relative to the head's largest element (error at most 2^-16 of that; bf16's own is 2^-9 of each element);
+//   P  = 64 P1 + P2, P = p scale_v relative to the tile's largest scale_v and the tile's largest p: 13 bits, error at most 2^-13 of it (with 11
+//        bits the result's error over long contexts doubled: the tile's largest p stands far above the rest).
+// Scales and biases are applied in fp32 outside:
+//   S = scale_k (sum_d code q_d) + bias_k sum_d q_d
+//   o = sum P (code - 8) + sum p (8 scale_v + bias_v)
+// The -8 is one more product (a constant row): over a long context o is a small mean of many values, and what is taken off must be
+// made of the same rounded P.  A tile of 32 tokens has a maximum and a scale of its own and is added to the running o in
+// fp32; its integer sums start at 1.5 * 2^23 as a bit pattern, so they need no conversion to be read as floats.
 //
-// Bound: memory.  head_dim + 8 bytes per cached token and head; the arithmetic is some 200 warp instructions per 16 tokens.
+// Bound: memory.  head_dim + 8 bytes per cached token and head; some 500 warp instructions per 32 tokens.
 //
 // Split.  A unit is 128 tokens of one (sequence, head); the units of the whole batch, in order, are cut into equal
 // contiguous shares, one per CTA, so ragged batches balance without a schedule from the host: every CTA adds up the lengths itself and
@@ -20,8 +25,15 @@
 //
 // Operand layout.  The inner index of a product may be permuted freely as long as both sides agree, so a lane loads 16
 // (head_dim 128) contiguous bytes of a key row and calls them its slice of every k step; queries are permuted once to match.  For the
-// values the pairs of a register have to be two tokens of one channel: two byte permutes interleave the words of neighbouring tokens.
-// Nothing passes through shared memory on the way in.
+// values the four bytes of a register have to be four tokens of one channel: byte permutes turn four tokens' words over.
+//
+// Feed.  Every warp copies its own tiles into a ring of three in shared memory (cp.async, 4.25 KB a tile), two tiles ahead of the one it
+// computes: 16 warps then have up to 139 KB of an SM in flight.  Loading straight into registers one tile ahead left the kernel
+// waiting on memory (163 us in the case below, and registers spilled).
+//
+// Measured on the way (4 sequences, 448 thousand tokens in all, 8 heads): codes as bf16 (16 + code by shift, and-or) 169 us, bound by the
+// logic pipe, which takes two cycles a warp instruction; shifts moved to the multiplier 186 us; codes as e4m3 (c * 2^-9 for every nibble) 216 us: that form of the
+// instruction is carried out through conversions, 6 cycles per SM against 2 for the integer one.
 #include "lm_device.cuh"
 #include "lm_host.h"
 
@@ -30,12 +42,13 @@ namespace {
 
 constexpr int kWarps = 4, kTile = 32, kUnit = kWarps * kTile;
 
-__device__ __forceinline__ void mma_bf16(float (&c)[4], const uint32_t a0, const uint32_t a1, const uint32_t a2, const uint32_t a3,
-                                         const uint32_t b0, const uint32_t b1) {
+// D = A B + C, 16 x 8 x 32, unsigned times signed bytes.
+__device__ __forceinline__ void mma_u8s8(int (&d)[4], const uint32_t a0, const uint32_t a1, const uint32_t a2, const uint32_t a3,
+                                         const uint32_t (&b)[2], const int (&c)[4]) {
     asm volatile(
-        "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+        "mma.sync.aligned.m16n8k32.row.col.s32.u8.s8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%11,%12,%13};"
+        : "=r"(d[0]), "=r"(d[1]), "=r"(d[2]), "=r"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b[0]), "r"(b[1]), "r"(c[0]), "r"(c[1]), "r"(c[2]), "r"(c[3]));
 }
 __device__ __forceinline__ uint32_t transpose8x8(uint32_t a) {
     uint32_t d;
@@ -47,11 +60,23 @@ __device__ __forceinline__ float ex2(float x) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
-// Codes in nibbles P and P + 4 of w as two bf16 numbers 16 + code.
-template <int P>
-__device__ __forceinline__ uint32_t codes16(uint32_t w) {
-    const uint32_t s = P == 0 ? w << 3 : w >> (4 * P - 3);
-    return (s & 0x00780078u) | 0x41804180u;
+// The power of two that brings the number with these bits into [2^(BITS - 1), 2^BITS), and its reciprocal (both normal numbers for
+// every exponent).
+template <int BITS>
+__device__ __forceinline__ void range_scale(uint32_t bits, float& up, float& down) {
+    const int e = max((int)((bits >> 23) & 255u), BITS + 7);
+    up = __int_as_float((253 + BITS - e) << 23);
+    down = __int_as_float((e + 1 - BITS) << 23);
+}
+// 1.5 * 2^23: adding it to a small float leaves the nearest integer in the low bits; integer sums that start at its bits are floats.
+constexpr float kMagic = 12582912.f;
+constexpr int kMagicBits = 0x4b400000;
+__device__ __forceinline__ uint32_t whole(float x) { return __float_as_uint(x + kMagic); }
+// Whole numbers of 16 bits in x, y, z, w: their high and low bytes, the low ones signed.
+__device__ __forceinline__ void split_bytes(int x, int y, int z, int w, uint32_t& high, uint32_t& low) {
+    low = __byte_perm(__byte_perm(x, y, 0x0040), __byte_perm(z, w, 0x0040), 0x5410);
+    x += 128; y += 128; z += 128; w += 128;
+    high = __byte_perm(__byte_perm(x, y, 0x0051), __byte_perm(z, w, 0x0051), 0x5410);
 }
 
 template <int BYTES> struct Words;
@@ -59,10 +84,29 @@ template <> struct Words<16> { uint4 v; __device__ uint32_t operator[](int i) co
 template <> struct Words<8> { uint2 v; __device__ uint32_t operator[](int i) const { return i == 0 ? v.x : v.y; } };
 template <> struct Words<4> { uint32_t v; __device__ uint32_t operator[](int) const { return v; } };
 template <int BYTES>
-__device__ __forceinline__ Words<BYTES> load_words(const uint8_t* p) {
+__device__ __forceinline__ Words<BYTES> read_words(const uint8_t* p) {
     Words<BYTES> w;
-    w.v = __ldg(reinterpret_cast<const decltype(w.v)*>(p));
+    w.v = *reinterpret_cast<const decltype(w.v)*>(p);
     return w;
+}
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int LEFT>
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }
+
+constexpr int kStages = 3;
+template <int D>
+struct Ring {
+    static constexpr int kRows = kTile * D / 2;              // bytes of a tile's key (or value) codes
+    static constexpr int kStage = 2 * kRows + 2 * kTile * 4; // keys, values, key parameters, value parameters
+    static constexpr int kWarp = kStages * kStage;
+};
+
+constexpr int kv_shared_bytes(int d, int gt) {
+    const int ring = kWarps * kStages * (kTile * d + 2 * kTile * 4), o = kWarps * gt * 8 * (d + 4) * 4;
+    return ring > o ? ring : o;
 }
 
 struct DecodeArgs {
@@ -83,11 +127,14 @@ __device__ __forceinline__ int units_of(const DecodeArgs& p, int s) {
 // P16: pages of 16 tokens, so the halves of a tile lie in different pages; all larger pages hold whole tiles.
 template <int D, int GT, bool P16>
 __global__ void __launch_bounds__(kWarps * 32, GT == 1 ? 4 : 2) kv_attention_kernel(DecodeArgs p) {
-    constexpr int kSteps = D / 16;             // k steps of S
+    constexpr int kSteps = D / 32;             // k steps of S
     constexpr int kMt = D / 16;                // 16-row tiles of o
     constexpr int KB = D / 8, VB = D / 16;     // bytes of a key / value row per lane
     constexpr int H = GT * 8;
-    __shared__ float s_o[kWarps][H][D + 4];
+    // the warps' rings; between two (sequence, head) parts the same memory holds the warps' o
+    extern __shared__ __align__(128) uint8_t s_bytes[];
+    float (*s_o)[H][D + 4] = reinterpret_cast<float (*)[H][D + 4]>(s_bytes);
+    uint8_t* const ring = s_bytes + (threadIdx.x / 32) * Ring<D>::kWarp;
     __shared__ float s_m[kWarps][H], s_l[kWarps][H];
     __shared__ int64_t s_scan[kWarps + 1];
     __shared__ int s_seq;
@@ -167,46 +214,62 @@ __global__ void __launch_bounds__(kWarps * 32, GT == 1 ? 4 : 2) kv_attention_ker
         const int len = a.lengths[seq];
         const int32_t* table = a.tables + (int64_t)seq * a.table_width;
 
-        // --- queries: columns g (+ 8) of the B operand, and the sums of columns 2 t, 2 t + 1
-        uint32_t qf[GT][kSteps][2];
-        float qsum[GT][2];
+        // --- queries: columns g (+ 8) of the B operand; sums and scales of columns 2 t, 2 t + 1
+        uint32_t q1[GT][kSteps][2], q2[GT][kSteps][2];
+        float qsum[GT][2], qdown[GT][2];
 #pragma unroll
         for (int n = 0; n < GT; ++n) {
             const int h = n * 8 + g;
+            uint4 w[kSteps];
             float sum = 0.f;
+            uint32_t top = 0;
 #pragma unroll
-            for (int j = 0; j < kSteps / 2; ++j) {
-                uint4 w = make_uint4(0, 0, 0, 0);
+            for (int j = 0; j < kSteps; ++j) {
+                w[j] = make_uint4(0, 0, 0, 0);
                 if (h < p.group)
-                    w = __ldg(reinterpret_cast<const uint4*>(a.q + seq * a.q_seq_stride + (int64_t)(head * p.group + h) * a.q_head_stride +
-                                                             t * (D / 4) + 8 * j));
-                qf[n][2 * j][0] = __byte_perm(w.x, w.z, 0x5410);
-                qf[n][2 * j][1] = __byte_perm(w.x, w.z, 0x7632);
-                qf[n][2 * j + 1][0] = __byte_perm(w.y, w.w, 0x5410);
-                qf[n][2 * j + 1][1] = __byte_perm(w.y, w.w, 0x7632);
-                sum += ((bf16_lo(w.x) + bf16_hi(w.x)) + (bf16_lo(w.y) + bf16_hi(w.y))) + ((bf16_lo(w.z) + bf16_hi(w.z)) + (bf16_lo(w.w) + bf16_hi(w.w)));
+                    w[j] = __ldg(reinterpret_cast<const uint4*>(a.q + seq * a.q_seq_stride + (int64_t)(head * p.group + h) * a.q_head_stride +
+                                                                t * (D / 4) + 8 * j));
+                const uint32_t x[4] = {w[j].x, w[j].y, w[j].z, w[j].w};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    sum += bf16_lo(x[i]) + bf16_hi(x[i]);
+                    top = max(top, max((x[i] << 16) & 0x7fffffffu, x[i] & 0x7fff0000u));
+                }
             }
+            top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+            top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
             sum += __shfl_xor_sync(0xffffffffu, sum, 1);
             sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-            qsum[n][0] = __shfl_sync(0xffffffffu, sum, 8 * t) * to_log2;
-            qsum[n][1] = __shfl_sync(0xffffffffu, sum, 8 * t + 4) * to_log2;
+            float up, down;
+            range_scale<15>(top, up, down);
+            up *= 32512.f / 32768.f;                 // so that the high byte stays within 127
+#pragma unroll
+            for (int j = 0; j < kSteps; ++j) {
+                split_bytes(whole(bf16_lo(w[j].x) * up), whole(bf16_lo(w[j].y) * up), whole(bf16_lo(w[j].z) * up), whole(bf16_lo(w[j].w) * up),
+                            q1[n][j][0], q2[n][j][0]);
+                split_bytes(whole(bf16_hi(w[j].x) * up), whole(bf16_hi(w[j].y) * up), whole(bf16_hi(w[j].z) * up), whole(bf16_hi(w[j].w) * up),
+                            q1[n][j][1], q2[n][j][1]);
+            }
+            sum *= to_log2;
+            down *= 32768.f / 32512.f * to_log2;
+            qsum[n][0] = __shfl_sync(0xffffffffu, sum, 8 * t);
+            qsum[n][1] = __shfl_sync(0xffffffffu, sum, 8 * t + 4);
+            qdown[n][0] = __shfl_sync(0xffffffffu, down, 8 * t);
+            qdown[n][1] = __shfl_sync(0xffffffffu, down, 8 * t + 4);
         }
 
         float o[GT][kMt][4];
-        float m[GT][2], l[GT][2], r[GT][2], z[GT][2];
+        float m[GT][2], l[GT][2], z[GT][2];
 #pragma unroll
         for (int n = 0; n < GT; ++n) {
 #pragma unroll
             for (int i = 0; i < kMt; ++i) o[n][i][0] = o[n][i][1] = o[n][i][2] = o[n][i][3] = 0.f;
 #pragma unroll
-            for (int e = 0; e < 2; ++e) { m[n][e] = -INFINITY; l[n][e] = r[n][e] = z[n][e] = 0.f; }
+            for (int e = 0; e < 2; ++e) { m[n][e] = -INFINITY; l[n][e] = z[n][e] = 0.f; }
         }
         bool bad = false;
 
         // --- tiles of 32 tokens: warp, warp + 4, ...
-        Words<KB> kw[2][2];
-        Words<VB> vw[2][4];
-        uint32_t kpar = 0, vpar = 0;
         int page0 = 0, page1 = 0;
         const int stop = min(len, u1 * kUnit);
         int tok = u0 * kUnit + warp * kTile;
@@ -225,70 +288,88 @@ __global__ void __launch_bounds__(kWarps * 32, GT == 1 ? 4 : 2) kv_attention_ker
             row0 = (((int64_t)page0 * heads + head) << p.page_shift) + (tk & ((1 << p.page_shift) - 1));
             row1 = P16 ? (((int64_t)page1 * heads + head) << p.page_shift) : row0 + 16;
         };
-        auto load_k = [&](int tk) {
-            if (tk >= stop) return;
+        constexpr int CH = D / 32;                          // 16-byte pieces of a row
+        const uint32_t ring_at = smem_u32(ring);
+        auto fetch = [&](int tk, int stage) {               // the tile at tk to a place in the ring; pages of the tile after it
+            if (tk < stop) {
+                set_rows(tk);
+                const uint32_t dst = ring_at + stage * Ring<D>::kStage + lane * 16;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) kw[e >> 1][e & 1] = load_words<KB>(kc + ((e < 2 ? row0 : row1) + g + 8 * (e & 1)) * (D / 2) + t * KB);
-            kpar = __ldg(kp + (lane < 16 ? row0 : row1) + (lane & 15));
-        };
-        auto load_v = [&](int tk) {
-            if (tk >= stop) return;
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                vw[e >> 2][e & 3] = load_words<VB>(vc + ((e < 4 ? row0 : row1) + 2 * t + (e & 1) + 8 * ((e >> 1) & 1)) * (D / 2) + g * VB);
-            vpar = __ldg(vp + (lane < 16 ? row0 : row1) + (lane & 15));
+                for (int i = 0; i < CH; ++i) {              // 32 / CH rows at a time: contiguous in a page
+                    const int64_t r = P16 && i >= CH / 2 ? row1 - 16 : row0;
+                    copy16(dst + i * 512, kc + r * (D / 2) + lane * 16 + i * 512);
+                    copy16(dst + Ring<D>::kRows + i * 512, vc + r * (D / 2) + lane * 16 + i * 512);
+                }
+                if (lane < 16) {
+                    const int64_t r = P16 && (lane & 4) ? row1 - 16 : row0;
+                    copy16(dst + 2 * Ring<D>::kRows, (lane < 8 ? kp : vp) + r + (lane & 7) * 4);
+                }
+                fetch_pages(tk + kUnit);
+            }
+            copies_commit();
         };
 
         fetch_pages(tok);
-        if (tok < stop) set_rows(tok);
-        load_k(tok);
-        load_v(tok);
-        fetch_pages(tok + kUnit);
+        fetch(tok, 0);
+        fetch(tok + kUnit, 1);
+        int stage = 0;
+        const int tv = (t & 1) | (t & 2) << 1, tg = (g & 4) | (g & 1) << 1 | (g >> 1 & 1);
         for (; tok < stop; tok += kUnit) {
-            const int next = tok + kUnit;
+            __syncwarp();                                   // every lane has read the tile that the next copy replaces
+            fetch(tok + 2 * kUnit, stage == 0 ? 2 : stage - 1);
+            copies_wait<kStages - 1>();
+            __syncwarp();
+            const uint8_t* const tile = ring + stage * Ring<D>::kStage;
+            const uint32_t* const params = reinterpret_cast<const uint32_t*>(tile + 2 * Ring<D>::kRows);
+            stage = stage == kStages - 1 ? 0 : stage + 1;
+            const int zero[4] = {0, 0, 0, 0};
             // S of both halves
             float s[GT][2][4];
 #pragma unroll
-            for (int n = 0; n < GT; ++n)
+            for (int h = 0; h < 2; ++h) {
+                int d[GT][4];
+                // row g of the tile is token tg = g with its two low bits exchanged: so the four tokens whose values a quad reads
+                // together (rows 0, 2, 4, 6) lie in different banks
+                const Words<KB> k0 = read_words<KB>(tile + (16 * h + tg) * (D / 2) + t * KB), k1 = read_words<KB>(tile + (16 * h + 8 + tg) * (D / 2) + t * KB);
 #pragma unroll
-                for (int h = 0; h < 2; ++h) s[n][h][0] = s[n][h][1] = s[n][h][2] = s[n][h][3] = 0.f;
+                for (int pass = 0; pass < 2; ++pass)
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
+                    for (int j = 0; j < kSteps; ++j) {
+                        const uint32_t w0 = k0[j], w1 = k1[j];
+                        const uint32_t a0 = w0 & 0x0f0f0f0fu, a1 = w1 & 0x0f0f0f0fu, a2 = (w0 >> 4) & 0x0f0f0f0fu, a3 = (w1 >> 4) & 0x0f0f0f0fu;
 #pragma unroll
-                for (int j = 0; j < kSteps / 2; ++j) {
-                    const uint32_t w0 = kw[h][0][j], w1 = kw[h][1][j];
-                    const uint32_t a00 = codes16<0>(w0), a01 = codes16<1>(w0), a02 = codes16<2>(w0), a03 = codes16<3>(w0);
-                    const uint32_t a10 = codes16<0>(w1), a11 = codes16<1>(w1), a12 = codes16<2>(w1), a13 = codes16<3>(w1);
-#pragma unroll
-                    for (int n = 0; n < GT; ++n) {
-                        mma_bf16(s[n][h], a00, a10, a01, a11, qf[n][2 * j][0], qf[n][2 * j][1]);
-                        mma_bf16(s[n][h], a02, a12, a03, a13, qf[n][2 * j + 1][0], qf[n][2 * j + 1][1]);
+                        for (int n = 0; n < GT; ++n) {
+                            if (pass == 1 && j == 0) { d[n][0] <<= 8; d[n][1] <<= 8; d[n][2] <<= 8; d[n][3] <<= 8; }
+                            if (pass == 0 && j == 0) mma_u8s8(d[n], a0, a1, a2, a3, q1[n][j], zero);
+                            else mma_u8s8(d[n], a0, a1, a2, a3, pass == 0 ? q1[n][j] : q2[n][j], d[n]);
+                        }
                     }
-                }
-            const uint32_t kq = kpar;
-            uint32_t vq = vpar;
-            if (tok + lane >= len) vq = 0;               // what lies past the length adds nothing, whatever it holds
-            if (next < stop) set_rows(next);
-            load_k(next);
+#pragma unroll
+                for (int n = 0; n < GT; ++n)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) s[n][h][i] = (float)d[n][i];
+            }
+            const uint32_t vq = tok + lane < len ? params[kTile + lane] : 0u;    // what lies past the length adds nothing, whatever it holds
             // scores in units of log2, tokens past the length out
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    const int i = 16 * h + 8 * e + g;
-                    const uint32_t w = __shfl_sync(0xffffffffu, kq, i);
-                    const float ks = bf16_lo(w), beta = fmaf(-16.f, ks, bf16_hi(w)), ksc = ks * to_log2;
+                    const int i = 16 * h + 8 * e + tg;
+                    const uint32_t w = params[i];
+                    const float ks = bf16_lo(w), kb = bf16_hi(w);
                     const bool in = tok + i < len;
 #pragma unroll
                     for (int n = 0; n < GT; ++n)
 #pragma unroll
                         for (int c = 0; c < 2; ++c) {
                             float& x = s[n][h][2 * e + c];
-                            x = in ? fmaf(ksc, x, beta * qsum[n][c]) : -INFINITY;
+                            x = in ? fmaf(ks, x * qdown[n][c], kb * qsum[n][c]) : -INFINITY;
                         }
                 }
+            // the tile's maxima and its values' largest scale
+            float mt[GT][2];
             bool grow = false;
-            float top[GT][2];
 #pragma unroll
             for (int n = 0; n < GT; ++n)
 #pragma unroll
@@ -297,67 +378,108 @@ __global__ void __launch_bounds__(kWarps * 32, GT == 1 ? 4 : 2) kv_attention_ker
                     x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
                     x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
                     x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
-                    top[n][c] = x;
-                    grow = grow || x > m[n][c] + 8.f;
+                    mt[n][c] = x;
+                    grow = grow || x > m[n][c];
                 }
-            // the running maximum moves only when it has to: powers up to 2^8 are as exact in bf16 and fp32
+            float v_up, v_down;
+            range_scale<13>(__reduce_max_sync(0xffffffffu, (vq << 16) & 0x7fffffffu), v_up, v_down);
+            v_up *= 8128.f / 8192.f;                 // so that P1 stays within 127
+            v_down *= 8192.f / 8128.f;
             if (__any_sync(0xffffffffu, grow)) {
 #pragma unroll
                 for (int n = 0; n < GT; ++n) {
                     float f[2];
 #pragma unroll
                     for (int c = 0; c < 2; ++c) {
-                        const float nm = fmaxf(m[n][c], top[n][c]);
+                        const float nm = fmaxf(m[n][c], mt[n][c]);
                         f[c] = m[n][c] == nm ? 1.f : ex2(m[n][c] - nm);
                         m[n][c] = nm;
-                        l[n][c] *= f[c]; r[n][c] *= f[c]; z[n][c] *= f[c];
+                        l[n][c] *= f[c]; z[n][c] *= f[c];
                     }
 #pragma unroll
                     for (int i = 0; i < kMt; ++i) { o[n][i][0] *= f[0]; o[n][i][1] *= f[1]; o[n][i][2] *= f[0]; o[n][i][3] *= f[1]; }
                 }
             }
-            uint32_t pf[GT][2][2];
+            // probabilities relative to the tile's maximum, and the two parts of P turned to the B operand's layout
+            uint32_t p1[GT][2], p2[GT][2];
+            int c1[GT][4], c2[GT][4];
+            float beta[GT][2];
+#pragma unroll
+            for (int n = 0; n < GT; ++n) {
+                float sl[2] = {0.f, 0.f}, sz[2] = {0.f, 0.f};
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    float x[2][2];
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const uint32_t w = __shfl_sync(0xffffffffu, vq, 16 * h + 8 * e + tg);
+                        const float vs = bf16_lo(w), mid = fmaf(8.f, vs, bf16_hi(w)), scaled = vs * v_up;
+#pragma unroll
+                        for (int c = 0; c < 2; ++c) {
+                            const float pr = ex2(s[n][h][2 * e + c] - mt[n][c]);
+                            sl[c] += pr;
+                            sz[c] = fmaf(pr, mid, sz[c]);
+                            x[c][e] = pr * scaled;
+                        }
+                    }
+                    // bytes of P1 and P2, columns 2 t and 2 t + 1, tokens g and g + 8 of the half
+                    const uint32_t x0 = __byte_perm(whole(x[0][0]), whole(x[0][1]), 0x5410), x1 = __byte_perm(whole(x[1][0]), whole(x[1][1]), 0x5410);
+                    p1[n][h] = transpose8x8(__byte_perm(x0 >> 6, x1 >> 6, 0x6420));
+                    p2[n][h] = transpose8x8(__byte_perm(x0, x1, 0x6420) & 0x3f3f3f3fu);
+                }
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    const float b = ex2(mt[n][c] - m[n][c]);
+                    l[n][c] = fmaf(b, sl[c], l[n][c]);
+                    z[n][c] = fmaf(b, sz[c], z[n][c]);
+                    beta[n][c] = b * v_down;
+                }
+                mma_u8s8(c1[n], 0x08080808u, 0x08080808u, 0x08080808u, 0x08080808u, p1[n], zero);     // 8 sum P1 and 8 sum P2, for every row
+                mma_u8s8(c2[n], 0x08080808u, 0x08080808u, 0x08080808u, 0x08080808u, p2[n], zero);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) { c1[n][i] = -c1[n][i]; c2[n][i] = kMagicBits - c2[n][i]; }
+            }
+            Words<VB> vw[2][4];
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const uint32_t w = __shfl_sync(0xffffffffu, vq, 16 * h + 8 * e + g);
-                    const float vs = bf16_lo(w), mid = fmaf(8.f, vs, bf16_hi(w));
+                for (int e = 0; e < 4; ++e)
+                    vw[h][e] = read_words<VB>(tile + Ring<D>::kRows + (16 * h + tv + 2 * (e & 1) + 8 * (e >> 1)) * (D / 2) + g * VB);
+#pragma unroll
+            for (int j = 0; j < VB / 4; ++j) {
+                uint32_t x[2][4];                    // [half][byte of the word]: that byte of rows 2 t, 2 t + 8, 2 t + 1, 2 t + 9
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const uint32_t t0 = __byte_perm(vw[h][0][j], vw[h][2][j], 0x5140), t1 = __byte_perm(vw[h][1][j], vw[h][3][j], 0x5140);
+                    const uint32_t t2 = __byte_perm(vw[h][0][j], vw[h][2][j], 0x7362), t3 = __byte_perm(vw[h][1][j], vw[h][3][j], 0x7362);
+                    x[h][0] = __byte_perm(t0, t1, 0x5410); x[h][1] = __byte_perm(t0, t1, 0x7632);
+                    x[h][2] = __byte_perm(t2, t3, 0x5410); x[h][3] = __byte_perm(t2, t3, 0x7632);
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t a0 = x[0][i] & 0x0f0f0f0fu, a1 = (x[0][i] >> 4) & 0x0f0f0f0fu;
+                    const uint32_t a2 = x[1][i] & 0x0f0f0f0fu, a3 = (x[1][i] >> 4) & 0x0f0f0f0fu;
 #pragma unroll
                     for (int n = 0; n < GT; ++n) {
-                        const float p0 = ex2(s[n][h][2 * e] - m[n][0]), p1 = ex2(s[n][h][2 * e + 1] - m[n][1]);
-                        const uint32_t pk = pack_bf16x2(p0 * vs, p1 * vs);
-                        l[n][0] += p0; l[n][1] += p1;
-                        z[n][0] = fmaf(p0, mid, z[n][0]); z[n][1] = fmaf(p1, mid, z[n][1]);
-                        r[n][0] += bf16_lo(pk); r[n][1] += bf16_hi(pk);
-                        pf[n][h][e] = transpose8x8(pk);
+                        int d[4];
+                        mma_u8s8(d, a0, a1, a2, a3, p1[n], c1[n]);
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) d[k] = (d[k] << 6) + c2[n][k];
+                        mma_u8s8(d, a0, a1, a2, a3, p2[n], d);
+                        float (&y)[4] = o[n][4 * j + i];
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) y[k] = fmaf(__int_as_float(d[k]) - kMagic, beta[n][k & 1], y[k]);
                     }
                 }
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int j = 0; j < VB / 4; ++j) {
-                    const uint32_t lo0 = __byte_perm(vw[h][0][j], vw[h][1][j], 0x5410), hi0 = __byte_perm(vw[h][0][j], vw[h][1][j], 0x7632);
-                    const uint32_t lo1 = __byte_perm(vw[h][2][j], vw[h][3][j], 0x5410), hi1 = __byte_perm(vw[h][2][j], vw[h][3][j], 0x7632);
-                    const uint32_t c0[8] = {codes16<0>(lo0), codes16<1>(lo0), codes16<2>(lo0), codes16<3>(lo0),
-                                            codes16<0>(hi0), codes16<1>(hi0), codes16<2>(hi0), codes16<3>(hi0)};
-                    const uint32_t c1[8] = {codes16<0>(lo1), codes16<1>(lo1), codes16<2>(lo1), codes16<3>(lo1),
-                                            codes16<0>(hi1), codes16<1>(hi1), codes16<2>(hi1), codes16<3>(hi1)};
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-#pragma unroll
-                        for (int n = 0; n < GT; ++n)
-                            mma_bf16(o[n][4 * j + i], c0[2 * i], c0[2 * i + 1], c1[2 * i], c1[2 * i + 1], pf[n][h][0], pf[n][h][1]);
-                }
-            load_v(next);
-            fetch_pages(next + kUnit);
+            }
         }
+        copies_wait<0>();
         bad = __any_sync(0xffffffffu, bad);
         if (bad && lane == 0) raise_status(a.status, MT_ERR_INVALID_ARG, seq);
 
         // --- join the warps
         constexpr int C = D / 8;                 // channels per lane group
-        __syncthreads();                         // the previous (sequence, head) has been read
+        __syncthreads();                         // every warp is done with its ring
 #pragma unroll
         for (int n = 0; n < GT; ++n) {
 #pragma unroll
@@ -365,12 +487,11 @@ __global__ void __launch_bounds__(kWarps * 32, GT == 1 ? 4 : 2) kv_attention_ker
 #pragma unroll
                 for (int x = 4; x < 32; x <<= 1) {
                     l[n][c] += __shfl_xor_sync(0xffffffffu, l[n][c], x);
-                    r[n][c] += __shfl_xor_sync(0xffffffffu, r[n][c], x);
                     z[n][c] += __shfl_xor_sync(0xffffffffu, z[n][c], x);
                 }
                 const int h = n * 8 + 2 * t + c;
                 if (g == 0) { s_m[warp][h] = m[n][c]; s_l[warp][h] = bad ? nan_f() : l[n][c]; }
-                const float shift = fmaf(-24.f, r[n][c], z[n][c]);
+                const float shift = z[n][c];
 #pragma unroll
                 for (int i = 0; i < kMt; ++i)    // rotated inside the lane group's channels against bank conflicts
                     *reinterpret_cast<float2*>(&s_o[warp][h][g * C + ((2 * i + 2 * g) & (C - 1))]) =
@@ -429,13 +550,28 @@ __global__ void __launch_bounds__(kWarps * 32, GT == 1 ? 4 : 2) kv_attention_ker
                 }
             }
         }
+        __syncthreads();                         // the joined parts have been read: the rings may be filled again
         at = min(seg1, end);
     }
 }
 
 }  // namespace
 
-cudaError_t configure_kv_attention() { return cudaSuccess; }
+typedef void (*KvAttentionKernel)(DecodeArgs);
+const KvAttentionKernel kKernels[2][2][2] = {
+    {{kv_attention_kernel<64, 1, false>, kv_attention_kernel<64, 1, true>}, {kv_attention_kernel<64, 2, false>, kv_attention_kernel<64, 2, true>}},
+    {{kv_attention_kernel<128, 1, false>, kv_attention_kernel<128, 1, true>}, {kv_attention_kernel<128, 2, false>, kv_attention_kernel<128, 2, true>}}};
+
+cudaError_t configure_kv_attention() {
+    for (int d = 0; d < 2; ++d)
+        for (int gt = 0; gt < 2; ++gt)
+            for (int p16 = 0; p16 < 2; ++p16) {
+                const cudaError_t e = cudaFuncSetAttribute(kKernels[d][gt][p16], cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                                           kv_shared_bytes(d ? 128 : 64, gt + 1));
+                if (e != cudaSuccess) return e;
+            }
+    return cudaSuccess;
+}
 
 mt_status launch_kv_attention(const KvAttentionArgs& a, const OpContext& c, cudaStream_t s) {
     DecodeArgs p;
@@ -456,12 +592,8 @@ mt_status launch_kv_attention(const KvAttentionArgs& a, const OpContext& c, cuda
     p.arrived = reinterpret_cast<unsigned*>(w);
     p.part_o = reinterpret_cast<float*>(w + kScratchZeroBytes);
     p.part_ml = reinterpret_cast<float*>(w + kScratchZeroBytes + o_bytes);
-    typedef void (*Kernel)(DecodeArgs);
-    static const Kernel kernels[2][2][2] = {
-        {{kv_attention_kernel<64, 1, false>, kv_attention_kernel<64, 1, true>}, {kv_attention_kernel<64, 2, false>, kv_attention_kernel<64, 2, true>}},
-        {{kv_attention_kernel<128, 1, false>, kv_attention_kernel<128, 1, true>}, {kv_attention_kernel<128, 2, false>, kv_attention_kernel<128, 2, true>}}};
-    const Kernel k = kernels[d == 128][gt - 1][a.c.page_tokens == 16];
-    return launch_pdl(k, dim3((unsigned)grid), dim3(kWarps * 32), 0, s, p) == cudaSuccess ? MT_OK : MT_ERR_CUDA;
+    return launch_pdl(kKernels[d == 128][gt - 1][a.c.page_tokens == 16], dim3((unsigned)grid), dim3(kWarps * 32),
+                      (size_t)kv_shared_bytes(d, gt), s, p) == cudaSuccess ? MT_OK : MT_ERR_CUDA;
 }
 
 }  // namespace mt
