@@ -71,7 +71,14 @@ __device__ __forceinline__ void range_scale(uint32_t bits, float& up, float& dow
 // 1.5 * 2^23: adding it to a small float leaves the nearest integer in the low bits; integer sums that start at its bits are floats.
 constexpr float kMagic = 12582912.f;
 constexpr int kMagicBits = 0x4b400000;
-__device__ __forceinline__ uint32_t whole(float x) { return __float_as_uint(x + kMagic); }
+__device__ __forceinline__ uint32_t whole(float x, float y) { return __float_as_uint(fmaf(x, y, kMagic)); }
+// y += (x - kMagic) * s on pairs.
+__device__ __forceinline__ void add_scaled(float2& y, int x0, int x1, float s0, float s1) {
+    asm("{\n\t.reg .b64 x, s, y, m;\n\t"
+        "mov.b64 x, {%2, %3};\n\tmov.b64 s, {%4, %5};\n\tmov.b64 y, {%0, %1};\n\tmov.b64 m, {%6, %6};\n\t"
+        "add.rn.f32x2 x, x, m;\n\tfma.rn.f32x2 y, x, s, y;\n\tmov.b64 {%0, %1}, y;\n\t}"
+        : "+f"(y.x), "+f"(y.y) : "r"(x0), "r"(x1), "f"(s0), "f"(s1), "f"(-kMagic));
+}
 // Whole numbers of 16 bits in x, y, z, w: their high and low bytes, the low ones signed.
 __device__ __forceinline__ void split_bytes(int x, int y, int z, int w, uint32_t& high, uint32_t& low) {
     low = __byte_perm(__byte_perm(x, y, 0x0040), __byte_perm(z, w, 0x0040), 0x5410);
@@ -199,7 +206,7 @@ __global__ void __launch_bounds__(kWarps * 32, GT == 1 ? 4 : 2) kv_attention_ker
 
     const uint8_t *kc = static_cast<const uint8_t*>(a.c.k_codes), *vc = static_cast<const uint8_t*>(a.c.v_codes);
     const uint32_t *kp = static_cast<const uint32_t*>(a.c.k_params), *vp = static_cast<const uint32_t*>(a.c.v_params);
-    const float to_log2 = a.scale * 1.44269504088896341f;
+    const float to_log2 = fabsf(a.scale) * 1.44269504088896341f;
 
     for (int64_t at = begin; at < end;) {
         // --- the (sequence, head) that unit `at` belongs to
@@ -242,28 +249,29 @@ __global__ void __launch_bounds__(kWarps * 32, GT == 1 ? 4 : 2) kv_attention_ker
             sum += __shfl_xor_sync(0xffffffffu, sum, 2);
             float up, down;
             range_scale<15>(top, up, down);
-            up *= 32512.f / 32768.f;                 // so that the high byte stays within 127
+            up *= copysignf(32512.f / 32768.f, a.scale);     // so that the high byte stays within 127; with the sign of the scale
 #pragma unroll
             for (int j = 0; j < kSteps; ++j) {
-                split_bytes(whole(bf16_lo(w[j].x) * up), whole(bf16_lo(w[j].y) * up), whole(bf16_lo(w[j].z) * up), whole(bf16_lo(w[j].w) * up),
+                split_bytes(whole(bf16_lo(w[j].x), up), whole(bf16_lo(w[j].y), up), whole(bf16_lo(w[j].z), up), whole(bf16_lo(w[j].w), up),
                             q1[n][j][0], q2[n][j][0]);
-                split_bytes(whole(bf16_hi(w[j].x) * up), whole(bf16_hi(w[j].y) * up), whole(bf16_hi(w[j].z) * up), whole(bf16_hi(w[j].w) * up),
+                split_bytes(whole(bf16_hi(w[j].x), up), whole(bf16_hi(w[j].y), up), whole(bf16_hi(w[j].z), up), whole(bf16_hi(w[j].w), up),
                             q1[n][j][1], q2[n][j][1]);
             }
-            sum *= to_log2;
-            down *= 32768.f / 32512.f * to_log2;
+            // scores are held in units of 1 / qdown: |scale| log2(e) / up; not zero, so that minus infinity stays what it is
+            sum *= up;
+            down = fmaxf(down * (32768.f / 32512.f * to_log2), 1e-30f);
             qsum[n][0] = __shfl_sync(0xffffffffu, sum, 8 * t);
             qsum[n][1] = __shfl_sync(0xffffffffu, sum, 8 * t + 4);
             qdown[n][0] = __shfl_sync(0xffffffffu, down, 8 * t);
             qdown[n][1] = __shfl_sync(0xffffffffu, down, 8 * t + 4);
         }
 
-        float o[GT][kMt][4];
+        float2 o[GT][2 * kMt];                   // channels g C + i, columns 2 t and 2 t + 1
         float m[GT][2], l[GT][2], z[GT][2];
 #pragma unroll
         for (int n = 0; n < GT; ++n) {
 #pragma unroll
-            for (int i = 0; i < kMt; ++i) o[n][i][0] = o[n][i][1] = o[n][i][2] = o[n][i][3] = 0.f;
+            for (int i = 0; i < 2 * kMt; ++i) o[n][i] = make_float2(0.f, 0.f);
 #pragma unroll
             for (int e = 0; e < 2; ++e) { m[n][e] = -INFINITY; l[n][e] = z[n][e] = 0.f; }
         }
@@ -327,46 +335,51 @@ __global__ void __launch_bounds__(kWarps * 32, GT == 1 ? 4 : 2) kv_attention_ker
             float s[GT][2][4];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                int d[GT][4];
+                int d1[GT][4], d2[GT][4];
                 // row g of the tile is token tg = g with its two low bits exchanged: so the four tokens whose values a quad reads
                 // together (rows 0, 2, 4, 6) lie in different banks
                 const Words<KB> k0 = read_words<KB>(tile + (16 * h + tg) * (D / 2) + t * KB), k1 = read_words<KB>(tile + (16 * h + 8 + tg) * (D / 2) + t * KB);
 #pragma unroll
-                for (int pass = 0; pass < 2; ++pass)
+                for (int j = 0; j < kSteps; ++j) {
+                    const uint32_t w0 = k0[j], w1 = k1[j];
+                    const uint32_t a0 = w0 & 0x0f0f0f0fu, a1 = w1 & 0x0f0f0f0fu, a2 = (w0 >> 4) & 0x0f0f0f0fu, a3 = (w1 >> 4) & 0x0f0f0f0fu;
 #pragma unroll
-                    for (int j = 0; j < kSteps; ++j) {
-                        const uint32_t w0 = k0[j], w1 = k1[j];
-                        const uint32_t a0 = w0 & 0x0f0f0f0fu, a1 = w1 & 0x0f0f0f0fu, a2 = (w0 >> 4) & 0x0f0f0f0fu, a3 = (w1 >> 4) & 0x0f0f0f0fu;
-#pragma unroll
-                        for (int n = 0; n < GT; ++n) {
-                            if (pass == 1 && j == 0) { d[n][0] <<= 8; d[n][1] <<= 8; d[n][2] <<= 8; d[n][3] <<= 8; }
-                            if (pass == 0 && j == 0) mma_u8s8(d[n], a0, a1, a2, a3, q1[n][j], zero);
-                            else mma_u8s8(d[n], a0, a1, a2, a3, pass == 0 ? q1[n][j] : q2[n][j], d[n]);
+                    for (int n = 0; n < GT; ++n) {
+                        if (j == 0) {
+                            mma_u8s8(d1[n], a0, a1, a2, a3, q1[n][j], zero);
+                            mma_u8s8(d2[n], a0, a1, a2, a3, q2[n][j], zero);
+                        } else {
+                            mma_u8s8(d1[n], a0, a1, a2, a3, q1[n][j], d1[n]);
+                            mma_u8s8(d2[n], a0, a1, a2, a3, q2[n][j], d2[n]);
                         }
                     }
+                }
 #pragma unroll
                 for (int n = 0; n < GT; ++n)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) s[n][h][i] = (float)d[n][i];
+                    for (int i = 0; i < 4; ++i) s[n][h][i] = (float)((d1[n][i] << 8) + d2[n][i]);
             }
             const uint32_t vq = tok + lane < len ? params[kTile + lane] : 0u;    // what lies past the length adds nothing, whatever it holds
-            // scores in units of log2, tokens past the length out
+            // scores in units of 1 / qdown
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    const int i = 16 * h + 8 * e + tg;
-                    const uint32_t w = params[i];
+                    const uint32_t w = params[16 * h + 8 * e + tg];
                     const float ks = bf16_lo(w), kb = bf16_hi(w);
-                    const bool in = tok + i < len;
 #pragma unroll
                     for (int n = 0; n < GT; ++n)
 #pragma unroll
-                        for (int c = 0; c < 2; ++c) {
-                            float& x = s[n][h][2 * e + c];
-                            x = in ? fmaf(ks, x * qdown[n][c], kb * qsum[n][c]) : -INFINITY;
-                        }
+                        for (int c = 0; c < 2; ++c) s[n][h][2 * e + c] = fmaf(ks, s[n][h][2 * e + c], kb * qsum[n][c]);
                 }
+            if (tok + kTile > len)                       // tokens past the length out
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e)
+                        if (tok + 16 * h + 8 * e + tg >= len)
+#pragma unroll
+                            for (int n = 0; n < GT; ++n) s[n][h][2 * e] = s[n][h][2 * e + 1] = -INFINITY;
             // the tile's maxima and its values' largest scale
             float mt[GT][2];
             bool grow = false;
@@ -392,12 +405,12 @@ __global__ void __launch_bounds__(kWarps * 32, GT == 1 ? 4 : 2) kv_attention_ker
 #pragma unroll
                     for (int c = 0; c < 2; ++c) {
                         const float nm = fmaxf(m[n][c], mt[n][c]);
-                        f[c] = m[n][c] == nm ? 1.f : ex2(m[n][c] - nm);
+                        f[c] = m[n][c] == nm ? 1.f : ex2((m[n][c] - nm) * qdown[n][c]);
                         m[n][c] = nm;
                         l[n][c] *= f[c]; z[n][c] *= f[c];
                     }
 #pragma unroll
-                    for (int i = 0; i < kMt; ++i) { o[n][i][0] *= f[0]; o[n][i][1] *= f[1]; o[n][i][2] *= f[0]; o[n][i][3] *= f[1]; }
+                    for (int i = 0; i < 2 * kMt; ++i) { o[n][i].x *= f[0]; o[n][i].y *= f[1]; }
                 }
             }
             // probabilities relative to the tile's maximum, and the two parts of P turned to the B operand's layout
@@ -407,29 +420,30 @@ __global__ void __launch_bounds__(kWarps * 32, GT == 1 ? 4 : 2) kv_attention_ker
 #pragma unroll
             for (int n = 0; n < GT; ++n) {
                 float sl[2] = {0.f, 0.f}, sz[2] = {0.f, 0.f};
+                const float shift[2] = {-mt[n][0] * qdown[n][0], -mt[n][1] * qdown[n][1]};
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    float x[2][2];
+                    uint32_t x[2][2];
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
                         const uint32_t w = __shfl_sync(0xffffffffu, vq, 16 * h + 8 * e + tg);
                         const float vs = bf16_lo(w), mid = fmaf(8.f, vs, bf16_hi(w)), scaled = vs * v_up;
 #pragma unroll
                         for (int c = 0; c < 2; ++c) {
-                            const float pr = ex2(s[n][h][2 * e + c] - mt[n][c]);
+                            const float pr = ex2(fmaf(s[n][h][2 * e + c], qdown[n][c], shift[c]));
                             sl[c] += pr;
                             sz[c] = fmaf(pr, mid, sz[c]);
-                            x[c][e] = pr * scaled;
+                            x[c][e] = whole(pr, scaled);
                         }
                     }
                     // bytes of P1 and P2, columns 2 t and 2 t + 1, tokens g and g + 8 of the half
-                    const uint32_t x0 = __byte_perm(whole(x[0][0]), whole(x[0][1]), 0x5410), x1 = __byte_perm(whole(x[1][0]), whole(x[1][1]), 0x5410);
+                    const uint32_t x0 = __byte_perm(x[0][0], x[0][1], 0x5410), x1 = __byte_perm(x[1][0], x[1][1], 0x5410);
                     p1[n][h] = transpose8x8(__byte_perm(x0 >> 6, x1 >> 6, 0x6420));
                     p2[n][h] = transpose8x8(__byte_perm(x0, x1, 0x6420) & 0x3f3f3f3fu);
                 }
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
-                    const float b = ex2(mt[n][c] - m[n][c]);
+                    const float b = ex2((mt[n][c] - m[n][c]) * qdown[n][c]);
                     l[n][c] = fmaf(b, sl[c], l[n][c]);
                     z[n][c] = fmaf(b, sz[c], z[n][c]);
                     beta[n][c] = b * v_down;
@@ -466,9 +480,8 @@ __global__ void __launch_bounds__(kWarps * 32, GT == 1 ? 4 : 2) kv_attention_ker
 #pragma unroll
                         for (int k = 0; k < 4; ++k) d[k] = (d[k] << 6) + c2[n][k];
                         mma_u8s8(d, a0, a1, a2, a3, p2[n], d);
-                        float (&y)[4] = o[n][4 * j + i];
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) y[k] = fmaf(__int_as_float(d[k]) - kMagic, beta[n][k & 1], y[k]);
+                        add_scaled(o[n][2 * (4 * j + i)], d[0], d[1], beta[n][0], beta[n][1]);
+                        add_scaled(o[n][2 * (4 * j + i) + 1], d[2], d[3], beta[n][0], beta[n][1]);
                     }
                 }
             }
@@ -490,12 +503,12 @@ __global__ void __launch_bounds__(kWarps * 32, GT == 1 ? 4 : 2) kv_attention_ker
                     z[n][c] += __shfl_xor_sync(0xffffffffu, z[n][c], x);
                 }
                 const int h = n * 8 + 2 * t + c;
-                if (g == 0) { s_m[warp][h] = m[n][c]; s_l[warp][h] = bad ? nan_f() : l[n][c]; }
+                if (g == 0) { s_m[warp][h] = m[n][c] == -INFINITY ? -INFINITY : m[n][c] * qdown[n][c]; s_l[warp][h] = bad ? nan_f() : l[n][c]; }
                 const float shift = z[n][c];
 #pragma unroll
                 for (int i = 0; i < kMt; ++i)    // rotated inside the lane group's channels against bank conflicts
                     *reinterpret_cast<float2*>(&s_o[warp][h][g * C + ((2 * i + 2 * g) & (C - 1))]) =
-                        make_float2(o[n][i][c] + shift, o[n][i][2 + c] + shift);
+                        c == 0 ? make_float2(o[n][2 * i].x + shift, o[n][2 * i + 1].x + shift) : make_float2(o[n][2 * i].y + shift, o[n][2 * i + 1].y + shift);
             }
         }
         __syncthreads();
