@@ -40,7 +40,7 @@
 namespace mt {
 namespace {
 
-constexpr int kWarps = 4, kTile = 32, kUnit = kWarps * kTile;
+constexpr int kWarps = 4, kTile = 32, kUnit = kWarps * kTile, kMaxParts = 64;
 
 // D = A B + C, 16 x 8 x 32, unsigned times signed bytes.
 __device__ __forceinline__ void mma_u8s8(int (&d)[4], const uint32_t a0, const uint32_t a1, const uint32_t a2, const uint32_t a3,
@@ -113,7 +113,8 @@ struct Ring {
 
 constexpr int kv_shared_bytes(int d, int gt) {
     const int ring = kWarps * kStages * (kTile * d + 2 * kTile * 4), o = kWarps * gt * 8 * (d + 4) * 4;
-    return ring > o ? ring : o;
+    const int join = (2 * (kMaxParts + 1) + 1) * gt * 8 * 4 + (gt * 8 * d > kWarps * 128 ? gt * 8 * d : kWarps * 128) * 4;
+    return ring > o ? (ring > join ? ring : join) : (o > join ? o : join);
 }
 
 struct DecodeArgs {
@@ -144,7 +145,7 @@ __global__ void __launch_bounds__(kWarps * 32, GT == 1 ? 4 : 2) kv_attention_ker
     uint8_t* const ring = s_bytes + (threadIdx.x / 32) * Ring<D>::kWarp;
     __shared__ float s_m[kWarps][H], s_l[kWarps][H];
     __shared__ int64_t s_scan[kWarps + 1];
-    __shared__ int s_seq;
+    __shared__ int s_longest[kWarps], s_seq;
     __shared__ int64_t s_base;
     __shared__ int s_last;
 
@@ -166,25 +167,31 @@ __global__ void __launch_bounds__(kWarps * 32, GT == 1 ? 4 : 2) kv_attention_ker
     // --- this CTA's share of the units: [begin, end); its first sequence and that sequence's first unit
     const int per = (n_seqs + kWarps * 32 - 1) / (kWarps * 32);
     int64_t mine = 0;
+    int longest = 0;
     for (int i = 0; i < per; ++i) {
         const int s = tid * per + i;
-        if (s < n_seqs) mine += (int64_t)units_of(p, s) * heads;
+        const int u = s < n_seqs ? units_of(p, s) : 0;
+        mine += (int64_t)u * heads;
+        longest = max(longest, u);
     }
+    longest = __reduce_max_sync(0xffffffffu, longest);
     int64_t incl = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
         const int64_t y = __shfl_up_sync(0xffffffffu, incl, o);
         if (lane >= o) incl += y;
     }
-    if (lane == 31) s_scan[warp] = incl;
+    if (lane == 31) { s_scan[warp] = incl; s_longest[warp] = longest; }
     __syncthreads();
     int64_t before = 0, total = 0;
 #pragma unroll
     for (int w = 0; w < kWarps; ++w) {
         if (w < warp) before += s_scan[w];
         total += s_scan[w];
+        longest = max(longest, s_longest[w]);
     }
-    const int64_t share = (total + gridDim.x - 1) / gridDim.x;
+    // equal shares, but no (sequence, head) in more than some kMaxParts parts: joining them is the work of one CTA
+    const int64_t share = max((total + gridDim.x - 1) / gridDim.x, (int64_t)(longest + kMaxParts - 1) / kMaxParts);
     const int64_t begin = share * blockIdx.x, end = min(begin + share, total);
     if (begin >= end) return;
     {
@@ -546,20 +553,56 @@ __global__ void __launch_bounds__(kWarps * 32, GT == 1 ? 4 : 2) kv_attention_ker
             __syncthreads();
             if (s_last) {
                 __threadfence();
-                for (int i = tid; i < p.group * D; i += kWarps * 32) {
-                    const int h = i / D, d = i % D;
-                    float mx = -INFINITY, so = 0.f, sl = 0.f;
-#pragma unroll 4
-                    for (int b = first; b <= last; ++b) {
-                        const int64_t k = (int64_t)(2 * b + (seg0 < share * b ? 0 : 1)) * H + h;
-                        const float2 ml = __ldcg(reinterpret_cast<const float2*>(p.part_ml) + k);
-                        const float x = __ldcg(p.part_o + k * D + d);
-                        const float nm = fmaxf(mx, ml.x), f0 = mx == nm ? 1.f : ex2(mx - nm), f1 = ml.x == nm ? 1.f : ex2(ml.x - nm);
-                        so = so * f0 + x * f1;
-                        sl = sl * f0 + ml.y * f1;
-                        mx = nm;
+                const int parts = last - first + 1;        // at most kMaxParts + 1
+                float* const s_f = reinterpret_cast<float*>(s_bytes);         // [parts][group]: maximum, then factor
+                float* const s_s = s_f + (kMaxParts + 1) * H;                 // [parts][group]: sum of p
+                float* const s_inv = s_s + (kMaxParts + 1) * H;               // [group]
+                float4* const s_part = reinterpret_cast<float4*>(s_inv + H);  // [slices][group * D / 4]
+                auto at_part = [&](int b) { return (int64_t)(2 * (first + b) + (seg0 < share * (first + b) ? 0 : 1)) * H; };
+                for (int i = tid; i < parts * p.group; i += kWarps * 32) {
+                    const float2 ml = __ldcg(reinterpret_cast<const float2*>(p.part_ml) + at_part(i / p.group) + i % p.group);
+                    s_f[i] = ml.x;
+                    s_s[i] = ml.y;
+                }
+                __syncthreads();
+                for (int h = warp; h < p.group; h += kWarps) {
+                    float mx = -INFINITY, sl = 0.f;
+                    for (int b = lane; b < parts; b += 32) mx = fmaxf(mx, s_f[b * p.group + h]);
+                    mx = warp_max(mx);
+                    for (int b = lane; b < parts; b += 32) {
+                        const float f = s_f[b * p.group + h] == mx ? 1.f : ex2(s_f[b * p.group + h] - mx);
+                        s_f[b * p.group + h] = f;
+                        sl = fmaf(f, s_s[b * p.group + h], sl);
                     }
-                    a.out[((int64_t)seq * a.q_heads + head * p.group + h) * D + d] = f_to_bf16(so / sl);
+                    sl = warp_sum(sl);
+                    if (lane == 0) s_inv[h] = 1.f / sl;
+                }
+                __syncthreads();
+                // a thread sums four channels over every slices-th part
+                const int items = p.group * D / 4, slices = items < kWarps * 32 ? kWarps * 32 / items : 1;
+                for (int i = tid; i < items * slices; i += kWarps * 32) {
+                    const int item = i % items, h = item / (D / 4);
+                    float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
+                    for (int b = i / items; b < parts; b += slices) {
+                        const float4 x = __ldcg(reinterpret_cast<const float4*>(p.part_o + at_part(b) * D) + item);
+                        const float f = s_f[b * p.group + h];
+                        y.x = fmaf(f, x.x, y.x); y.y = fmaf(f, x.y, y.y); y.z = fmaf(f, x.z, y.z); y.w = fmaf(f, x.w, y.w);
+                    }
+                    s_part[i] = y;
+                }
+                __syncthreads();
+                for (int i = tid; i < items; i += kWarps * 32) {
+                    float4 y = s_part[i];
+                    for (int k = 1; k < slices; ++k) {
+                        const float4 x = s_part[k * items + i];
+                        y.x += x.x; y.y += x.y; y.z += x.z; y.w += x.w;
+                    }
+                    const float inv = s_inv[i / (D / 4)];
+                    uint2 w;
+                    w.x = pack_bf16x2(y.x * inv, y.y * inv);
+                    w.y = pack_bf16x2(y.z * inv, y.w * inv);
+                    reinterpret_cast<uint2*>(a.out + ((int64_t)seq * a.q_heads + head * p.group) * D)[i] = w;
                 }
             }
         }
