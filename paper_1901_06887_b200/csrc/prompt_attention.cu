@@ -1,59 +1,550 @@
-// Causal attention over packed prompts.  First form: one warp per (token, head), online softmax, fp32.
+// Causal attention over packed prompts on the tensor cores.
+//
+// Mathematics.  o_i = sum_{j <= i} p_ij v_j / sum_{j <= i} p_ij, p_ij = 2^(c (q_i . k_j - m_i)), c = scale log2(e), in one pass over blocks of
+// 128 keys.  m_i is a running reference, not the maximum: it moves, and the sums so far are rescaled, only when a block's maximum lies
+// more than 8 above it (in log2); until then p is at most 2^8, which fp32 sums and the bf16 p hold as exactly as 1.
+//
+// Tile.  A CTA owns two tiles of 128 rows (one tensor-memory accumulator each) and streams the keys and values that either needs.
+// A row is a (token, head) pair: R heads that share a key/value head (the largest power of two in the group) are packed into the rows, so
+// short prompts fill the tile and the keys are read once for R heads.  Rows of a tile then lie in one block of 128 keys, so only
+// a tile's last block is masked.
+//
+// Roles (12 warps): warps 0-3 and 4-7 are the softmax of the two tiles, one row per thread; warp 8 copies (TMA), warp 9 issues the
+// matrix instructions, warps 10 and 11 clean masked value blocks.  S = Q K^T goes to tensor memory, comes to registers, goes back as bf16 P
+// over the columns of S, and P V takes P from there.  While one tile is in its softmax the other has the tensor cores.
+//
+// Masked positions.  p of a masked key is zero, but zero times an infinity is NaN, so values that some row must not see are made
+// harmless in shared memory before the product: rows past the sequence's end are zeroed, and an element that is not finite in a
+// masked block is zeroed and noted, the first token per channel; rows at or after that token get NaN there in the epilogue.
+//
+// Order of work.  Tiles of all sequences, longest first, dealt back and forth over one CTA per SM; every CTA derives the list from the
+// offsets (sequences ranked by length; tile numbers between the lengths of ranks r and r + 1 exist for exactly r + 1 sequences).
 #include "lm_device.cuh"
 #include "lm_host.h"
 
 namespace mt {
 namespace {
 
-__device__ int find_seq(const int32_t* offsets, int n_seqs, int tok) {
-    for (int s = 0; s < n_seqs; ++s)
-        if (offsets[s] <= tok && tok < offsets[s + 1]) return s;
-    return -1;
+constexpr int kThreads = 384;
+constexpr int kBlock = 128;                   // keys per block, rows per tile
+constexpr int kHalf = kBlock * 128;           // bytes of a 128-row, 64-channel operand
+constexpr int kMaxSeqs = 512;                 // sequences of one launch
+constexpr float kSlack = 8.f;
+
+template <int D> __host__ __device__ constexpr int slots() { return D == 128 ? 4 : 8; }
+template <int D> __host__ __device__ constexpr int operand_bytes() { return kHalf * (D / 64); }
+
+struct Control {
+    uint64_t q_full[2], q_empty, s_full[2], p_ready[2], o_ready[2], epi_done[2], kv_full[8], kv_empty[8], v_raw[8], v_clean[8];
+    uint32_t tmem;
+    int abort;
+    int poison[2];                            // round + 1 of a tile with notes
+    unsigned long long first_bad[2][128];     // per channel: (0x7fffffff - round, first token that is not finite); later rounds win the minimum
+    int start[kMaxSeqs], len[kMaxSeqs], order[kMaxSeqs], before[kMaxSeqs + 1];
+    int total;
+};
+template <int D> constexpr int shared_bytes() { return 1024 + (2 + slots<D>()) * operand_bytes<D>() + (int)sizeof(Control); }
+
+struct PromptParams {
+    const int32_t* offsets;
+    int n_seqs, seq0, n_tokens;
+    int q_heads, group, pack, pack_shift;     // pack: heads packed into a tile's rows
+    float c;                                  // |scale| log2(e)
+    int negate;                               // scale < 0
+    uint16_t* out;
+    int32_t* status;
+};
+
+// D (+)= A B with A in tensor memory.
+__device__ __forceinline__ void umma_bf16_tmem_a(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t"
+        ".reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t"
+        "}\n"
+        ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&v)[16]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+        ::"r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]), "r"(v[10]),
+        "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15])
+        : "memory");
+}
+__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map, int c0, int c1, int c2, uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+        ::"r"(dst), "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(bar)
+        : "memory");
+}
+__device__ __forceinline__ float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// Operand descriptors, 128-byte swizzle.  Keys and queries: channels contiguous (the product's inner index).  Values: the inner index is the
+// token, channels are the outer one: 8-token groups 1024 bytes apart, 64-channel halves kHalf apart.
+__device__ __forceinline__ uint64_t desc_outer_major(uint32_t smem_addr) {
+    uint64_t d = 0;
+    d |= static_cast<uint64_t>((smem_addr & 0x3FFFF) >> 4);
+    d |= static_cast<uint64_t>(kHalf >> 4) << 16;
+    d |= static_cast<uint64_t>(1024 >> 4) << 32;
+    d |= static_cast<uint64_t>(1) << 46;
+    d |= static_cast<uint64_t>(2) << 61;
+    return d;
+}
+
+struct Item {
+    int seq, start, len, t0, pack;            // first row of the sequence, its length, first token of the tile pair, head pack
+    int nb[2];                                // key blocks of the two tiles (0: no rows)
+};
+
+__device__ __forceinline__ bool get_item(const Control& s, const PromptParams& p, int round, Item& it) {
+    const int packs = p.q_heads >> p.pack_shift;
+    const int64_t x = (int64_t)round * gridDim.x + ((round & 1) ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
+    if (x >= (int64_t)s.total * packs) return false;
+    const int k = (int)(x / packs);
+    it.pack = (int)(x % packs);
+    const int tokens = 256 >> p.pack_shift;   // of the tile pair
+    int lo = 0, hi = p.n_seqs - 1;            // rank r with before[r] <= k < before[r + 1]
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (s.before[mid] <= k) lo = mid; else hi = mid - 1;
+    }
+    const int q = k - s.before[lo];
+    const int tile = (s.len[s.order[lo]] + tokens - 1) / tokens - 1 - q / (lo + 1);
+    it.seq = s.order[q % (lo + 1)];
+    it.start = s.start[it.seq];
+    it.len = s.len[it.seq];
+    it.t0 = tile * tokens;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int first = it.t0 + i * (tokens / 2), last = min(first + tokens / 2, it.len) - 1;
+        it.nb[i] = first < it.len ? last / kBlock + 1 : 0;
+    }
+    return true;
 }
 
 template <int D>
-__global__ void prompt_simple(PromptArgs a) {
-    pdl_launch_dependents();
-    pdl_wait();
-    const int warp = (blockIdx.x * blockDim.x + threadIdx.x) / 32, lane = threadIdx.x & 31;
-    const int tok = warp / a.d.q_heads, h = warp % a.d.q_heads;
-    if (warp == 0 && lane == 0)
-        for (int i = 0; i < a.d.n_seqs; ++i)
-            if (a.offsets[i] < 0 || a.offsets[i + 1] < a.offsets[i] || a.offsets[i + 1] > a.d.n_tokens)
-                raise_status(a.status, MT_ERR_INVALID_ARG, i);
-    if (tok >= a.d.n_tokens) return;
-    const int s = find_seq(a.offsets, a.d.n_seqs, tok);
-    if (s < 0) return;
-    const int lo = a.offsets[s];
-    if (lo < 0 || a.offsets[s + 1] > a.d.n_tokens) return;
-    const int hk = h / (a.d.q_heads / a.d.kv_heads);
-    constexpr int E = D / 32;
-    float q[E], o[E] = {}, m = -INFINITY, l = 0.f;
-    for (int e = 0; e < E; ++e) q[e] = bf16_to_f(a.q[tok * a.d.q_token_stride + h * a.d.q_head_stride + lane + 32 * e]) * a.d.scale;
-    for (int j = lo; j <= tok; ++j) {
-        float x = 0.f;
-        for (int e = 0; e < E; ++e) x += q[e] * bf16_to_f(a.k[j * a.d.k_token_stride + hk * a.d.k_head_stride + lane + 32 * e]);
-        x = warp_sum(x);
-        const float mn = fmaxf(m, x), c = (m == mn) ? 1.f : __expf(m - mn), p = __expf(x - mn);
-        for (int e = 0; e < E; ++e)
-            o[e] = o[e] * c + p * bf16_to_f(a.v[j * a.d.v_token_stride + hk * a.d.v_head_stride + lane + 32 * e]);
-        l = l * c + p;
-        m = mn;
+__global__ void __launch_bounds__(kThreads, 1)
+prompt_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
+                        const __grid_constant__ CUtensorMap map_v, const PromptParams p) {
+    extern __shared__ uint8_t smem_raw[];
+    constexpr int kSlots = slots<D>(), kOp = operand_bytes<D>();
+    const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
+    uint8_t* const smem = smem_raw + (base - raw);
+    Control& s = *reinterpret_cast<Control*>(smem + (2 + kSlots) * kOp);
+    const uint32_t q_smem = base, kv_smem = base + 2 * kOp;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    volatile int* const abort_flag = &s.abort;
+    auto bar = [](const uint64_t& b) { return smem_u32(&b); };
+
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(bar(s.q_full[i]), 1); mbar_init(bar(s.s_full[i]), 1); mbar_init(bar(s.p_ready[i]), 128);
+            mbar_init(bar(s.o_ready[i]), 1); mbar_init(bar(s.epi_done[i]), 256);
+            s.poison[i] = 0;
+        }
+        mbar_init(bar(s.q_empty), 1);
+        for (int i = 0; i < kSlots; ++i) { mbar_init(bar(s.kv_full[i]), 1); mbar_init(bar(s.kv_empty[i]), 1); mbar_init(bar(s.v_raw[i]), 1); mbar_init(bar(s.v_clean[i]), 64); }
+        s.abort = 0;
+        fence_mbar_init();
     }
-    for (int e = 0; e < E; ++e)
-        a.out[((int64_t)tok * a.d.q_heads + h) * D + lane + 32 * e] = f_to_bf16(o[e] / l);
+    if (threadIdx.x < 256) s.first_bad[threadIdx.x >> 7][threadIdx.x & 127] = ~0ull;
+    if (warp == 9 && lane == 0) { prefetch_tensormap(&map_q); prefetch_tensormap(&map_k); prefetch_tensormap(&map_v); }
+    pdl_wait();
+    // All of tensor memory, taken only when the predecessor is done with its share, and before a successor may start and ask for its own.
+    if (warp == 8) {
+        tmem_alloc(smem_u32(&s.tmem), 512);
+        tmem_relinquish();
+    }
+
+    // --- the list of tiles: sequences ranked by length
+    const int tokens = 256 >> p.pack_shift;
+    for (int i = threadIdx.x; i < p.n_seqs; i += kThreads) {
+        const int a = p.offsets[i], b = p.offsets[i + 1];
+        const bool bad = a < 0 || b < a || b > p.n_tokens;
+        if (bad && blockIdx.x == 0) raise_status(p.status, MT_ERR_INVALID_ARG, p.seq0 + i);
+        s.start[i] = a;
+        s.len[i] = bad ? 0 : b - a;
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < p.n_seqs; i += kThreads) {
+        const int n = s.len[i];
+        int rank = 0;
+        for (int j = 0; j < p.n_seqs; ++j) { const int m = s.len[j]; rank += (m > n || (m == n && j < i)) ? 1 : 0; }
+        s.order[rank] = i;
+    }
+    __syncthreads();
+    if (warp == 0) {                            // before[r]: tiles whose number is shared by fewer than r + 1 sequences
+        int run = 0;
+        for (int r0 = 0; r0 < p.n_seqs; r0 += 32) {
+            const int r = r0 + lane;
+            int v = 0;
+            if (r < p.n_seqs) {
+                const int mine = (s.len[s.order[r]] + tokens - 1) / tokens;
+                const int next = r + 1 < p.n_seqs ? (s.len[s.order[r + 1]] + tokens - 1) / tokens : 0;
+                v = (r + 1) * (mine - next);
+            }
+            int incl = v;
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) {
+                const int y = __shfl_up_sync(0xffffffffu, incl, d);
+                if (lane >= d) incl += y;
+            }
+            if (r < p.n_seqs) s.before[r] = run + incl - v;
+            run += __shfl_sync(0xffffffffu, incl, 31);
+        }
+        if (lane == 0) { s.before[p.n_seqs] = run; s.total = run; }
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    pdl_launch_dependents();
+    const uint32_t tmem = s.tmem;
+    const uint32_t tmem_s = tmem, tmem_o = tmem + 256;         // S (and P) of tile i: + 128 i; O: + D i
+    const int head_of_pack = p.pack;
+
+    if (warp == 8) {
+        // ------------------------------------------------------------------------------------------ copies
+        if (lane == 0) {
+            int fill = 0;                        // operands put into the ring so far
+            uint32_t raw_phase = 0, raw_used = 0;
+            bool ok = true;
+            Item it;
+            for (int round = 0; ok && get_item(s, p, round, it); ++round) {
+                if (round > 0) ok = mbar_wait(bar(s.q_empty), (round - 1) & 1, abort_flag, p.status, 200);
+                if (!ok) break;
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    if (it.nb[i] == 0) continue;
+                    mbar_expect_tx(bar(s.q_full[i]), kOp);
+                    for (int h = 0; h < D / 64; ++h)
+                        tma_load_3d(q_smem + i * kOp + h * kHalf, &map_q, h * 64, it.pack * head_of_pack, it.start + it.t0 + i * (tokens / 2), bar(s.q_full[i]));
+                }
+                const int kv_head = it.pack * p.pack / p.group;
+                const int nb = max(it.nb[0], it.nb[1]);
+                for (int x = 0; ok && x < 2 * nb; ++x, ++fill) {
+                    const int slot = fill % kSlots, use = fill / kSlots;
+                    if (use > 0) ok = mbar_wait(bar(s.kv_empty[slot]), (use - 1) & 1, abort_flag, p.status, 201);
+                    if (!ok) break;
+                    // a masked value block goes to the cleaners first: its bytes count on v_raw, and v_clean says when it may be used
+                    const bool masked = (x & 1) && ((x >> 1) == it.nb[0] - 1 || (x >> 1) == it.nb[1] - 1);
+                    const uint32_t full = masked ? bar(s.v_raw[slot]) : bar(s.kv_full[slot]);
+                    mbar_expect_tx(full, kOp);
+                    for (int h = 0; h < D / 64; ++h)
+                        tma_load_3d(kv_smem + slot * kOp + h * kHalf, (x & 1) ? &map_v : &map_k, h * 64, kv_head, it.start + (x >> 1) * kBlock, full);
+                    if (masked) {
+                        mbar_arrive(bar(s.kv_full[slot]));
+                        raw_phase ^= 1u << slot;
+                        raw_used |= 1u << slot;
+                    }
+                }
+            }
+            if (!ok) {                           // let copies in flight land before the memory goes
+                for (int x = max(0, fill - kSlots); x < fill; ++x) mbar_wait_short(bar(s.kv_full[x % kSlots]), (x / kSlots) & 1);
+                for (int i = 0; i < kSlots; ++i)
+                    if (raw_used >> i & 1) mbar_wait_short(bar(s.v_raw[i]), (raw_phase >> i & 1) ^ 1);
+            }
+        }
+    } else if (warp == 9) {
+        // ------------------------------------------------------------------------------------------ matrix instructions
+        if (lane == 0) {
+            constexpr uint32_t kIdPv = make_idesc_bf16(128, D) | (1u << 16);
+            const uint32_t id_qk = make_idesc_bf16(128, kBlock) | (p.negate ? 1u << 13 : 0u);
+            int fill = 0, n_q[2] = {0, 0}, n_p[2] = {0, 0};
+            uint32_t clean_phase = 0;
+            bool ok = true;
+            Item it;
+            auto wait = [&](const uint64_t& b, int parity, int where) { ok = ok && mbar_wait(bar(b), parity & 1, abort_flag, p.status, where); };
+            for (int round = 0; ok && get_item(s, p, round, it); ++round) {
+                const int nb = max(it.nb[0], it.nb[1]);
+                auto qk = [&](int i, int j) {
+                    const int slot = (fill + 2 * j) % kSlots;
+#pragma unroll
+                    for (int k = 0; k < D / 16; ++k) {
+                        const uint32_t off = (k / 4) * kHalf + (k % 4) * 32;
+                        umma_bf16(tmem_s + 128 * i, make_kmajor_sw128_desc(q_smem + i * kOp + off, 1024),
+                                  make_kmajor_sw128_desc(kv_smem + slot * kOp + off, 1024), id_qk, k > 0);
+                    }
+                    umma_commit(bar(s.s_full[i]));
+                };
+                wait(s.kv_full[fill % kSlots], fill / kSlots, 210);
+                for (int i = 0; i < 2 && ok; ++i)
+                    if (it.nb[i] > 0) {
+                        wait(s.q_full[i], n_q[i]++, 211);
+                        if (!ok) break;
+                        tc_fence_after();
+                        qk(i, 0);
+                    }
+                if (!ok) break;
+                umma_commit(bar(s.kv_empty[fill % kSlots]));
+                if (nb == 1) umma_commit(bar(s.q_empty));
+                for (int j = 0; ok && j < nb; ++j) {
+                    const int vx = fill + 2 * j + 1, vslot = vx % kSlots, kx = vx + 1;
+                    wait(s.kv_full[vslot], vx / kSlots, 212);
+                    if (j == it.nb[0] - 1 || j == it.nb[1] - 1) {
+                        wait(s.v_clean[vslot], clean_phase >> vslot, 213);
+                        clean_phase ^= 1u << vslot;
+                    }
+                    if (!ok) break;
+                    for (int i = 0; i < 2; ++i) {
+                        if (j < it.nb[i]) {
+                            wait(s.p_ready[i], n_p[i]++, 214);
+                            if (!ok) break;
+                            tc_fence_after();
+#pragma unroll
+                            for (int k = 0; k < kBlock / 16; ++k)
+                                umma_bf16_tmem_a(tmem_o + D * i, tmem_s + 128 * i + 8 * k, desc_outer_major(kv_smem + vslot * kOp + k * 2048), kIdPv,
+                                                 j > 0 || k > 0);
+                            umma_commit(bar(s.o_ready[i]));
+                        }
+                        if (j + 1 < it.nb[i]) {
+                            wait(s.kv_full[kx % kSlots], kx / kSlots, 215);
+                            if (!ok) break;
+                            tc_fence_after();
+                            qk(i, j + 1);
+                        }
+                    }
+                    if (!ok) break;
+                    umma_commit(bar(s.kv_empty[vslot]));
+                    if (j + 1 < nb) umma_commit(bar(s.kv_empty[kx % kSlots]));
+                    if (j + 2 == nb) umma_commit(bar(s.q_empty));
+                }
+                fill += 2 * nb;
+            }
+        }
+    } else if (warp >= 10) {
+        // ------------------------------------------------------------------------------------------ masked value blocks
+        const int t = threadIdx.x - 320;         // rows t and t + 64
+        int fill = 0;
+        uint32_t raw_phase = 0;
+        bool ok = true;
+        Item it;
+        for (int round = 0; ok && get_item(s, p, round, it); ++round) {
+            const int nb = max(it.nb[0], it.nb[1]), buf = round & 1;
+            if (round >= 2) {                    // the notes of two tiles ago have been read
+                ok = mbar_wait(bar(s.epi_done[buf]), ((round >> 1) - 1) & 1, abort_flag, p.status, 220);
+                if (!ok) break;
+            }
+            for (int j = it.nb[0] - 1; ok && j < nb; ++j) {
+                if (!(j == it.nb[0] - 1 || j == it.nb[1] - 1)) continue;
+                const int slot = (fill + 2 * j + 1) % kSlots;
+                ok = mbar_wait(bar(s.v_raw[slot]), (raw_phase >> slot) & 1, abort_flag, p.status, 221);
+                if (!ok) break;
+                raw_phase ^= 1u << slot;
+                uint8_t* const v = smem + (2 + slot) * kOp;
+                for (int r = t; r < kBlock; r += 64) {
+                    const int tok = j * kBlock + r;
+#pragma unroll
+                    for (int c = 0; c < D / 8; ++c) {
+                        uint4* const at = reinterpret_cast<uint4*>(v + (c / 8) * kHalf + r * 128 + (((c & 7) ^ (r & 7)) << 4));
+                        if (tok >= it.len) { *at = make_uint4(0, 0, 0, 0); continue; }
+                        const uint4 w = *at;
+                        const uint32_t x[4] = {w.x, w.y, w.z, w.w};
+                        uint32_t any = 0;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) any |= ((x[e] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
+                        if (any) {
+                            const unsigned long long note = (unsigned long long)(0x7fffffff - round) << 32 | (uint32_t)tok;
+                            uint32_t y[4];
+                            for (int e = 0; e < 4; ++e) {
+                                y[e] = x[e];
+                                if ((x[e] & 0x7f80u) == 0x7f80u) { y[e] &= 0xffff0000u; atomicMin(&s.first_bad[buf][c * 8 + 2 * e], note); }
+                                if ((x[e] & 0x7f800000u) == 0x7f800000u) { y[e] &= 0x0000ffffu; atomicMin(&s.first_bad[buf][c * 8 + 2 * e + 1], note); }
+                            }
+                            *at = make_uint4(y[0], y[1], y[2], y[3]);
+                            s.poison[buf] = round + 1;
+                        }
+                    }
+                }
+                fence_proxy_async_smem();
+                __threadfence_block();
+                mbar_arrive(bar(s.v_clean[slot]));
+            }
+            fill += 2 * nb;
+        }
+    } else {
+        // ------------------------------------------------------------------------------------------ softmax, one row per thread
+        const int i = warp >> 2;
+        const int r = threadIdx.x & 127;
+        const uint32_t lanes = (uint32_t)(warp & 3) << 21;     // tensor-memory lane of the warp's first row, in the address's upper half
+        const uint32_t my_s = tmem_s + 128 * i + lanes, my_o = tmem_o + D * i + lanes;
+        int n_s = 0, n_o = 0;
+        bool ok = true;
+        Item it;
+        for (int round = 0; ok && get_item(s, p, round, it); ++round) {
+            const int nb = it.nb[i], buf = round & 1;
+            const int tok = it.t0 + i * (tokens / 2) + (r >> p.pack_shift);
+            float m = 0.f, l = 0.f;
+            for (int j = 0; j < nb; ++j) {
+                ok = mbar_wait(bar(s.s_full[i]), n_s++ & 1, abort_flag, p.status, 230);
+                if (!ok) break;
+                tc_fence_after();
+                uint32_t x[4][32];
+#pragma unroll
+                for (int c = 0; c < 4; ++c) tmem_ld32(my_s + 32 * c, x[c]);
+                tmem_ld_wait();
+                if (j == nb - 1) {
+                    const int lim = tok - j * kBlock;          // keys of the block up to here are seen
+#pragma unroll
+                    for (int c = 0; c < 4; ++c)
+#pragma unroll
+                        for (int e = 0; e < 32; ++e)
+                            if (32 * c + e > lim) x[c][e] = 0xff800000u;
+                }
+                float mx = -INFINITY;
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) mx = fmaxf(mx, __uint_as_float(x[c][e]));
+                if (j == 0) {
+                    m = mx;
+                } else if (__any_sync(0xffffffffu, (mx - m) * p.c > kSlack)) {
+                    // (a row moves on its own account only, so its bits do not depend on its neighbours)
+                    const float nm = (mx - m) * p.c > kSlack ? mx : m, f = m == nm ? 1.f : ex2((m - nm) * p.c);
+                    m = nm;
+                    l *= f;
+                    ok = mbar_wait(bar(s.o_ready[i]), (n_o - 1) & 1, abort_flag, p.status, 231);
+                    if (!ok) break;
+                    tc_fence_after();
+#pragma unroll 1
+                    for (int c = 0; c < D / 16; ++c) {
+                        uint32_t y[16];
+                        asm volatile(
+                            "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+                            : "=r"(y[0]), "=r"(y[1]), "=r"(y[2]), "=r"(y[3]), "=r"(y[4]), "=r"(y[5]), "=r"(y[6]), "=r"(y[7]), "=r"(y[8]), "=r"(y[9]),
+                              "=r"(y[10]), "=r"(y[11]), "=r"(y[12]), "=r"(y[13]), "=r"(y[14]), "=r"(y[15])
+                            : "r"(my_o + 16 * c) : "memory");
+                        tmem_ld_wait();
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) y[e] = __float_as_uint(__uint_as_float(y[e]) * f);
+                        tmem_st16(my_o + 16 * c, y);
+                    }
+                }
+                const float shift = -m * p.c;
+                float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    uint32_t w[16];
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const float a = ex2(fmaf(__uint_as_float(x[c][2 * e]), p.c, shift));
+                        const float b = ex2(fmaf(__uint_as_float(x[c][2 * e + 1]), p.c, shift));
+                        sum[e & 1] += a;
+                        sum[2 + (e & 1)] += b;
+                        w[e] = pack_bf16x2(a, b);
+                    }
+                    tmem_st16(my_s + 16 * c, w);
+                }
+                l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+                tmem_st_wait();
+                tc_fence_before();
+                mbar_arrive(bar(s.p_ready[i]));
+                ++n_o;
+            }
+            if (!ok) break;
+            if (nb > 0) {
+                ok = mbar_wait(bar(s.o_ready[i]), (n_o - 1) & 1, abort_flag, p.status, 232);
+                if (!ok) break;
+                tc_fence_after();
+                const float inv = 1.f / l;
+                const bool poison = *(volatile int*)&s.poison[buf] == round + 1;
+                const int head = it.pack * p.pack + (r & (p.pack - 1));
+                uint16_t* const out = p.out + ((int64_t)(it.start + tok) * p.q_heads + head) * D;
+#pragma unroll
+                for (int c = 0; c < D / 32; ++c) {
+                    uint32_t y[32];
+                    tmem_ld32(my_o + 32 * c, y);
+                    tmem_ld_wait();
+                    if (poison) {
+                        const unsigned long long note = (unsigned long long)(0x7fffffff - round) << 32 | (uint32_t)tok;
+#pragma unroll
+                        for (int e = 0; e < 32; ++e)
+                            if (s.first_bad[buf][32 * c + e] <= note) y[e] = 0x7fffffffu;     // an older round's note is larger
+                    }
+                    if (tok < it.len) {
+#pragma unroll
+                        for (int v = 0; v < 4; ++v) {
+                            uint4 w;
+                            w.x = pack_bf16x2(__uint_as_float(y[8 * v]) * inv, __uint_as_float(y[8 * v + 1]) * inv);
+                            w.y = pack_bf16x2(__uint_as_float(y[8 * v + 2]) * inv, __uint_as_float(y[8 * v + 3]) * inv);
+                            w.z = pack_bf16x2(__uint_as_float(y[8 * v + 4]) * inv, __uint_as_float(y[8 * v + 5]) * inv);
+                            w.w = pack_bf16x2(__uint_as_float(y[8 * v + 6]) * inv, __uint_as_float(y[8 * v + 7]) * inv);
+                            reinterpret_cast<uint4*>(out)[c * 4 + v] = w;
+                        }
+                    }
+                }
+                tc_fence_before();
+            }
+            mbar_arrive(bar(s.epi_done[buf]));
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 8) {
+        tc_fence_after();
+        tmem_dealloc(tmem, 512);
+    }
+}
+
+mt_status encode_rows(const OpContext& c, CUtensorMap* map, const uint16_t* ptr, int d, int heads, int tokens, int64_t head_stride,
+                      int64_t token_stride, int box_heads, int box_tokens) {
+    const cuuint64_t dims[3] = {(cuuint64_t)d, (cuuint64_t)heads, (cuuint64_t)tokens};
+    const cuuint64_t strides[2] = {(cuuint64_t)head_stride * 2, (cuuint64_t)token_stride * 2};
+    const cuuint32_t box[3] = {64, (cuuint32_t)box_heads, (cuuint32_t)box_tokens};
+    const cuuint32_t one[3] = {1, 1, 1};
+    const CUresult r = c.encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<uint16_t*>(ptr), dims, strides, box, one,
+                                CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? MT_OK : MT_ERR_CUDA;
 }
 
 }  // namespace
 
-cudaError_t configure_prompt_attention() { return cudaSuccess; }
+cudaError_t configure_prompt_attention() {
+    cudaError_t e = cudaFuncSetAttribute(prompt_attention_kernel<64>, cudaFuncAttributeMaxDynamicSharedMemorySize, shared_bytes<64>());
+    if (e == cudaSuccess)
+        e = cudaFuncSetAttribute(prompt_attention_kernel<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, shared_bytes<128>());
+    return e;
+}
 
-mt_status launch_prompt_attention(const PromptArgs& a, const OpContext&, cudaStream_t s) {
-    const int64_t warps = (int64_t)a.d.n_tokens * a.d.q_heads;
-    const dim3 grid((unsigned)((warps + 7) / 8));
-    const cudaError_t e = a.d.head_dim == 64 ? launch_pdl(prompt_simple<64>, grid, dim3(256), 0, s, a)
-                                             : launch_pdl(prompt_simple<128>, grid, dim3(256), 0, s, a);
-    return e == cudaSuccess ? MT_OK : MT_ERR_CUDA;
+mt_status launch_prompt_attention(const PromptArgs& a, const OpContext& c, cudaStream_t s) {
+    const mt_prompt_desc& d = a.d;
+    PromptParams p;
+    p.n_tokens = d.n_tokens;
+    p.q_heads = d.q_heads;
+    p.group = d.q_heads / d.kv_heads;
+    p.pack = 1;
+    p.pack_shift = 0;
+    while (p.pack < 16 && p.group % (2 * p.pack) == 0) { p.pack *= 2; ++p.pack_shift; }
+    p.c = fmaxf(fabsf(d.scale) * 1.44269504088896341f, 1e-30f);   // not zero: minus infinity has to stay what it is
+    p.negate = d.scale < 0.f;
+    p.out = a.out;
+    p.status = a.status;
+    CUtensorMap mq, mk, mv;
+    mt_status st = encode_rows(c, &mq, a.q, d.head_dim, d.q_heads, d.n_tokens, d.q_head_stride, d.q_token_stride, p.pack, 128 / p.pack);
+    if (st == MT_OK) st = encode_rows(c, &mk, a.k, d.head_dim, d.kv_heads, d.n_tokens, d.k_head_stride, d.k_token_stride, 1, kBlock);
+    if (st == MT_OK) st = encode_rows(c, &mv, a.v, d.head_dim, d.kv_heads, d.n_tokens, d.v_head_stride, d.v_token_stride, 1, kBlock);
+    if (st != MT_OK) return st;
+    for (int seq0 = 0; seq0 < d.n_seqs; seq0 += kMaxSeqs) {
+        p.seq0 = seq0;
+        p.n_seqs = d.n_seqs - seq0 < kMaxSeqs ? d.n_seqs - seq0 : kMaxSeqs;
+        p.offsets = a.offsets + seq0;
+        // no more CTAs than there can be tiles
+        const int64_t most = (((int64_t)d.n_tokens * p.pack + 255) / 256 + p.n_seqs) * (d.q_heads / p.pack);
+        const unsigned grid = (unsigned)(most < c.sm_count ? most : c.sm_count);
+        const cudaError_t e = d.head_dim == 64
+            ? launch_pdl(prompt_attention_kernel<64>, dim3(grid), dim3(kThreads), (size_t)shared_bytes<64>(), s, mq, mk, mv, p)
+            : launch_pdl(prompt_attention_kernel<128>, dim3(grid), dim3(kThreads), (size_t)shared_bytes<128>(), s, mq, mk, mv, p);
+        if (e != cudaSuccess) return MT_ERR_CUDA;
+        if (d.n_seqs - seq0 <= kMaxSeqs) break;
+    }
+    return MT_OK;
 }
 
 }  // namespace mt
