@@ -56,14 +56,17 @@ struct PromptParams {
 };
 
 // D (+)= A B with A in tensor memory.
-__device__ __forceinline__ void umma_bf16_tmem_a(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+template <bool ACC>
+__device__ __forceinline__ void umma_tmem_a_lohi(uint32_t d_tmem, uint32_t a_tmem, uint32_t b_lo, uint32_t idesc) {
     asm volatile(
         "{\n\t"
         ".reg .pred p;\n\t"
-        "setp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t"
+        ".reg .b64 db;\n\t"
+        "setp.ne.b32 p, %5, 0;\n\t"
+        "mov.b64 db, {%2, %3};\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %4, p;\n\t"
         "}\n"
-        ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
+        ::"r"(d_tmem), "r"(a_tmem), "r"(b_lo), "r"(kDescHiSw128), "r"(idesc), "n"(ACC ? 1 : 0)
         : "memory");
 }
 __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&v)[16]) {
@@ -86,17 +89,10 @@ __device__ __forceinline__ float ex2(float x) {
     return y;
 }
 
-// Operand descriptors, 128-byte swizzle.  Keys and queries: channels contiguous (the product's inner index).  Values: the inner index is the
-// token, channels are the outer one: 8-token groups 1024 bytes apart, 64-channel halves kHalf apart.
-__device__ __forceinline__ uint64_t desc_outer_major(uint32_t smem_addr) {
-    uint64_t d = 0;
-    d |= static_cast<uint64_t>((smem_addr & 0x3FFFF) >> 4);
-    d |= static_cast<uint64_t>(kHalf >> 4) << 16;
-    d |= static_cast<uint64_t>(1024 >> 4) << 32;
-    d |= static_cast<uint64_t>(1) << 46;
-    d |= static_cast<uint64_t>(2) << 61;
-    return d;
-}
+// Descriptor words of the values, 128-byte swizzle with the channels contiguous: the product's inner index is the token (8-token groups 1024
+// bytes apart, as in the row-major form), and the 64-channel halves lie kHalf apart.
+constexpr uint32_t kHalfField = static_cast<uint32_t>(kHalf >> 4) << 16;
+__device__ __forceinline__ uint32_t desc_lo_values(uint32_t smem_addr) { return ((smem_addr & 0x3FFFFu) >> 4) | kHalfField; }
 
 struct Item {
     int seq, start, len, t0, pack;            // first row of the sequence, its length, first token of the tile pair, head pack
@@ -253,70 +249,87 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
         }
     } else if (warp == 9) {
         // ------------------------------------------------------------------------------------------ matrix instructions
-        if (lane == 0) {
-            constexpr uint32_t kIdPv = make_idesc_bf16(128, D) | (1u << 16);
-            const uint32_t id_qk = make_idesc_bf16(128, kBlock) | (p.negate ? 1u << 13 : 0u);
-            int fill = 0, n_q[2] = {0, 0}, n_p[2] = {0, 0};
-            uint32_t clean_phase = 0;
-            bool ok = true;
-            Item it;
-            auto wait = [&](const uint64_t& b, int parity, int where) { ok = ok && mbar_wait(bar(b), parity & 1, abort_flag, p.status, where); };
-            for (int round = 0; ok && get_item(s, p, round, it); ++round) {
-                const int nb = max(it.nb[0], it.nb[1]);
-                auto qk = [&](int i, int j) {
-                    const int slot = (fill + 2 * j) % kSlots;
+        // The whole warp walks the loop, so that addresses stay warp-uniform; one elected lane issues.  (One lane alone, with descriptors
+        // built per instruction, took 115 cycles for each of them: 1900 for the sixteen that a tile's block needs, against 512 of work.)
+        const bool leader = elect_one();
+        constexpr uint32_t kIdPv = make_idesc_bf16(128, D) | (1u << 16);
+        const uint32_t id_qk = make_idesc_bf16(128, kBlock) | (p.negate ? 1u << 13 : 0u);
+        const uint32_t q_lo = desc_lo(q_smem), k_lo = desc_lo(kv_smem), v_lo = desc_lo_values(kv_smem);
+        const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
+        constexpr uint32_t kOpLo = kOp >> 4;
+        uint32_t fill = 0, n_q0 = 0, n_q1 = 0, n_p0 = 0, n_p1 = 0, clean_phase = 0;
+        bool ok = true;
+        Item it;
+        auto wait = [&](const uint64_t& b, uint32_t parity, int where) { ok = ok && mbar_wait(bar(b), parity & 1, abort_flag, p.status, where); };
+        auto qk = [&](int i, uint32_t slot) {
+            if (leader) {
+                const uint32_t d = tm + 128 * i, a = q_lo + i * kOpLo, b = k_lo + slot * kOpLo;
+                umma_bf16_lohi<false>(d, a, b, id_qk);
 #pragma unroll
-                    for (int k = 0; k < D / 16; ++k) {
-                        const uint32_t off = (k / 4) * kHalf + (k % 4) * 32;
-                        umma_bf16(tmem_s + 128 * i, make_kmajor_sw128_desc(q_smem + i * kOp + off, 1024),
-                                  make_kmajor_sw128_desc(kv_smem + slot * kOp + off, 1024), id_qk, k > 0);
-                    }
-                    umma_commit(bar(s.s_full[i]));
-                };
-                wait(s.kv_full[fill % kSlots], fill / kSlots, 210);
-                for (int i = 0; i < 2 && ok; ++i)
-                    if (it.nb[i] > 0) {
-                        wait(s.q_full[i], n_q[i]++, 211);
-                        if (!ok) break;
-                        tc_fence_after();
-                        qk(i, 0);
-                    }
+                for (int k = 1; k < D / 16; ++k) {
+                    const uint32_t off = (k / 4) * (kHalf >> 4) + (k % 4) * 2;
+                    umma_bf16_lohi<true>(d, a + off, b + off, id_qk);
+                }
+                umma_commit(bar(s.s_full[i]));
+            }
+        };
+        auto pv = [&](int i, uint32_t slot, bool first) {
+            if (leader) {
+                const uint32_t d = tm + 256 + D * i, a = tm + 128 * i, b = v_lo + slot * kOpLo;
+                if (first) umma_tmem_a_lohi<false>(d, a, b, kIdPv);
+                else umma_tmem_a_lohi<true>(d, a, b, kIdPv);
+#pragma unroll
+                for (int k = 1; k < kBlock / 16; ++k) umma_tmem_a_lohi<true>(d, a + 8 * k, b + (2048 >> 4) * k, kIdPv);
+                umma_commit(bar(s.o_ready[i]));
+            }
+        };
+        for (int round = 0; ok && get_item(s, p, round, it); ++round) {
+            const int nb0 = __shfl_sync(0xffffffffu, it.nb[0], 0), nb1 = __shfl_sync(0xffffffffu, it.nb[1], 0), nb = max(nb0, nb1);
+            uint32_t slot = fill % kSlots;
+            wait(s.kv_full[slot], fill / kSlots, 210);
+            wait(s.q_full[0], n_q0++, 211);
+            if (!ok) break;
+            tc_fence_after();
+            qk(0, slot);
+            if (nb1 > 0) {
+                wait(s.q_full[1], n_q1++, 211);
                 if (!ok) break;
-                umma_commit(bar(s.kv_empty[fill % kSlots]));
+                tc_fence_after();
+                qk(1, slot);
+            }
+            if (leader) {
+                umma_commit(bar(s.kv_empty[slot]));
                 if (nb == 1) umma_commit(bar(s.q_empty));
-                for (int j = 0; ok && j < nb; ++j) {
-                    const int vx = fill + 2 * j + 1, vslot = vx % kSlots, kx = vx + 1;
-                    wait(s.kv_full[vslot], vx / kSlots, 212);
-                    if (j == it.nb[0] - 1 || j == it.nb[1] - 1) {
-                        wait(s.v_clean[vslot], clean_phase >> vslot, 213);
-                        clean_phase ^= 1u << vslot;
-                    }
+            }
+            for (int j = 0; ok && j < nb; ++j) {
+                const uint32_t vx = fill + 2 * j + 1, vslot = vx % kSlots, kslot = (vx + 1) % kSlots, kpar = (vx + 1) / kSlots;
+                wait(s.kv_full[vslot], vx / kSlots, 212);
+                if (j == nb0 - 1 || j == nb1 - 1) {
+                    wait(s.v_clean[vslot], clean_phase >> vslot, 213);
+                    clean_phase ^= 1u << vslot;
+                }
+                if (j + 1 < nb) wait(s.kv_full[kslot], kpar, 215);
+                if (j < nb0) {
+                    wait(s.p_ready[0], n_p0++, 214);
                     if (!ok) break;
-                    for (int i = 0; i < 2; ++i) {
-                        if (j < it.nb[i]) {
-                            wait(s.p_ready[i], n_p[i]++, 214);
-                            if (!ok) break;
-                            tc_fence_after();
-#pragma unroll
-                            for (int k = 0; k < kBlock / 16; ++k)
-                                umma_bf16_tmem_a(tmem_o + D * i, tmem_s + 128 * i + 8 * k, desc_outer_major(kv_smem + vslot * kOp + k * 2048), kIdPv,
-                                                 j > 0 || k > 0);
-                            umma_commit(bar(s.o_ready[i]));
-                        }
-                        if (j + 1 < it.nb[i]) {
-                            wait(s.kv_full[kx % kSlots], kx / kSlots, 215);
-                            if (!ok) break;
-                            tc_fence_after();
-                            qk(i, j + 1);
-                        }
-                    }
+                    tc_fence_after();
+                    pv(0, vslot, j == 0);
+                    if (j + 1 < nb0) qk(0, kslot);
+                }
+                if (j < nb1) {
+                    wait(s.p_ready[1], n_p1++, 214);
                     if (!ok) break;
+                    tc_fence_after();
+                    pv(1, vslot, j == 0);
+                    if (j + 1 < nb1) qk(1, kslot);
+                }
+                if (leader) {
                     umma_commit(bar(s.kv_empty[vslot]));
-                    if (j + 1 < nb) umma_commit(bar(s.kv_empty[kx % kSlots]));
+                    if (j + 1 < nb) umma_commit(bar(s.kv_empty[kslot]));
                     if (j + 2 == nb) umma_commit(bar(s.q_empty));
                 }
-                fill += 2 * nb;
             }
+            fill += 2 * nb;
         }
     } else if (warp >= 10) {
         // ------------------------------------------------------------------------------------------ masked value blocks
