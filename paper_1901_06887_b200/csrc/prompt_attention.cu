@@ -29,21 +29,25 @@ constexpr int kThreads = 384;
 constexpr int kBlock = 128;                   // keys per block, rows per tile
 constexpr int kHalf = kBlock * 128;           // bytes of a 128-row, 64-channel operand
 constexpr int kMaxSeqs = 512;                 // sequences of one launch
+constexpr int kItems = 256;                   // tiles of a CTA that are looked up once, at the start
 constexpr float kSlack = 8.f;
 
 template <int D> __host__ __device__ constexpr int slots() { return D == 128 ? 4 : 8; }
 template <int D> __host__ __device__ constexpr int operand_bytes() { return kHalf * (D / 64); }
 
 struct Control {
-    uint64_t q_full[2], q_empty, s_full[2], p_ready[2], o_ready[2], epi_done[2], kv_full[8], kv_empty[8], v_raw[8], v_clean[8];
+    uint64_t q_full[2], q_empty, s_full[2], p_half[2], p_ready[2], o_ready[2], epi_done[2], kv_full[8], kv_empty[8], v_raw[8], v_clean[8];
     uint32_t tmem;
     int abort;
     int poison[2];                            // round + 1 of a tile with notes
     unsigned long long first_bad[2][128];     // per channel: (0x7fffffff - round, first token that is not finite); later rounds win the minimum
     int start[kMaxSeqs], len[kMaxSeqs], order[kMaxSeqs], before[kMaxSeqs + 1];
     int total;
+    int4 item[kItems];                        // this CTA's first tiles: row of the sequence's start, its length, first token, head pack
 };
-template <int D> constexpr int shared_bytes() { return 1024 + (2 + slots<D>()) * operand_bytes<D>() + (int)sizeof(Control); }
+constexpr int kControlBytes = ((int)sizeof(Control) + 127) / 128 * 128;
+constexpr int kStageBytes = 8 * 2048;           // output staging of the eight softmax warps
+template <int D> constexpr int shared_bytes() { return 1024 + (2 + slots<D>()) * operand_bytes<D>() + kControlBytes + kStageBytes; }
 
 struct PromptParams {
     const int32_t* offsets;
@@ -89,22 +93,45 @@ __device__ __forceinline__ float ex2(float x) {
     return y;
 }
 
+// Pairs of fp32 in one instruction.
+struct Pair { uint64_t v; };
+__device__ __forceinline__ Pair pair_of(float a, float b) {
+    Pair p;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(p.v) : "f"(a), "f"(b));
+    return p;
+}
+__device__ __forceinline__ void unpair(Pair p, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(p.v)); }
+__device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c) {
+    Pair d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+    return d;
+}
+__device__ __forceinline__ Pair add2(Pair a, Pair b) {
+    Pair d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d.v) : "l"(a.v), "l"(b.v));
+    return d;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float d;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
 // Descriptor words of the values, 128-byte swizzle with the channels contiguous: the product's inner index is the token (8-token groups 1024
 // bytes apart, as in the row-major form), and the 64-channel halves lie kHalf apart.
 constexpr uint32_t kHalfField = static_cast<uint32_t>(kHalf >> 4) << 16;
 __device__ __forceinline__ uint32_t desc_lo_values(uint32_t smem_addr) { return ((smem_addr & 0x3FFFFu) >> 4) | kHalfField; }
 
 struct Item {
-    int seq, start, len, t0, pack;            // first row of the sequence, its length, first token of the tile pair, head pack
+    int start, len, t0, pack;                 // first row of the sequence, its length, first token of the tile pair, head pack
     int nb[2];                                // key blocks of the two tiles (0: no rows)
 };
 
-__device__ __forceinline__ bool get_item(const Control& s, const PromptParams& p, int round, Item& it) {
+// The tile pair of a round, or a length of 0 behind the last.
+__device__ __forceinline__ int4 find_item(const Control& s, const PromptParams& p, int round) {
     const int packs = p.q_heads >> p.pack_shift;
     const int64_t x = (int64_t)round * gridDim.x + ((round & 1) ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
-    if (x >= (int64_t)s.total * packs) return false;
+    if (x >= (int64_t)s.total * packs) return make_int4(0, 0, 0, 0);
     const int k = (int)(x / packs);
-    it.pack = (int)(x % packs);
     const int tokens = 256 >> p.pack_shift;   // of the tile pair
     int lo = 0, hi = p.n_seqs - 1;            // rank r with before[r] <= k < before[r + 1]
     while (lo < hi) {
@@ -113,16 +140,19 @@ __device__ __forceinline__ bool get_item(const Control& s, const PromptParams& p
     }
     const int q = k - s.before[lo];
     const int tile = (s.len[s.order[lo]] + tokens - 1) / tokens - 1 - q / (lo + 1);
-    it.seq = s.order[q % (lo + 1)];
-    it.start = s.start[it.seq];
-    it.len = s.len[it.seq];
-    it.t0 = tile * tokens;
+    const int seq = s.order[q % (lo + 1)];
+    return make_int4(s.start[seq], s.len[seq], tile * tokens, (int)(x - (int64_t)k * packs));
+}
+__device__ __forceinline__ bool get_item(const Control& s, const PromptParams& p, int round, Item& it) {
+    const int4 v = round < kItems ? s.item[round] : find_item(s, p, round);
+    it.start = v.x; it.len = v.y; it.t0 = v.z; it.pack = v.w;
+    const int half = 128 >> p.pack_shift;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-        const int first = it.t0 + i * (tokens / 2), last = min(first + tokens / 2, it.len) - 1;
+        const int first = it.t0 + i * half, last = min(first + half, it.len) - 1;
         it.nb[i] = first < it.len ? last / kBlock + 1 : 0;
     }
-    return true;
+    return it.len > 0;
 }
 
 template <int D>
@@ -141,7 +171,7 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < 2; ++i) {
-            mbar_init(bar(s.q_full[i]), 1); mbar_init(bar(s.s_full[i]), 1); mbar_init(bar(s.p_ready[i]), 128);
+            mbar_init(bar(s.q_full[i]), 1); mbar_init(bar(s.s_full[i]), 1); mbar_init(bar(s.p_half[i]), 128); mbar_init(bar(s.p_ready[i]), 128);
             mbar_init(bar(s.o_ready[i]), 1); mbar_init(bar(s.epi_done[i]), 256);
             s.poison[i] = 0;
         }
@@ -197,6 +227,8 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
         }
         if (lane == 0) { s.before[p.n_seqs] = run; s.total = run; }
     }
+    __syncthreads();
+    if (threadIdx.x < kItems) s.item[threadIdx.x] = find_item(s, p, threadIdx.x);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -273,13 +305,24 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
                 umma_commit(bar(s.s_full[i]));
             }
         };
-        auto pv = [&](int i, uint32_t slot, bool first) {
+        // the first 64 keys go while the second half of P is still in its exponentials
+        auto pv = [&](int i, uint32_t slot, bool first, uint32_t n) {
+            const uint32_t d = tm + 256 + D * i, a = tm + 128 * i, b = v_lo + slot * kOpLo;
+            wait(s.p_half[i], n, 214);
+            if (!ok) return;
+            tc_fence_after();
             if (leader) {
-                const uint32_t d = tm + 256 + D * i, a = tm + 128 * i, b = v_lo + slot * kOpLo;
                 if (first) umma_tmem_a_lohi<false>(d, a, b, kIdPv);
                 else umma_tmem_a_lohi<true>(d, a, b, kIdPv);
 #pragma unroll
-                for (int k = 1; k < kBlock / 16; ++k) umma_tmem_a_lohi<true>(d, a + 8 * k, b + (2048 >> 4) * k, kIdPv);
+                for (int k = 1; k < kBlock / 32; ++k) umma_tmem_a_lohi<true>(d, a + 8 * k, b + (2048 >> 4) * k, kIdPv);
+            }
+            wait(s.p_ready[i], n, 216);
+            if (!ok) return;
+            tc_fence_after();
+            if (leader) {
+#pragma unroll
+                for (int k = kBlock / 32; k < kBlock / 16; ++k) umma_tmem_a_lohi<true>(d, a + 8 * k, b + (2048 >> 4) * k, kIdPv);
                 umma_commit(bar(s.o_ready[i]));
             }
         };
@@ -310,17 +353,13 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
                 }
                 if (j + 1 < nb) wait(s.kv_full[kslot], kpar, 215);
                 if (j < nb0) {
-                    wait(s.p_ready[0], n_p0++, 214);
+                    pv(0, vslot, j == 0, n_p0++);
                     if (!ok) break;
-                    tc_fence_after();
-                    pv(0, vslot, j == 0);
                     if (j + 1 < nb0) qk(0, kslot);
                 }
                 if (j < nb1) {
-                    wait(s.p_ready[1], n_p1++, 214);
+                    pv(1, vslot, j == 0, n_p1++);
                     if (!ok) break;
-                    tc_fence_after();
-                    pv(1, vslot, j == 0);
                     if (j + 1 < nb1) qk(1, kslot);
                 }
                 if (leader) {
@@ -353,25 +392,30 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
                 uint8_t* const v = smem + (2 + slot) * kOp;
                 for (int r = t; r < kBlock; r += 64) {
                     const int tok = j * kBlock + r;
+                    auto piece = [&](int c) { return reinterpret_cast<uint4*>(v + (c / 8) * kHalf + r * 128 + (((c & 7) ^ (r & 7)) << 4)); };
+                    if (tok >= it.len) {
+#pragma unroll
+                        for (int c = 0; c < D / 8; ++c) *piece(c) = make_uint4(0, 0, 0, 0);
+                        continue;
+                    }
+                    uint32_t any = 0;
 #pragma unroll
                     for (int c = 0; c < D / 8; ++c) {
-                        uint4* const at = reinterpret_cast<uint4*>(v + (c / 8) * kHalf + r * 128 + (((c & 7) ^ (r & 7)) << 4));
-                        if (tok >= it.len) { *at = make_uint4(0, 0, 0, 0); continue; }
-                        const uint4 w = *at;
-                        const uint32_t x[4] = {w.x, w.y, w.z, w.w};
-                        uint32_t any = 0;
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) any |= ((x[e] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
-                        if (any) {
-                            const unsigned long long note = (unsigned long long)(0x7fffffff - round) << 32 | (uint32_t)tok;
-                            uint32_t y[4];
-                            for (int e = 0; e < 4; ++e) {
-                                y[e] = x[e];
-                                if ((x[e] & 0x7f80u) == 0x7f80u) { y[e] &= 0xffff0000u; atomicMin(&s.first_bad[buf][c * 8 + 2 * e], note); }
-                                if ((x[e] & 0x7f800000u) == 0x7f800000u) { y[e] &= 0x0000ffffu; atomicMin(&s.first_bad[buf][c * 8 + 2 * e + 1], note); }
-                            }
-                            *at = make_uint4(y[0], y[1], y[2], y[3]);
-                            s.poison[buf] = round + 1;
+                        const uint4 w = *piece(c);
+                        any |= ((w.x & 0x7f807f80u) + 0x00800080u) | ((w.y & 0x7f807f80u) + 0x00800080u) | ((w.z & 0x7f807f80u) + 0x00800080u) |
+                               ((w.w & 0x7f807f80u) + 0x00800080u);
+                    }
+                    if ((any & 0x80008000u) == 0) continue;
+                    const unsigned long long note = (unsigned long long)(0x7fffffff - round) << 32 | (uint32_t)tok;
+                    s.poison[buf] = round + 1;
+#pragma unroll 1
+                    for (int c = 0; c < D / 8; ++c) {
+                        uint32_t* const w = reinterpret_cast<uint32_t*>(piece(c));
+                        for (int e = 0; e < 4; ++e) {
+                            uint32_t y = w[e];
+                            if ((y & 0x7f80u) == 0x7f80u) { y &= 0xffff0000u; atomicMin(&s.first_bad[buf][c * 8 + 2 * e], note); }
+                            if ((y & 0x7f800000u) == 0x7f800000u) { y &= 0x0000ffffu; atomicMin(&s.first_bad[buf][c * 8 + 2 * e + 1], note); }
+                            w[e] = y;
                         }
                     }
                 }
@@ -410,11 +454,14 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
                         for (int e = 0; e < 32; ++e)
                             if (32 * c + e > lim) x[c][e] = 0xff800000u;
                 }
-                float mx = -INFINITY;
+                float mx4[4];
 #pragma unroll
-                for (int c = 0; c < 4; ++c)
+                for (int c = 0; c < 4; ++c) {
+                    mx4[c] = fmaxf(__uint_as_float(x[c][0]), __uint_as_float(x[c][1]));
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) mx = fmaxf(mx, __uint_as_float(x[c][e]));
+                    for (int e = 2; e < 32; e += 2) mx4[c] = max3(mx4[c], __uint_as_float(x[c][e]), __uint_as_float(x[c][e + 1]));
+                }
+                const float mx = fmaxf(max3(mx4[0], mx4[1], mx4[2]), mx4[3]);
                 if (j == 0) {
                     m = mx;
                 } else if (__any_sync(0xffffffffu, (mx - m) * p.c > kSlack)) {
@@ -440,21 +487,32 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
                     }
                 }
                 const float shift = -m * p.c;
-                float sum[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int c = 0; c < 4; ++c) {
+                const Pair c2 = pair_of(p.c, p.c), shift2 = pair_of(shift, shift);
+                Pair sum[2] = {pair_of(0.f, 0.f), pair_of(0.f, 0.f)};
+                auto chunk = [&](int c) {
                     uint32_t w[16];
 #pragma unroll
                     for (int e = 0; e < 16; ++e) {
-                        const float a = ex2(fmaf(__uint_as_float(x[c][2 * e]), p.c, shift));
-                        const float b = ex2(fmaf(__uint_as_float(x[c][2 * e + 1]), p.c, shift));
-                        sum[e & 1] += a;
-                        sum[2 + (e & 1)] += b;
+                        const Pair y = fma2(pair_of(__uint_as_float(x[c][2 * e]), __uint_as_float(x[c][2 * e + 1])), c2, shift2);
+                        float a, b;
+                        unpair(y, a, b);
+                        a = ex2(a);
+                        b = ex2(b);
+                        sum[e & 1] = add2(sum[e & 1], pair_of(a, b));
                         w[e] = pack_bf16x2(a, b);
                     }
                     tmem_st16(my_s + 16 * c, w);
-                }
-                l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+                };
+                chunk(0);
+                chunk(1);
+                tmem_st_wait();
+                tc_fence_before();
+                mbar_arrive(bar(s.p_half[i]));
+                chunk(2);
+                chunk(3);
+                float sa, sb;
+                unpair(add2(sum[0], sum[1]), sa, sb);
+                l += sa + sb;
                 tmem_st_wait();
                 tc_fence_before();
                 mbar_arrive(bar(s.p_ready[i]));
@@ -467,8 +525,10 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
                 tc_fence_after();
                 const float inv = 1.f / l;
                 const bool poison = *(volatile int*)&s.poison[buf] == round + 1;
-                const int head = it.pack * p.pack + (r & (p.pack - 1));
-                uint16_t* const out = p.out + ((int64_t)(it.start + tok) * p.q_heads + head) * D;
+                // 32 channels at a time through shared memory, so that four lanes store 64 contiguous bytes of a row: a row per lane
+                // would touch 32 lines with every store
+                uint4* const stage = reinterpret_cast<uint4*>(smem + (2 + kSlots) * kOp + kControlBytes) + warp * 128;
+                const int sub = lane & 3;
 #pragma unroll
                 for (int c = 0; c < D / 32; ++c) {
                     uint32_t y[32];
@@ -480,16 +540,25 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
                         for (int e = 0; e < 32; ++e)
                             if (s.first_bad[buf][32 * c + e] <= note) y[e] = 0x7fffffffu;     // an older round's note is larger
                     }
-                    if (tok < it.len) {
+                    __syncwarp();
 #pragma unroll
-                        for (int v = 0; v < 4; ++v) {
-                            uint4 w;
-                            w.x = pack_bf16x2(__uint_as_float(y[8 * v]) * inv, __uint_as_float(y[8 * v + 1]) * inv);
-                            w.y = pack_bf16x2(__uint_as_float(y[8 * v + 2]) * inv, __uint_as_float(y[8 * v + 3]) * inv);
-                            w.z = pack_bf16x2(__uint_as_float(y[8 * v + 4]) * inv, __uint_as_float(y[8 * v + 5]) * inv);
-                            w.w = pack_bf16x2(__uint_as_float(y[8 * v + 6]) * inv, __uint_as_float(y[8 * v + 7]) * inv);
-                            reinterpret_cast<uint4*>(out)[c * 4 + v] = w;
-                        }
+                    for (int v = 0; v < 4; ++v) {
+                        uint4 w;
+                        w.x = pack_bf16x2(__uint_as_float(y[8 * v]) * inv, __uint_as_float(y[8 * v + 1]) * inv);
+                        w.y = pack_bf16x2(__uint_as_float(y[8 * v + 2]) * inv, __uint_as_float(y[8 * v + 3]) * inv);
+                        w.z = pack_bf16x2(__uint_as_float(y[8 * v + 4]) * inv, __uint_as_float(y[8 * v + 5]) * inv);
+                        w.w = pack_bf16x2(__uint_as_float(y[8 * v + 6]) * inv, __uint_as_float(y[8 * v + 7]) * inv);
+                        stage[lane * 4 + (v ^ ((lane >> 1) & 3))] = w;
+                    }
+                    __syncwarp();
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) {
+                        const int row = v * 8 + (lane >> 2), of_tile = (warp & 3) * 32 + row;
+                        const int row_tok = it.t0 + i * (tokens / 2) + (of_tile >> p.pack_shift);
+                        const int head = it.pack * p.pack + (of_tile & (p.pack - 1));
+                        const uint4 w = stage[row * 4 + (sub ^ ((row >> 1) & 3))];
+                        if (row_tok < it.len)
+                            reinterpret_cast<uint4*>(p.out + ((int64_t)(it.start + row_tok) * p.q_heads + head) * D)[c * 4 + sub] = w;
                     }
                 }
                 tc_fence_before();
