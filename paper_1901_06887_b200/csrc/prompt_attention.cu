@@ -239,6 +239,7 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
 
     if (warp == 8) {
         // ------------------------------------------------------------------------------------------ copies
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
         if (lane == 0) {
             int fill = 0;                        // operands put into the ring so far
             uint32_t raw_phase = 0, raw_used = 0;
@@ -281,6 +282,7 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
         }
     } else if (warp == 9) {
         // ------------------------------------------------------------------------------------------ matrix instructions
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
         // The whole warp walks the loop, so that addresses stay warp-uniform; one elected lane issues.  (One lane alone, with descriptors
         // built per instruction, took 115 cycles for each of them: 1900 for the sixteen that a tile's block needs, against 512 of work.)
         const bool leader = elect_one();
@@ -372,6 +374,7 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
         }
     } else if (warp >= 10) {
         // ------------------------------------------------------------------------------------------ masked value blocks
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
         const int t = threadIdx.x - 320;         // rows t and t + 64
         int fill = 0;
         uint32_t raw_phase = 0;
@@ -427,6 +430,8 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
         }
     } else {
         // ------------------------------------------------------------------------------------------ softmax, one row per thread
+        // registers move here: 256 threads x 208 + 128 x 88 = the launch's 384 x 168
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
         const int i = warp >> 2;
         const int r = threadIdx.x & 127;
         const uint32_t lanes = (uint32_t)(warp & 3) << 21;     // tensor-memory lane of the warp's first row, in the address's upper half
