@@ -1,78 +1,373 @@
-// Log probability of given tokens, entropy, likeliest alternatives.  First form: one CTA per row, several passes.
+// Log probability of given tokens, entropy and the likeliest alternatives of rows of logits.
+//
+// Mathematics.  With m = max x, S = sum e^(x - m), W = sum (x - m) e^(x - m):  log p_t = x_t - m - log S,  entropy = log S - W / S.
+// One pass over the logits: every thread keeps (m, S, W) of its share, rescaled when its maximum moves.
+//
+// Alternatives.  The pass also leaves the largest logit of each thread and of each group of four.  The k-th largest of the 64 groups' is a bound
+// that the k-th largest logit cannot lie below, so only the threads that reach it look at their share again (from L2) and put what reaches it on
+// a list; it holds little more than k entries.  The list is ranked by counting, every entry against every other, on (value, lower index first), so the result
+// does not depend on the order of arrival.  Where too many logits reach the bound (long ties, values sorted into one share) the exact k-th
+// largest is found by its bits, eight at a time, from histograms of the row, and ties at it are taken from the front of the row.
+//
+// Split.  A row is cut into parts so that the rows fill the GPU (a part has at least kMinPart logits); a part leaves (m, S, W) and its sorted
+// alternatives in scratch, and the last CTA of a row to arrive joins them.  Minus infinity adds nothing and is no alternative.
+//
+// Bound: memory for many rows (bf16: 12 logits a cycle and SM, 0.75 of the rate of exponentials); latency for few.
 #include "lm_device.cuh"
 #include "lm_host.h"
 
 namespace mt {
 namespace {
 
-__device__ float logit(const LogprobArgs& a, int64_t row, int i) {
-    const int64_t at = row * a.row_stride + i;
-    return (a.fp32 ? static_cast<const float*>(a.logits)[at] : bf16_to_f(static_cast<const uint16_t*>(a.logits)[at])) + 0.f;
+constexpr int kThreads = 256, kWarps = kThreads / 32;
+constexpr int kMaxTop = 32;
+constexpr int kGroups = 64;                // at least kMaxTop
+constexpr int kList = 1024;                // entries the first list may take
+constexpr int kMinPart = 4096;             // logits of a part, at least
+constexpr int kMaxParts = 64;
+constexpr float kLog2e = 1.44269504088896341f;
+static_assert(kThreads == 4 * kGroups && kGroups >= kMaxTop && kGroups >= kMaxParts, "");
+
+struct Part {                              // one part's results in scratch
+    float m, s, w;                         // maximum, sums
+    int bad;                               // NaN or plus infinity seen
+    uint32_t value[kMaxTop];               // alternatives as ordered bits (0: none) ...
+    int32_t index[kMaxTop];
+};
+
+struct Params {
+    LogprobArgs a;
+    int parts;
+    int part_len;                          // a multiple of 8
+    unsigned* arrived;                     // [rows], zero between calls
+    Part* part;                            // [rows][parts]
+};
+
+__device__ __forceinline__ float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
 }
-// Grows with (value, lower index).
-__device__ unsigned long long rank_key(float x, int i) {
-    const int b = __float_as_int(x);
-    return (unsigned long long)((uint32_t)(b ^ ((b >> 31) & 0x7fffffff)) ^ 0x80000000u) << 32 | (uint32_t)(~i);
+// Bits that grow with the value (minus zero counts as zero); 0 is below every number, so it can stand for "nothing".
+__device__ __forceinline__ uint32_t ordered(float x) {
+    const uint32_t b = __float_as_uint(x + 0.f);
+    return b ^ (static_cast<uint32_t>(static_cast<int32_t>(b) >> 31) | 0x80000000u);
+}
+__device__ __forceinline__ float unordered(uint32_t o) {
+    return __uint_as_float(o & 0x80000000u ? o ^ 0x80000000u : ~o);
+}
+constexpr uint32_t kOrderedMinusInf = 0x007fffffu;         // ordered(-inf)
+
+template <bool FP32> struct Vec;
+template <> struct Vec<true> {
+    static constexpr int N = 4;
+    float x[4];
+    __device__ void load(const void* p) {
+        const float4 v = *reinterpret_cast<const float4*>(p);
+        x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w;
+    }
+};
+template <> struct Vec<false> {
+    static constexpr int N = 8;
+    float x[8];
+    __device__ void load(const void* p) {
+        const uint4 v = *reinterpret_cast<const uint4*>(p);
+        x[0] = bf16_lo(v.x); x[1] = bf16_hi(v.x); x[2] = bf16_lo(v.y); x[3] = bf16_hi(v.y);
+        x[4] = bf16_lo(v.z); x[5] = bf16_hi(v.z); x[6] = bf16_lo(v.w); x[7] = bf16_hi(v.w);
+    }
+};
+template <bool FP32>
+__device__ __forceinline__ float logit_at(const void* row, int i) {
+    return FP32 ? static_cast<const float*>(row)[i] : bf16_to_f(static_cast<const uint16_t*>(row)[i]);
 }
 
-__global__ void __launch_bounds__(256) token_logprobs_simple(LogprobArgs a) {
+// A part of a row, [lo, hi): elements in front of the first 16-byte boundary, whole vectors, the rest.
+struct Span {
+    int lo, hi, vec0, n_vec, tail;         // vectors start at vec0; tail: first element behind them
+};
+template <bool FP32>
+__device__ __forceinline__ Span span_of(const void* row, int lo, int hi) {
+    constexpr int N = Vec<FP32>::N, B = FP32 ? 4 : 2;
+    const uintptr_t at = reinterpret_cast<uintptr_t>(row) + (uintptr_t)lo * B;
+    Span s;
+    s.lo = lo; s.hi = hi;
+    s.vec0 = min(hi, lo + (int)(((16 - (at & 15)) & 15) / B));
+    s.n_vec = (hi - s.vec0) / N;
+    s.tail = s.vec0 + s.n_vec * N;
+    return s;
+}
+// Calls f(value, index) for every element of this thread's share; the same share in every pass.
+template <bool FP32, class F>
+__device__ __forceinline__ void for_share(const void* row, const Span& s, int t, F f) {
+    constexpr int N = Vec<FP32>::N, B = FP32 ? 4 : 2;
+    for (int v = t; v < s.n_vec; v += kThreads) {
+        Vec<FP32> x;
+        x.load(static_cast<const char*>(row) + (size_t)(s.vec0 + v * N) * B);
+#pragma unroll
+        for (int e = 0; e < N; ++e) f(x.x[e], s.vec0 + v * N + e);
+    }
+    if (t < s.vec0 - s.lo) f(logit_at<FP32>(row, s.lo + t), s.lo + t);
+    if (t < s.hi - s.tail) f(logit_at<FP32>(row, s.tail + t), s.tail + t);
+}
+
+struct Stats {
+    float m, s, w;                         // s = sum e^(x - m), w = sum (x - m) e^(x - m)
+};
+__device__ __forceinline__ float exp_of(float x) { return ex2(x * kLog2e); }
+// Joins b to a; both may be empty (m = -inf, s = w = 0).
+__device__ __forceinline__ void join(Stats& a, float m, float s, float w) {
+    const float nm = fmaxf(a.m, m);
+    if (nm == -INFINITY) return;
+    const float da = fmaxf(a.m - nm, -1e4f), db = fmaxf(m - nm, -1e4f), fa = exp_of(da), fb = exp_of(db);     // (-1e4: far below, and finite)
+    const float wa = fmaf(da, a.s, a.w) * fa, wb = fmaf(db, s, w) * fb;
+    a.s = a.s * fa + s * fb;
+    a.w = wa + wb;
+    a.m = nm;
+}
+
+// Sorts the list of n <= kList (value, index) entries by counting and writes the first `top` (value descending, index ascending).
+__device__ __forceinline__ void rank_list(const uint32_t* value, const int32_t* index, int n, int top, uint32_t* out_value, int32_t* out_index, int t) {
+    for (int i = t; i < n; i += kThreads) {
+        const uint32_t v = value[i];
+        const int32_t at = index[i];
+        int rank = 0;
+        for (int j = 0; j < n; ++j) rank += (value[j] > v || (value[j] == v && index[j] < at)) ? 1 : 0;
+        if (rank < top) { out_value[rank] = v; out_index[rank] = at; }
+    }
+}
+
+template <bool FP32>
+__global__ void __launch_bounds__(kThreads) token_logprobs_kernel(const Params p) {
+    __shared__ float s_m[kWarps], s_s[kWarps], s_w[kWarps];
+    __shared__ int s_bad, s_n, s_last;
+    __shared__ uint32_t s_best[kGroups], s_bound, s_value[kList], s_top_value[kMaxTop], s_hist[256], s_pick[2];
+    __shared__ int32_t s_index[kList], s_top_index[kMaxTop], s_warp_n[kWarps];
+    const LogprobArgs& a = p.a;
+    const int t = threadIdx.x, lane = t & 31, warp = t / 32, top = a.top;
+    const int64_t row_i = blockIdx.x / p.parts;
+    const int part = blockIdx.x % p.parts;
     pdl_launch_dependents();
     pdl_wait();
-    __shared__ float red[2][8];
-    __shared__ int bad_row;
-    __shared__ unsigned long long best[8], chosen;
-    const int64_t row = blockIdx.x;
-    const int t = threadIdx.x, lane = t & 31, w = t / 32;
-    if (t == 0) bad_row = 0;
-    __syncthreads();
-    float m = -INFINITY;
+    const void* const row = static_cast<const char*>(a.logits) + row_i * a.row_stride * (FP32 ? 4 : 2);
+    const int lo = part * p.part_len, hi = min(a.vocab, lo + p.part_len);
+    const Span span = span_of<FP32>(row, min(lo, a.vocab), hi > lo ? hi : min(lo, a.vocab));
+    if (t == 0) { s_bad = 0; s_n = 0; }
+
+    // --- one pass: statistics and the share's largest logit
+    constexpr int N = Vec<FP32>::N, B = FP32 ? 4 : 2;
+    Stats st = {-INFINITY, 0.f, 0.f};
+    float best = -INFINITY;
     bool bad = false;
-    for (int i = t; i < a.vocab; i += 256) { const float x = logit(a, row, i); bad = bad || !(x < INFINITY); m = fmaxf(m, x); }
-    if (bad) bad_row = 1;
-    m = warp_max(m);
-    if (lane == 0) red[0][w] = m;
-    __syncthreads();
-    for (int i = 0; i < 8; ++i) m = fmaxf(m, red[0][i]);
-    const bool none = bad_row || m == -INFINITY;
-    __syncthreads();
-    float s = 0.f, e = 0.f;
-    for (int i = t; i < a.vocab && !none; i += 256) {
-        const float z = logit(a, row, i) - m, p = expf(z);
-        s += p;
-        if (p > 0.f) e += p * z;
-    }
-    s = warp_sum(s); e = warp_sum(e);
-    if (lane == 0) { red[0][w] = s; red[1][w] = e; }
-    __syncthreads();
-    s = e = 0.f;
-    for (int i = 0; i < 8; ++i) { s += red[0][i]; e += red[1][i]; }
-    const float ls = logf(s);
-    if (t == 0) {
-        const int tok = a.tokens[row];
-        const bool in = tok >= 0 && tok < a.vocab;
-        a.logprobs[row] = none || !in ? nan_f() : logit(a, row, tok) - m - ls;
-        if (a.entropies) a.entropies[row] = none ? nan_f() : ls - e / s;
-    }
-    unsigned long long last = ~0ull;
-    for (int k = 0; k < a.top; ++k) {
-        unsigned long long b = 0;
-        for (int i = t; i < a.vocab && !none; i += 256) {
-            const float x = logit(a, row, i);
-            const unsigned long long key = rank_key(x, i);
-            if (x > -INFINITY && key < last && key > b) b = key;
+    auto add = [&](const float* x, int n) {
+        float mx = x[0];
+#pragma unroll
+        for (int e = 1; e < N; ++e)
+            if (e < n) asm("max.NaN.f32 %0, %0, %1;" : "+f"(mx) : "f"(x[e]));
+        bad = bad || !(mx < INFINITY);
+        best = fmaxf(best, mx);
+        if (mx > st.m) {                       // the sums move to the new maximum
+            const float d = fmaxf(st.m - mx, -1e4f), f = exp_of(d);
+            st.w = fmaf(d, st.s, st.w) * f;
+            st.s *= f;
+            st.m = mx;
         }
-        for (int o = 16; o; o >>= 1) { const unsigned long long y = __shfl_xor_sync(0xffffffffu, b, o); b = y > b ? y : b; }
-        if (lane == 0) best[w] = b;
+        if (st.m == -INFINITY) return;
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+            if (e < n) {
+                const float d = fmaxf(x[e] - st.m, -1e4f), q = exp_of(d);       // (minus infinity: q = 0, d finite)
+                st.s += q;
+                st.w = fmaf(q, d, st.w);
+            }
+    };
+    {
+        const char* const base = static_cast<const char*>(row) + (size_t)span.vec0 * B;
+        int v = t;
+        for (; v + 3 * kThreads < span.n_vec; v += 4 * kThreads) {       // four loads in flight
+            Vec<FP32> x[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) x[u].load(base + (size_t)(v + u * kThreads) * 16);
+#pragma unroll
+            for (int u = 0; u < 4; ++u) add(x[u].x, N);
+        }
+        for (; v < span.n_vec; v += kThreads) {
+            Vec<FP32> x;
+            x.load(base + (size_t)v * 16);
+            add(x.x, N);
+        }
+        float x[N];
+        if (t < span.vec0 - span.lo) { x[0] = logit_at<FP32>(row, span.lo + t); add(x, 1); }
+        if (t < span.hi - span.tail) { x[0] = logit_at<FP32>(row, span.tail + t); add(x, 1); }
+    }
+    const uint32_t mine_best = ordered(best);
+    {
+        uint32_t g = max(mine_best, __shfl_xor_sync(0xffffffffu, mine_best, 1));
+        g = max(g, __shfl_xor_sync(0xffffffffu, g, 2));
+        if ((t & 3) == 0) s_best[t >> 2] = g;
+    }
+#pragma unroll
+    for (int o = 16; o; o >>= 1)
+        join(st, __shfl_xor_sync(0xffffffffu, st.m, o), __shfl_xor_sync(0xffffffffu, st.s, o), __shfl_xor_sync(0xffffffffu, st.w, o));
+    if (lane == 0) { s_m[warp] = st.m; s_s[warp] = st.s; s_w[warp] = st.w; }
+    __syncthreads();
+    if (bad) s_bad = 1;
+
+    // --- alternatives of this part
+    int n_top = 0;
+    if (top > 0) {
+        // bound: the top-th largest of the groups' largest (by counting; where several are equal the run that covers place `top` decides)
+        if (t < kGroups) {
+            const uint32_t mine = s_best[t];
+            int above = 0, same = 0;
+#pragma unroll 8
+            for (int j = 0; j < kGroups; ++j) { above += s_best[j] > mine; same += s_best[j] == mine; }
+            if (above < top && above + same >= top) s_bound = mine;
+        }
+        __syncthreads();
+        const uint32_t bound = max(s_bound, kOrderedMinusInf + 1u);
+        if (mine_best >= bound)
+            for_share<FP32>(row, span, t, [&](float x, int i) {
+                const uint32_t o = ordered(x);
+                if (o >= bound) {
+                    const int at = atomicAdd(&s_n, 1);
+                    if (at < kList) { s_value[at] = o; s_index[at] = i; }
+                }
+            });
+        __syncthreads();
+        int n = s_n;
+        if (n > kList) {
+            // the exact top-th largest value, from its bits, eight at a time
+            uint32_t prefix = 0;
+            int need = top;
+            for (int shift = 24; shift >= 0; shift -= 8) {
+                __syncthreads();
+                s_hist[t] = 0;
+                __syncthreads();
+                for_share<FP32>(row, span, t, [&](float x, int) {
+                    const uint32_t o = ordered(x);
+                    if (o > kOrderedMinusInf && (shift == 24 || (o >> (shift + 8)) == (prefix >> (shift + 8)))) atomicAdd(&s_hist[(o >> shift) & 255u], 1u);
+                });
+                __syncthreads();
+                if (t == 0) {
+                    int digit = 255, left = need;
+                    while (digit > 0 && (int)s_hist[digit] < left) left -= (int)s_hist[digit--];
+                    s_pick[0] = (uint32_t)digit;
+                    s_pick[1] = (uint32_t)left;
+                }
+                __syncthreads();
+                prefix |= s_pick[0] << shift;
+                need = (int)s_pick[1];
+            }
+            // what lies above it (fewer than top), then the first `need` that equal it, in order of the row
+            if (t == 0) s_n = 0;
+            __syncthreads();
+            for_share<FP32>(row, span, t, [&](float x, int i) {
+                const uint32_t o = ordered(x);
+                if (o > prefix) {
+                    const int at = atomicAdd(&s_n, 1);
+                    if (at < kList) { s_value[at] = o; s_index[at] = i; }
+                }
+            });
+            __syncthreads();
+            n = s_n;
+            for (int i0 = span.lo; i0 < span.hi && need > 0; i0 += kThreads) {
+                const int i = i0 + t;
+                const bool hit = i < span.hi && ordered(logit_at<FP32>(row, i)) == prefix;
+                const unsigned mask = __ballot_sync(0xffffffffu, hit);
+                if (lane == 0) s_warp_n[warp] = __popc(mask);
+                __syncthreads();
+                int before = 0, all = 0;
+#pragma unroll
+                for (int w = 0; w < kWarps; ++w) { if (w < warp) before += s_warp_n[w]; all += s_warp_n[w]; }
+                const int at = before + __popc(mask & ((1u << lane) - 1u));
+                if (hit && at < need) { s_value[n + at] = prefix; s_index[n + at] = i; }
+                const int took = min(all, need);
+                n += took;
+                need -= took;
+                __syncthreads();
+            }
+        }
+        n_top = min(n, top);
+        rank_list(s_value, s_index, n, top, s_top_value, s_top_index, t);
+    }
+    __syncthreads();
+
+    // --- this part's statistics
+    Stats all = {s_m[0], s_s[0], s_w[0]};
+#pragma unroll
+    for (int w = 1; w < kWarps; ++w) join(all, s_m[w], s_s[w], s_w[w]);
+    int row_bad = s_bad;
+
+    if (p.parts > 1) {
+        Part& mine = p.part[row_i * p.parts + part];
+        if (t == 0) { __stcg(&mine.m, all.m); __stcg(&mine.s, all.s); __stcg(&mine.w, all.w); __stcg(&mine.bad, row_bad); }
+        if (t < top) { __stcg(&mine.value[t], t < n_top ? s_top_value[t] : 0u); __stcg(&mine.index[t], t < n_top ? s_top_index[t] : -1); }
+        __threadfence();
         __syncthreads();
         if (t == 0) {
-            for (int i = 0; i < 8; ++i) b = best[i] > b ? best[i] : b;
-            chosen = b;
-            const int id = b ? (int)~(uint32_t)b : -1;
-            a.top_ids[row * a.top + k] = id;
-            a.top_logprobs[row * a.top + k] = none ? nan_f() : id < 0 ? -INFINITY : logit(a, row, id) - m - ls;
+            s_last = atomicAdd(p.arrived + row_i, 1u) == (unsigned)(p.parts - 1);
+            if (s_last) p.arrived[row_i] = 0u;
         }
         __syncthreads();
-        last = chosen;
+        if (!s_last) return;
+        __threadfence();
+        const Part* const parts = p.part + row_i * p.parts;
+        // statistics: every warp joins all of them, two a lane, in an order of its own making but always the same
+        all = {-INFINITY, 0.f, 0.f};
+        row_bad = 0;
+        for (int b = lane; b < p.parts; b += 32) {
+            join(all, __ldcg(&parts[b].m), __ldcg(&parts[b].s), __ldcg(&parts[b].w));
+            row_bad |= __ldcg(&parts[b].bad);
+        }
+#pragma unroll
+        for (int o = 16; o; o >>= 1) {
+            join(all, __shfl_xor_sync(0xffffffffu, all.m, o), __shfl_xor_sync(0xffffffffu, all.s, o), __shfl_xor_sync(0xffffffffu, all.w, o));
+            row_bad |= __shfl_xor_sync(0xffffffffu, row_bad, o);
+        }
+        if (top > 0) {
+            // the same bound over the parts' lists: the top-th largest of the parts' largest leaves at most top lists to take from
+            const uint32_t head = t < p.parts ? __ldcg(&parts[t].value[0]) : 0u;
+            if (t == 0) { s_n = 0; s_bound = 0u; }
+            if (t < kGroups) s_best[t] = head;
+            __syncthreads();
+            if (t < kGroups) {
+                int above = 0, same = 0;
+#pragma unroll 8
+                for (int j = 0; j < kGroups; ++j) { above += s_best[j] > head; same += s_best[j] == head; }
+                if (above < top && above + same >= top) s_bound = head;
+            }
+            __syncthreads();
+            const uint32_t bound = max(s_bound, 1u);
+            for (int i = t; i < p.parts * top; i += kThreads) {
+                const Part& q = parts[i / top];
+                if (s_best[i / top] < bound) continue;
+                const uint32_t v = __ldcg(&q.value[i % top]);
+                if (v >= bound) {
+                    const int at = atomicAdd(&s_n, 1);
+                    if (at < kList) { s_value[at] = v; s_index[at] = __ldcg(&q.index[i % top]); }
+                }
+            }
+            __syncthreads();
+            const int n = min(s_n, kList);
+            n_top = min(n, top);
+            rank_list(s_value, s_index, n, top, s_top_value, s_top_index, t);
+            __syncthreads();
+        }
+    }
+
+    // --- outputs
+    const bool none = row_bad || !(all.s > 0.f);
+    const float log_s = logf(all.s);
+    if (t == 0) {
+        const int tok = a.tokens[row_i];
+        const bool in = tok >= 0 && tok < a.vocab;
+        a.logprobs[row_i] = none || !in ? nan_f() : logit_at<FP32>(row, tok) - all.m - log_s;
+        if (a.entropies) a.entropies[row_i] = none ? nan_f() : log_s - all.w / all.s;
+    }
+    if (t < top) {
+        const bool there = t < n_top;
+        a.top_ids[row_i * top + t] = none || !there ? -1 : s_top_index[t];
+        a.top_logprobs[row_i * top + t] = none ? nan_f() : there ? unordered(s_top_value[t]) - all.m - log_s : -INFINITY;
     }
 }
 
@@ -80,8 +375,28 @@ __global__ void __launch_bounds__(256) token_logprobs_simple(LogprobArgs a) {
 
 cudaError_t configure_token_logprobs() { return cudaSuccess; }
 
-mt_status launch_token_logprobs(const LogprobArgs& a, const OpContext&, cudaStream_t s) {
-    return launch_pdl(token_logprobs_simple, dim3((unsigned)a.n), dim3(256), 0, s, a) == cudaSuccess ? MT_OK : MT_ERR_CUDA;
+mt_status launch_token_logprobs(const LogprobArgs& a, const OpContext& c, cudaStream_t s) {
+    Params p;
+    p.a = a;
+    // parts: enough for four CTAs an SM, none shorter than kMinPart
+    int64_t want = (4LL * c.sm_count + a.n - 1) / a.n;
+    const int64_t most = (a.vocab + kMinPart - 1) / kMinPart;
+    if (want > most) want = most;
+    if (want > kMaxParts) want = kMaxParts;
+    p.parts = want > 1 && a.n < (1 << 20) ? (int)want : 1;
+    p.part_len = ((a.vocab + p.parts - 1) / p.parts + 7) / 8 * 8;
+    p.arrived = nullptr;
+    p.part = nullptr;
+    if (p.parts > 1) {
+        uint8_t* w = nullptr;
+        mt_status st = op_scratch(s, kScratchZeroBytes + (size_t)a.n * p.parts * sizeof(Part), &w);
+        if (st != MT_OK) return st;
+        p.arrived = reinterpret_cast<unsigned*>(w);
+        p.part = reinterpret_cast<Part*>(w + kScratchZeroBytes);
+    }
+    const int64_t grid = (int64_t)a.n * p.parts;
+    const cudaError_t e = launch_pdl(a.fp32 ? token_logprobs_kernel<true> : token_logprobs_kernel<false>, dim3((unsigned)grid), dim3(kThreads), 0, s, p);
+    return e == cudaSuccess ? MT_OK : MT_ERR_CUDA;
 }
 
 }  // namespace mt
