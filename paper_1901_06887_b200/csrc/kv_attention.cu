@@ -55,11 +55,6 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t a) {
     asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(a));
     return d;
 }
-__device__ __forceinline__ float ex2(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
 // The power of two that brings the number with these bits into [2^(BITS - 1), 2^BITS), and its reciprocal (both normal numbers for
 // every exponent).
 template <int BITS>

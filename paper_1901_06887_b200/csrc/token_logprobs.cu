@@ -4,7 +4,7 @@
 // One pass over the logits: every thread keeps (m, S, W) of its share, rescaled when its maximum moves.
 //
 // Alternatives.  The pass also leaves the largest logit of each thread and of each group of four.  The k-th largest of the 64 groups' is a bound
-// that the k-th largest logit cannot lie below, so only the threads that reach it look at their share again (from L2) and put what reaches it on
+// that the k-th largest logit cannot lie below, so only the shares that reach it are looked at again (from L2, a warp at a time) and what reaches it is put on
 // a list; it holds little more than k entries.  The list is ranked by counting, every entry against every other, on (value, lower index first), so the result
 // does not depend on the order of arrival.  Where too many logits reach the bound (long ties, values sorted into one share) the exact k-th
 // largest is found by its bits, eight at a time, from histograms of the row, and ties at it are taken from the front of the row.
@@ -43,11 +43,6 @@ struct Params {
     Part* part;                            // [rows][parts]
 };
 
-__device__ __forceinline__ float ex2(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
 // Bits that grow with the value (minus zero counts as zero); 0 is below every number, so it can stand for "nothing".
 __device__ __forceinline__ uint32_t ordered(float x) {
     const uint32_t b = __float_as_uint(x + 0.f);
@@ -58,22 +53,35 @@ __device__ __forceinline__ float unordered(uint32_t o) {
 }
 constexpr uint32_t kOrderedMinusInf = 0x007fffffu;         // ordered(-inf)
 
+// Sixteen bytes of logits.
 template <bool FP32> struct Vec;
 template <> struct Vec<true> {
     static constexpr int N = 4;
-    float x[4];
-    __device__ void load(const void* p) {
-        const float4 v = *reinterpret_cast<const float4*>(p);
-        x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w;
+    uint4 v;
+    __device__ __forceinline__ float operator[](int e) const { return __uint_as_float(e == 0 ? v.x : e == 1 ? v.y : e == 2 ? v.z : v.w); }
+    __device__ __forceinline__ float max_nan() const {          // NaN if any is
+        float m = __uint_as_float(v.x);
+        asm("max.NaN.f32 %0, %0, %1;" : "+f"(m) : "f"(__uint_as_float(v.y)));
+        asm("max.NaN.f32 %0, %0, %1;" : "+f"(m) : "f"(__uint_as_float(v.z)));
+        asm("max.NaN.f32 %0, %0, %1;" : "+f"(m) : "f"(__uint_as_float(v.w)));
+        return m;
     }
 };
 template <> struct Vec<false> {
     static constexpr int N = 8;
-    float x[8];
-    __device__ void load(const void* p) {
-        const uint4 v = *reinterpret_cast<const uint4*>(p);
-        x[0] = bf16_lo(v.x); x[1] = bf16_hi(v.x); x[2] = bf16_lo(v.y); x[3] = bf16_hi(v.y);
-        x[4] = bf16_lo(v.z); x[5] = bf16_hi(v.z); x[6] = bf16_lo(v.w); x[7] = bf16_hi(v.w);
+    uint4 v;
+    __device__ __forceinline__ float operator[](int e) const {
+        const uint32_t w = e < 2 ? v.x : e < 4 ? v.y : e < 6 ? v.z : v.w;
+        return e & 1 ? bf16_hi(w) : bf16_lo(w);
+    }
+    __device__ __forceinline__ float max_nan() const {          // two at a time
+        uint32_t m = v.x;
+        asm("max.NaN.bf16x2 %0, %0, %1;" : "+r"(m) : "r"(v.y));
+        asm("max.NaN.bf16x2 %0, %0, %1;" : "+r"(m) : "r"(v.z));
+        asm("max.NaN.bf16x2 %0, %0, %1;" : "+r"(m) : "r"(v.w));
+        float a = bf16_lo(m);
+        asm("max.NaN.f32 %0, %0, %1;" : "+f"(a) : "f"(bf16_hi(m)));
+        return a;
     }
 };
 template <bool FP32>
@@ -102,12 +110,26 @@ __device__ __forceinline__ void for_share(const void* row, const Span& s, int t,
     constexpr int N = Vec<FP32>::N, B = FP32 ? 4 : 2;
     for (int v = t; v < s.n_vec; v += kThreads) {
         Vec<FP32> x;
-        x.load(static_cast<const char*>(row) + (size_t)(s.vec0 + v * N) * B);
+        x.v = *reinterpret_cast<const uint4*>(static_cast<const char*>(row) + (size_t)(s.vec0 + v * N) * B);
 #pragma unroll
-        for (int e = 0; e < N; ++e) f(x.x[e], s.vec0 + v * N + e);
+        for (int e = 0; e < N; ++e) f(x[e], s.vec0 + v * N + e);
     }
     if (t < s.vec0 - s.lo) f(logit_at<FP32>(row, s.lo + t), s.lo + t);
     if (t < s.hi - s.tail) f(logit_at<FP32>(row, s.tail + t), s.tail + t);
+}
+
+// The same for ANOTHER thread's share (thread `of` of this part), by a whole warp at once.
+template <bool FP32, class F>
+__device__ __forceinline__ void for_share_of(const void* row, const Span& s, int of, int lane, F f) {
+    constexpr int N = Vec<FP32>::N, B = FP32 ? 4 : 2;
+    for (int v = of + lane * kThreads; v < s.n_vec; v += 32 * kThreads) {
+        Vec<FP32> x;
+        x.v = *reinterpret_cast<const uint4*>(static_cast<const char*>(row) + (size_t)(s.vec0 + v * N) * B);
+#pragma unroll
+        for (int e = 0; e < N; ++e) f(x[e], s.vec0 + v * N + e);
+    }
+    if (lane == 0 && of < s.vec0 - s.lo) f(logit_at<FP32>(row, s.lo + of), s.lo + of);
+    if (lane == 1 && of < s.hi - s.tail) f(logit_at<FP32>(row, s.tail + of), s.tail + of);
 }
 
 struct Stats {
@@ -158,11 +180,7 @@ __global__ void __launch_bounds__(kThreads) token_logprobs_kernel(const Params p
     Stats st = {-INFINITY, 0.f, 0.f};
     float best = -INFINITY;
     bool bad = false;
-    auto add = [&](const float* x, int n) {
-        float mx = x[0];
-#pragma unroll
-        for (int e = 1; e < N; ++e)
-            if (e < n) asm("max.NaN.f32 %0, %0, %1;" : "+f"(mx) : "f"(x[e]));
+    auto reach = [&](float mx) {               // false: nothing but minus infinity so far
         bad = bad || !(mx < INFINITY);
         best = fmaxf(best, mx);
         if (mx > st.m) {                       // the sums move to the new maximum
@@ -171,33 +189,51 @@ __global__ void __launch_bounds__(kThreads) token_logprobs_kernel(const Params p
             st.s *= f;
             st.m = mx;
         }
-        if (st.m == -INFINITY) return;
+        return st.m > -INFINITY;
+    };
+    auto add = [&](const Vec<FP32>& x) {
+        if (!reach(x.max_nan())) return;
+        const Pair m2 = pair_of(-st.m, -st.m), c2 = pair_of(kLog2e, kLog2e);
+        Pair s2 = pair_of(0.f, 0.f), w2 = pair_of(0.f, 0.f);
 #pragma unroll
-        for (int e = 0; e < N; ++e)
-            if (e < n) {
-                const float d = fmaxf(x[e] - st.m, -1e4f), q = exp_of(d);       // (minus infinity: q = 0, d finite)
-                st.s += q;
-                st.w = fmaf(q, d, st.w);
-            }
+        for (int e = 0; e < N; e += 2) {
+            float d0, d1, q0, q1;
+            unpair(add2(pair_of(x[e], x[e + 1]), m2), d0, d1);
+            const Pair d = pair_of(fmaxf(d0, -1e4f), fmaxf(d1, -1e4f));         // (minus infinity: q = 0, d finite)
+            unpair(mul2(d, c2), q0, q1);
+            const Pair q = pair_of(ex2(q0), ex2(q1));
+            s2 = add2(s2, q);
+            w2 = fma2(q, d, w2);
+        }
+        float y0, y1;
+        unpair(s2, y0, y1);
+        st.s += y0 + y1;
+        unpair(w2, y0, y1);
+        st.w += y0 + y1;
+    };
+    auto add_one = [&](float x) {
+        if (!reach(x)) return;
+        const float d = fmaxf(x - st.m, -1e4f), q = exp_of(d);
+        st.s += q;
+        st.w = fmaf(q, d, st.w);
     };
     {
-        const char* const base = static_cast<const char*>(row) + (size_t)span.vec0 * B;
+        const uint4* const base = reinterpret_cast<const uint4*>(static_cast<const char*>(row) + (size_t)span.vec0 * B);
         int v = t;
         for (; v + 3 * kThreads < span.n_vec; v += 4 * kThreads) {       // four loads in flight
             Vec<FP32> x[4];
 #pragma unroll
-            for (int u = 0; u < 4; ++u) x[u].load(base + (size_t)(v + u * kThreads) * 16);
+            for (int u = 0; u < 4; ++u) x[u].v = __ldg(base + v + u * kThreads);
 #pragma unroll
-            for (int u = 0; u < 4; ++u) add(x[u].x, N);
+            for (int u = 0; u < 4; ++u) add(x[u]);
         }
         for (; v < span.n_vec; v += kThreads) {
             Vec<FP32> x;
-            x.load(base + (size_t)v * 16);
-            add(x.x, N);
+            x.v = __ldg(base + v);
+            add(x);
         }
-        float x[N];
-        if (t < span.vec0 - span.lo) { x[0] = logit_at<FP32>(row, span.lo + t); add(x, 1); }
-        if (t < span.hi - span.tail) { x[0] = logit_at<FP32>(row, span.tail + t); add(x, 1); }
+        if (t < span.vec0 - span.lo) add_one(logit_at<FP32>(row, span.lo + t));
+        if (t < span.hi - span.tail) add_one(logit_at<FP32>(row, span.tail + t));
     }
     const uint32_t mine_best = ordered(best);
     {
@@ -225,8 +261,8 @@ __global__ void __launch_bounds__(kThreads) token_logprobs_kernel(const Params p
         }
         __syncthreads();
         const uint32_t bound = max(s_bound, kOrderedMinusInf + 1u);
-        if (mine_best >= bound)
-            for_share<FP32>(row, span, t, [&](float x, int i) {
+        for (unsigned who = __ballot_sync(0xffffffffu, mine_best >= bound); who; who &= who - 1)
+            for_share_of<FP32>(row, span, t - lane + __ffs(who) - 1, lane, [&](float x, int i) {
                 const uint32_t o = ordered(x);
                 if (o >= bound) {
                     const int at = atomicAdd(&s_n, 1);
