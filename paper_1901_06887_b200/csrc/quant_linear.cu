@@ -1,4 +1,16 @@
-// Products of a mixed batch of rows with the tenants' 4-bit weights.  First form: one warp per (row, 16 outputs).
+// Products of a mixed batch of rows with the tenants' 4-bit weights: y_r = sum_k scale (code - 8) x_rk + bias, tenant by tenant.
+//
+// Mathematics.  The codes enter the matrix instructions as the exact bf16 numbers code - 8 (four bits set into the mantissa of 128, then an
+// exact subtraction of 136) with the weights as the 16-row operand and up to 64 of the tenant's rows as columns; the sum over 64 (or 32)
+// inputs is multiplied with the group's scale in fp32 and added up in fp32.  Nothing is rounded but the sums.
+//
+// Bound: memory, K / 2 + 2 K / group bytes per output and tenant, whatever the number of its rows (up to some 16; beyond, the matrix
+// instructions).  The packed order makes a warp's load 512 contiguous bytes that are the operand of four instructions; the rows' slices of the
+// inner index are chosen so that a lane's inputs are 16 contiguous bytes too, so nothing passes through shared memory on the way in.
+//
+// Split.  A CTA takes (tenant, 16 outputs) units in turn, its eight warps every eighth block of 64 inputs; they join through shared memory.
+// Which tenants occur is found out by every CTA for itself from the ids (at most 256 a launch): no bucketing launch, and only tenants that
+// occur cost anything.
 #include "lm_device.cuh"
 #include "lm_host.h"
 
@@ -35,43 +47,183 @@ __global__ void quant_pack_kernel(const uint8_t* __restrict__ codes, const uint1
     }
 }
 
-__global__ void quant_linear_simple(QuantLinearArgs a) {
-    pdl_launch_dependents();
-    pdl_wait();
-    const int tiles = (a.N + 15) / 16;
-    const int warp = (blockIdx.x * blockDim.x + threadIdx.x) / 32, lane = threadIdx.x & 31;
-    const int r = warp / tiles, tile = warp % tiles;
-    if (r >= a.n) return;
-    const int id = a.ids[r], g = lane / 4, t = lane & 3;
-    const bool bad = id < 0 || id >= a.tenants;
-    float acc[2] = {};
-    if (!bad) {
-        const uint8_t* base = a.packed + (size_t)id * quant_tenant_bytes(a.K, a.N, a.group);
-        const uint4* codes = reinterpret_cast<const uint4*>(base) + (size_t)tile * (a.K / 64) * 32;
-        const uint16_t* sc = reinterpret_cast<const uint16_t*>(base + quant_codes_bytes(a.K, a.N)) + (size_t)tile * (a.K / a.group) * 16;
-        for (int kb = 0; kb < a.K / 64; ++kb) {
-            const uint4 w = codes[kb * 32 + lane];
-            const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
-            for (int i = 0; i < 4; ++i) {
-                const int k0 = kb * 64 + 32 * (i & 1) + 8 * t;
-                float p = 0.f;
-                for (int j = 0; j < 8; ++j)
-                    p += bf16_to_f(a.x[r * a.x_stride + k0 + j]) * (float)((int)((ws[i] >> (4 * (j / 2) + 16 * (j & 1))) & 15) - 8);
-                acc[i >> 1] += p * bf16_to_f(sc[(k0 / a.group) * 16 + g * 2 + (i >> 1)]);
+constexpr int kThreads = 256, kWarps = 8;
+
+__device__ __forceinline__ void mma_bf16(float (&c)[4], const uint32_t a0, const uint32_t a1, const uint32_t a2, const uint32_t a3,
+                                         const uint32_t b0, const uint32_t b1) {
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// Codes in nibbles P and P + 4 of w as two bf16 numbers code - 8.
+template <int P>
+__device__ __forceinline__ uint32_t centred(uint32_t w) {
+    uint32_t d;
+    asm("add.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(((w >> (4 * P)) & 0x000f000fu) | 0x43004300u), "r"(0xc308c308u));   // 128 + code - 136
+    return d;
+}
+
+struct Shared {
+    int ids[kQuantRowsPerLaunch], slot[kQuantRowsPerLaunch], order[kQuantRowsPerLaunch];
+    int tenant[kQuantRowsPerLaunch], begin[kQuantRowsPerLaunch + 1];
+    int warp_n[kWarps];
+    int n_slots, n_valid;
+};
+
+// One unit: 16 outputs of one tenant for up to 8 NT rows (s.order[r0 ..]).
+template <int NT, bool G32>
+__device__ __forceinline__ void unit(const QuantLinearArgs& a, const Shared& s, float* red, const uint8_t* base, size_t codes_bytes, int tile, int r0,
+                                     int rows, int tenant) {
+    const int tid = threadIdx.x, warp = tid / 32, lane = tid & 31, g = lane >> 2, t = lane & 3;
+    const int kblocks = a.K / 64, groups = a.K / a.group;
+    const uint4* const codes = reinterpret_cast<const uint4*>(base) + (size_t)tile * kblocks * 32 + lane;
+    const uint32_t* const scales = reinterpret_cast<const uint32_t*>(base + codes_bytes) + (size_t)tile * groups * 8 + g;
+    const int per = G32 ? 1 : a.group / 64;          // blocks per group (G32: two groups per block)
+    const uint16_t* x[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) x[n] = n * 8 + g < rows ? a.x + (int64_t)s.order[r0 + n * 8 + g] * a.x_stride + 8 * t : nullptr;
+    float acc[NT][4];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) acc[n][0] = acc[n][1] = acc[n][2] = acc[n][3] = 0.f;
+
+    constexpr int U = NT == 1 ? 4 : NT == 2 ? 2 : 1;      // blocks in flight
+    for (int kb0 = warp; kb0 < kblocks; kb0 += U * kWarps) {
+        uint4 w[U];
+        uint32_t sc[U][2];
+        uint4 xv[U][NT][2];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int kb = kb0 + u * kWarps;
+            w[u] = make_uint4(0x88888888u, 0x88888888u, 0x88888888u, 0x88888888u);
+            sc[u][0] = sc[u][1] = 0u;
+            if (kb < kblocks) {
+                w[u] = __ldcs(codes + (size_t)kb * 32);
+                sc[u][0] = __ldg(scales + (size_t)(G32 ? 2 * kb : kb / per) * 8);
+                if (G32) sc[u][1] = __ldg(scales + (size_t)(2 * kb + 1) * 8);
+            }
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                xv[u][n][0] = xv[u][n][1] = make_uint4(0u, 0u, 0u, 0u);
+                if (kb < kblocks && x[n]) {
+                    xv[u][n][0] = __ldg(reinterpret_cast<const uint4*>(x[n] + kb * 64));
+                    xv[u][n][1] = __ldg(reinterpret_cast<const uint4*>(x[n] + kb * 64 + 32));
+                }
             }
         }
-    } else if (tile == 0 && lane == 0) {
-        raise_status(a.status, MT_ERR_BAD_MODEL_ID, a.row0 + r);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            float c[NT][4];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {                // inputs 0..31 and 32..63 of the block
+                const uint32_t lo = h == 0 ? w[u].x : w[u].y, hi = h == 0 ? w[u].z : w[u].w;      // rows g and g + 8
+                const uint32_t a00 = centred<0>(lo), a01 = centred<1>(lo), a02 = centred<2>(lo), a03 = centred<3>(lo);
+                const uint32_t a10 = centred<0>(hi), a11 = centred<1>(hi), a12 = centred<2>(hi), a13 = centred<3>(hi);
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    if (h == 0 || G32) c[n][0] = c[n][1] = c[n][2] = c[n][3] = 0.f;
+                    const uint4 v = xv[u][n][h];
+                    mma_bf16(c[n], a00, a10, a01, a11, v.x, v.y);
+                    mma_bf16(c[n], a02, a12, a03, a13, v.z, v.w);
+                    if (h == 1 || G32) {
+                        const float s0 = bf16_lo(sc[u][G32 ? h : 0]), s1 = bf16_hi(sc[u][G32 ? h : 0]);
+                        acc[n][0] = fmaf(s0, c[n][0], acc[n][0]); acc[n][1] = fmaf(s0, c[n][1], acc[n][1]);
+                        acc[n][2] = fmaf(s1, c[n][2], acc[n][2]); acc[n][3] = fmaf(s1, c[n][3], acc[n][3]);
+                    }
+                }
+            }
+        }
     }
-    for (int i = 0; i < 2; ++i) {
-        float v = acc[i];
-        v += __shfl_xor_sync(0xffffffffu, v, 1);
-        v += __shfl_xor_sync(0xffffffffu, v, 2);
-        const int row = tile * 16 + g + 8 * i;
-        if (t != 0 || row >= a.N) continue;
-        v = bad ? nan_f() : v + (a.bias ? a.bias[(size_t)id * a.N + row] : 0.f);
-        if (a.y_fp32) static_cast<float*>(a.y)[r * a.y_stride + row] = v;
-        else static_cast<uint16_t*>(a.y)[r * a.y_stride + row] = f_to_bf16(v);
+    // join the warps: red[warp][column][16 outputs, padded to 20]
+    __syncthreads();                                       // the unit before this has been read
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        float* const r = red + ((warp * NT + n) * 8 + 2 * t) * 20 + g;
+        r[0] = acc[n][0]; r[20] = acc[n][1]; r[8] = acc[n][2]; r[28] = acc[n][3];
+    }
+    __syncthreads();
+    for (int i = tid; i < rows * 16; i += kThreads) {
+        const int col = i >> 4, o = i & 15, out = tile * 16 + o;
+        if (out >= a.N) continue;
+        float v = 0.f;
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) v += red[(w * NT * 8 + col) * 20 + o];
+        if (a.bias) v += __ldg(a.bias + (size_t)tenant * a.N + out);
+        const int64_t at = (int64_t)s.order[r0 + col] * a.y_stride + out;
+        if (a.y_fp32) static_cast<float*>(a.y)[at] = v;
+        else static_cast<uint16_t*>(a.y)[at] = f_to_bf16(v);
+    }
+}
+
+// MAXT: largest number of column tiles a pass may take (a launch of n rows never needs more than n of them).
+template <int MAXT, bool G32>
+__global__ void __launch_bounds__(kThreads, MAXT <= 2 ? 3 : 2) quant_linear_kernel(const QuantLinearArgs a) {
+    __shared__ Shared s;
+    __shared__ float red[kWarps * MAXT * 8 * 20];
+    const int tid = threadIdx.x, warp = tid / 32, lane = tid & 31;
+    pdl_launch_dependents();
+    pdl_wait();
+    // --- rows by tenant: slots in order of first appearance, rows of a slot in order of the batch, rows with a bad id last
+    const int id = tid < a.n ? a.ids[tid] : -1;
+    const bool good = id >= 0 && id < a.tenants;
+    s.ids[tid] = good ? id : -1;
+    if (tid < a.n && !good && blockIdx.x == 0) raise_status(a.status, MT_ERR_BAD_MODEL_ID, a.row0 + tid);
+    __syncthreads();
+    int first = tid;
+    if (good)
+        for (int j = 0; j < tid; ++j)
+            if (s.ids[j] == id) { first = j; break; }
+    const unsigned firsts = __ballot_sync(0xffffffffu, good && first == tid);
+    if (lane == 0) s.warp_n[warp] = __popc(firsts);
+    __syncthreads();
+    int slot = __popc(firsts & ((1u << lane) - 1u)), n_slots = 0;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) {
+        if (w < warp) slot += s.warp_n[w];
+        n_slots += s.warp_n[w];
+    }
+    if (good && first == tid) { s.slot[tid] = slot; s.tenant[slot] = id; }
+    __syncthreads();
+    const int mine = good ? s.slot[first] : n_slots;       // (written by first occurrences only: stable from here on)
+    __syncthreads();
+    s.slot[tid] = tid < a.n ? mine : 0x7fffffff;
+    __syncthreads();
+    if (tid < a.n) {
+        int at = 0, same = 0;
+        for (int j = 0; j < a.n; ++j) {
+            const int sj = s.slot[j];
+            at += (sj < mine || (sj == mine && j < tid)) ? 1 : 0;
+            same += (sj == mine && j < tid) ? 1 : 0;
+        }
+        s.order[at] = tid;
+        if (same == 0) s.begin[mine] = at;
+    }
+    if (tid == 0) s.n_slots = n_slots;
+    const int n_valid = __syncthreads_count(good);
+    if (tid == 0) s.begin[n_slots] = n_valid;
+    __syncthreads();
+
+    for (int i = n_valid; i < a.n; ++i) {                  // rows with a bad id
+        const int64_t at = (int64_t)s.order[i] * a.y_stride;
+        for (int o = blockIdx.x * kThreads + tid; o < a.N; o += gridDim.x * kThreads) {
+            if (a.y_fp32) static_cast<float*>(a.y)[at + o] = nan_f();
+            else static_cast<uint16_t*>(a.y)[at + o] = 0x7fff;
+        }
+    }
+
+    const int tiles = (a.N + 15) / 16;
+    const size_t codes_bytes = quant_codes_bytes(a.K, a.N), tenant_bytes = quant_tenant_bytes(a.K, a.N, a.group);
+    const int64_t units = (int64_t)tiles * n_slots;
+    for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
+        const int sl = (int)(u / tiles), tile = (int)(u - (int64_t)sl * tiles), tenant = s.tenant[sl];
+        const uint8_t* const base = a.packed + (size_t)tenant * tenant_bytes;
+        for (int r0 = s.begin[sl], end = s.begin[sl + 1]; r0 < end; r0 += 64) {
+            const int rows = min(end - r0, 64);
+            if (MAXT == 1 || rows <= 8) unit<1, G32>(a, s, red, base, codes_bytes, tile, r0, rows, tenant);
+            else if (MAXT == 2 || rows <= 16) unit<(MAXT < 2 ? MAXT : 2), G32>(a, s, red, base, codes_bytes, tile, r0, rows, tenant);
+            else if (rows <= 32) unit<(MAXT < 4 ? MAXT : 4), G32>(a, s, red, base, codes_bytes, tile, r0, rows, tenant);
+            else unit<(MAXT < 8 ? MAXT : 8), G32>(a, s, red, base, codes_bytes, tile, r0, rows, tenant);
+        }
     }
 }
 
@@ -89,9 +241,16 @@ cudaError_t launch_quant_pack(const uint8_t* codes, const uint16_t* scales, int 
     return cudaGetLastError();
 }
 
-cudaError_t launch_quant_linear(const QuantLinearArgs& a, int, cudaStream_t s) {
-    const int64_t warps = (int64_t)a.n * ((a.N + 15) / 16);
-    return launch_pdl(quant_linear_simple, dim3((unsigned)((warps + 7) / 8)), dim3(256), 0, s, a);
+cudaError_t launch_quant_linear(const QuantLinearArgs& a, int sm_count, cudaStream_t s) {
+    const bool g32 = a.group == 32;
+    const int most_slots = a.n < a.tenants ? a.n : a.tenants;
+    const int64_t units = (int64_t)((a.N + 15) / 16) * most_slots;
+    const int maxt = a.n <= 8 ? 1 : a.n <= 16 ? 2 : 8;
+    int64_t grid = (int64_t)sm_count * (maxt <= 2 ? 3 : 2);
+    if (grid > units) grid = units;
+    auto k = g32 ? (maxt == 1 ? quant_linear_kernel<1, true> : maxt == 2 ? quant_linear_kernel<2, true> : quant_linear_kernel<8, true>)
+                 : (maxt == 1 ? quant_linear_kernel<1, false> : maxt == 2 ? quant_linear_kernel<2, false> : quant_linear_kernel<8, false>);
+    return launch_pdl(k, dim3((unsigned)grid), dim3(kThreads), 0, s, a);
 }
 
 }  // namespace mt
