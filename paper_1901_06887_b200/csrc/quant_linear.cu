@@ -49,12 +49,13 @@ __global__ void quant_pack_kernel(const uint8_t* __restrict__ codes, const uint1
 
 constexpr int kThreads = 256, kWarps = 8;
 
-__device__ __forceinline__ void mma_bf16(float (&c)[4], const uint32_t a0, const uint32_t a1, const uint32_t a2, const uint32_t a3,
-                                         const uint32_t b0, const uint32_t b1) {
+// D = A B + C
+__device__ __forceinline__ void mma_bf16(float (&d)[4], const uint32_t a0, const uint32_t a1, const uint32_t a2, const uint32_t a3,
+                                         const uint32_t b0, const uint32_t b1, const float (&c)[4]) {
     asm volatile(
-        "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+        "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%11,%12,%13};"
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(c[0]), "f"(c[1]), "f"(c[2]), "f"(c[3]));
 }
 // Codes in nibbles P and P + 4 of w as two bf16 numbers code - 8.
 template <int P>
@@ -76,63 +77,66 @@ template <int NT, bool G32>
 __device__ __forceinline__ void unit(const QuantLinearArgs& a, const Shared& s, float* red, const uint8_t* base, size_t codes_bytes, int tile, int r0,
                                      int rows, int tenant) {
     const int tid = threadIdx.x, warp = tid / 32, lane = tid & 31, g = lane >> 2, t = lane & 3;
-    const int kblocks = a.K / 64, groups = a.K / a.group;
+    const int kblocks = a.K / 64, groups = a.groups;
     const uint4* const codes = reinterpret_cast<const uint4*>(base) + (size_t)tile * kblocks * 32 + lane;
     const uint32_t* const scales = reinterpret_cast<const uint32_t*>(base + codes_bytes) + (size_t)tile * groups * 8 + g;
-    const int per = G32 ? 1 : a.group / 64;          // blocks per group (G32: two groups per block)
-    const uint16_t* x[NT];
+    const uint16_t* x[NT];                       // (columns behind the last row repeat a row; they are not written)
 #pragma unroll
-    for (int n = 0; n < NT; ++n) x[n] = n * 8 + g < rows ? a.x + (int64_t)s.order[r0 + n * 8 + g] * a.x_stride + 8 * t : nullptr;
+    for (int n = 0; n < NT; ++n) x[n] = a.x + (int64_t)s.order[r0 + min(n * 8 + g, rows - 1)] * a.x_stride + 8 * t;
     float acc[NT][4];
 #pragma unroll
     for (int n = 0; n < NT; ++n) acc[n][0] = acc[n][1] = acc[n][2] = acc[n][3] = 0.f;
 
-    constexpr int U = NT == 1 ? 4 : NT == 2 ? 2 : 1;      // blocks in flight
-    for (int kb0 = warp; kb0 < kblocks; kb0 += U * kWarps) {
-        uint4 w[U];
-        uint32_t sc[U][2];
-        uint4 xv[U][NT][2];
+    struct Block {
+        uint4 w, x[NT][2];
+        uint32_t s0, s1;
+    };
+    auto load = [&](Block& b, int kb) {
+        b.w = __ldcs(codes + (size_t)kb * 32);
+        b.s0 = __ldg(scales + (size_t)(G32 ? 2 * kb : (int)__umulhi(kb + 1, a.per_magic)) * 8);       // kb / (blocks per group)
+        if (G32) b.s1 = __ldg(scales + (size_t)(2 * kb + 1) * 8);
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int kb = kb0 + u * kWarps;
-            w[u] = make_uint4(0x88888888u, 0x88888888u, 0x88888888u, 0x88888888u);
-            sc[u][0] = sc[u][1] = 0u;
-            if (kb < kblocks) {
-                w[u] = __ldcs(codes + (size_t)kb * 32);
-                sc[u][0] = __ldg(scales + (size_t)(G32 ? 2 * kb : kb / per) * 8);
-                if (G32) sc[u][1] = __ldg(scales + (size_t)(2 * kb + 1) * 8);
-            }
+        for (int n = 0; n < NT; ++n) {
+            b.x[n][0] = __ldg(reinterpret_cast<const uint4*>(x[n] + (size_t)kb * 64));
+            b.x[n][1] = __ldg(reinterpret_cast<const uint4*>(x[n] + (size_t)kb * 64 + 32));
+        }
+    };
+    auto use = [&](const Block& b) {
+        const float zero[4] = {0.f, 0.f, 0.f, 0.f};
+        float c[NT][4];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {                // inputs 0..31 and 32..63 of the block
+            const uint32_t lo = h == 0 ? b.w.x : b.w.y, hi = h == 0 ? b.w.z : b.w.w;      // rows g and g + 8
+            const uint32_t a00 = centred<0>(lo), a01 = centred<1>(lo), a02 = centred<2>(lo), a03 = centred<3>(lo);
+            const uint32_t a10 = centred<0>(hi), a11 = centred<1>(hi), a12 = centred<2>(hi), a13 = centred<3>(hi);
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
-                xv[u][n][0] = xv[u][n][1] = make_uint4(0u, 0u, 0u, 0u);
-                if (kb < kblocks && x[n]) {
-                    xv[u][n][0] = __ldg(reinterpret_cast<const uint4*>(x[n] + kb * 64));
-                    xv[u][n][1] = __ldg(reinterpret_cast<const uint4*>(x[n] + kb * 64 + 32));
+                const uint4 v = b.x[n][h];
+                if (h == 0 || G32) mma_bf16(c[n], a00, a10, a01, a11, v.x, v.y, zero);
+                else mma_bf16(c[n], a00, a10, a01, a11, v.x, v.y, c[n]);
+                mma_bf16(c[n], a02, a12, a03, a13, v.z, v.w, c[n]);
+                if (h == 1 || G32) {
+                    const uint32_t sc = G32 && h == 1 ? b.s1 : b.s0;
+                    const float s0 = bf16_lo(sc), s1 = bf16_hi(sc);
+                    acc[n][0] = fmaf(s0, c[n][0], acc[n][0]); acc[n][1] = fmaf(s0, c[n][1], acc[n][1]);
+                    acc[n][2] = fmaf(s1, c[n][2], acc[n][2]); acc[n][3] = fmaf(s1, c[n][3], acc[n][3]);
                 }
             }
         }
+    };
+    constexpr int U = NT == 1 ? 4 : NT == 2 ? 2 : 1;      // blocks in flight
+    int kb = warp;
+    for (; kb + (U - 1) * kWarps < kblocks; kb += U * kWarps) {
+        Block b[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            float c[NT][4];
+        for (int u = 0; u < U; ++u) load(b[u], kb + u * kWarps);
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {                // inputs 0..31 and 32..63 of the block
-                const uint32_t lo = h == 0 ? w[u].x : w[u].y, hi = h == 0 ? w[u].z : w[u].w;      // rows g and g + 8
-                const uint32_t a00 = centred<0>(lo), a01 = centred<1>(lo), a02 = centred<2>(lo), a03 = centred<3>(lo);
-                const uint32_t a10 = centred<0>(hi), a11 = centred<1>(hi), a12 = centred<2>(hi), a13 = centred<3>(hi);
-#pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    if (h == 0 || G32) c[n][0] = c[n][1] = c[n][2] = c[n][3] = 0.f;
-                    const uint4 v = xv[u][n][h];
-                    mma_bf16(c[n], a00, a10, a01, a11, v.x, v.y);
-                    mma_bf16(c[n], a02, a12, a03, a13, v.z, v.w);
-                    if (h == 1 || G32) {
-                        const float s0 = bf16_lo(sc[u][G32 ? h : 0]), s1 = bf16_hi(sc[u][G32 ? h : 0]);
-                        acc[n][0] = fmaf(s0, c[n][0], acc[n][0]); acc[n][1] = fmaf(s0, c[n][1], acc[n][1]);
-                        acc[n][2] = fmaf(s1, c[n][2], acc[n][2]); acc[n][3] = fmaf(s1, c[n][3], acc[n][3]);
-                    }
-                }
-            }
-        }
+        for (int u = 0; u < U; ++u) use(b[u]);
+    }
+    for (; kb < kblocks; kb += kWarps) {
+        Block b;
+        load(b, kb);
+        use(b);
     }
     // join the warps: red[warp][column][16 outputs, padded to 20]
     __syncthreads();                                       // the unit before this has been read
@@ -157,7 +161,7 @@ __device__ __forceinline__ void unit(const QuantLinearArgs& a, const Shared& s, 
 
 // MAXT: largest number of column tiles a pass may take (a launch of n rows never needs more than n of them).
 template <int MAXT, bool G32>
-__global__ void __launch_bounds__(kThreads, MAXT <= 2 ? 3 : 2) quant_linear_kernel(const QuantLinearArgs a) {
+__global__ void __launch_bounds__(kThreads, MAXT <= 4 ? 3 : 2) quant_linear_kernel(const QuantLinearArgs a) {
     __shared__ Shared s;
     __shared__ float red[kWarps * MAXT * 8 * 20];
     const int tid = threadIdx.x, warp = tid / 32, lane = tid & 31;
@@ -245,12 +249,18 @@ cudaError_t launch_quant_linear(const QuantLinearArgs& a, int sm_count, cudaStre
     const bool g32 = a.group == 32;
     const int most_slots = a.n < a.tenants ? a.n : a.tenants;
     const int64_t units = (int64_t)((a.N + 15) / 16) * most_slots;
-    const int maxt = a.n <= 8 ? 1 : a.n <= 16 ? 2 : 8;
-    int64_t grid = (int64_t)sm_count * (maxt <= 2 ? 3 : 2);
+    const int maxt = a.n <= 8 ? 1 : a.n <= 16 ? 2 : a.n <= 32 ? 4 : 8;
+    int64_t grid = (int64_t)sm_count * (maxt <= 4 ? 3 : 2);
     if (grid > units) grid = units;
-    auto k = g32 ? (maxt == 1 ? quant_linear_kernel<1, true> : maxt == 2 ? quant_linear_kernel<2, true> : quant_linear_kernel<8, true>)
-                 : (maxt == 1 ? quant_linear_kernel<1, false> : maxt == 2 ? quant_linear_kernel<2, false> : quant_linear_kernel<8, false>);
-    return launch_pdl(k, dim3((unsigned)grid), dim3(kThreads), 0, s, a);
+    typedef void (*Kernel)(QuantLinearArgs);
+    static const Kernel kernels[2][4] = {
+        {quant_linear_kernel<1, false>, quant_linear_kernel<2, false>, quant_linear_kernel<4, false>, quant_linear_kernel<8, false>},
+        {quant_linear_kernel<1, true>, quant_linear_kernel<2, true>, quant_linear_kernel<4, true>, quant_linear_kernel<8, true>}};
+    QuantLinearArgs b = a;
+    b.groups = a.K / a.group;
+    const uint32_t per = g32 ? 1u : (uint32_t)a.group / 64u;
+    b.per_magic = 0xffffffffu / per;
+    return launch_pdl(kernels[g32][maxt == 1 ? 0 : maxt == 2 ? 1 : maxt == 4 ? 2 : 3], dim3((unsigned)grid), dim3(kThreads), 0, s, b);
 }
 
 }  // namespace mt
