@@ -70,9 +70,10 @@ struct QuantLinearArgs {
     int64_t y_stride;
     int y_fp32;
     int32_t* status;
-    // filled in by the launcher: groups per row; floor((2^32 - 1) / d) for d blocks per group, with which the high word of
+    // filled in by the launcher: bytes of a tenant's codes and of all it has; groups per row; tiles of 16 outputs; floor((2^32 - 1) / d) for d blocks per group, with which the high word of
     // (n + 1) times it is n / d for (n + 1) d < 2^32
-    int groups;
+    size_t codes_bytes, tenant_bytes;
+    int groups, tiles;
     uint32_t per_magic;
 };
 cudaError_t configure_quant_linear();

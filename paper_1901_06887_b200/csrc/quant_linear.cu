@@ -6,9 +6,12 @@
 //
 // Bound: memory, K / 2 + 2 K / group bytes per output and tenant, whatever the number of its rows (up to some 16; beyond, the matrix
 // instructions).  The packed order makes a warp's load 512 contiguous bytes that are the operand of four instructions; the rows' slices of the
-// inner index are chosen so that a lane's inputs are 16 contiguous bytes too, so nothing passes through shared memory on the way in.
+// inner index are chosen so that a lane's inputs are 16 contiguous bytes too.
 //
-// Split.  A CTA takes (tenant, 16 outputs) units in turn, its eight warps every eighth block of 64 inputs; they join through shared memory.
+// Split.  A CTA takes (tenant, 32 outputs) units in turn, its eight warps every eighth block of 64 inputs; they join through shared memory.
+// Every warp copies its blocks ahead into a ring of its own (cp.async, three blocks ahead, on through the units to come), so the joins and
+// the ends of units do not empty the pipe: loading into registers unit by unit left the kernel waiting for memory (93 us for 8 tenants of
+// 4096 -> 16384, 24 rows).  Two tiles of 16 outputs share the rows' loads and the loop: what is left is bound by instructions.
 // Which tenants occur is found out by every CTA for itself from the ids (at most 256 a launch): no bucketing launch, and only tenants that
 // occur cost anything.
 #include "lm_device.cuh"
@@ -65,93 +68,140 @@ __device__ __forceinline__ uint32_t centred(uint32_t w) {
     return d;
 }
 
+constexpr int kStages = 4, kCodes = 1024, kStageBytes = kCodes + 128;        // a block's codes and scales of two tiles of 16 outputs
+
 struct Shared {
     int ids[kQuantRowsPerLaunch], slot[kQuantRowsPerLaunch], order[kQuantRowsPerLaunch];
     int tenant[kQuantRowsPerLaunch], begin[kQuantRowsPerLaunch + 1];
+    int group_slot[kQuantRowsPerLaunch], group_row[kQuantRowsPerLaunch];       // groups of at most 64 rows of one tenant
     int warp_n[kWarps];
-    int n_slots, n_valid;
 };
 
-// One unit: 16 outputs of one tenant for up to 8 NT rows (s.order[r0 ..]).
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+
+// Units in turn: pairs of tiles of one group of rows, gridDim.x apart.
+struct Cursor {
+    int group, pair;
+    __device__ __forceinline__ void next(int pairs) {
+        pair += gridDim.x;
+        while (pair >= pairs) { pair -= pairs; ++group; }
+    }
+};
+
+// A warp's blocks of all its units, in order: unit, then blocks warp, warp + 8, ...; copied ahead into the warp's ring.
+template <bool G32>
+struct Stream {
+    const QuantLinearArgs& a;
+    const Shared& s;
+    int warp, lane, kblocks, pairs, n_groups;
+    Cursor at;
+    int kb, left;                             // left: blocks still to be copied
+    const uint8_t *codes, *scales;            // this lane's, of the current unit
+    int64_t second;                           // bytes from the first tile's codes to the second's
+    uint32_t ring;                            // shared memory of this lane's piece of stage 0
+    int in;                                   // byte offset of the stage to fill
+
+    __device__ __forceinline__ void seek() {  // to the unit's first block
+        kb = warp;
+        if (at.group >= n_groups) return;
+        const uint8_t* const base = a.packed + (size_t)s.tenant[s.group_slot[at.group]] * a.tenant_bytes;
+        const int tile = 2 * at.pair, other = min(tile + 1, a.tiles - 1);       // (a missing second tile is the first again, and not written)
+        codes = base + ((size_t)tile * kblocks + warp) * 512 + lane * 16;
+        second = (int64_t)(other - tile) * kblocks * 512;
+        constexpr int L = G32 ? 4 : 2;        // lanes per tile's scales
+        scales = base + a.codes_bytes + (size_t)(lane < L ? tile : other) * a.groups * 32 + (lane % L) * 16;
+    }
+    __device__ __forceinline__ void issue() { // the next block, if there is one
+        if (left > 0) {
+            --left;
+            const uint32_t dst = ring + in;
+            copy16(dst, codes);
+            copy16(dst + 512, codes + second);
+            if (lane < (G32 ? 8 : 4)) copy16(dst + kCodes, scales + (G32 ? 2u * kb : __umulhi(kb + 1, a.per_magic)) * 32u);   // kb / (blocks per group)
+            codes += kWarps * 512;
+            kb += kWarps;
+            if (kb >= kblocks) { at.next(pairs); seek(); }
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        in = in == (kStages - 1) * kStageBytes ? 0 : in + kStageBytes;
+    }
+};
+
+// One unit: 32 outputs of one tenant for up to 8 NT rows (s.order[r0 ..]).
 template <int NT, bool G32>
-__device__ __forceinline__ void unit(const QuantLinearArgs& a, const Shared& s, float* red, const uint8_t* base, size_t codes_bytes, int tile, int r0,
-                                     int rows, int tenant) {
+__device__ __forceinline__ void unit(const QuantLinearArgs& a, const Shared& s, Stream<G32>& st, int& out_stage, float* red, const uint8_t* ring,
+                                     int pair, int r0, int rows, int tenant) {
     const int tid = threadIdx.x, warp = tid / 32, lane = tid & 31, g = lane >> 2, t = lane & 3;
-    const int kblocks = a.K / 64, groups = a.groups;
-    const uint4* const codes = reinterpret_cast<const uint4*>(base) + (size_t)tile * kblocks * 32 + lane;
-    const uint32_t* const scales = reinterpret_cast<const uint32_t*>(base + codes_bytes) + (size_t)tile * groups * 8 + g;
+    const int kblocks = a.K / 64;
     const uint16_t* x[NT];                       // (columns behind the last row repeat a row; they are not written)
 #pragma unroll
-    for (int n = 0; n < NT; ++n) x[n] = a.x + (int64_t)s.order[r0 + min(n * 8 + g, rows - 1)] * a.x_stride + 8 * t;
-    float acc[NT][4];
+    for (int n = 0; n < NT; ++n) x[n] = a.x + (int64_t)s.order[r0 + min(n * 8 + g, rows - 1)] * a.x_stride + warp * 64 + 8 * t;
+    float acc[2][NT][4];
 #pragma unroll
-    for (int n = 0; n < NT; ++n) acc[n][0] = acc[n][1] = acc[n][2] = acc[n][3] = 0.f;
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) acc[i][n][0] = acc[i][n][1] = acc[i][n][2] = acc[i][n][3] = 0.f;
+    const float zero[4] = {0.f, 0.f, 0.f, 0.f};
 
-    struct Block {
-        uint4 w, x[NT][2];
-        uint32_t s0, s1;
-    };
-    auto load = [&](Block& b, int kb) {
-        b.w = __ldcs(codes + (size_t)kb * 32);
-        b.s0 = __ldg(scales + (size_t)(G32 ? 2 * kb : (int)__umulhi(kb + 1, a.per_magic)) * 8);       // kb / (blocks per group)
-        if (G32) b.s1 = __ldg(scales + (size_t)(2 * kb + 1) * 8);
+    for (int kb = warp; kb < kblocks; kb += kWarps) {
+        uint4 xv[NT][2];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-            b.x[n][0] = __ldg(reinterpret_cast<const uint4*>(x[n] + (size_t)kb * 64));
-            b.x[n][1] = __ldg(reinterpret_cast<const uint4*>(x[n] + (size_t)kb * 64 + 32));
+            xv[n][0] = __ldg(reinterpret_cast<const uint4*>(x[n]));
+            xv[n][1] = __ldg(reinterpret_cast<const uint4*>(x[n] + 32));
+            x[n] += kWarps * 64;
         }
-    };
-    auto use = [&](const Block& b) {
-        const float zero[4] = {0.f, 0.f, 0.f, 0.f};
-        float c[NT][4];
+        __syncwarp();                            // every lane has read the block that the next copy replaces
+        st.issue();
+        asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
+        __syncwarp();
+        const uint8_t* const block = ring + out_stage;
+        out_stage = out_stage == (kStages - 1) * kStageBytes ? 0 : out_stage + kStageBytes;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {                // inputs 0..31 and 32..63 of the block
-            const uint32_t lo = h == 0 ? b.w.x : b.w.y, hi = h == 0 ? b.w.z : b.w.w;      // rows g and g + 8
-            const uint32_t a00 = centred<0>(lo), a01 = centred<1>(lo), a02 = centred<2>(lo), a03 = centred<3>(lo);
-            const uint32_t a10 = centred<0>(hi), a11 = centred<1>(hi), a12 = centred<2>(hi), a13 = centred<3>(hi);
+        for (int i = 0; i < 2; ++i) {
+            const uint4 w = *reinterpret_cast<const uint4*>(block + i * 512 + lane * 16);
+            float c[NT][4];
 #pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                const uint4 v = b.x[n][h];
-                if (h == 0 || G32) mma_bf16(c[n], a00, a10, a01, a11, v.x, v.y, zero);
-                else mma_bf16(c[n], a00, a10, a01, a11, v.x, v.y, c[n]);
-                mma_bf16(c[n], a02, a12, a03, a13, v.z, v.w, c[n]);
-                if (h == 1 || G32) {
-                    const uint32_t sc = G32 && h == 1 ? b.s1 : b.s0;
-                    const float s0 = bf16_lo(sc), s1 = bf16_hi(sc);
-                    acc[n][0] = fmaf(s0, c[n][0], acc[n][0]); acc[n][1] = fmaf(s0, c[n][1], acc[n][1]);
-                    acc[n][2] = fmaf(s1, c[n][2], acc[n][2]); acc[n][3] = fmaf(s1, c[n][3], acc[n][3]);
+            for (int h = 0; h < 2; ++h) {                // inputs 0..31 and 32..63 of the block
+                const uint32_t lo = h == 0 ? w.x : w.y, hi = h == 0 ? w.z : w.w;      // rows g and g + 8
+                const uint32_t a00 = centred<0>(lo), a01 = centred<1>(lo), a02 = centred<2>(lo), a03 = centred<3>(lo);
+                const uint32_t a10 = centred<0>(hi), a11 = centred<1>(hi), a12 = centred<2>(hi), a13 = centred<3>(hi);
+                const uint32_t sc = *reinterpret_cast<const uint32_t*>(block + kCodes + i * (G32 ? 64 : 32) + (G32 && h == 1 ? 32 : 0) + g * 4);
+                const float s0 = bf16_lo(sc), s1 = bf16_hi(sc);
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    const uint4 v = xv[n][h];
+                    if (h == 0 || G32) mma_bf16(c[n], a00, a10, a01, a11, v.x, v.y, zero);
+                    else mma_bf16(c[n], a00, a10, a01, a11, v.x, v.y, c[n]);
+                    mma_bf16(c[n], a02, a12, a03, a13, v.z, v.w, c[n]);
+                    if (h == 1 || G32) {
+                        float (&y)[4] = acc[i][n];
+                        y[0] = fmaf(s0, c[n][0], y[0]); y[1] = fmaf(s0, c[n][1], y[1]);
+                        y[2] = fmaf(s1, c[n][2], y[2]); y[3] = fmaf(s1, c[n][3], y[3]);
+                    }
                 }
             }
         }
-    };
-    constexpr int U = NT == 1 ? 4 : NT == 2 ? 2 : 1;      // blocks in flight
-    int kb = warp;
-    for (; kb + (U - 1) * kWarps < kblocks; kb += U * kWarps) {
-        Block b[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) load(b[u], kb + u * kWarps);
-#pragma unroll
-        for (int u = 0; u < U; ++u) use(b[u]);
     }
-    for (; kb < kblocks; kb += kWarps) {
-        Block b;
-        load(b, kb);
-        use(b);
-    }
-    // join the warps: red[warp][column][16 outputs, padded to 20]
+    // join the warps: red[warp][column][32 outputs, padded to 36]
     __syncthreads();                                       // the unit before this has been read
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        float* const r = red + ((warp * NT + n) * 8 + 2 * t) * 20 + g;
-        r[0] = acc[n][0]; r[20] = acc[n][1]; r[8] = acc[n][2]; r[28] = acc[n][3];
-    }
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            float* const r = red + ((warp * NT + n) * 8 + 2 * t) * 36 + 16 * i + g;
+            const float (&y)[4] = acc[i][n];
+            r[0] = y[0]; r[36] = y[1]; r[8] = y[2]; r[44] = y[3];
+        }
     __syncthreads();
-    for (int i = tid; i < rows * 16; i += kThreads) {
-        const int col = i >> 4, o = i & 15, out = tile * 16 + o;
+    for (int i = tid; i < rows * 32; i += kThreads) {
+        const int col = i >> 5, o = i & 31, out = pair * 32 + o;
         if (out >= a.N) continue;
         float v = 0.f;
 #pragma unroll
-        for (int w = 0; w < kWarps; ++w) v += red[(w * NT * 8 + col) * 20 + o];
+        for (int w = 0; w < kWarps; ++w) v += red[(w * NT * 8 + col) * 36 + o];
         if (a.bias) v += __ldg(a.bias + (size_t)tenant * a.N + out);
         const int64_t at = (int64_t)s.order[r0 + col] * a.y_stride + out;
         if (a.y_fp32) static_cast<float*>(a.y)[at] = v;
@@ -161,9 +211,11 @@ __device__ __forceinline__ void unit(const QuantLinearArgs& a, const Shared& s, 
 
 // MAXT: largest number of column tiles a pass may take (a launch of n rows never needs more than n of them).
 template <int MAXT, bool G32>
-__global__ void __launch_bounds__(kThreads, MAXT <= 4 ? 3 : 2) quant_linear_kernel(const QuantLinearArgs a) {
+__global__ void __launch_bounds__(kThreads, MAXT == 1 ? 4 : MAXT == 2 ? 3 : MAXT == 4 ? 2 : 1) quant_linear_kernel(const QuantLinearArgs a) {
     __shared__ Shared s;
-    __shared__ float red[kWarps * MAXT * 8 * 20];
+    extern __shared__ __align__(128) uint8_t s_bytes[];          // the warps' rings, then the join
+    uint8_t* const ring = s_bytes + (threadIdx.x / 32) * (kStages * kStageBytes);
+    float* const red = reinterpret_cast<float*>(s_bytes + kWarps * kStages * kStageBytes);
     const int tid = threadIdx.x, warp = tid / 32, lane = tid & 31;
     pdl_launch_dependents();
     pdl_wait();
@@ -202,10 +254,17 @@ __global__ void __launch_bounds__(kThreads, MAXT <= 4 ? 3 : 2) quant_linear_kern
         s.order[at] = tid;
         if (same == 0) s.begin[mine] = at;
     }
-    if (tid == 0) s.n_slots = n_slots;
     const int n_valid = __syncthreads_count(good);
     if (tid == 0) s.begin[n_slots] = n_valid;
     __syncthreads();
+    if (tid < n_slots) {                                   // groups of at most 64 rows
+        int at = 0;
+        for (int j = 0; j < tid; ++j) at += (s.begin[j + 1] - s.begin[j] + 63) / 64;
+        for (int r = s.begin[tid]; r < s.begin[tid + 1]; r += 64, ++at) { s.group_slot[at] = tid; s.group_row[at] = r; }
+        if (tid == n_slots - 1) s.warp_n[0] = at;
+    }
+    __syncthreads();
+    const int n_groups = n_slots > 0 ? s.warp_n[0] : 0;
 
     for (int i = n_valid; i < a.n; ++i) {                  // rows with a bad id
         const int64_t at = (int64_t)s.order[i] * a.y_stride;
@@ -215,25 +274,42 @@ __global__ void __launch_bounds__(kThreads, MAXT <= 4 ? 3 : 2) quant_linear_kern
         }
     }
 
-    const int tiles = (a.N + 15) / 16;
-    const size_t codes_bytes = quant_codes_bytes(a.K, a.N), tenant_bytes = quant_tenant_bytes(a.K, a.N, a.group);
-    const int64_t units = (int64_t)tiles * n_slots;
-    for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
-        const int sl = (int)(u / tiles), tile = (int)(u - (int64_t)sl * tiles), tenant = s.tenant[sl];
-        const uint8_t* const base = a.packed + (size_t)tenant * tenant_bytes;
-        for (int r0 = s.begin[sl], end = s.begin[sl + 1]; r0 < end; r0 += 64) {
-            const int rows = min(end - r0, 64);
-            if (MAXT == 1 || rows <= 8) unit<1, G32>(a, s, red, base, codes_bytes, tile, r0, rows, tenant);
-            else if (MAXT == 2 || rows <= 16) unit<(MAXT < 2 ? MAXT : 2), G32>(a, s, red, base, codes_bytes, tile, r0, rows, tenant);
-            else if (rows <= 32) unit<(MAXT < 4 ? MAXT : 4), G32>(a, s, red, base, codes_bytes, tile, r0, rows, tenant);
-            else unit<(MAXT < 8 ? MAXT : 8), G32>(a, s, red, base, codes_bytes, tile, r0, rows, tenant);
-        }
+    const int pairs = (a.tiles + 1) / 2, kblocks = a.K / 64;
+    Cursor at = {0, (int)blockIdx.x};
+    while (at.pair >= pairs) { at.pair -= pairs; ++at.group; }
+    const int64_t units = (int64_t)pairs * n_groups;
+    const int my_units = blockIdx.x < units ? (int)((units - 1 - blockIdx.x) / gridDim.x) + 1 : 0, my_blocks = warp < kblocks ? (kblocks - 1 - warp) / kWarps + 1 : 0;
+    Stream<G32> st{a, s, warp, lane, kblocks, pairs, n_groups, at, 0, my_units * my_blocks, nullptr, nullptr, 0, smem_u32(ring) + lane * 16, 0};
+    st.seek();
+    for (int i = 0; i < kStages - 1; ++i) st.issue();
+    int out_stage = 0;
+    for (; at.group < n_groups; at.next(pairs)) {
+        const int sl = s.group_slot[at.group], tenant = s.tenant[sl];
+        const int r0 = s.group_row[at.group], rows = min(s.begin[sl + 1] - r0, 64);
+        if (MAXT == 1 || rows <= 8) unit<1, G32>(a, s, st, out_stage, red, ring, at.pair, r0, rows, tenant);
+        else if (MAXT == 2 || rows <= 16) unit<(MAXT < 2 ? MAXT : 2), G32>(a, s, st, out_stage, red, ring, at.pair, r0, rows, tenant);
+        else if (MAXT == 4 || rows <= 32) unit<(MAXT < 4 ? MAXT : 4), G32>(a, s, st, out_stage, red, ring, at.pair, r0, rows, tenant);
+        else unit<(MAXT < 8 ? MAXT : 8), G32>(a, s, st, out_stage, red, ring, at.pair, r0, rows, tenant);
     }
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
 }
+
+constexpr int shared_bytes(int maxt) { return kWarps * kStages * kStageBytes + kWarps * maxt * 8 * 36 * 4; }
+typedef void (*Kernel)(QuantLinearArgs);
+const Kernel kKernels[2][4] = {
+    {quant_linear_kernel<1, false>, quant_linear_kernel<2, false>, quant_linear_kernel<4, false>, quant_linear_kernel<8, false>},
+    {quant_linear_kernel<1, true>, quant_linear_kernel<2, true>, quant_linear_kernel<4, true>, quant_linear_kernel<8, true>}};
 
 }  // namespace
 
-cudaError_t configure_quant_linear() { return cudaSuccess; }
+cudaError_t configure_quant_linear() {
+    for (int g = 0; g < 2; ++g)
+        for (int i = 0; i < 4; ++i) {
+            const cudaError_t e = cudaFuncSetAttribute(kKernels[g][i], cudaFuncAttributeMaxDynamicSharedMemorySize, shared_bytes(1 << i));
+            if (e != cudaSuccess) return e;
+        }
+    return cudaSuccess;
+}
 
 cudaError_t launch_quant_pack(const uint8_t* codes, const uint16_t* scales, int tenants, int K, int N, int group, void* packed,
                               cudaStream_t s) {
@@ -248,19 +324,17 @@ cudaError_t launch_quant_pack(const uint8_t* codes, const uint16_t* scales, int 
 cudaError_t launch_quant_linear(const QuantLinearArgs& a, int sm_count, cudaStream_t s) {
     const bool g32 = a.group == 32;
     const int most_slots = a.n < a.tenants ? a.n : a.tenants;
-    const int64_t units = (int64_t)((a.N + 15) / 16) * most_slots;
-    const int maxt = a.n <= 8 ? 1 : a.n <= 16 ? 2 : a.n <= 32 ? 4 : 8;
-    int64_t grid = (int64_t)sm_count * (maxt <= 4 ? 3 : 2);
+    const int64_t units = (int64_t)((a.N + 31) / 32) * most_slots;      // (more groups only where a tenant has over 64 rows)
+    const int v = a.n <= 8 ? 0 : a.n <= 16 ? 1 : a.n <= 32 ? 2 : 3;       // up to 8 << v rows of a tenant
+    int64_t grid = (int64_t)sm_count * (v == 0 ? 4 : v == 1 ? 3 : v == 2 ? 2 : 1);
     if (grid > units) grid = units;
-    typedef void (*Kernel)(QuantLinearArgs);
-    static const Kernel kernels[2][4] = {
-        {quant_linear_kernel<1, false>, quant_linear_kernel<2, false>, quant_linear_kernel<4, false>, quant_linear_kernel<8, false>},
-        {quant_linear_kernel<1, true>, quant_linear_kernel<2, true>, quant_linear_kernel<4, true>, quant_linear_kernel<8, true>}};
     QuantLinearArgs b = a;
+    b.codes_bytes = quant_codes_bytes(a.K, a.N);
+    b.tenant_bytes = quant_tenant_bytes(a.K, a.N, a.group);
     b.groups = a.K / a.group;
-    const uint32_t per = g32 ? 1u : (uint32_t)a.group / 64u;
-    b.per_magic = 0xffffffffu / per;
-    return launch_pdl(kernels[g32][maxt == 1 ? 0 : maxt == 2 ? 1 : maxt == 4 ? 2 : 3], dim3((unsigned)grid), dim3(kThreads), 0, s, b);
+    b.tiles = (a.N + 15) / 16;
+    b.per_magic = 0xffffffffu / (g32 ? 1u : (uint32_t)a.group / 64u);
+    return launch_pdl(kKernels[g32][v], dim3((unsigned)grid), dim3(kThreads), (size_t)shared_bytes(1 << v), s, b);
 }
 
 }  // namespace mt
