@@ -139,10 +139,21 @@ def _ptr(x) -> Optional[int]:
     return x.data_ptr()
 
 
+_raw_stream = None
+
+
 def _stream_handle(stream) -> Optional[int]:
+    global _raw_stream
     if stream is None:
-        import torch
-        return torch.cuda.current_stream().cuda_stream
+        if _raw_stream is None:
+            import torch
+            raw, dev = getattr(torch._C, "_cuda_getCurrentRawStream", None), getattr(torch._C, "_cuda_getDevice", None)
+            torch.cuda.current_stream()          # (initialises CUDA)
+            if raw is not None and dev is not None:
+                _raw_stream = lambda: raw(dev())     # torch.cuda.current_stream().cuda_stream without the stream object: 0.2 instead of 3 us
+            else:
+                _raw_stream = lambda: torch.cuda.current_stream().cuda_stream
+        return _raw_stream()
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream
@@ -341,29 +352,44 @@ def mt_bucket_noalloc(model_ids, n: int, n_models: int, counts_out, offsets_out,
 
 # ------------------------------------------------------------------------------------------------
 # Operators of language-model tenants.  These take torch tensors on the context's device and read sizes and strides from
-# them; a tensor of another type, shape or place is refused here (MT_ERR_INVALID_ARG), sizes are judged by the library.
+# them; a tensor of another type, shape or place is refused here (MT_ERR_INVALID_ARG), sizes are judged by the library.  A
+# call's time on the host is the floor of a token step, so the checks are few, flat expressions: 3 to 5 us a call.
 # ------------------------------------------------------------------------------------------------
-def _need(ok: bool, where: str) -> None:
-    if not ok:
-        raise MtError(1, where)
+class _Types:
+    bf16 = f32 = i32 = i64 = u8 = None
+
+
+def _types():
+    if _Types.bf16 is None:
+        import torch
+        _Types.f32, _Types.i32, _Types.i64, _Types.u8, _Types.bf16 = torch.float32, torch.int32, torch.int64, torch.uint8, torch.bfloat16
+    return _Types
+
+
+def _refuse(where: str) -> None:
+    raise MtError(1, where)
 
 
 def mt_prompt_attention(q, k, v, offsets, out, scale: Optional[float] = None, stream=None) -> None:
     """Causal attention over packed prompts: q bf16 [n, q_heads, dim], k and v [n, kv_heads, dim] (any token and head strides),
     offsets int32 [sequences + 1], out bf16 [n, q_heads, dim] contiguous.  scale: 1 / sqrt(dim) if None."""
-    where = "mt_prompt_attention"
-    import torch
-    bf16 = torch.bfloat16
-    n, hq, d = q.shape
-    qs, ks, vs = q.stride(), k.stride(), v.stride()
-    _need(q.dtype == bf16 and k.dtype == bf16 and v.dtype == bf16 and out.dtype == bf16 and offsets.dtype == torch.int32 and
-          q.is_cuda and k.is_cuda and v.is_cuda and out.is_cuda and offsets.is_cuda and k.shape == v.shape and
-          k.shape[0] == n and k.shape[2] == d and out.shape == q.shape and out.is_contiguous() and offsets.is_contiguous() and
-          offsets.dim() == 1 and offsets.shape[0] > 0 and (n == 0 or (qs[2] == 1 and ks[2] == 1 and vs[2] == 1)), where)
-    desc = PromptDesc(n, offsets.shape[0] - 1, hq, k.shape[1], d, d ** -0.5 if scale is None else scale, qs[0], qs[1], ks[0], ks[1],
-                      vs[0], vs[1])
-    _check(lib().mt_prompt_attention(ctypes.byref(desc), q.data_ptr(), k.data_ptr(), v.data_ptr(), offsets.data_ptr(), out.data_ptr(),
-                                     _stream_handle(stream)), where)
+    T = _types()
+    bf16 = T.bf16
+    n, hq, d = shape = q.shape
+    nk, hk, dk = kshape = k.shape
+    q0, q1, q2 = q.stride()
+    k0, k1, k2 = k.stride()
+    v0, v1, v2 = v.stride()
+    if not (q.dtype is bf16 and k.dtype is bf16 and v.dtype is bf16 and out.dtype is bf16 and offsets.dtype is T.i32 and q.is_cuda and
+            k.is_cuda and v.is_cuda and out.is_cuda and offsets.is_cuda and nk == n and dk == d and v.shape == kshape and
+            out.shape == shape and out.is_contiguous() and offsets.dim() == 1 and offsets.is_contiguous() and offsets.numel() > 0 and
+            (n == 0 or q2 == k2 == v2 == 1)):
+        _refuse("mt_prompt_attention")
+    desc = PromptDesc(n, offsets.numel() - 1, hq, hk, d, d ** -0.5 if scale is None else scale, q0, q1, k0, k1, v0, v1)
+    code = (_lib or lib()).mt_prompt_attention(ctypes.byref(desc), q.data_ptr(), k.data_ptr(), v.data_ptr(), offsets.data_ptr(), out.data_ptr(),
+                                               _stream_handle(stream))
+    if code:
+        raise MtError(code, "mt_prompt_attention")
 
 
 class KvCache:
@@ -371,11 +397,12 @@ class KvCache:
     [pages, kv_heads, page_tokens, 2] (scale, bias), contiguous.  Keeps them alive; allocates nothing."""
 
     def __init__(self, k_codes, k_params, v_codes, v_params):
-        import torch
+        T = _types()
         pages, heads, page, half = k_codes.shape
         for c, p in ((k_codes, k_params), (v_codes, v_params)):
-            _need(c.dtype == torch.uint8 and p.dtype == torch.bfloat16 and c.is_cuda and p.is_cuda and c.is_contiguous() and
-                  p.is_contiguous() and tuple(c.shape) == (pages, heads, page, half) and tuple(p.shape) == (pages, heads, page, 2), "KvCache")
+            if not (c.dtype is T.u8 and p.dtype is T.bf16 and c.is_cuda and p.is_cuda and c.is_contiguous() and p.is_contiguous() and
+                    tuple(c.shape) == (pages, heads, page, half) and tuple(p.shape) == (pages, heads, page, 2)):
+                _refuse("KvCache")
         self.tensors = (k_codes, k_params, v_codes, v_params)
         self.heads, self.dim = heads, 2 * half
         self.desc = KvCacheDesc(pages, page, heads, 2 * half, *[x.data_ptr() for x in self.tensors])
@@ -394,41 +421,47 @@ class KvCache:
 
 def mt_kv_append(cache: KvCache, k, v, slots, stream=None) -> None:
     """Round k and v, bf16 [n, kv_heads, dim] (any token and head strides), to 4 bits and write token i to slot slots[i] (int64 [n])."""
-    where = "mt_kv_append"
-    import torch
-    n, (ks, vs) = k.shape[0], (k.stride(), v.stride())
-    _need(k.dtype == torch.bfloat16 and v.dtype == torch.bfloat16 and slots.dtype == torch.int64 and k.is_cuda and v.is_cuda and
-          slots.is_cuda and k.shape == v.shape and tuple(k.shape[1:]) == (cache.heads, cache.dim) and slots.shape == (n,) and
-          slots.is_contiguous() and (n == 0 or (ks[2] == 1 and vs[2] == 1)), where)
-    _check(lib().mt_kv_append(cache.ref, k.data_ptr(), ks[0], ks[1], v.data_ptr(), vs[0], vs[1], slots.data_ptr(), n,
-                              _stream_handle(stream)), where)
+    T = _types()
+    n, h, d = shape = k.shape
+    k0, k1, k2 = k.stride()
+    v0, v1, v2 = v.stride()
+    if not (k.dtype is T.bf16 and v.dtype is T.bf16 and slots.dtype is T.i64 and k.is_cuda and v.is_cuda and slots.is_cuda and
+            v.shape == shape and h == cache.heads and d == cache.dim and slots.dim() == 1 and slots.numel() == n and slots.is_contiguous() and
+            (n == 0 or k2 == v2 == 1)):
+        _refuse("mt_kv_append")
+    code = (_lib or lib()).mt_kv_append(cache.ref, k.data_ptr(), k0, k1, v.data_ptr(), v0, v1, slots.data_ptr(), n, _stream_handle(stream))
+    if code:
+        raise MtError(code, "mt_kv_append")
 
 
 def mt_kv_read(cache: KvCache, slots, k_out, v_out, stream=None) -> None:
     """The cached values of slots (int64 [n]) as bf16 [n, kv_heads, dim]."""
-    where = "mt_kv_read"
-    import torch
-    n = slots.shape[0]
-    shape = (n, cache.heads, cache.dim)
-    _need(k_out.dtype == torch.bfloat16 and v_out.dtype == torch.bfloat16 and slots.dtype == torch.int64 and slots.dim() == 1 and
-          k_out.is_cuda and v_out.is_cuda and slots.is_cuda and k_out.shape == shape and v_out.shape == shape and
-          k_out.is_contiguous() and v_out.is_contiguous() and slots.is_contiguous(), where)
-    _check(lib().mt_kv_read(cache.ref, slots.data_ptr(), n, k_out.data_ptr(), v_out.data_ptr(), _stream_handle(stream)), where)
+    T = _types()
+    n, h, d = shape = k_out.shape
+    if not (k_out.dtype is T.bf16 and v_out.dtype is T.bf16 and slots.dtype is T.i64 and slots.dim() == 1 and slots.numel() == n and
+            k_out.is_cuda and v_out.is_cuda and slots.is_cuda and v_out.shape == shape and h == cache.heads and d == cache.dim and
+            k_out.is_contiguous() and v_out.is_contiguous() and slots.is_contiguous()):
+        _refuse("mt_kv_read")
+    code = (_lib or lib()).mt_kv_read(cache.ref, slots.data_ptr(), n, k_out.data_ptr(), v_out.data_ptr(), _stream_handle(stream))
+    if code:
+        raise MtError(code, "mt_kv_read")
 
 
 def mt_kv_attention(cache: KvCache, q, tables, lengths, out, scale: Optional[float] = None, stream=None) -> None:
     """One new token per sequence over its cached tokens: q bf16 [sequences, q_heads, dim] (any strides), tables int32
     [sequences, width], lengths int32 [sequences], out bf16 like q, contiguous.  scale: 1 / sqrt(dim) if None."""
-    where = "mt_kv_attention"
-    import torch
-    n, hq, d = q.shape
-    qs = q.stride()
-    _need(q.dtype == torch.bfloat16 and out.dtype == torch.bfloat16 and tables.dtype == torch.int32 and lengths.dtype == torch.int32 and
-          q.is_cuda and out.is_cuda and tables.is_cuda and lengths.is_cuda and d == cache.dim and out.shape == q.shape and
-          tables.dim() == 2 and tables.shape[0] == n and lengths.shape == (n,) and out.is_contiguous() and
-          tables.is_contiguous() and lengths.is_contiguous() and (n == 0 or qs[2] == 1), where)
-    _check(lib().mt_kv_attention(cache.ref, q.data_ptr(), qs[0], qs[1], tables.data_ptr(), tables.shape[1], lengths.data_ptr(), n, hq,
-                                 d ** -0.5 if scale is None else scale, out.data_ptr(), _stream_handle(stream)), where)
+    T = _types()
+    n, hq, d = shape = q.shape
+    q0, q1, q2 = q.stride()
+    rows, width = tables.shape
+    if not (q.dtype is T.bf16 and out.dtype is T.bf16 and tables.dtype is T.i32 and lengths.dtype is T.i32 and q.is_cuda and out.is_cuda and
+            tables.is_cuda and lengths.is_cuda and d == cache.dim and out.shape == shape and rows == n and lengths.dim() == 1 and
+            lengths.numel() == n and out.is_contiguous() and tables.is_contiguous() and lengths.is_contiguous() and (n == 0 or q2 == 1)):
+        _refuse("mt_kv_attention")
+    code = (_lib or lib()).mt_kv_attention(cache.ref, q.data_ptr(), q0, q1, tables.data_ptr(), width, lengths.data_ptr(), n, hq,
+                                           d ** -0.5 if scale is None else scale, out.data_ptr(), _stream_handle(stream))
+    if code:
+        raise MtError(code, "mt_kv_attention")
 
 
 def mt_quant_packed_bytes(in_features: int, out_features: int, group: int) -> int:
@@ -440,16 +473,16 @@ def mt_quant_packed_bytes(in_features: int, out_features: int, group: int) -> in
 
 def mt_quant_pack(codes, scales, packed, stream=None) -> None:
     """codes uint8 [tenants, out, in / 2], scales bf16 [tenants, out, in / group] -> packed uint8 [tenants, mt_quant_packed_bytes]."""
-    where = "mt_quant_pack"
-    import torch
-    _need(codes.dtype == torch.uint8 and scales.dtype == torch.bfloat16 and packed.dtype == torch.uint8 and codes.is_cuda and
-          scales.is_cuda and packed.is_cuda and codes.dim() == 3 and scales.dim() == 3 and codes.shape[:2] == scales.shape[:2] and
-          codes.is_contiguous() and scales.is_contiguous() and packed.is_contiguous() and scales.shape[2] > 0 and
-          2 * codes.shape[2] % scales.shape[2] == 0, where)
+    T = _types()
+    if not (codes.dtype is T.u8 and scales.dtype is T.bf16 and packed.dtype is T.u8 and codes.is_cuda and scales.is_cuda and packed.is_cuda and
+            codes.dim() == 3 and scales.dim() == 3 and codes.shape[:2] == scales.shape[:2] and codes.is_contiguous() and
+            scales.is_contiguous() and packed.is_contiguous() and scales.shape[2] > 0 and 2 * codes.shape[2] % scales.shape[2] == 0):
+        _refuse("mt_quant_pack")
     t, n, half = codes.shape
     group = 2 * half // scales.shape[2]
-    _need(packed.numel() >= t * mt_quant_packed_bytes(2 * half, n, group), where)
-    _check(lib().mt_quant_pack(codes.data_ptr(), scales.data_ptr(), t, 2 * half, n, group, packed.data_ptr(), _stream_handle(stream)), where)
+    if packed.numel() < t * mt_quant_packed_bytes(2 * half, n, group):
+        _refuse("mt_quant_pack")
+    _check(lib().mt_quant_pack(codes.data_ptr(), scales.data_ptr(), t, 2 * half, n, group, packed.data_ptr(), _stream_handle(stream)), "mt_quant_pack")
 
 
 class QuantBank:
@@ -459,10 +492,11 @@ class QuantBank:
         import torch
         t, n, half = codes.shape
         k = 2 * half
-        _need(scales.dim() == 3 and scales.shape[2] > 0 and k % scales.shape[2] == 0, "QuantBank")
+        if scales.dim() != 3 or scales.shape[2] <= 0 or k % scales.shape[2]:
+            _refuse("QuantBank")
         group = k // scales.shape[2]
-        if bias is not None:
-            _need(bias.dtype == torch.float32 and bias.is_cuda and bias.is_contiguous() and tuple(bias.shape) == (t, n), "QuantBank")
+        if bias is not None and not (bias.dtype is torch.float32 and bias.is_cuda and bias.is_contiguous() and tuple(bias.shape) == (t, n)):
+            _refuse("QuantBank")
         self.packed = torch.empty((t, mt_quant_packed_bytes(k, n, group)), dtype=torch.uint8, device=codes.device)
         mt_quant_pack(codes, scales, self.packed, stream)
         self.bias, self.in_features, self.out_features = bias, k, n
@@ -472,34 +506,43 @@ class QuantBank:
 
 def mt_quant_linear(x, ids, bank: QuantBank, y, stream=None) -> None:
     """y[i] = weight[ids[i]] x[i] + bias[ids[i]]: x bf16 [n, in] (any row stride), ids int32 [n], y bf16 or fp32 [n, out]."""
-    where = "mt_quant_linear"
-    import torch
+    T = _types()
     n, k = x.shape
-    yt = y.dtype
-    _need(x.dtype == torch.bfloat16 and ids.dtype == torch.int32 and (yt == torch.bfloat16 or yt == torch.float32) and x.is_cuda and
-          ids.is_cuda and y.is_cuda and k == bank.in_features and tuple(y.shape) == (n, bank.out_features) and ids.shape == (n,) and
-          ids.is_contiguous() and (n == 0 or (x.stride(1) == 1 and (y.stride(1) == 1 or bank.out_features == 1))), where)
-    _check(lib().mt_quant_linear(bank.ref, x.data_ptr(), x.stride(0), ids.data_ptr(), n, y.data_ptr(), y.stride(0),
-                                 1 if yt == torch.float32 else 0, _stream_handle(stream)), where)
+    rows, out = y.shape
+    x0, x1 = x.stride()
+    y0, y1 = y.stride()
+    wide = y.dtype is T.f32
+    if not (x.dtype is T.bf16 and ids.dtype is T.i32 and (wide or y.dtype is T.bf16) and x.is_cuda and ids.is_cuda and y.is_cuda and
+            k == bank.in_features and rows == n and out == bank.out_features and ids.dim() == 1 and ids.numel() == n and
+            ids.is_contiguous() and (n == 0 or (x1 == 1 and (y1 == 1 or out == 1)))):
+        _refuse("mt_quant_linear")
+    code = (_lib or lib()).mt_quant_linear(bank.ref, x.data_ptr(), x0, ids.data_ptr(), n, y.data_ptr(), y0, 1 if wide else 0, _stream_handle(stream))
+    if code:
+        raise MtError(code, "mt_quant_linear")
 
 
 def mt_token_logprobs(logits, tokens, logprobs, entropies=None, top_ids=None, top_logprobs=None, stream=None) -> None:
     """logits bf16 or fp32 [n, vocab] (any row stride), tokens int32 [n] -> logprobs fp32 [n], entropies fp32 [n] (or None),
     top_ids int32 [n, top] and top_logprobs fp32 [n, top] (or None)."""
-    where = "mt_token_logprobs"
-    import torch
+    T = _types()
+    f32, top = T.f32, 0
     n, vocab = logits.shape
-    f32, top = torch.float32, 0
-    ok = (logits.dtype == torch.bfloat16 or logits.dtype == f32) and tokens.dtype == torch.int32 and logprobs.dtype == f32 and \
-        logits.is_cuda and tokens.is_cuda and logprobs.is_cuda and tokens.shape == (n,) and logprobs.shape == (n,) and \
-        tokens.is_contiguous() and logprobs.is_contiguous() and (n == 0 or vocab <= 1 or logits.stride(1) == 1)
+    s0, s1 = logits.stride()
+    wide = logits.dtype is f32
+    ok = (wide or logits.dtype is T.bf16) and tokens.dtype is T.i32 and logprobs.dtype is f32 and logits.is_cuda and tokens.is_cuda and \
+        logprobs.is_cuda and tokens.dim() == 1 and tokens.numel() == n and logprobs.dim() == 1 and logprobs.numel() == n and \
+        tokens.is_contiguous() and logprobs.is_contiguous() and (n == 0 or vocab <= 1 or s1 == 1)
     if entropies is not None:
-        ok = ok and entropies.dtype == f32 and entropies.is_cuda and entropies.shape == (n,) and entropies.is_contiguous()
-    if top_ids is not None or top_logprobs is not None:
-        ok = ok and top_ids is not None and top_logprobs is not None and top_ids.dtype == torch.int32 and top_logprobs.dtype == f32 and \
+        ok = ok and entropies.dtype is f32 and entropies.is_cuda and entropies.dim() == 1 and entropies.numel() == n and entropies.is_contiguous()
+    if ok and (top_ids is not None or top_logprobs is not None):
+        ok = top_ids is not None and top_logprobs is not None and top_ids.dtype is T.i32 and top_logprobs.dtype is f32 and \
             top_ids.is_cuda and top_logprobs.is_cuda and top_ids.dim() == 2 and top_ids.shape[0] == n and \
             top_ids.shape == top_logprobs.shape and top_ids.is_contiguous() and top_logprobs.is_contiguous()
         top = top_ids.shape[1] if ok else 0
-    _need(ok, where)
-    _check(lib().mt_token_logprobs(logits.data_ptr(), 1 if logits.dtype == f32 else 0, logits.stride(0), n, vocab, tokens.data_ptr(), top,
-                                   logprobs.data_ptr(), _ptr(entropies), _ptr(top_ids), _ptr(top_logprobs), _stream_handle(stream)), where)
+    if not ok:
+        _refuse("mt_token_logprobs")
+    code = (_lib or lib()).mt_token_logprobs(logits.data_ptr(), 1 if wide else 0, s0, n, vocab, tokens.data_ptr(), top, logprobs.data_ptr(),
+                                             None if entropies is None else entropies.data_ptr(), None if top_ids is None else top_ids.data_ptr(),
+                                             None if top_logprobs is None else top_logprobs.data_ptr(), _stream_handle(stream))
+    if code:
+        raise MtError(code, "mt_token_logprobs")
