@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from typing import List, Optional, Sequence, Tuple
 
 import numpy as np
@@ -49,11 +50,8 @@ class LayerDesc(ctypes.Structure):
                 ("weight", ctypes.c_void_p), ("bias", ctypes.c_void_p)]
 
 
-class PromptDesc(ctypes.Structure):
-    _fields_ = [(k, ctypes.c_int32) for k in ("n_tokens", "n_seqs", "q_heads", "kv_heads", "head_dim")] + \
-               [("scale", ctypes.c_float)] + \
-               [(k, ctypes.c_int64) for k in ("q_token_stride", "q_head_stride", "k_token_stride", "k_head_stride",
-                                              "v_token_stride", "v_head_stride")]
+# mt_prompt_desc as bytes: n_tokens, n_seqs, q_heads, kv_heads, head_dim, scale, then token and head strides of q, k, v
+_prompt_desc = struct.Struct("=5if6q").pack
 
 
 class KvCacheDesc(ctypes.Structure):
@@ -385,8 +383,8 @@ def mt_prompt_attention(q, k, v, offsets, out, scale: Optional[float] = None, st
             out.shape == shape and out.is_contiguous() and offsets.dim() == 1 and offsets.is_contiguous() and offsets.numel() > 0 and
             (n == 0 or q2 == k2 == v2 == 1)):
         _refuse("mt_prompt_attention")
-    desc = PromptDesc(n, offsets.numel() - 1, hq, hk, d, d ** -0.5 if scale is None else scale, q0, q1, k0, k1, v0, v1)
-    code = (_lib or lib()).mt_prompt_attention(ctypes.byref(desc), q.data_ptr(), k.data_ptr(), v.data_ptr(), offsets.data_ptr(), out.data_ptr(),
+    desc = _prompt_desc(n, offsets.numel() - 1, hq, hk, d, d ** -0.5 if scale is None else scale, q0, q1, k0, k1, v0, v1)
+    code = (_lib or lib()).mt_prompt_attention(desc, q.data_ptr(), k.data_ptr(), v.data_ptr(), offsets.data_ptr(), out.data_ptr(),
                                                _stream_handle(stream))
     if code:
         raise MtError(code, "mt_prompt_attention")

@@ -1187,7 +1187,8 @@ namespace mt {
 mt_status op_begin(std::unique_lock<std::mutex>* lk, OpContext* out) {
     *lk = std::unique_lock<std::mutex>(g_mu);
     if (!g.init) return MT_ERR_NOT_INIT;
-    CU_OK(cudaSetDevice(g.device));
+    int current = -1;
+    if (cudaGetDevice(&current) != cudaSuccess || current != g.device) CU_OK(cudaSetDevice(g.device));
     out->sm_count = g.sm_count;
     out->status = g.d_status;
     out->encode = g.encode;

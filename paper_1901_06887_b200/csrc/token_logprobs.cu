@@ -9,8 +9,10 @@
 // does not depend on the order of arrival.  Where too many logits reach the bound (long ties, values sorted into one share) the exact k-th
 // largest is found by its bits, eight at a time, from histograms of the row, and ties at it are taken from the front of the row.
 //
-// Split.  A row is cut into parts so that the rows fill the GPU (a part has at least kMinPart logits); a part leaves (m, S, W) and its sorted
-// alternatives in scratch, and the last CTA of a row to arrive joins them.  Minus infinity adds nothing and is no alternative.
+// Split.  Few long rows are cut into 2, 4 or 8 parts, one CTA each, that form a cluster: the first joins the others' statistics and sorted
+// alternatives out of their shared memory (a part leaves at most kMaxTop of them).  Joining through device memory and a counter instead cost a
+// fence, an atomic and three more round trips, some 10 us for 8 rows of 32000.  A part whose logits fit in registers is not read a second time.
+// Minus infinity adds nothing and is no alternative.
 //
 // Bound: memory for many rows (bf16: 12 logits a cycle and SM, 0.75 of the rate of exponentials); latency for few.
 #include "lm_device.cuh"
@@ -23,24 +25,16 @@ constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kMaxTop = 32;
 constexpr int kGroups = 64;                // at least kMaxTop
 constexpr int kList = 1024;                // entries the first list may take
-constexpr int kMinPart = 4096;             // logits of a part, at least
-constexpr int kMaxParts = 64;
+constexpr int kMinPart = 2048;             // logits of a part, at least
+constexpr int kMaxParts = 8;
+constexpr int kHold = 4;                   // vectors of a thread that stay in registers
 constexpr float kLog2e = 1.44269504088896341f;
-static_assert(kThreads == 4 * kGroups && kGroups >= kMaxTop && kGroups >= kMaxParts, "");
-
-struct Part {                              // one part's results in scratch
-    float m, s, w;                         // maximum, sums
-    int bad;                               // NaN or plus infinity seen
-    uint32_t value[kMaxTop];               // alternatives as ordered bits (0: none) ...
-    int32_t index[kMaxTop];
-};
+static_assert(kThreads == 4 * kGroups && kGroups >= kMaxTop && kThreads >= kMaxParts * kMaxTop, "");
 
 struct Params {
     LogprobArgs a;
-    int parts;
+    int parts;                             // CTAs of a cluster
     int part_len;                          // a multiple of 8
-    unsigned* arrived;                     // [rows], zero between calls
-    Part* part;                            // [rows][parts]
 };
 
 // Bits that grow with the value (minus zero counts as zero); 0 is below every number, so it can stand for "nothing".
@@ -136,15 +130,30 @@ struct Stats {
     float m, s, w;                         // s = sum e^(x - m), w = sum (x - m) e^(x - m)
 };
 __device__ __forceinline__ float exp_of(float x) { return ex2(x * kLog2e); }
-// Joins b to a; both may be empty (m = -inf, s = w = 0).
-__device__ __forceinline__ void join(Stats& a, float m, float s, float w) {
-    const float nm = fmaxf(a.m, m);
-    if (nm == -INFINITY) return;
-    const float da = fmaxf(a.m - nm, -1e4f), db = fmaxf(m - nm, -1e4f), fa = exp_of(da), fb = exp_of(db);     // (-1e4: far below, and finite)
-    const float wa = fmaf(da, a.s, a.w) * fa, wb = fmaf(db, s, w) * fb;
-    a.s = a.s * fa + s * fb;
-    a.w = wa + wb;
-    a.m = nm;
+// Moves sums to another maximum, not below the own.
+__device__ __forceinline__ void move_to(Stats& a, float m) {
+    const float d = fmaxf(a.m - m, -1e4f), f = exp_of(d);                   // (-1e4: far below, and finite)
+    a.w = m > -INFINITY ? fmaf(d, a.s, a.w) * f : 0.f;
+    a.s = m > -INFINITY ? a.s * f : 0.f;
+    a.m = m;
+}
+// Joins the sums of 2^k neighbouring lanes.
+template <int WIDTH>
+__device__ __forceinline__ void join_lanes(Stats& a) {
+    float m = a.m;
+#pragma unroll
+    for (int o = WIDTH / 2; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    move_to(a, m);
+#pragma unroll
+    for (int o = WIDTH / 2; o; o >>= 1) {
+        a.s += __shfl_xor_sync(0xffffffffu, a.s, o);
+        a.w += __shfl_xor_sync(0xffffffffu, a.w, o);
+    }
+}
+__device__ __forceinline__ uint32_t remote_u32(const void* p, uint32_t rank) {
+    uint32_t v;
+    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(map_to_cta(smem_u32(p), rank)) : "memory");
+    return v;
 }
 
 // Sorts the list of n <= kList (value, index) entries by counting and writes the first `top` (value descending, index ascending).
@@ -158,10 +167,12 @@ __device__ __forceinline__ void rank_list(const uint32_t* value, const int32_t* 
     }
 }
 
-template <bool FP32>
+// HOLD: a part has at most kHold vectors a thread.
+template <bool FP32, bool HOLD>
 __global__ void __launch_bounds__(kThreads) token_logprobs_kernel(const Params p) {
     __shared__ float s_m[kWarps], s_s[kWarps], s_w[kWarps];
-    __shared__ int s_bad, s_n, s_last;
+    __shared__ int s_n, s_n_top;
+    __shared__ Stats s_all;
     __shared__ uint32_t s_best[kGroups], s_bound, s_value[kList], s_top_value[kMaxTop], s_hist[256], s_pick[2];
     __shared__ int32_t s_index[kList], s_top_index[kMaxTop], s_warp_n[kWarps];
     const LogprobArgs& a = p.a;
@@ -171,9 +182,9 @@ __global__ void __launch_bounds__(kThreads) token_logprobs_kernel(const Params p
     pdl_launch_dependents();
     pdl_wait();
     const void* const row = static_cast<const char*>(a.logits) + row_i * a.row_stride * (FP32 ? 4 : 2);
-    const int lo = part * p.part_len, hi = min(a.vocab, lo + p.part_len);
-    const Span span = span_of<FP32>(row, min(lo, a.vocab), hi > lo ? hi : min(lo, a.vocab));
-    if (t == 0) { s_bad = 0; s_n = 0; }
+    const int lo = min(a.vocab, part * p.part_len), hi = min(a.vocab, lo + p.part_len);
+    const Span span = span_of<FP32>(row, lo, hi);
+    if (t == 0) s_n = 0;
 
     // --- one pass: statistics and the share's largest logit
     constexpr int N = Vec<FP32>::N, B = FP32 ? 4 : 2;
@@ -217,8 +228,24 @@ __global__ void __launch_bounds__(kThreads) token_logprobs_kernel(const Params p
         st.s += q;
         st.w = fmaf(q, d, st.w);
     };
-    {
-        const uint4* const base = reinterpret_cast<const uint4*>(static_cast<const char*>(row) + (size_t)span.vec0 * B);
+    // the given token's logit, long before it is needed
+    float at_token = nan_f();
+    if (part == 0 && t == 0) {
+        const int tok = a.tokens[row_i];
+        if (tok >= 0 && tok < a.vocab) at_token = logit_at<FP32>(row, tok);
+    }
+    Vec<FP32> held[HOLD ? kHold : 1];
+    const uint4* const base = reinterpret_cast<const uint4*>(static_cast<const char*>(row) + (size_t)span.vec0 * B);
+    if (HOLD) {
+        constexpr uint32_t kNone = FP32 ? 0xff800000u : 0xff80ff80u;       // minus infinity, as often as it fits
+#pragma unroll
+        for (int u = 0; u < kHold; ++u) {
+            held[u].v = make_uint4(kNone, kNone, kNone, kNone);
+            if (t + u * kThreads < span.n_vec) held[u].v = __ldg(base + t + u * kThreads);
+        }
+#pragma unroll
+        for (int u = 0; u < kHold; ++u) add(held[u]);
+    } else {
         int v = t;
         for (; v + 3 * kThreads < span.n_vec; v += 4 * kThreads) {       // four loads in flight
             Vec<FP32> x[4];
@@ -232,21 +259,19 @@ __global__ void __launch_bounds__(kThreads) token_logprobs_kernel(const Params p
             x.v = __ldg(base + v);
             add(x);
         }
-        if (t < span.vec0 - span.lo) add_one(logit_at<FP32>(row, span.lo + t));
-        if (t < span.hi - span.tail) add_one(logit_at<FP32>(row, span.tail + t));
     }
+    const bool has_head = t < span.vec0 - span.lo, has_tail = t < span.hi - span.tail;
+    if (has_head) add_one(logit_at<FP32>(row, span.lo + t));
+    if (has_tail) add_one(logit_at<FP32>(row, span.tail + t));
     const uint32_t mine_best = ordered(best);
     {
         uint32_t g = max(mine_best, __shfl_xor_sync(0xffffffffu, mine_best, 1));
         g = max(g, __shfl_xor_sync(0xffffffffu, g, 2));
         if ((t & 3) == 0) s_best[t >> 2] = g;
     }
-#pragma unroll
-    for (int o = 16; o; o >>= 1)
-        join(st, __shfl_xor_sync(0xffffffffu, st.m, o), __shfl_xor_sync(0xffffffffu, st.s, o), __shfl_xor_sync(0xffffffffu, st.w, o));
+    join_lanes<32>(st);
     if (lane == 0) { s_m[warp] = st.m; s_s[warp] = st.s; s_w[warp] = st.w; }
-    __syncthreads();
-    if (bad) s_bad = 1;
+    const int row_bad = __syncthreads_or(bad);
 
     // --- alternatives of this part
     int n_top = 0;
@@ -261,14 +286,26 @@ __global__ void __launch_bounds__(kThreads) token_logprobs_kernel(const Params p
         }
         __syncthreads();
         const uint32_t bound = max(s_bound, kOrderedMinusInf + 1u);
-        for (unsigned who = __ballot_sync(0xffffffffu, mine_best >= bound); who; who &= who - 1)
-            for_share_of<FP32>(row, span, t - lane + __ffs(who) - 1, lane, [&](float x, int i) {
-                const uint32_t o = ordered(x);
-                if (o >= bound) {
-                    const int at = atomicAdd(&s_n, 1);
-                    if (at < kList) { s_value[at] = o; s_index[at] = i; }
-                }
-            });
+        auto take = [&](float x, int i) {
+            const uint32_t o = ordered(x);
+            if (o >= bound) {
+                const int at = atomicAdd(&s_n, 1);
+                if (at < kList) { s_value[at] = o; s_index[at] = i; }
+            }
+        };
+        if (HOLD) {
+            if (mine_best >= bound) {
+#pragma unroll
+                for (int u = 0; u < kHold; ++u)
+#pragma unroll
+                    for (int e = 0; e < N; ++e) take(held[u][e], span.vec0 + (t + u * kThreads) * N + e);
+                if (has_head) take(logit_at<FP32>(row, span.lo + t), span.lo + t);
+                if (has_tail) take(logit_at<FP32>(row, span.tail + t), span.tail + t);
+            }
+        } else {
+            for (unsigned who = __ballot_sync(0xffffffffu, mine_best >= bound); who; who &= who - 1)
+                for_share_of<FP32>(row, span, t - lane + __ffs(who) - 1, lane, take);
+        }
         __syncthreads();
         int n = s_n;
         if (n > kList) {
@@ -328,76 +365,75 @@ __global__ void __launch_bounds__(kThreads) token_logprobs_kernel(const Params p
     }
     __syncthreads();
 
-    // --- this part's statistics
-    Stats all = {s_m[0], s_s[0], s_w[0]};
-#pragma unroll
-    for (int w = 1; w < kWarps; ++w) join(all, s_m[w], s_s[w], s_w[w]);
-    int row_bad = s_bad;
-
+    // --- statistics of the part, then of the row; all outputs come from the first warp of the row's first part
+    Stats all = {-INFINITY, 0.f, 0.f};
+    int none = row_bad;
+    if (warp == 0) {
+        if (lane < kWarps) all = {s_m[lane], s_s[lane], s_w[lane]};
+        join_lanes<kWarps>(all);
+        all.m = __shfl_sync(0xffffffffu, all.m, 0);
+        all.s = __shfl_sync(0xffffffffu, all.s, 0);
+        all.w = __shfl_sync(0xffffffffu, all.w, 0);
+    }
     if (p.parts > 1) {
-        Part& mine = p.part[row_i * p.parts + part];
-        if (t == 0) { __stcg(&mine.m, all.m); __stcg(&mine.s, all.s); __stcg(&mine.w, all.w); __stcg(&mine.bad, row_bad); }
-        if (t < top) { __stcg(&mine.value[t], t < n_top ? s_top_value[t] : 0u); __stcg(&mine.index[t], t < n_top ? s_top_index[t] : -1); }
-        __threadfence();
-        __syncthreads();
-        if (t == 0) {
-            s_last = atomicAdd(p.arrived + row_i, 1u) == (unsigned)(p.parts - 1);
-            if (s_last) p.arrived[row_i] = 0u;
-        }
-        __syncthreads();
-        if (!s_last) return;
-        __threadfence();
-        const Part* const parts = p.part + row_i * p.parts;
-        // statistics: every warp joins all of them, two a lane, in an order of its own making but always the same
-        all = {-INFINITY, 0.f, 0.f};
-        row_bad = 0;
-        for (int b = lane; b < p.parts; b += 32) {
-            join(all, __ldcg(&parts[b].m), __ldcg(&parts[b].s), __ldcg(&parts[b].w));
-            row_bad |= __ldcg(&parts[b].bad);
-        }
-#pragma unroll
-        for (int o = 16; o; o >>= 1) {
-            join(all, __shfl_xor_sync(0xffffffffu, all.m, o), __shfl_xor_sync(0xffffffffu, all.s, o), __shfl_xor_sync(0xffffffffu, all.w, o));
-            row_bad |= __shfl_xor_sync(0xffffffffu, row_bad, o);
-        }
-        if (top > 0) {
-            // the same bound over the parts' lists: the top-th largest of the parts' largest leaves at most top lists to take from
-            const uint32_t head = t < p.parts ? __ldcg(&parts[t].value[0]) : 0u;
-            if (t == 0) { s_n = 0; s_bound = 0u; }
-            if (t < kGroups) s_best[t] = head;
-            __syncthreads();
-            if (t < kGroups) {
-                int above = 0, same = 0;
-#pragma unroll 8
-                for (int j = 0; j < kGroups; ++j) { above += s_best[j] > head; same += s_best[j] == head; }
-                if (above < top && above + same >= top) s_bound = head;
+        // a NaN as the sum tells of a row that is not one
+        if (t == 0) { s_all = all; if (row_bad) s_all.s = nan_f(); s_n_top = n_top; }
+        cluster_sync_all();
+        if (part == 0) {
+            // everybody's alternatives: list b at b * top, sorted, what is missing as zeros
+            const int b = top > 0 ? t / top : p.parts, k = top > 0 ? t - b * top : 0;
+            uint32_t value = 0;
+            int32_t index = -1;
+            if (b < p.parts) {
+                if (k < (int)remote_u32(&s_n_top, b)) {
+                    value = remote_u32(&s_top_value[k], b);
+                    index = (int32_t)remote_u32(&s_top_index[k], b);
+                }
+                s_value[t] = value;
+                s_index[t] = index;
+            }
+            if (warp == 0) {
+                all = {-INFINITY, 0.f, 0.f};
+                if (lane < p.parts) {
+                    all.m = __uint_as_float(remote_u32(&s_all.m, lane));
+                    all.s = __uint_as_float(remote_u32(&s_all.s, lane));
+                    all.w = __uint_as_float(remote_u32(&s_all.w, lane));
+                }
+                none = __any_sync(0xffffffffu, all.s != all.s);
+                join_lanes<kMaxParts>(all);
+                all.m = __shfl_sync(0xffffffffu, all.m, 0);
+                all.s = __shfl_sync(0xffffffffu, all.s, 0);
+                all.w = __shfl_sync(0xffffffffu, all.w, 0);
             }
             __syncthreads();
-            const uint32_t bound = max(s_bound, 1u);
-            for (int i = t; i < p.parts * top; i += kThreads) {
-                const Part& q = parts[i / top];
-                if (s_best[i / top] < bound) continue;
-                const uint32_t v = __ldcg(&q.value[i % top]);
-                if (v >= bound) {
-                    const int at = atomicAdd(&s_n, 1);
-                    if (at < kList) { s_value[at] = v; s_index[at] = __ldcg(&q.index[i % top]); }
+            // an entry's rank: what stands before it in the lists of lower parts (an equal value there has a lower index) and of higher ones
+            int rank = kMaxTop;
+            if (value != 0) {
+                rank = k;
+                for (int o = 0; o < p.parts; ++o) {
+                    if (o == b) continue;
+                    int first = 0, end = top;              // first entry that does not stand before this one
+                    while (first < end) {
+                        const int mid = (first + end) >> 1;
+                        const uint32_t v = s_value[o * top + mid];
+                        if (v > value || (v == value && o < b)) first = mid + 1; else end = mid;
+                    }
+                    rank += first;
                 }
             }
-            __syncthreads();
-            const int n = min(s_n, kList);
-            n_top = min(n, top);
-            rank_list(s_value, s_index, n, top, s_top_value, s_top_index, t);
-            __syncthreads();
+            n_top = min(top, __syncthreads_count(value != 0));
+            if (rank < top) { s_top_value[rank] = value; s_top_index[rank] = index; }
         }
+        cluster_sync_all();                    // nobody's shared memory goes before it has been read
+        if (part != 0) return;
     }
 
     // --- outputs
-    const bool none = row_bad || !(all.s > 0.f);
+    if (warp != 0) return;
+    if (!(all.s > 0.f)) none = 1;
     const float log_s = logf(all.s);
     if (t == 0) {
-        const int tok = a.tokens[row_i];
-        const bool in = tok >= 0 && tok < a.vocab;
-        a.logprobs[row_i] = none || !in ? nan_f() : logit_at<FP32>(row, tok) - all.m - log_s;
+        a.logprobs[row_i] = none ? nan_f() : at_token - all.m - log_s;
         if (a.entropies) a.entropies[row_i] = none ? nan_f() : log_s - all.w / all.s;
     }
     if (t < top) {
@@ -414,24 +450,26 @@ cudaError_t configure_token_logprobs() { return cudaSuccess; }
 mt_status launch_token_logprobs(const LogprobArgs& a, const OpContext& c, cudaStream_t s) {
     Params p;
     p.a = a;
-    // parts: enough for four CTAs an SM, none shorter than kMinPart
-    int64_t want = (4LL * c.sm_count + a.n - 1) / a.n;
-    const int64_t most = (a.vocab + kMinPart - 1) / kMinPart;
-    if (want > most) want = most;
-    if (want > kMaxParts) want = kMaxParts;
-    p.parts = want > 1 && a.n < (1 << 20) ? (int)want : 1;
+    // parts: as long as the rows leave the GPU with fewer than four CTAs an SM and a part keeps kMinPart logits
+    p.parts = 1;
+    while (p.parts < kMaxParts && (int64_t)a.n * p.parts * 2 <= 4LL * c.sm_count && a.vocab / (p.parts * 2) >= kMinPart) p.parts *= 2;
     p.part_len = ((a.vocab + p.parts - 1) / p.parts + 7) / 8 * 8;
-    p.arrived = nullptr;
-    p.part = nullptr;
-    if (p.parts > 1) {
-        uint8_t* w = nullptr;
-        mt_status st = op_scratch(s, kScratchZeroBytes + (size_t)a.n * p.parts * sizeof(Part), &w);
-        if (st != MT_OK) return st;
-        p.arrived = reinterpret_cast<unsigned*>(w);
-        p.part = reinterpret_cast<Part*>(w + kScratchZeroBytes);
-    }
-    const int64_t grid = (int64_t)a.n * p.parts;
-    const cudaError_t e = launch_pdl(a.fp32 ? token_logprobs_kernel<true> : token_logprobs_kernel<false>, dim3((unsigned)grid), dim3(kThreads), 0, s, p);
+    const bool hold = (p.part_len + (a.fp32 ? 3 : 7)) / (a.fp32 ? 4 : 8) <= kHold * kThreads;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)((int64_t)a.n * p.parts));
+    cfg.blockDim = dim3(kThreads);
+    cfg.stream = s;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)p.parts;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = p.parts > 1 ? 2 : 1;
+    ++g_kernel_launches;
+    const cudaError_t e = a.fp32 ? (hold ? cudaLaunchKernelEx(&cfg, token_logprobs_kernel<true, true>, p) : cudaLaunchKernelEx(&cfg, token_logprobs_kernel<true, false>, p))
+                                 : (hold ? cudaLaunchKernelEx(&cfg, token_logprobs_kernel<false, true>, p) : cudaLaunchKernelEx(&cfg, token_logprobs_kernel<false, false>, p));
     return e == cudaSuccess ? MT_OK : MT_ERR_CUDA;
 }
 
