@@ -68,7 +68,10 @@ __device__ __forceinline__ uint32_t centred(uint32_t w) {
     return d;
 }
 
-constexpr int kStages = 4, kCodes = 1024, kStageBytes = kCodes + 128;        // a block's codes and scales of two tiles of 16 outputs
+constexpr int kCodes = 1024, kStageBytes = kCodes + 128;        // a block's codes and scales of two tiles of 16 outputs
+// Places in a warp's ring: eight for calls of few rows, where a warp has about that many blocks altogether and waits once for all of them
+// (4096 x 4096, one row: 7.9 us against 10.1 with four); four where the columns' partial sums need the memory.
+__host__ __device__ constexpr int stages(int maxt) { return maxt == 1 ? 8 : 4; }
 
 struct Shared {
     int ids[kQuantRowsPerLaunch], slot[kQuantRowsPerLaunch], order[kQuantRowsPerLaunch];
@@ -91,7 +94,7 @@ struct Cursor {
 };
 
 // A warp's blocks of all its units, in order: unit, then blocks warp, warp + 8, ...; copied ahead into the warp's ring.
-template <bool G32>
+template <bool G32, int STAGES>
 struct Stream {
     const QuantLinearArgs& a;
     const Shared& s;
@@ -125,13 +128,13 @@ struct Stream {
             if (kb >= kblocks) { at.next(pairs); seek(); }
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
-        in = in == (kStages - 1) * kStageBytes ? 0 : in + kStageBytes;
+        in = in == (STAGES - 1) * kStageBytes ? 0 : in + kStageBytes;
     }
 };
 
 // One unit: 32 outputs of one tenant for up to 8 NT rows (s.order[r0 ..]).
-template <int NT, bool G32>
-__device__ __forceinline__ void unit(const QuantLinearArgs& a, const Shared& s, Stream<G32>& st, int& out_stage, float* red, const uint8_t* ring,
+template <int NT, bool G32, int STAGES>
+__device__ __forceinline__ void unit(const QuantLinearArgs& a, const Shared& s, Stream<G32, STAGES>& st, int& out_stage, float* red, const uint8_t* ring,
                                      int pair, int r0, int rows, int tenant) {
     const int tid = threadIdx.x, warp = tid / 32, lane = tid & 31, g = lane >> 2, t = lane & 3;
     const int kblocks = a.K / 64;
@@ -155,10 +158,10 @@ __device__ __forceinline__ void unit(const QuantLinearArgs& a, const Shared& s, 
         }
         __syncwarp();                            // every lane has read the block that the next copy replaces
         st.issue();
-        asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
+        asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 1) : "memory");
         __syncwarp();
         const uint8_t* const block = ring + out_stage;
-        out_stage = out_stage == (kStages - 1) * kStageBytes ? 0 : out_stage + kStageBytes;
+        out_stage = out_stage == (STAGES - 1) * kStageBytes ? 0 : out_stage + kStageBytes;
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             const uint4 w = *reinterpret_cast<const uint4*>(block + i * 512 + lane * 16);
@@ -211,7 +214,8 @@ __device__ __forceinline__ void unit(const QuantLinearArgs& a, const Shared& s, 
 
 // MAXT: largest number of column tiles a pass may take (a launch of n rows never needs more than n of them).
 template <int MAXT, bool G32>
-__global__ void __launch_bounds__(kThreads, MAXT == 1 ? 4 : MAXT == 2 ? 3 : MAXT == 4 ? 2 : 1) quant_linear_kernel(const QuantLinearArgs a) {
+__global__ void __launch_bounds__(kThreads, MAXT <= 2 ? 3 : MAXT == 4 ? 2 : 1) quant_linear_kernel(const QuantLinearArgs a) {
+    constexpr int kStages = stages(MAXT);
     __shared__ Shared s;
     extern __shared__ __align__(128) uint8_t s_bytes[];          // the warps' rings, then the join
     uint8_t* const ring = s_bytes + (threadIdx.x / 32) * (kStages * kStageBytes);
@@ -279,22 +283,22 @@ __global__ void __launch_bounds__(kThreads, MAXT == 1 ? 4 : MAXT == 2 ? 3 : MAXT
     while (at.pair >= pairs) { at.pair -= pairs; ++at.group; }
     const int64_t units = (int64_t)pairs * n_groups;
     const int my_units = blockIdx.x < units ? (int)((units - 1 - blockIdx.x) / gridDim.x) + 1 : 0, my_blocks = warp < kblocks ? (kblocks - 1 - warp) / kWarps + 1 : 0;
-    Stream<G32> st{a, s, warp, lane, kblocks, pairs, n_groups, at, 0, my_units * my_blocks, nullptr, nullptr, 0, smem_u32(ring) + lane * 16, 0};
+    Stream<G32, kStages> st{a, s, warp, lane, kblocks, pairs, n_groups, at, 0, my_units * my_blocks, nullptr, nullptr, 0, smem_u32(ring) + lane * 16, 0};
     st.seek();
     for (int i = 0; i < kStages - 1; ++i) st.issue();
     int out_stage = 0;
     for (; at.group < n_groups; at.next(pairs)) {
         const int sl = s.group_slot[at.group], tenant = s.tenant[sl];
         const int r0 = s.group_row[at.group], rows = min(s.begin[sl + 1] - r0, 64);
-        if (MAXT == 1 || rows <= 8) unit<1, G32>(a, s, st, out_stage, red, ring, at.pair, r0, rows, tenant);
-        else if (MAXT == 2 || rows <= 16) unit<(MAXT < 2 ? MAXT : 2), G32>(a, s, st, out_stage, red, ring, at.pair, r0, rows, tenant);
-        else if (MAXT == 4 || rows <= 32) unit<(MAXT < 4 ? MAXT : 4), G32>(a, s, st, out_stage, red, ring, at.pair, r0, rows, tenant);
-        else unit<(MAXT < 8 ? MAXT : 8), G32>(a, s, st, out_stage, red, ring, at.pair, r0, rows, tenant);
+        if (MAXT == 1 || rows <= 8) unit<1, G32, kStages>(a, s, st, out_stage, red, ring, at.pair, r0, rows, tenant);
+        else if (MAXT == 2 || rows <= 16) unit<(MAXT < 2 ? MAXT : 2), G32, kStages>(a, s, st, out_stage, red, ring, at.pair, r0, rows, tenant);
+        else if (MAXT == 4 || rows <= 32) unit<(MAXT < 4 ? MAXT : 4), G32, kStages>(a, s, st, out_stage, red, ring, at.pair, r0, rows, tenant);
+        else unit<(MAXT < 8 ? MAXT : 8), G32, kStages>(a, s, st, out_stage, red, ring, at.pair, r0, rows, tenant);
     }
     asm volatile("cp.async.wait_group 0;" ::: "memory");
 }
 
-constexpr int shared_bytes(int maxt) { return kWarps * kStages * kStageBytes + kWarps * maxt * 8 * 36 * 4; }
+constexpr int shared_bytes(int maxt) { return kWarps * stages(maxt) * kStageBytes + kWarps * maxt * 8 * 36 * 4; }
 typedef void (*Kernel)(QuantLinearArgs);
 const Kernel kKernels[2][4] = {
     {quant_linear_kernel<1, false>, quant_linear_kernel<2, false>, quant_linear_kernel<4, false>, quant_linear_kernel<8, false>},
@@ -326,7 +330,7 @@ cudaError_t launch_quant_linear(const QuantLinearArgs& a, int sm_count, cudaStre
     const int most_slots = a.n < a.tenants ? a.n : a.tenants;
     const int64_t units = (int64_t)((a.N + 31) / 32) * most_slots;      // (more groups only where a tenant has over 64 rows)
     const int v = a.n <= 8 ? 0 : a.n <= 16 ? 1 : a.n <= 32 ? 2 : 3;       // up to 8 << v rows of a tenant
-    int64_t grid = (int64_t)sm_count * (v == 0 ? 4 : v == 1 ? 3 : v == 2 ? 2 : 1);
+    int64_t grid = (int64_t)sm_count * (v <= 1 ? 3 : v == 2 ? 2 : 1);
     if (grid > units) grid = units;
     QuantLinearArgs b = a;
     b.codes_bytes = quant_codes_bytes(a.K, a.N);
