@@ -61,7 +61,7 @@ mt_status op_scratch(cudaStream_t s, size_t bytes, uint8_t** out) {
     if (e && e->bytes >= bytes) { *out = e->block; return MT_OK; }
     if (!e && g_n_scratch == kMaxStreams) return MT_ERR_OOM;
     if (e && g_n_retired == kMaxRetired) return MT_ERR_OOM;
-    size_t want = e ? 2 * e->bytes : kScratchZeroBytes + (8u << 20);
+    size_t want = e ? 2 * e->bytes : (16u << 20);
     if (want < bytes) want = bytes;
     void* p = nullptr;
     cudaError_t err = cudaMalloc(&p, want);
@@ -71,8 +71,6 @@ mt_status op_scratch(cudaStream_t s, size_t bytes, uint8_t** out) {
         err = cudaMalloc(&p, want);
     }
     if (err != cudaSuccess) { cudaGetLastError(); return to_status(err); }
-    err = cudaMemsetAsync(p, 0, kScratchZeroBytes, s);
-    if (err != cudaSuccess) { cudaFree(p); return to_status(err); }
     if (e) g_retired[g_n_retired++] = e->block;
     else { e = &g_scratch[g_n_scratch++]; e->stream = s; }
     e->block = static_cast<uint8_t*>(p);

@@ -95,9 +95,7 @@ struct LogprobArgs {
 cudaError_t configure_token_logprobs();
 mt_status launch_token_logprobs(const LogprobArgs& a, const OpContext& c, cudaStream_t s);
 
-// Scratch of at least `bytes` on stream `s`, kept until mt_shutdown; the first kScratchZeroBytes are zero when they are
-// handed out for the first time and every kernel leaves them zero.  (Mutex held.)
-constexpr size_t kScratchZeroBytes = 4u << 20;
+// Scratch of at least `bytes` (256-byte aligned, contents left over from earlier calls) on stream `s`, kept until mt_shutdown.  (Mutex held.)
 mt_status op_scratch(cudaStream_t s, size_t bytes, uint8_t** out);
 
 }  // namespace mt
