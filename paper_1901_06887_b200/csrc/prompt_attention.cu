@@ -443,11 +443,13 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
                     for (int e = 2; e < 32; e += 2) mx4[c] = max3(mx4[c], __uint_as_float(x[c][e]), __uint_as_float(x[c][e + 1]));
                 }
                 const float mx = fmaxf(max3(mx4[0], mx4[1], mx4[2]), mx4[3]);
+                // (a row without weight so far, all its scores minus infinity, starts again; m stays finite)
+                const bool move = (mx - m) * p.c > kSlack || l == 0.f;
                 if (j == 0) {
-                    m = mx;
-                } else if (__any_sync(0xffffffffu, (mx - m) * p.c > kSlack)) {
+                    m = mx > -INFINITY ? mx : 0.f;
+                } else if (__any_sync(0xffffffffu, move)) {
                     // (a row moves on its own account only, so its bits do not depend on its neighbours)
-                    const float nm = (mx - m) * p.c > kSlack ? mx : m, f = m == nm ? 1.f : ex2((m - nm) * p.c);
+                    const float nm = move && mx > -INFINITY ? mx : m, f = m == nm || l == 0.f ? 1.f : ex2((m - nm) * p.c);
                     m = nm;
                     l *= f;
                     ok = mbar_wait(bar(s.o_ready[i]), (n_o - 1) & 1, abort_flag, p.status, 231);

@@ -160,3 +160,31 @@ def test_other_stream_and_graph():
     graph.replay()
     torch.cuda.synchronize()
     assert torch.equal(out, want)
+
+
+def test_scores_that_rise_along_the_sequence():
+    """Each 128 keys lie far above all before them, by less and by more than what the running reference allows, and fall again."""
+    for step in (5.0, 40.0, 400.0, 3000.0):
+        q, k, v, off = make([700], 2, 1, 64, seed=11)
+        q, k = q.clone(), 0.1 * k
+        q[..., 0] = 1.0
+        level = torch.tensor([0, 1, 2, 4, 3, 5], device="cuda")[torch.arange(700, device="cuda") // 128]
+        k[:, 0, 0] = (level * step).to(torch.bfloat16)
+        k[300, 0, 0] = k[300, 0, 0] + torch.tensor(2 * step, device="cuda").to(torch.bfloat16)     # one key inside a block, in its first half
+        k[480, 0, 0] = k[480, 0, 0] + torch.tensor(3 * step, device="cuda").to(torch.bfloat16)     # and one in a second half
+        check(q, k, v, off, scale=0.5)
+
+
+def test_first_block_without_weight():
+    """Scores of minus infinity in all of the first 128 keys; the rest decides, however low it lies."""
+    q, k, v, off = make([400], 1, 1, 64, seed=12)
+    q, k = q.clone(), k.clone()
+    q[..., 0] = 1.0
+    k[:128, 0, 0] = float("-inf")
+    k[128:, 0, 0] = -1000.0
+    out = torch.empty(q.shape, dtype=torch.bfloat16, device="cuda")
+    mt.mt_prompt_attention(q, k, v, torch.from_numpy(off).cuda(), out)
+    torch.cuda.synchronize()
+    o, a = prompt_reference(q[128:], k[128:], v[128:], [0, 272], 0.125)       # the first 128 keys weigh nothing
+    assert (np.abs(out[128:].double().cpu().numpy() - o) <= attention_bound(o, a)).all()
+    assert torch.isnan(out[:128]).all()
