@@ -194,7 +194,8 @@ mt_status mt_cache_sim_destroy(void* sim);
 
 /* Synchronise `stream`, then report and clear the sticky device-side status of the calls so far:
  * *status_out is MT_OK, MT_ERR_BAD_MODEL_ID or MT_ERR_NOT_RESIDENT (with the smallest offending arrival index of the
- * first such batch in *bad_request_index_out, else -1) or MT_ERR_TIMEOUT.  Either out pointer may be NULL. */
+ * first such batch in *bad_request_index_out, else -1), MT_ERR_TIMEOUT, or MT_ERR_INVALID_ARG from an operator of the
+ * language-model tenants (below) with the index of the sequence, token or row.  Either out pointer may be NULL. */
 mt_status mt_get_async_status(void* stream, int32_t* status_out, int32_t* bad_request_index_out);
 
 const char* mt_status_string(mt_status s);
@@ -212,8 +213,9 @@ mt_status mt_debug_last_bucketing(int32_t* counts_host, int32_t* offsets_host, i
  * Afterwards mt_get_async_status reports MT_ERR_TIMEOUT and the context stays usable. */
 mt_status mt_debug_wait_timeout(int32_t limit_ms, void* stream);
 
-/* Test / bench hook: *count_out = number of kernels this library has enqueued on behalf of mt_infer and
- * mt_infer_host since it was loaded (registration and the no-allocation call are not counted). */
+/* Test / bench hook: *count_out = number of kernels this library has enqueued on behalf of mt_infer,
+ * mt_infer_host and the operators of language-model tenants since it was loaded (registration and the no-allocation call
+ * are not counted). */
 mt_status mt_debug_launch_count(int64_t* count_out);
 
 /* Cost-aware scheduling (Sec. 3.2: a DNN's work per layer is fixed by its shape, so the cost of every work item is
@@ -303,28 +305,29 @@ mt_status mt_bucket_noalloc(const int32_t* model_ids, int32_t n, int32_t n_model
  *
  * They need mt_init (else MT_ERR_NOT_INIT) but no registered model: every array is the caller's.  Unless marked "host",
  * pointers are device memory of the context's device.  Each call only enqueues kernels on `stream` and returns; arrays
- * must stay valid, and unchanged where they are inputs, until the stream has passed the call.  mt_kv_attention and
- * mt_token_logprobs use scratch that the library keeps PER STREAM, so calls on different streams may overlap; the
- * first call on a stream, and one that needs more than any before, allocates it (that call may synchronise; make it
- * before a stream capture).  At most 64 streams may use them (then MT_ERR_OOM).  Scratch goes away with mt_shutdown.
- * All of them may be captured into CUDA graphs; replays of graphs that were captured on ONE stream must not overlap.
+ * must stay valid, and unchanged where they are inputs, until the stream has passed the call.  mt_kv_attention uses
+ * scratch that the library keeps PER STREAM, so calls on different streams may overlap; the first call on a stream, and
+ * one that needs more than any before, allocates it (that call may synchronise; make it before a stream capture).  At
+ * most 64 streams may use it (then MT_ERR_OOM).  Scratch goes away with mt_shutdown.  All of them may be captured into
+ * CUDA graphs; replays of graphs with mt_kv_attention that were captured on ONE stream must not overlap.
  *
  * Refusals: MT_ERR_INVALID_ARG null pointer, negative size, unknown type, misaligned pointer; MT_ERR_UNSUPPORTED a
  * size or stride outside what the kernels take; nothing is enqueued then.  A count of zero is a no-op.  What only the
  * device can see (an id, page, slot, length or offset out of range) never faults: the rows concerned are NaN (or left
  * out, where rows are written to a cache), and the sticky status of mt_get_async_status is MT_ERR_BAD_MODEL_ID (ids) or
- * MT_ERR_INVALID_ARG, with the smallest index concerned. */
+ * MT_ERR_INVALID_ARG, with the smallest index concerned.  mt_prompt_attention, whose kernel waits on barriers, can also
+ * report MT_ERR_TIMEOUT there (a wait that gave up; its output is then incomplete). */
 typedef enum { MT_BF16 = 0, MT_FP32 = 1 } mt_dtype;
 
 /* Attention over whole prompts, causal, packed one behind the other: sequence s is rows offsets[s] .. offsets[s+1]-1.
  *   o[i][h] = sum over j <= i of the same sequence of softmax_j(scale * q[i][h] . k[j][h / g]) v[j][h / g],
- * g = q_heads / kv_heads.  q [n_tokens][q_heads][head_dim], k and v [n_tokens][kv_heads][head_dim], bf16, each with its own
- * strides (elements) between tokens and heads and head_dim contiguous, so the three may be slices of one projection's
- * output; out bf16, contiguous [n_tokens][q_heads][head_dim], must not overlap the inputs.  offsets: int32 [n_seqs + 1], not decreasing,
- * between 0 and n_tokens; rows outside every sequence are not written.  A sequence that breaks this is not computed (its
+ * g = q_heads / kv_heads.  q [n_tokens][q_heads][head_dim], k and v [n_tokens][kv_heads][head_dim], bf16, each with its
+ * own strides (elements) between tokens and heads and head_dim contiguous, so the three may be slices of one projection's
+ * output; out bf16, contiguous [n_tokens][q_heads][head_dim], must not overlap the inputs.  offsets: int32 [n_seqs + 1],
+ * not decreasing, between 0 and n_tokens; rows outside every sequence are not written.  A sequence that breaks this is not computed (its
  * rows, where it has any, are left as they were; sticky status, index of the sequence).  Scores and sums are fp32; the
  * probabilities are rounded to bf16 before they meet v.  A masked position never shows: infinities and NaN in k or v of
- * later tokens or other sequences leave an output as it is.
+ * later tokens or other sequences leave an output as it is.  (An infinity of v in a position that IS seen may come out as NaN.)
  * Limits: head_dim 64 or 128; q_heads a multiple of kv_heads; pointers 16-byte aligned; strides multiples of 8, a head
  * stride of at least head_dim, a token stride of at least head_dim, each below 2^36. */
 typedef struct {
@@ -348,15 +351,16 @@ typedef struct {
 /* Rounds the rows of n tokens to 4 bits and writes token i to slot slots[i] = page * page_tokens + place (int64).
  * bias = the row's least element, scale = (largest - least) / 15 rounded to bf16, code = the nearest of the sixteen levels
  * (ties to even).  A row with an infinity or NaN, or whose spread passes fp32, reads back as NaN.  k and v: bf16
- * [n][kv_heads][head_dim] with strides (elements, multiples of 8) between tokens and heads, 16-byte aligned.  A slot of -1 leaves its
- * token out; any other slot outside the cache does too and sets the sticky status.  Two tokens of one call must not name the
- * same slot. */
+ * [n][kv_heads][head_dim] with strides (elements, multiples of 8) between tokens and heads, 16-byte aligned.  A slot of -1
+ * leaves its token out; any other slot outside the cache does too and sets the sticky status.  Two tokens of one call must
+ * not name the same slot. */
 mt_status mt_kv_append(const mt_kv_cache* cache_host, const void* k, int64_t k_token_stride, int64_t k_head_stride,
                        const void* v, int64_t v_token_stride, int64_t v_head_stride, const int64_t* slots, int32_t n,
                        void* stream);
 
-/* The values of n slots, rounded to bf16: k_out and v_out [n][kv_heads][head_dim], contiguous (what a prompt that goes on from cached tokens, or a move to
- * another cache, needs).  A slot of -1 gives zeros; any other slot outside the cache gives NaN and sets the sticky status. */
+/* The values of n slots, rounded to bf16: k_out and v_out [n][kv_heads][head_dim], contiguous (what a prompt that goes on
+ * from cached tokens, or a move to another cache, needs).  A slot of -1 gives zeros; any other slot outside the cache gives
+ * NaN and sets the sticky status. */
 mt_status mt_kv_read(const mt_kv_cache* cache_host, const int64_t* slots, int32_t n, void* k_out, void* v_out, void* stream);
 
 /* Attention of ONE new token per sequence over its cached tokens:
@@ -365,8 +369,9 @@ mt_status mt_kv_read(const mt_kv_cache* cache_host, const int64_t* slots, int32_
  * sequence's last page are not read; lengths int32 [n_seqs].  A sequence without tokens gives zeros.  A length below zero or
  * beyond table_width pages, or a page outside the cache, gives NaN rows and the sticky status.  q bf16
  * [n_seqs][q_heads][head_dim] with strides (elements, multiples of 8), 16-byte aligned; out bf16, contiguous.
- * Codes meet the products as whole numbers (exact in bf16), scales and biases are applied in fp32; probabilities times the
- * value's scale are rounded to bf16 before they meet the codes.
+ * Codes meet the products as whole numbers, with exact sums.  For that a head's query is rounded to 16 bits relative to its
+ * largest element, and probability times value scale to 13 bits relative to the largest among 32 tokens; all scales,
+ * biases and sums are fp32.
  * Limits: q_heads = g * kv_heads with g at most 16; n_seqs * kv_heads below 2^20. */
 mt_status mt_kv_attention(const mt_kv_cache* cache_host, const void* q, int64_t q_seq_stride, int64_t q_head_stride,
                           const int32_t* tables, int32_t table_width, const int32_t* lengths, int32_t n_seqs,
@@ -387,9 +392,9 @@ mt_status mt_quant_pack(const uint8_t* codes, const void* scales, int32_t tenant
                         int32_t out_features, int32_t group, void* packed, void* stream);
 
 /* y[i] = weight[ids[i]] x[i] + bias[ids[i]] for a mixed batch of n rows.  x bf16, rows x_stride elements apart (a multiple
- * of 8), 16-byte aligned; y bf16 or fp32 by y_dtype, rows y_stride elements apart.  Products and sums are fp32, codes enter as whole numbers.  An id outside
- * [0, tenants) gives a NaN row and the sticky status.  Any n; made for the few rows of a token step (each distinct tenant's weights are read once
- * per 64 of its rows, at most 256 rows a launch). */
+ * of 8), 16-byte aligned; y bf16 or fp32 by y_dtype, rows y_stride elements apart.  Products and sums are fp32, codes enter
+ * as whole numbers.  An id outside [0, tenants) gives a NaN row and the sticky status.  Any n; made for the few rows of a
+ * token step (each distinct tenant's weights are read once per 64 of its rows, at most 256 rows a launch). */
 mt_status mt_quant_linear(const mt_quant_bank* bank_host, const void* x, int64_t x_stride, const int32_t* ids, int32_t n,
                           void* y, int64_t y_stride, int32_t y_dtype, void* stream);
 
