@@ -368,11 +368,13 @@ mt_status mt_kv_read(const mt_kv_cache* cache_host, const int64_t* slots, int32_
  * token j of sequence s in page tables[s][j / page_tokens], place j % page_tokens.  tables int32 [n_seqs][table_width], entries past a
  * sequence's last page are not read; lengths int32 [n_seqs].  A sequence without tokens gives zeros.  A length below zero or
  * beyond table_width pages, or a page outside the cache, gives NaN rows and the sticky status.  q bf16
- * [n_seqs][q_heads][head_dim] with strides (elements, multiples of 8), 16-byte aligned; out bf16, contiguous.
+ * [n_seqs][q_heads][head_dim] with strides (elements, multiples of 8), 16-byte aligned; out bf16, contiguous, must not
+ * overlap q or the cache.
  * Codes meet the products as whole numbers, with exact sums.  For that a head's query is rounded to 16 bits relative to its
  * largest element, and probability times value scale to 13 bits relative to the largest among 32 tokens; all scales,
  * biases and sums are fp32.
- * Limits: q_heads = g * kv_heads with g at most 16; n_seqs * kv_heads below 2^20. */
+ * Limits: q_heads = g * kv_heads with g at most 16; n_seqs * kv_heads below 2^20; table_width * page_tokens below
+ * 2^31 - 64. */
 mt_status mt_kv_attention(const mt_kv_cache* cache_host, const void* q, int64_t q_seq_stride, int64_t q_head_stride,
                           const int32_t* tables, int32_t table_width, const int32_t* lengths, int32_t n_seqs,
                           int32_t q_heads, float scale, void* out, void* stream);
@@ -393,7 +395,7 @@ mt_status mt_quant_pack(const uint8_t* codes, const void* scales, int32_t tenant
 
 /* y[i] = weight[ids[i]] x[i] + bias[ids[i]] for a mixed batch of n rows.  x bf16, rows x_stride elements apart (a multiple
  * of 8), 16-byte aligned; y bf16 or fp32 by y_dtype, rows y_stride elements apart.  Products and sums are fp32, codes enter
- * as whole numbers.  An id outside [0, tenants) gives a NaN row and the sticky status.  Any n; made for the few rows of a
+ * as whole numbers; y must not overlap x.  An id outside [0, tenants) gives a NaN row and the sticky status.  Any n; made for the few rows of a
  * token step (each distinct tenant's weights are read once per 64 of its rows, at most 256 rows a launch). */
 mt_status mt_quant_linear(const mt_quant_bank* bank_host, const void* x, int64_t x_stride, const int32_t* ids, int32_t n,
                           void* y, int64_t y_stride, int32_t y_dtype, void* stream);

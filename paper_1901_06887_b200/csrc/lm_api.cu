@@ -157,7 +157,7 @@ mt_status mt_kv_attention(const mt_kv_cache* cache, const void* q, int64_t q_seq
     if (st != MT_OK) return st;
     if (n_seqs < 0 || q_heads <= 0 || table_width < 0) return MT_ERR_INVALID_ARG;
     if (q_heads % cache->kv_heads || q_heads / cache->kv_heads > 16) return MT_ERR_UNSUPPORTED;
-    if ((int64_t)n_seqs * cache->kv_heads >= (1 << 20) || (int64_t)table_width * cache->page_tokens > INT_MAX) return MT_ERR_UNSUPPORTED;
+    if ((int64_t)n_seqs * cache->kv_heads >= (1 << 20) || (int64_t)table_width * cache->page_tokens > INT_MAX - 64) return MT_ERR_UNSUPPORTED;
     if (bad_stride(q_seq_stride, 0) || bad_stride(q_head_stride, 0)) return MT_ERR_UNSUPPORTED;
     std::unique_lock<std::mutex> lk;
     OpContext c;

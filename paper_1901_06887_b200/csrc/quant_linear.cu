@@ -9,7 +9,7 @@
 // inner index are chosen so that a lane's inputs are 16 contiguous bytes too.
 //
 // Split.  A CTA takes (tenant, 32 outputs) units in turn, its eight warps every eighth block of 64 inputs; they join through shared memory.
-// Every warp copies its blocks ahead into a ring of its own (cp.async, three blocks ahead, on through the units to come), so the joins and
+// Every warp copies its blocks ahead into a ring of its own (cp.async, three or seven blocks ahead, on through the units to come), so the joins and
 // the ends of units do not empty the pipe: loading into registers unit by unit left the kernel waiting for memory (93 us for 8 tenants of
 // 4096 -> 16384, 24 rows).  Two tiles of 16 outputs share the rows' loads and the loop: what is left is bound by instructions.
 // Which tenants occur is found out by every CTA for itself from the ids (at most 256 a launch): no bucketing launch, and only tenants that
