@@ -350,7 +350,7 @@ def mt_bucket_noalloc(model_ids, n: int, n_models: int, counts_out, offsets_out,
 
 # ------------------------------------------------------------------------------------------------
 # Operators of language-model tenants.  These take torch tensors on the context's device and read sizes and strides from
-# them; a tensor of another type, shape or place is refused here (MT_ERR_INVALID_ARG), sizes are judged by the library.  A
+# them; a tensor of another type, shape or place is refused here (MT_ERR_INVALID_ARG), sizes are checked by the library.  A
 # call's time on the host is the floor of a token step, so the checks are few, flat expressions: 3 to 5 us a call.
 # ------------------------------------------------------------------------------------------------
 class _Types:
