@@ -371,7 +371,7 @@ mt_status mt_kv_read(const mt_kv_cache* cache_host, const int64_t* slots, int32_
  * [n_seqs][q_heads][head_dim] with strides (elements, multiples of 8), 16-byte aligned; out bf16, contiguous, must not
  * overlap q or the cache.
  * Codes meet the products as whole numbers, with exact sums.  For that a head's query is rounded to 16 bits relative to its
- * largest element, and probability times value scale to 13 bits relative to the largest among 32 tokens; all scales,
+ * largest element, and probability times value scale to 14 bits relative to the largest such product among 32 tokens; all scales,
  * biases and sums are fp32.
  * Limits: q_heads = g * kv_heads with g at most 16; n_seqs * kv_heads below 2^20; table_width * page_tokens below
  * 2^31 - 64. */

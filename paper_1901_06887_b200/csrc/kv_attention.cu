@@ -6,13 +6,15 @@
 // four codes cost one mask, or a shift and a mask, where a floating type takes two instructions for every two codes.  The other
 // operand is rounded to whole numbers and cut into two signed bytes:
 //   q' = 256 q1 + q2, relative to the head's largest element (error at most 2^-16 of that; bf16's own is 2^-9 of each element);
-//   P  = 64 P1 + P2, P = p scale_v relative to the tile's largest scale_v and the tile's largest p: 13 bits, error at most 2^-13 of it (with 11
-//        bits the result's error over long contexts doubled: the tile's largest p stands far above the rest).
+//   P  = 128 P1 + P2, P = p scale_v relative to the head's largest such product in the tile: 14 bits, error at most 2^-14 of it (with 11
+//        bits the result's error over long contexts doubled: the tile's largest p stands far above the rest).  The largest PRODUCT, not the
+//        largest p and the largest scale_v: where one token has the weight and another the scale, as a first token of small values beside
+//        ordinary ones, all products lie far below those two together and would keep few bits or none.
 // Scales and biases are applied in fp32 outside:
 //   S = scale_k (sum_d code q_d) + bias_k sum_d q_d
 //   o = sum P (code - 8) + sum p (8 scale_v + bias_v)
 // The -8 is one more product (a constant row): over a long context o is a small mean of many values, and what is taken off must be
-// made of the same rounded P.  A tile of 32 tokens has a maximum and a scale of its own and is added to the running o in
+// made of the same rounded P.  Every head of a tile of 32 tokens has a scale of P of its own; the tile is added to the running o in
 // fp32; its integer sums start at 1.5 * 2^23 as a bit pattern, so they need no conversion to be read as floats.
 //
 // Bound: memory.  head_dim + 8 bytes per cached token and head; some 500 warp instructions per 32 tokens.
@@ -70,6 +72,19 @@ __device__ __forceinline__ void range_scale(uint32_t bits, float& up, float& dow
 constexpr float kMagic = 12582912.f;
 constexpr int kMagicBits = 0x4b400000;
 __device__ __forceinline__ uint32_t whole(float x, float y) { return __float_as_uint(fmaf(x, y, kMagic)); }
+// The factor that brings the products of a column, the largest of which has the exponent of `bits`, to below 2^14 - 1/2, and its reciprocal:
+// a power of two, times 1 - 2^-14 and 1 + 2^-14.  P then is 2^14 - 1 at most, and P1 stays within 127.  (32 such P times 8 stay below 2^22, what
+// kMagic leaves room for.)  Products below 2^-106 of the largest weight's lose bits.
+__device__ __forceinline__ void product_scale(uint32_t bits, float& up, float& down) {
+    const uint32_t e = max(bits & 0x7f800000u, 21u << 23);
+    up = __uint_as_float((267u << 23) - 1024u - e);
+    down = __uint_as_float(e + 512u - (13u << 23));
+}
+__device__ __forceinline__ uint32_t max_u16x2(uint32_t a, uint32_t b) {
+    uint32_t d;
+    asm("max.u16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+}
 // y += (x - kMagic) * s on pairs.
 __device__ __forceinline__ void add_scaled(float2& y, int x0, int x1, float s0, float s1) {
     asm("{\n\t.reg .b64 x, s, y, m;\n\t"
@@ -388,31 +403,25 @@ __global__ void __launch_bounds__(kWarps * 32, GT == 1 ? 4 : 2) kv_attention_ker
                         if (tok + 16 * h + 8 * e + tg >= len)
 #pragma unroll
                             for (int n = 0; n < GT; ++n) s[n][h][2 * e] = s[n][h][2 * e + 1] = -INFINITY;
-            // the tile's maxima and its values' largest scale
-            float mt[GT][2];
+            // the running maxima, looked at across the lanes only where one of them rises (over a long context that is soon rare)
             bool grow = false;
+            float mt[GT][2];
 #pragma unroll
             for (int n = 0; n < GT; ++n)
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
-                    float x = fmaxf(fmaxf(s[n][0][c], s[n][0][2 + c]), fmaxf(s[n][1][c], s[n][1][2 + c]));
-                    x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
-                    x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
-                    x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
-                    mt[n][c] = x;
-                    grow = grow || x > m[n][c];
+                    mt[n][c] = fmaxf(fmaxf(s[n][0][c], s[n][0][2 + c]), fmaxf(s[n][1][c], s[n][1][2 + c]));
+                    grow = grow || mt[n][c] > m[n][c];
                 }
-            float v_up, v_down;
-            range_scale<13>(__reduce_max_sync(0xffffffffu, (vq << 16) & 0x7fffffffu), v_up, v_down);
-            v_up *= 8128.f / 8192.f;                 // so that P1 stays within 127
-            v_down *= 8192.f / 8128.f;
             if (__any_sync(0xffffffffu, grow)) {
 #pragma unroll
                 for (int n = 0; n < GT; ++n) {
                     float f[2];
 #pragma unroll
                     for (int c = 0; c < 2; ++c) {
-                        const float nm = fmaxf(m[n][c], mt[n][c]);
+                        float nm = fmaxf(m[n][c], mt[n][c]);
+#pragma unroll
+                        for (int x = 4; x < 32; x <<= 1) nm = fmaxf(nm, __shfl_xor_sync(0xffffffffu, nm, x));
                         f[c] = m[n][c] == nm ? 1.f : ex2((m[n][c] - nm) * qdown[n][c]);
                         m[n][c] = nm;
                         l[n][c] *= f[c]; z[n][c] *= f[c];
@@ -421,41 +430,50 @@ __global__ void __launch_bounds__(kWarps * 32, GT == 1 ? 4 : 2) kv_attention_ker
                     for (int i = 0; i < 2 * kMt; ++i) { o[n][i].x *= f[0]; o[n][i].y *= f[1]; }
                 }
             }
-            // probabilities relative to the tile's maximum, and the two parts of P turned to the B operand's layout
+            // probabilities, their products with the value scales, and the two parts of P turned to the B operand's layout
             uint32_t p1[GT][2], p2[GT][2];
             int c1[GT][4], c2[GT][4];
             float beta[GT][2];
 #pragma unroll
             for (int n = 0; n < GT; ++n) {
-                float sl[2] = {0.f, 0.f}, sz[2] = {0.f, 0.f};
-                const float shift[2] = {-mt[n][0] * qdown[n][0], -mt[n][1] * qdown[n][1]};
+                float sl[2] = {0.f, 0.f}, sz[2] = {0.f, 0.f}, y[2][2][2], top[2] = {0.f, 0.f};
+                const float shift[2] = {-m[n][0] * qdown[n][0], -m[n][1] * qdown[n][1]};
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    uint32_t x[2][2];
+                for (int h = 0; h < 2; ++h)
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
                         const uint32_t w = __shfl_sync(0xffffffffu, vq, 16 * h + 8 * e + tg);
-                        const float vs = bf16_lo(w), mid = fmaf(8.f, vs, bf16_hi(w)), scaled = vs * v_up;
+                        const float vs = bf16_lo(w), mid = fmaf(8.f, vs, bf16_hi(w));
 #pragma unroll
                         for (int c = 0; c < 2; ++c) {
                             const float pr = ex2(fmaf(s[n][h][2 * e + c], qdown[n][c], shift[c]));
                             sl[c] += pr;
                             sz[c] = fmaf(pr, mid, sz[c]);
-                            x[c][e] = whole(pr, scaled);
+                            y[h][e][c] = pr * vs;
+                            top[c] = fmaxf(top[c], fabsf(y[h][e][c]));
                         }
                     }
+                // the exponent of each column's largest product; two columns' upper halves go round together
+                uint32_t both = __byte_perm(__float_as_uint(top[0]), __float_as_uint(top[1]), 0x7632);
+#pragma unroll
+                for (int x = 4; x < 32; x <<= 1) both = max_u16x2(both, __shfl_xor_sync(0xffffffffu, both, x));
+                float up[2];
+                product_scale(both << 16, up[0], beta[n][0]);
+                product_scale(both, up[1], beta[n][1]);
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    uint32_t x[2][2];
+#pragma unroll
+                    for (int e = 0; e < 2; ++e)
+#pragma unroll
+                        for (int c = 0; c < 2; ++c) x[c][e] = whole(y[h][e][c], up[c]);
                     // bytes of P1 and P2, columns 2 t and 2 t + 1, tokens g and g + 8 of the half
                     const uint32_t x0 = __byte_perm(x[0][0], x[0][1], 0x5410), x1 = __byte_perm(x[1][0], x[1][1], 0x5410);
-                    p1[n][h] = transpose8x8(__byte_perm(x0 >> 6, x1 >> 6, 0x6420));
-                    p2[n][h] = transpose8x8(__byte_perm(x0, x1, 0x6420) & 0x3f3f3f3fu);
+                    p1[n][h] = transpose8x8(__byte_perm(x0 >> 7, x1 >> 7, 0x6420));
+                    p2[n][h] = transpose8x8(__byte_perm(x0, x1, 0x6420) & 0x7f7f7f7fu);
                 }
 #pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    const float b = ex2((mt[n][c] - m[n][c]) * qdown[n][c]);
-                    l[n][c] = fmaf(b, sl[c], l[n][c]);
-                    z[n][c] = fmaf(b, sz[c], z[n][c]);
-                    beta[n][c] = b * v_down;
-                }
+                for (int c = 0; c < 2; ++c) { l[n][c] += sl[c]; z[n][c] += sz[c]; }
                 mma_u8s8(c1[n], 0x08080808u, 0x08080808u, 0x08080808u, 0x08080808u, p1[n], zero);     // 8 sum P1 and 8 sum P2, for every row
                 mma_u8s8(c2[n], 0x08080808u, 0x08080808u, 0x08080808u, 0x08080808u, p2[n], zero);
 #pragma unroll
@@ -486,7 +504,7 @@ __global__ void __launch_bounds__(kWarps * 32, GT == 1 ? 4 : 2) kv_attention_ker
                         int d[4];
                         mma_u8s8(d, a0, a1, a2, a3, p1[n], c1[n]);
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) d[k] = (d[k] << 6) + c2[n][k];
+                        for (int k = 0; k < 4; ++k) d[k] = (d[k] << 7) + c2[n][k];
                         mma_u8s8(d, a0, a1, a2, a3, p2[n], d);
                         add_scaled(o[n][2 * (4 * j + i)], d[0], d[1], beta[n][0], beta[n][1]);
                         add_scaled(o[n][2 * (4 * j + i) + 1], d[2], d[3], beta[n][0], beta[n][1]);
