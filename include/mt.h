@@ -370,9 +370,10 @@ mt_status mt_kv_read(const mt_kv_cache* cache_host, const int64_t* slots, int32_
  * beyond table_width pages, or a page outside the cache, gives NaN rows and the sticky status.  q bf16
  * [n_seqs][q_heads][head_dim] with strides (elements, multiples of 8), 16-byte aligned; out bf16, contiguous, must not
  * overlap q or the cache.
- * Codes meet the products as whole numbers, with exact sums.  For that a head's query is rounded to 16 bits relative to its
- * largest element, and probability times value scale to 14 bits relative to the largest such product among 32 tokens; all scales,
- * biases and sums are fp32.
+ * Codes meet the products as whole numbers, with exact sums.  For that, elements of a query below 2^-6 of the head's largest
+ * are rounded to multiples of 2^-14 of it (they meet a key's codes less 7.5; the middle of its range meets the query as it
+ * is), and probability times value scale to 14 bits relative to the largest such product among 32 tokens; all scales, biases
+ * and sums are fp32.
  * Limits: q_heads = g * kv_heads with g at most 16; n_seqs * kv_heads below 2^20; table_width * page_tokens below
  * 2^31 - 64. */
 mt_status mt_kv_attention(const mt_kv_cache* cache_host, const void* q, int64_t q_seq_stride, int64_t q_head_stride,

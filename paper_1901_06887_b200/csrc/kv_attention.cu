@@ -5,14 +5,16 @@
 // K and V rows are code * scale + bias.  The codes go into integer matrix instructions (u8 times s8, exact 32-bit sums) as they stand:
 // four codes cost one mask, or a shift and a mask, where a floating type takes two instructions for every two codes.  The other
 // operand is rounded to whole numbers and cut into two signed bytes:
-//   q' = 256 q1 + q2, relative to the head's largest element (error at most 2^-16 of that; bf16's own is 2^-9 of each element);
+//   q' = 256 q1 + q2: an element of at least 2^-6 of the head's largest stays what it is, a smaller one errs by some 2^-15 of the largest at most;
 //   P  = 128 P1 + P2, P = p scale_v relative to the head's largest such product in the tile: 14 bits, error at most 2^-14 of it (with 11
 //        bits the result's error over long contexts doubled: the tile's largest p stands far above the rest).  The largest PRODUCT, not the
 //        largest p and the largest scale_v: where one token has the weight and another the scale, as a first token of small values beside
 //        ordinary ones, all products lie far below those two together and would keep few bits or none.
 // Scales and biases are applied in fp32 outside:
-//   S = scale_k (sum_d code q_d) + bias_k sum_d q_d
+//   S = scale_k (sum_d (code - 7.5) q'_d) + (bias_k + 7.5 scale_k) sum_d q_d
 //   o = sum P (code - 8) + sum p (8 scale_v + bias_v)
+// The 7.5 terms are one whole number a head, 7.5 sum (q - q'), that the integer sums start with: without it errors of the small elements that
+// agree in sign (a query of one large element and many alike) met the codes' middle in every channel, and an output was off by 2 % at 1 to 64.
 // The -8 is one more product (a constant row): over a long context o is a small mean of many values, and what is taken off must be
 // made of the same rounded P.  Every head of a tile of 32 tokens has a scale of P of its own; the tile is added to the running o in
 // fp32; its integer sums start at 1.5 * 2^23 as a bit pattern, so they need no conversion to be read as floats.
@@ -60,13 +62,12 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t a) {
     asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(a));
     return d;
 }
-// The power of two that brings the number with these bits into [2^(BITS - 1), 2^BITS), and its reciprocal (both normal numbers for
-// every exponent).
-template <int BITS>
-__device__ __forceinline__ void range_scale(uint32_t bits, float& up, float& down) {
-    const int e = max((int)((bits >> 23) & 255u), BITS + 7);
-    up = __int_as_float((253 + BITS - e) << 23);
-    down = __int_as_float((e + 1 - BITS) << 23);
+// The power of two that brings the bf16 number with these bits into [2^14, 2^15), and its reciprocal (both normal numbers for every exponent); with
+// a mantissa of ones into [2^13, 2^14), as 2^15 - 2^7 has no high byte.  A power of two: elements within 2^6 of the largest are whole numbers then.
+__device__ __forceinline__ void query_scale(uint32_t bits, float& up, float& down) {
+    const int e = max((int)((bits + 0x10000u) >> 23 & 255u), 22);
+    up = __int_as_float((268 - e) << 23);
+    down = __int_as_float((e - 14) << 23);
 }
 // 1.5 * 2^23: adding it to a small float leaves the nearest integer in the low bits; integer sums that start at its bits are floats.
 constexpr float kMagic = 12582912.f;
@@ -291,11 +292,11 @@ __global__ void __launch_bounds__(kWarps * 32, GT == 1 ? 4 : 2) kv_attention_ker
         // --- queries: columns g (+ 8) of the B operand; sums and scales of columns 2 t, 2 t + 1
         uint32_t q1[GT][kSteps][2], q2[GT][kSteps][2];
         float qsum[GT][2], qdown[GT][2];
+        int qmid[GT][2];                         // what the middle of a key's range (code 7.5) loses by the query's rounding
 #pragma unroll
         for (int n = 0; n < GT; ++n) {
             const int h = n * 8 + g;
             uint4 w[kSteps];
-            float sum = 0.f;
             uint32_t top = 0;
 #pragma unroll
             for (int j = 0; j < kSteps; ++j) {
@@ -305,32 +306,41 @@ __global__ void __launch_bounds__(kWarps * 32, GT == 1 ? 4 : 2) kv_attention_ker
                                                                 t * (D / 4) + 8 * j));
                 const uint32_t x[4] = {w[j].x, w[j].y, w[j].z, w[j].w};
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    sum += bf16_lo(x[i]) + bf16_hi(x[i]);
-                    top = max(top, max((x[i] << 16) & 0x7fffffffu, x[i] & 0x7fff0000u));
-                }
+                for (int i = 0; i < 4; ++i) top = max(top, max((x[i] << 16) & 0x7fffffffu, x[i] & 0x7fff0000u));
             }
             top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
             top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-            sum += __shfl_xor_sync(0xffffffffu, sum, 1);
-            sum += __shfl_xor_sync(0xffffffffu, sum, 2);
             float up, down;
-            range_scale<15>(top, up, down);
-            up *= copysignf(32512.f / 32768.f, a.scale);     // so that the high byte stays within 127; with the sign of the scale
+            query_scale(top, up, down);
+            up = copysignf(up, a.scale);                     // with the sign of the scale
+            float sum = 0.f;                                 // of the elements, and of their whole numbers
+            uint32_t rounded = 0;
+            auto whole_q = [&](float x) {
+                const uint32_t r = whole(x, up);
+                sum = fmaf(x, up, sum);
+                rounded += r;
+                return r;
+            };
 #pragma unroll
             for (int j = 0; j < kSteps; ++j) {
-                split_bytes(whole(bf16_lo(w[j].x), up), whole(bf16_lo(w[j].y), up), whole(bf16_lo(w[j].z), up), whole(bf16_lo(w[j].w), up),
-                            q1[n][j][0], q2[n][j][0]);
-                split_bytes(whole(bf16_hi(w[j].x), up), whole(bf16_hi(w[j].y), up), whole(bf16_hi(w[j].z), up), whole(bf16_hi(w[j].w), up),
-                            q1[n][j][1], q2[n][j][1]);
+                split_bytes(whole_q(bf16_lo(w[j].x)), whole_q(bf16_lo(w[j].y)), whole_q(bf16_lo(w[j].z)), whole_q(bf16_lo(w[j].w)), q1[n][j][0], q2[n][j][0]);
+                split_bytes(whole_q(bf16_hi(w[j].x)), whole_q(bf16_hi(w[j].y)), whole_q(bf16_hi(w[j].z)), whole_q(bf16_hi(w[j].w)), q1[n][j][1], q2[n][j][1]);
             }
+            rounded -= (D / 4) * (uint32_t)kMagicBits;
+#pragma unroll
+            for (int x = 1; x < 4; x <<= 1) {
+                sum += __shfl_xor_sync(0xffffffffu, sum, x);
+                rounded += __shfl_xor_sync(0xffffffffu, rounded, x);
+            }
+            const int middle = __float2int_rn(7.5f * (sum - (float)(int)rounded));
             // scores are held in units of 1 / qdown: |scale| log2(e) / up; not zero, so that minus infinity stays what it is
-            sum *= up;
-            down = fmaxf(down * (32768.f / 32512.f * to_log2), 1e-30f);
+            down = fmaxf(down * to_log2, 1e-30f);
             qsum[n][0] = __shfl_sync(0xffffffffu, sum, 8 * t);
             qsum[n][1] = __shfl_sync(0xffffffffu, sum, 8 * t + 4);
             qdown[n][0] = __shfl_sync(0xffffffffu, down, 8 * t);
             qdown[n][1] = __shfl_sync(0xffffffffu, down, 8 * t + 4);
+            qmid[n][0] = __shfl_sync(0xffffffffu, middle, 8 * t);
+            qmid[n][1] = __shfl_sync(0xffffffffu, middle, 8 * t + 4);
         }
 
         float2 o[GT][2 * kMt];                   // channels g C + i, columns 2 t and 2 t + 1
@@ -370,7 +380,8 @@ __global__ void __launch_bounds__(kWarps * 32, GT == 1 ? 4 : 2) kv_attention_ker
                     for (int n = 0; n < GT; ++n) {
                         if (j == 0) {
                             mma_u8s8(d1[n], a0, a1, a2, a3, q1[n][j], zero);
-                            mma_u8s8(d2[n], a0, a1, a2, a3, q2[n][j], zero);
+                            const int mid[4] = {qmid[n][0], qmid[n][1], qmid[n][0], qmid[n][1]};
+                            mma_u8s8(d2[n], a0, a1, a2, a3, q2[n][j], mid);
                         } else {
                             mma_u8s8(d1[n], a0, a1, a2, a3, q1[n][j], d1[n]);
                             mma_u8s8(d2[n], a0, a1, a2, a3, q2[n][j], d2[n]);

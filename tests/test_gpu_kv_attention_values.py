@@ -104,3 +104,25 @@ def test_appended_rows_of_mixed_size(dim, page):
     q = torch.randn((1, heads * group, dim), generator=g, device="cuda").to(torch.bfloat16)
     q[0, ::2] = q[0, ::2].abs()                                  # these give the constant row most of the weight
     check(cache, q, order.tolist(), n, 2 * dim ** -0.5)
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("group", [1, 4, 16])
+@pytest.mark.parametrize("top", [16.0, 64.0, 128.0])
+def test_a_query_with_one_large_element(dim, group, top):
+    """The other elements are alike, so what their rounding takes off adds up over the channels.  The large one meets keys of
+    zero.  Half of the keys have codes of ordinary size, the other half hardly any; values tell the two apart."""
+    init()
+    g = torch.Generator(device="cuda").manual_seed(group)
+    n = 64
+    cache = random_cache(2, 32, 1, dim, g)
+    kc, kp, vc, vp = cache.tensors
+    kp[..., 0], kp[..., 1] = 0.25, -1.75
+    kp[:, :, ::2] = 0.0
+    kc[..., 0] = (kc[..., 0] & 0xf0) | 7                         # channel 0: 7 * 0.25 - 1.75 = 0
+    vp[..., 0], vp[..., 1] = 0.0, 1.0
+    vp[:, :, ::2, 1] = -1.0
+    q = torch.empty((1, group, dim), dtype=torch.bfloat16, device="cuda")
+    q[:] = torch.linspace(0.25, 0.75, group, device="cuda")[None, :, None] + 0.0068
+    q[:, :, 0] = top
+    check(cache, q, [0, 1], n, dim ** -0.5)
