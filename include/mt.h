@@ -306,10 +306,13 @@ mt_status mt_bucket_noalloc(const int32_t* model_ids, int32_t n, int32_t n_model
  * They need mt_init (else MT_ERR_NOT_INIT) but no registered model: every array is the caller's.  Unless marked "host",
  * pointers are device memory of the context's device.  Each call only enqueues kernels on `stream` and returns; arrays
  * must stay valid, and unchanged where they are inputs, until the stream has passed the call.  mt_kv_attention uses
- * scratch that the library keeps PER STREAM, so calls on different streams may overlap; the first call on a stream, and
- * one that needs more than any before, allocates it (that call may synchronise; make it before a stream capture).  At
- * most 64 streams may use it (then MT_ERR_OOM).  Scratch goes away with mt_shutdown.  All of them may be captured into
- * CUDA graphs; replays of graphs with mt_kv_attention that were captured on ONE stream must not overlap.
+ * scratch that the library keeps PER STREAM (by the stream's id, so the per-thread default stream counts once per thread):
+ * calls on different streams may overlap.  The first call on a stream, and one that needs more than any before, allocates
+ * and may synchronise the stream.  At most 64 streams have scratch at a time; a call on another one waits for the device and
+ * takes over what was used longest ago.  All of them may be captured into CUDA graphs, with no call before it.  Scratch of a
+ * captured call belongs to its graph: graphs may be replayed on any stream, beside each other and beside calls (two
+ * instances of one graph must not overlap); it is used again for other graphs when the graph and its instances are gone.
+ * All scratch goes away with mt_shutdown, after which a graph with mt_kv_attention must not be replayed.
  *
  * Refusals: MT_ERR_INVALID_ARG null pointer, negative size, unknown type, misaligned pointer; MT_ERR_UNSUPPORTED a
  * size or stride outside what the kernels take; nothing is enqueued then.  A count of zero is a no-op.  What only the

@@ -2,7 +2,9 @@
 // computes is in the kernels of the other files.
 #include <cuda_runtime.h>
 
+#include <atomic>
 #include <climits>
+#include <new>
 
 #include "../../include/mt.h"
 #include "lm_host.h"
@@ -13,18 +15,42 @@ namespace {
 using namespace mt;
 
 // Scratch belongs to a stream: calls on one stream are in order, so one block serves all of them, and calls on different
-// streams never share one.  A block that has become too small is kept until shutdown (a captured graph may still name it);
-// sizes at least double, so that costs at most what is in use.
+// streams never share one.  A stream is known by its id, not by its handle: the handle of the per-thread default stream stands
+// for one stream per thread, and a destroyed stream's handle may come back while its last call still runs.
 struct Scratch {
-    cudaStream_t stream;
+    unsigned long long stream;
+    uint64_t used;              // call that used it last
     uint8_t* block;
     size_t bytes;
 };
-constexpr int kMaxStreams = 64, kMaxRetired = 512;
+constexpr int kMaxStreams = 64;
 Scratch g_scratch[kMaxStreams];
 int g_n_scratch = 0;
-uint8_t* g_retired[kMaxRetired];
-int g_n_retired = 0;
+uint64_t g_scratch_calls = 0;
+
+// A captured call's scratch belongs to the graph, which may be replayed on any stream: one block per stream of a capture, given
+// back when the graph and its instances are gone (a user object of the graph says so, on a thread of CUDA's).
+struct GraphBlock {
+    std::atomic<int> owners;    // this list, and a graph
+    unsigned long long capture;
+    const void* stream;
+    uint8_t* block;
+    size_t bytes;
+    GraphBlock* next;
+};
+GraphBlock* g_graph_blocks = nullptr;
+
+void give_up(GraphBlock* b) {
+    if (b->owners.fetch_sub(1) == 1) delete b;
+}
+void CUDART_CB graph_is_gone(void* b) { give_up(static_cast<GraphBlock*>(b)); }
+
+// Allocating is no part of any capture, this thread's or another's.
+struct OutsideCaptures {
+    cudaStreamCaptureMode mode = cudaStreamCaptureModeRelaxed;
+    OutsideCaptures() { cudaThreadExchangeStreamCaptureMode(&mode); }
+    ~OutsideCaptures() { cudaThreadExchangeStreamCaptureMode(&mode); }
+};
 
 bool misaligned(const void* p, uintptr_t to = 16) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) != 0; }
 bool bad_stride(int64_t s, int64_t least) { return s < least || (s & 7) != 0 || s >= (int64_t(1) << 36); }
@@ -54,35 +80,108 @@ mt_status check_quant(int K, int N, int group) {
 
 namespace mt {
 
-mt_status op_scratch(cudaStream_t s, size_t bytes, uint8_t** out) {
-    Scratch* e = nullptr;
-    for (int i = 0; i < g_n_scratch && !e; ++i)
-        if (g_scratch[i].stream == s) e = &g_scratch[i];
-    if (e && e->bytes >= bytes) { *out = e->block; return MT_OK; }
-    if (!e && g_n_scratch == kMaxStreams) return MT_ERR_OOM;
-    if (e && g_n_retired == kMaxRetired) return MT_ERR_OOM;
-    size_t want = e ? 2 * e->bytes : (16u << 20);
-    if (want < bytes) want = bytes;
+static mt_status allocate(size_t bytes, size_t least, uint8_t** out, size_t* got) {
+    OutsideCaptures mode;
     void* p = nullptr;
-    cudaError_t err = cudaMalloc(&p, want);
-    if (err == cudaErrorMemoryAllocation && want > bytes) {
+    cudaError_t err = cudaMalloc(&p, bytes);
+    if (err == cudaErrorMemoryAllocation && bytes > least) {
         cudaGetLastError();
-        want = bytes;
-        err = cudaMalloc(&p, want);
+        err = cudaMalloc(&p, bytes = least);
     }
     if (err != cudaSuccess) { cudaGetLastError(); return to_status(err); }
-    if (e) g_retired[g_n_retired++] = e->block;
-    else { e = &g_scratch[g_n_scratch++]; e->stream = s; }
-    e->block = static_cast<uint8_t*>(p);
-    e->bytes = want;
+    *out = static_cast<uint8_t*>(p);
+    *got = bytes;
+    return MT_OK;
+}
+
+static mt_status graph_scratch(unsigned long long capture, const void* stream, cudaGraph_t graph, size_t bytes, uint8_t** out) {
+    GraphBlock* b = nullptr;
+    for (GraphBlock* x = g_graph_blocks; x; x = x->next) {
+        const bool taken = x->owners.load() > 1;
+        if (x->bytes < bytes) continue;
+        if (taken && x->capture == capture && x->stream == stream) { *out = x->block; return MT_OK; }
+        if (!taken && (!b || x->bytes < b->bytes)) b = x;
+    }
+    if (!b) {
+        uint8_t* block;
+        size_t got;
+        const mt_status st = allocate((bytes + 0xfffff) & ~size_t(0xfffff), bytes, &block, &got);
+        if (st != MT_OK) return st;
+        b = new (std::nothrow) GraphBlock{{1}, 0, nullptr, block, got, g_graph_blocks};
+        if (!b) { OutsideCaptures mode; cudaFree(block); return MT_ERR_OOM; }
+        g_graph_blocks = b;
+    }
+    cudaUserObject_t owner;
+    cudaError_t e = cudaUserObjectCreate(&owner, b, graph_is_gone, 1, cudaUserObjectNoDestructorSync);
+    if (e != cudaSuccess) { cudaGetLastError(); return to_status(e); }
+    b->capture = capture;
+    b->stream = stream;
+    b->owners.fetch_add(1);
+    e = cudaGraphRetainUserObject(graph, owner, 1, cudaGraphUserObjectMove);
+    if (e != cudaSuccess) { cudaGetLastError(); cudaUserObjectRelease(owner, 1); return to_status(e); }
+    *out = b->block;
+    return MT_OK;
+}
+
+mt_status op_scratch(cudaStream_t s, size_t bytes, uint8_t** out) {
+    cudaStreamCaptureStatus capturing = cudaStreamCaptureStatusNone;
+    unsigned long long capture = 0, id = ~0ull;
+    cudaGraph_t graph = nullptr;
+    cudaError_t err = cudaSuccess;
+    const bool legacy = s == nullptr || s == cudaStreamLegacy;      // one stream, never captured: asking would cost a step 0.4 us
+    if (!legacy) err = cudaStreamGetCaptureInfo(s, &capturing, &capture, &graph);
+    if (err == cudaSuccess && capturing != cudaStreamCaptureStatusNone) {       // (the id of a capturing stream must not be asked for)
+        if (capturing != cudaStreamCaptureStatusActive) return MT_ERR_CUDA;
+        static thread_local char this_thread;
+        return graph_scratch(capture, s == cudaStreamPerThread ? static_cast<const void*>(&this_thread) : s, graph, bytes, out);
+    }
+    if (err == cudaSuccess && !legacy) err = cudaStreamGetId(s, &id);
+    if (err != cudaSuccess) { cudaGetLastError(); return to_status(err); }
+
+    Scratch *e = nullptr, *oldest = g_scratch;
+    for (int i = 0; i < g_n_scratch && !e; ++i) {
+        if (g_scratch[i].stream == id) e = &g_scratch[i];
+        if (g_scratch[i].used < oldest->used) oldest = &g_scratch[i];
+    }
+    if (!e && g_n_scratch == kMaxStreams) {       // another stream's block, once nothing can be using it
+        OutsideCaptures mode;
+        err = cudaDeviceSynchronize();
+        if (err != cudaSuccess) { cudaGetLastError(); return to_status(err); }
+        e = oldest;
+        e->stream = id;
+    }
+    if (!e || e->bytes < bytes) {
+        size_t want = e ? 2 * e->bytes : (16u << 20), got;
+        if (want < bytes) want = bytes;
+        uint8_t* block;
+        const mt_status st = allocate(want, bytes, &block, &got);
+        if (st != MT_OK) return st;
+        if (e) {
+            OutsideCaptures mode;
+            cudaStreamSynchronize(s);             // calls in flight read the block that goes
+            cudaFree(e->block);
+        } else {
+            e = &g_scratch[g_n_scratch++];
+            e->stream = id;
+        }
+        e->block = block;
+        e->bytes = got;
+    }
+    e->used = ++g_scratch_calls;
     *out = e->block;
     return MT_OK;
 }
 
 void op_free_scratch() {
     for (int i = 0; i < g_n_scratch; ++i) cudaFree(g_scratch[i].block);
-    for (int i = 0; i < g_n_retired; ++i) cudaFree(g_retired[i]);
-    g_n_scratch = g_n_retired = 0;
+    g_n_scratch = 0;
+    for (GraphBlock* b = g_graph_blocks; b;) {
+        GraphBlock* const next = b->next;
+        cudaFree(b->block);
+        give_up(b);
+        b = next;
+    }
+    g_graph_blocks = nullptr;
 }
 
 cudaError_t configure_operators() {

@@ -95,7 +95,8 @@ struct LogprobArgs {
 cudaError_t configure_token_logprobs();
 mt_status launch_token_logprobs(const LogprobArgs& a, const OpContext& c, cudaStream_t s);
 
-// Scratch of at least `bytes` (256-byte aligned, contents left over from earlier calls) on stream `s`, kept until mt_shutdown.  (Mutex held.)
+// Scratch of at least `bytes` (256-byte aligned, contents left over from earlier calls) for work on stream `s`: the stream's, or the
+// graph's that `s` is captured into.  (Mutex held.)
 mt_status op_scratch(cudaStream_t s, size_t bytes, uint8_t** out);
 
 }  // namespace mt
