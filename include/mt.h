@@ -194,8 +194,9 @@ mt_status mt_cache_sim_destroy(void* sim);
 
 /* Synchronise `stream`, then report and clear the sticky device-side status of the calls so far:
  * *status_out is MT_OK, MT_ERR_BAD_MODEL_ID or MT_ERR_NOT_RESIDENT (with the smallest offending arrival index of the
- * first such batch in *bad_request_index_out, else -1), MT_ERR_TIMEOUT, or MT_ERR_INVALID_ARG from an operator of the
- * language-model tenants (below) with the index of the sequence, token or row.  Either out pointer may be NULL. */
+ * first such batch in *bad_request_index_out, else -1), MT_ERR_TIMEOUT, or, where no batch had an error, that of the first
+ * call of an operator of the language-model tenants (below) that had one, MT_ERR_INVALID_ARG or MT_ERR_BAD_MODEL_ID with the
+ * smallest index of that call's sequences, tokens or rows concerned.  Either out pointer may be NULL. */
 mt_status mt_get_async_status(void* stream, int32_t* status_out, int32_t* bad_request_index_out);
 
 const char* mt_status_string(mt_status s);
@@ -318,7 +319,7 @@ mt_status mt_bucket_noalloc(const int32_t* model_ids, int32_t n, int32_t n_model
  * size or stride outside what the kernels take; nothing is enqueued then.  A count of zero is a no-op.  What only the
  * device can see (an id, page, slot, length or offset out of range) never faults: the rows concerned are NaN (or left
  * out, where rows are written to a cache), and the sticky status of mt_get_async_status is MT_ERR_BAD_MODEL_ID (ids) or
- * MT_ERR_INVALID_ARG, with the smallest index concerned.  mt_prompt_attention, whose kernel waits on barriers, can also
+ * MT_ERR_INVALID_ARG, with the smallest index concerned of the first such call.  mt_prompt_attention, whose kernel waits on barriers, can also
  * report MT_ERR_TIMEOUT there (a wait that gave up; its output is then incomplete). */
 typedef enum { MT_BF16 = 0, MT_FP32 = 1 } mt_dtype;
 

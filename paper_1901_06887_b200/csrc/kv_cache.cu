@@ -33,7 +33,7 @@ constexpr int kThreads = 256;
 // tokens, which lie side by side in a projection's output (append and read of 8191 tokens of 8 heads: 29 us together, instructions bound the first, 22 us, and memory the second, 12).
 template <int D, int ITEMS>
 __global__ void __launch_bounds__(kThreads) kv_append_kernel(CachePtrs kc, CachePtrs vc, int64_t n_slots, int page_shift, KvRows k, KvRows v,
-                                                             const int64_t* __restrict__ slots, int n, int token0, int32_t* status) {
+                                                             const int64_t* __restrict__ slots, int n, int token0, OpStatus status) {
     constexpr int L = D / 8, kTokens = kThreads / L;            // lanes per row, rows of a run
     pdl_launch_dependents();
     pdl_wait();
@@ -118,7 +118,7 @@ __global__ void __launch_bounds__(kThreads) kv_append_kernel(CachePtrs kc, Cache
 template <int D, int ITEMS>
 __global__ void __launch_bounds__(kThreads) kv_read_kernel(CachePtrs kc, CachePtrs vc, int64_t n_slots, int page_shift,
                                                            const int64_t* __restrict__ slots, int n, uint16_t* __restrict__ k_out,
-                                                           uint16_t* __restrict__ v_out, int token0, int32_t* status) {
+                                                           uint16_t* __restrict__ v_out, int token0, OpStatus status) {
     constexpr int L = D / 8, kTokens = kThreads / L;
     pdl_launch_dependents();
     pdl_wait();
@@ -175,7 +175,7 @@ int runs_of(int n, int tokens) { return (int)((n + (int64_t)tokens - 1) / tokens
 
 }  // namespace
 
-cudaError_t launch_kv_append(const mt_kv_cache& c, const KvRows& k, const KvRows& v, const int64_t* slots, int n, int32_t* status,
+cudaError_t launch_kv_append(const mt_kv_cache& c, const KvRows& k, const KvRows& v, const int64_t* slots, int n, const OpStatus& status,
                              cudaStream_t s) {
     const CachePtrs kc = {static_cast<uint8_t*>(c.k_codes), static_cast<uint32_t*>(c.k_params)};
     const CachePtrs vc = {static_cast<uint8_t*>(c.v_codes), static_cast<uint32_t*>(c.v_params)};
@@ -193,7 +193,7 @@ cudaError_t launch_kv_append(const mt_kv_cache& c, const KvRows& k, const KvRows
     return e;
 }
 
-cudaError_t launch_kv_read(const mt_kv_cache& c, const int64_t* slots, int n, uint16_t* k_out, uint16_t* v_out, int32_t* status,
+cudaError_t launch_kv_read(const mt_kv_cache& c, const int64_t* slots, int n, uint16_t* k_out, uint16_t* v_out, const OpStatus& status,
                            cudaStream_t s) {
     const CachePtrs kc = {static_cast<uint8_t*>(c.k_codes), static_cast<uint32_t*>(c.k_params)};
     const CachePtrs vc = {static_cast<uint8_t*>(c.v_codes), static_cast<uint32_t*>(c.v_params)};

@@ -15,7 +15,7 @@ struct PromptArgs {
     const uint16_t *q, *k, *v;
     const int32_t* offsets;
     uint16_t* out;
-    int32_t* status;
+    OpStatus status;
 };
 cudaError_t configure_prompt_attention();
 mt_status launch_prompt_attention(const PromptArgs& a, const OpContext& c, cudaStream_t s);
@@ -25,9 +25,9 @@ struct KvRows {                     // rows [n][heads][head_dim] bf16 with strid
     int64_t token_stride, head_stride;
 };
 cudaError_t launch_kv_append(const mt_kv_cache& c, const KvRows& k, const KvRows& v, const int64_t* slots, int n,
-                             int32_t* status, cudaStream_t s);
+                             const OpStatus& status, cudaStream_t s);
 cudaError_t launch_kv_read(const mt_kv_cache& c, const int64_t* slots, int n, uint16_t* k_out, uint16_t* v_out,
-                           int32_t* status, cudaStream_t s);
+                           const OpStatus& status, cudaStream_t s);
 
 struct KvAttentionArgs {
     mt_kv_cache c;
@@ -39,7 +39,7 @@ struct KvAttentionArgs {
     int n_seqs, q_heads;
     float scale;
     uint16_t* out;
-    int32_t* status;
+    OpStatus status;
 };
 cudaError_t configure_kv_attention();
 mt_status launch_kv_attention(const KvAttentionArgs& a, const OpContext& c, cudaStream_t s);
@@ -69,7 +69,7 @@ struct QuantLinearArgs {
     void* y;
     int64_t y_stride;
     int y_fp32;
-    int32_t* status;
+    OpStatus status;
     // filled in by the launcher: bytes of a tenant's codes and of all it has; groups per row; tiles of 16 outputs; floor((2^32 - 1) / d) for d blocks per group, with which the high word of
     // (n + 1) times it is n / d for (n + 1) d < 2^32
     size_t codes_bytes, tenant_bytes;
@@ -90,7 +90,7 @@ struct LogprobArgs {
     float *logprobs, *entropies;
     int32_t* top_ids;
     float* top_logprobs;
-    int32_t* status;
+    OpStatus status;
 };
 cudaError_t configure_token_logprobs();
 mt_status launch_token_logprobs(const LogprobArgs& a, const OpContext& c, cudaStream_t s);

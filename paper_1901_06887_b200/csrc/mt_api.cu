@@ -207,8 +207,11 @@ std::mutex g_mu;
         }                                                             \
     } while (0)
 
+uint32_t g_op_calls = 0;         // calls of language-model operators since the status was last read
+
 mt_status reset_status_word() {
-    const int32_t init[ST_WORDS] = {MT_OK, INT_MAX, 0, 0};
+    const int32_t init[ST_WORDS] = {MT_OK, INT_MAX, 0, 0, -1, -1};
+    g_op_calls = 0;
     CU_OK(cudaMemcpy(g.d_status, init, sizeof init, cudaMemcpyHostToDevice));
     return MT_OK;
 }
@@ -1190,7 +1193,8 @@ mt_status op_begin(std::unique_lock<std::mutex>* lk, OpContext* out) {
     int current = -1;
     if (cudaGetDevice(&current) != cudaSuccess || current != g.device) CU_OK(cudaSetDevice(g.device));
     out->sm_count = g.sm_count;
-    out->status = g.d_status;
+    out->status = {g.d_status, g_op_calls};
+    if (g_op_calls < (1u << 28) - 1) ++g_op_calls;
     out->encode = g.encode;
     return MT_OK;
 }
@@ -1641,8 +1645,13 @@ mt_status mt_get_async_status(void* stream, int32_t* status_out, int32_t* bad_re
     CU_OK(cudaStreamSynchronize(static_cast<cudaStream_t>(stream)));
     int32_t w[ST_WORDS];
     CU_OK(cudaMemcpy(w, g.d_status, sizeof w, cudaMemcpyDeviceToHost));
-    if (status_out) *status_out = w[ST_CODE];
-    if (bad_request_index_out) *bad_request_index_out = (w[ST_BAD_INDEX] == INT_MAX) ? -1 : w[ST_BAD_INDEX];
+    int32_t code = w[ST_CODE], index = w[ST_BAD_INDEX] == INT_MAX ? -1 : w[ST_BAD_INDEX];
+    if (code == MT_OK && (w[ST_OP] != -1 || w[ST_OP + 1] != -1)) {
+        code = w[ST_OP + 1] & 15;
+        index = w[ST_OP];
+    }
+    if (status_out) *status_out = code;
+    if (bad_request_index_out) *bad_request_index_out = index;
     if (w[ST_CODE] == MT_ERR_TIMEOUT && getenv("MT_LOG")) fprintf(stderr, "[mt] device wait gave up at site %d\n", w[ST_WHERE]);
     return reset_status_word();
 }

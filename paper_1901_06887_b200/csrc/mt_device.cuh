@@ -48,8 +48,9 @@ struct __align__(16) WorkItem {
 };
 constexpr int32_t kItemFinal = 1;
 
-// Sticky status word written by kernels: [0] status code, [1] first bad arrival index, [2] where a wait gave up.
-enum { ST_CODE = 0, ST_BAD_INDEX = 1, ST_WHERE = 2, ST_WORDS = 4 };
+// Sticky status word written by kernels: [0] status code, [1] first bad arrival index, [2] where a wait gave up; [4], [5]
+// the first error of a language-model operator as one 64-bit number: call number << 36 | code << 32 | index, all ones if none.
+enum { ST_CODE = 0, ST_BAD_INDEX = 1, ST_WHERE = 2, ST_OP = 4, ST_WORDS = 6 };
 
 // Tile geometry of the tensor-core executors.
 constexpr int BM = 128;          // accumulator rows (TMEM lanes)

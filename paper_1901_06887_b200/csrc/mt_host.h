@@ -35,9 +35,13 @@ typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t,
 
 // What the operators of language-model tenants (lm_api.cu) take from the context.  op_begin locks the library's mutex into
 // *lk, makes the context's device current and fills *out, or says MT_ERR_NOT_INIT.
+struct OpStatus {
+    int32_t* word;
+    uint32_t call;           // number of the call since the status was last read, 28 bits
+};
 struct OpContext {
     int sm_count;
-    int32_t* status;
+    OpStatus status;
     EncodeTiledFn encode;
 };
 mt_status op_begin(std::unique_lock<std::mutex>* lk, OpContext* out);

@@ -56,7 +56,7 @@ struct PromptParams {
     float c;                                  // |scale| log2(e)
     int negate;                               // scale < 0
     uint16_t* out;
-    int32_t* status;
+    OpStatus status;
 };
 
 // D (+)= A B with A in tensor memory.
@@ -222,7 +222,7 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
             bool ok = true;
             Item it;
             for (int round = 0; ok && get_item(s, p, round, it); ++round) {
-                if (round > 0) ok = mbar_wait(bar(s.q_empty), (round - 1) & 1, abort_flag, p.status, 200);
+                if (round > 0) ok = mbar_wait(bar(s.q_empty), (round - 1) & 1, abort_flag, p.status.word, 200);
                 if (!ok) break;
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
@@ -235,7 +235,7 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
                 const int nb = max(it.nb[0], it.nb[1]);
                 for (int x = 0; ok && x < 2 * nb; ++x, ++fill) {
                     const int slot = fill % kSlots, use = fill / kSlots;
-                    if (use > 0) ok = mbar_wait(bar(s.kv_empty[slot]), (use - 1) & 1, abort_flag, p.status, 201);
+                    if (use > 0) ok = mbar_wait(bar(s.kv_empty[slot]), (use - 1) & 1, abort_flag, p.status.word, 201);
                     if (!ok) break;
                     // a masked value block goes to the cleaners first: its bytes count on v_raw, and v_clean says when it may be used
                     const bool masked = (x & 1) && ((x >> 1) == it.nb[0] - 1 || (x >> 1) == it.nb[1] - 1);
@@ -270,7 +270,7 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
         uint32_t fill = 0, n_q0 = 0, n_q1 = 0, n_p0 = 0, n_p1 = 0, clean_phase = 0;
         bool ok = true;
         Item it;
-        auto wait = [&](const uint64_t& b, uint32_t parity, int where) { ok = ok && mbar_wait(bar(b), parity & 1, abort_flag, p.status, where); };
+        auto wait = [&](const uint64_t& b, uint32_t parity, int where) { ok = ok && mbar_wait(bar(b), parity & 1, abort_flag, p.status.word, where); };
         auto qk = [&](int i, uint32_t slot) {
             if (leader) {
                 const uint32_t d = tm + 128 * i, a = q_lo + i * kOpLo, b = k_lo + slot * kOpLo;
@@ -359,13 +359,13 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
         for (int round = 0; ok && get_item(s, p, round, it); ++round) {
             const int nb = max(it.nb[0], it.nb[1]), buf = round & 1;
             if (round >= 2) {                    // the notes of two tiles ago have been read
-                ok = mbar_wait(bar(s.epi_done[buf]), ((round >> 1) - 1) & 1, abort_flag, p.status, 220);
+                ok = mbar_wait(bar(s.epi_done[buf]), ((round >> 1) - 1) & 1, abort_flag, p.status.word, 220);
                 if (!ok) break;
             }
             for (int j = it.nb[0] - 1; ok && j < nb; ++j) {
                 if (!(j == it.nb[0] - 1 || j == it.nb[1] - 1)) continue;
                 const int slot = (fill + 2 * j + 1) % kSlots;
-                ok = mbar_wait(bar(s.v_raw[slot]), (raw_phase >> slot) & 1, abort_flag, p.status, 221);
+                ok = mbar_wait(bar(s.v_raw[slot]), (raw_phase >> slot) & 1, abort_flag, p.status.word, 221);
                 if (!ok) break;
                 raw_phase ^= 1u << slot;
                 uint8_t* const v = smem + (2 + slot) * kOp;
@@ -420,7 +420,7 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
             const int tok = it.t0 + i * (tokens / 2) + (r >> p.pack_shift);
             float m = 0.f, l = 0.f;
             for (int j = 0; j < nb; ++j) {
-                ok = mbar_wait(bar(s.s_full[i]), n_s++ & 1, abort_flag, p.status, 230);
+                ok = mbar_wait(bar(s.s_full[i]), n_s++ & 1, abort_flag, p.status.word, 230);
                 if (!ok) break;
                 tc_fence_after();
                 uint32_t x[4][32];
@@ -452,7 +452,7 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
                     const float nm = move && mx > -INFINITY ? mx : m, f = m == nm || l == 0.f ? 1.f : ex2((m - nm) * p.c);
                     m = nm;
                     l *= f;
-                    ok = mbar_wait(bar(s.o_ready[i]), (n_o - 1) & 1, abort_flag, p.status, 231);
+                    ok = mbar_wait(bar(s.o_ready[i]), (n_o - 1) & 1, abort_flag, p.status.word, 231);
                     if (!ok) break;
                     tc_fence_after();
 #pragma unroll 1
@@ -503,7 +503,7 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
             }
             if (!ok) break;
             if (nb > 0) {
-                ok = mbar_wait(bar(s.o_ready[i]), (n_o - 1) & 1, abort_flag, p.status, 232);
+                ok = mbar_wait(bar(s.o_ready[i]), (n_o - 1) & 1, abort_flag, p.status.word, 232);
                 if (!ok) break;
                 tc_fence_after();
                 const float inv = 1.f / l;
