@@ -319,8 +319,9 @@ mt_status mt_bucket_noalloc(const int32_t* model_ids, int32_t n, int32_t n_model
  * size or stride outside what the kernels take; nothing is enqueued then.  A count of zero is a no-op.  What only the
  * device can see (an id, page, slot, length or offset out of range) never faults: the rows concerned are NaN (or left
  * out, where rows are written to a cache), and the sticky status of mt_get_async_status is MT_ERR_BAD_MODEL_ID (ids) or
- * MT_ERR_INVALID_ARG, with the smallest index concerned of the first such call.  mt_prompt_attention, whose kernel waits on barriers, can also
- * report MT_ERR_TIMEOUT there (a wait that gave up; its output is then incomplete). */
+ * MT_ERR_INVALID_ARG, with the smallest index concerned of the first such call (mt_token_logprobs raises nothing).
+ * mt_prompt_attention, whose kernel waits on barriers, can also report MT_ERR_TIMEOUT there (a wait that gave up; its
+ * output is then incomplete). */
 typedef enum { MT_BF16 = 0, MT_FP32 = 1 } mt_dtype;
 
 /* Attention over whole prompts, causal, packed one behind the other: sequence s is rows offsets[s] .. offsets[s+1]-1.
@@ -406,7 +407,8 @@ mt_status mt_quant_linear(const mt_quant_bank* bank_host, const void* x, int64_t
                           void* y, int64_t y_stride, int32_t y_dtype, void* stream);
 
 /* For n rows of `vocab` logits (bf16 or fp32 by dtype, row_stride elements apart, any alignment of whole elements):
- *   logprobs[i]        log of the softmax at tokens[i]; NaN if that is outside [0, vocab)
+ *   logprobs[i]        log of the softmax at tokens[i]; NaN if that is outside [0, vocab), which is no error: a row without a
+ *                      given token (the last one of a prompt) has -1 there, and nothing is raised in the sticky status
  *   entropies[i]       - sum p log p, in nats
  *   top_ids[i][0..top-1], top_logprobs[i][..]   the likeliest tokens, best first, equal logits by the lower index
  * A logit of minus infinity has probability zero: it adds nothing and is no alternative; where fewer than `top` remain, the

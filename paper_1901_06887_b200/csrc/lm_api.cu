@@ -339,7 +339,7 @@ mt_status mt_token_logprobs(const void* logits, int32_t dtype, int64_t row_strid
         return MT_ERR_INVALID_ARG;
     LogprobArgs a;
     a.logits = logits; a.fp32 = dtype == MT_FP32; a.row_stride = row_stride; a.n = n; a.vocab = vocab; a.tokens = tokens; a.top = top;
-    a.logprobs = logprobs; a.entropies = entropies; a.top_ids = top_ids; a.top_logprobs = top_logprobs; a.status = c.status;
+    a.logprobs = logprobs; a.entropies = entropies; a.top_ids = top_ids; a.top_logprobs = top_logprobs;
     return launch_token_logprobs(a, c, static_cast<cudaStream_t>(stream));
 }
 

@@ -90,7 +90,6 @@ struct LogprobArgs {
     float *logprobs, *entropies;
     int32_t* top_ids;
     float* top_logprobs;
-    OpStatus status;
 };
 cudaError_t configure_token_logprobs();
 mt_status launch_token_logprobs(const LogprobArgs& a, const OpContext& c, cudaStream_t s);
