@@ -389,7 +389,8 @@ mt_status mt_kv_attention(const mt_kv_cache* cache_host, const void* q, int64_t 
  * [out_features][in_features / 2] (even inputs in the low nibble), one bf16 scale per `group` inputs of a row
  * ([out_features][in_features / group]).  mt_quant_pack lays codes [tenants][..] and scales [tenants][..] out in the kernel's
  * order, once; `packed` takes tenants * mt_quant_packed_bytes bytes, 16-byte aligned, and holds all that mt_quant_linear reads.
- * Limits: in_features a multiple of 64 and of group, below 2^22; group 32, 64 or a larger multiple of 64. */
+ * Limits: in_features a multiple of 64 and of group, below 2^22; group 32, 64 or a larger multiple of 64; out_features below
+ * 2^31 - 2^20. */
 typedef struct {
     int32_t tenants, in_features, out_features, group;
     const void* packed;

@@ -72,6 +72,7 @@ mt_status check_cache(const mt_kv_cache* c) {
 
 mt_status check_quant(int K, int N, int group) {
     if (K <= 0 || N <= 0 || group <= 0) return MT_ERR_INVALID_ARG;
+    if (N > INT_MAX - (1 << 20)) return MT_ERR_UNSUPPORTED;         // the kernels round N up, and step past it
     if (K >= (1 << 22) || K % 64 || K % group || !(group == 32 || group % 64 == 0)) return MT_ERR_UNSUPPORTED;
     return MT_OK;
 }

@@ -1,0 +1,28 @@
+"""Refusals of the language-model operators by their numbers alone: scales that are no numbers, layers too wide to index (host
+code only, no GPU)."""
+import ctypes
+
+import pytest
+
+from lm_util import code_of
+from paper_1901_06887_b200 import binding as mt, build
+
+
+@pytest.fixture(scope="module")
+def lib():
+    build.build_lib()
+    mt.mt_shutdown()
+    return mt.lib()
+
+
+@pytest.mark.parametrize("n", [(1 << 31) - (1 << 20), (1 << 31) - 16, (1 << 31) - 1])
+def test_layers_too_wide(lib, n):
+    assert code_of(mt.mt_quant_packed_bytes, 64, n, 64) == 4
+    assert lib.mt_quant_pack(None, None, 1, 64, n, 64, None, None) == 4
+    bank = ctypes.byref(mt.QuantBankDesc(1, 64, n, 64, 16, None))
+    assert lib.mt_quant_linear(bank, None, 64, None, 1, None, n, 0, None) == 4
+
+
+def test_the_widest_layer(lib):
+    n = (1 << 31) - (1 << 20) - 1
+    assert mt.mt_quant_packed_bytes(128, n, 64) == (n + 1) * 64 + (n + 1) * 4
