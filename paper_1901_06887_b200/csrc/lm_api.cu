@@ -4,6 +4,7 @@
 
 #include <atomic>
 #include <climits>
+#include <cmath>
 #include <new>
 
 #include "../../include/mt.h"
@@ -199,7 +200,7 @@ extern "C" {
 
 mt_status mt_prompt_attention(const mt_prompt_desc* d, const void* q, const void* k, const void* v, const int32_t* offsets,
                               void* out, void* stream) {
-    if (!d || d->n_tokens < 0 || d->n_seqs < 0 || d->q_heads <= 0 || d->kv_heads <= 0) return MT_ERR_INVALID_ARG;
+    if (!d || d->n_tokens < 0 || d->n_seqs < 0 || d->q_heads <= 0 || d->kv_heads <= 0 || !std::isfinite(d->scale)) return MT_ERR_INVALID_ARG;
     if (!(d->head_dim == 64 || d->head_dim == 128) || d->q_heads % d->kv_heads || d->q_heads > 65535) return MT_ERR_UNSUPPORTED;
     if (d->n_tokens > (1 << 30)) return MT_ERR_UNSUPPORTED;
     const int64_t hd = d->head_dim;
@@ -255,7 +256,7 @@ mt_status mt_kv_attention(const mt_kv_cache* cache, const void* q, int64_t q_seq
                           float scale, void* out, void* stream) {
     mt_status st = check_cache(cache);
     if (st != MT_OK) return st;
-    if (n_seqs < 0 || q_heads <= 0 || table_width < 0) return MT_ERR_INVALID_ARG;
+    if (n_seqs < 0 || q_heads <= 0 || table_width < 0 || !std::isfinite(scale)) return MT_ERR_INVALID_ARG;
     if (q_heads % cache->kv_heads || q_heads / cache->kv_heads > 16) return MT_ERR_UNSUPPORTED;
     if ((int64_t)n_seqs * cache->kv_heads >= (1 << 20) || (int64_t)table_width * cache->page_tokens > INT_MAX - 64) return MT_ERR_UNSUPPORTED;
     if (bad_stride(q_seq_stride, 0) || bad_stride(q_head_stride, 0)) return MT_ERR_UNSUPPORTED;

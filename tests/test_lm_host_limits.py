@@ -15,6 +15,14 @@ def lib():
     return mt.lib()
 
 
+@pytest.mark.parametrize("scale", [float("nan"), float("inf"), float("-inf")])
+def test_scales_that_are_no_numbers(lib, scale):
+    desc = mt._prompt_desc(4, 1, 2, 1, 64, scale, 128, 64, 64, 64, 64, 64)
+    assert lib.mt_prompt_attention(desc, None, None, None, None, None, None) == 1
+    cache = ctypes.byref(mt.KvCacheDesc(2, 16, 2, 64, 16, 16, 16, 16))
+    assert lib.mt_kv_attention(cache, None, 256, 64, None, 2, None, 1, 4, scale, None, None) == 1
+
+
 @pytest.mark.parametrize("n", [(1 << 31) - (1 << 20), (1 << 31) - 16, (1 << 31) - 1])
 def test_layers_too_wide(lib, n):
     assert code_of(mt.mt_quant_packed_bytes, 64, n, 64) == 4
