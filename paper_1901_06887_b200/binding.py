@@ -157,12 +157,20 @@ def _stream_handle(stream) -> Optional[int]:
     return stream.cuda_stream
 
 
+_device = None          # the context's device
+
+
 def mt_init(device: int = 0, max_models: int = 1024, max_batch: int = 0) -> None:
+    global _device
     _check(lib().mt_init(device, max_models, max_batch), "mt_init")
+    if _device is None:      # (a context that is there keeps its device)
+        _device = int(device)
 
 
 def mt_shutdown() -> None:
+    global _device
     _check(lib().mt_shutdown(), "mt_shutdown")
+    _device = None
 
 
 def mt_register_model(layers: Sequence) -> int:
@@ -365,21 +373,30 @@ def _types():
 
 
 def _refuse(where: str) -> None:
-    raise MtError(1, where)
+    raise MtError(1, where) from None
+
+
+def _place(t) -> int:
+    """Where a call's tensors have to be: on the context's device (without a context, together; the library then says so)."""
+    return t.get_device() if _device is None else _device
 
 
 def mt_prompt_attention(q, k, v, offsets, out, scale: Optional[float] = None, stream=None) -> None:
     """Causal attention over packed prompts: q bf16 [n, q_heads, dim], k and v [n, kv_heads, dim] (any token and head strides),
     offsets int32 [sequences + 1], out bf16 [n, q_heads, dim] contiguous.  scale: 1 / sqrt(dim) if None."""
     T = _types()
-    bf16 = T.bf16
-    n, hq, d = shape = q.shape
-    nk, hk, dk = kshape = k.shape
-    q0, q1, q2 = q.stride()
-    k0, k1, k2 = k.stride()
-    v0, v1, v2 = v.stride()
-    if not (q.dtype is bf16 and k.dtype is bf16 and v.dtype is bf16 and out.dtype is bf16 and offsets.dtype is T.i32 and q.is_cuda and
-            k.is_cuda and v.is_cuda and out.is_cuda and offsets.is_cuda and nk == n and dk == d and v.shape == kshape and
+    bf16, at = T.bf16, _place(q)
+    try:
+        n, hq, d = shape = q.shape
+        nk, hk, dk = kshape = k.shape
+        q0, q1, q2 = q.stride()
+        k0, k1, k2 = k.stride()
+        v0, v1, v2 = v.stride()
+    except ValueError:
+        _refuse("mt_prompt_attention")
+    if not (q.dtype is bf16 and k.dtype is bf16 and v.dtype is bf16 and out.dtype is bf16 and offsets.dtype is T.i32 and
+            q.get_device() == k.get_device() == v.get_device() == out.get_device() == offsets.get_device() == at and
+            q.is_cuda and nk == n and dk == d and v.shape == kshape and
             out.shape == shape and out.is_contiguous() and offsets.dim() == 1 and offsets.is_contiguous() and offsets.numel() > 0 and
             (n == 0 or q2 == k2 == v2 == 1)):
         _refuse("mt_prompt_attention")
@@ -395,10 +412,13 @@ class KvCache:
     [pages, kv_heads, page_tokens, 2] (scale, bias), contiguous.  Keeps them alive; allocates nothing."""
 
     def __init__(self, k_codes, k_params, v_codes, v_params):
-        T = _types()
-        pages, heads, page, half = k_codes.shape
+        T, at = _types(), _place(k_codes)
+        try:
+            pages, heads, page, half = k_codes.shape
+        except ValueError:
+            _refuse("KvCache")
         for c, p in ((k_codes, k_params), (v_codes, v_params)):
-            if not (c.dtype is T.u8 and p.dtype is T.bf16 and c.is_cuda and p.is_cuda and c.is_contiguous() and p.is_contiguous() and
+            if not (c.dtype is T.u8 and p.dtype is T.bf16 and c.is_cuda and c.get_device() == p.get_device() == at and c.is_contiguous() and p.is_contiguous() and
                     tuple(c.shape) == (pages, heads, page, half) and tuple(p.shape) == (pages, heads, page, 2)):
                 _refuse("KvCache")
         self.tensors = (k_codes, k_params, v_codes, v_params)
@@ -419,11 +439,15 @@ class KvCache:
 
 def mt_kv_append(cache: KvCache, k, v, slots, stream=None) -> None:
     """Round k and v, bf16 [n, kv_heads, dim] (any token and head strides), to 4 bits and write token i to slot slots[i] (int64 [n])."""
-    T = _types()
-    n, h, d = shape = k.shape
-    k0, k1, k2 = k.stride()
-    v0, v1, v2 = v.stride()
-    if not (k.dtype is T.bf16 and v.dtype is T.bf16 and slots.dtype is T.i64 and k.is_cuda and v.is_cuda and slots.is_cuda and
+    T, at = _types(), _place(k)
+    try:
+        n, h, d = shape = k.shape
+        k0, k1, k2 = k.stride()
+        v0, v1, v2 = v.stride()
+    except ValueError:
+        _refuse("mt_kv_append")
+    if not (k.dtype is T.bf16 and v.dtype is T.bf16 and slots.dtype is T.i64 and k.is_cuda and
+            k.get_device() == v.get_device() == slots.get_device() == at and
             v.shape == shape and h == cache.heads and d == cache.dim and slots.dim() == 1 and slots.numel() == n and slots.is_contiguous() and
             (n == 0 or k2 == v2 == 1)):
         _refuse("mt_kv_append")
@@ -434,10 +458,13 @@ def mt_kv_append(cache: KvCache, k, v, slots, stream=None) -> None:
 
 def mt_kv_read(cache: KvCache, slots, k_out, v_out, stream=None) -> None:
     """The cached values of slots (int64 [n]) as bf16 [n, kv_heads, dim]."""
-    T = _types()
-    n, h, d = shape = k_out.shape
+    T, at = _types(), _place(k_out)
+    try:
+        n, h, d = shape = k_out.shape
+    except ValueError:
+        _refuse("mt_kv_read")
     if not (k_out.dtype is T.bf16 and v_out.dtype is T.bf16 and slots.dtype is T.i64 and slots.dim() == 1 and slots.numel() == n and
-            k_out.is_cuda and v_out.is_cuda and slots.is_cuda and v_out.shape == shape and h == cache.heads and d == cache.dim and
+            k_out.is_cuda and k_out.get_device() == v_out.get_device() == slots.get_device() == at and v_out.shape == shape and h == cache.heads and d == cache.dim and
             k_out.is_contiguous() and v_out.is_contiguous() and slots.is_contiguous()):
         _refuse("mt_kv_read")
     code = (_lib or lib()).mt_kv_read(cache.ref, slots.data_ptr(), n, k_out.data_ptr(), v_out.data_ptr(), _stream_handle(stream))
@@ -448,12 +475,15 @@ def mt_kv_read(cache: KvCache, slots, k_out, v_out, stream=None) -> None:
 def mt_kv_attention(cache: KvCache, q, tables, lengths, out, scale: Optional[float] = None, stream=None) -> None:
     """One new token per sequence over its cached tokens: q bf16 [sequences, q_heads, dim] (any strides), tables int32
     [sequences, width], lengths int32 [sequences], out bf16 like q, contiguous.  scale: 1 / sqrt(dim) if None."""
-    T = _types()
-    n, hq, d = shape = q.shape
-    q0, q1, q2 = q.stride()
-    rows, width = tables.shape
-    if not (q.dtype is T.bf16 and out.dtype is T.bf16 and tables.dtype is T.i32 and lengths.dtype is T.i32 and q.is_cuda and out.is_cuda and
-            tables.is_cuda and lengths.is_cuda and d == cache.dim and out.shape == shape and rows == n and lengths.dim() == 1 and
+    T, at = _types(), _place(q)
+    try:
+        n, hq, d = shape = q.shape
+        q0, q1, q2 = q.stride()
+        rows, width = tables.shape
+    except ValueError:
+        _refuse("mt_kv_attention")
+    if not (q.dtype is T.bf16 and out.dtype is T.bf16 and tables.dtype is T.i32 and lengths.dtype is T.i32 and q.is_cuda and
+            q.get_device() == out.get_device() == tables.get_device() == lengths.get_device() == at and d == cache.dim and out.shape == shape and rows == n and lengths.dim() == 1 and
             lengths.numel() == n and out.is_contiguous() and tables.is_contiguous() and lengths.is_contiguous() and (n == 0 or q2 == 1)):
         _refuse("mt_kv_attention")
     code = (_lib or lib()).mt_kv_attention(cache.ref, q.data_ptr(), q0, q1, tables.data_ptr(), width, lengths.data_ptr(), n, hq,
@@ -471,8 +501,9 @@ def mt_quant_packed_bytes(in_features: int, out_features: int, group: int) -> in
 
 def mt_quant_pack(codes, scales, packed, stream=None) -> None:
     """codes uint8 [tenants, out, in / 2], scales bf16 [tenants, out, in / group] -> packed uint8 [tenants, mt_quant_packed_bytes]."""
-    T = _types()
-    if not (codes.dtype is T.u8 and scales.dtype is T.bf16 and packed.dtype is T.u8 and codes.is_cuda and scales.is_cuda and packed.is_cuda and
+    T, at = _types(), _place(codes)
+    if not (codes.dtype is T.u8 and scales.dtype is T.bf16 and packed.dtype is T.u8 and codes.is_cuda and
+            codes.get_device() == scales.get_device() == packed.get_device() == at and
             codes.dim() == 3 and scales.dim() == 3 and codes.shape[:2] == scales.shape[:2] and codes.is_contiguous() and
             scales.is_contiguous() and packed.is_contiguous() and scales.shape[2] > 0 and 2 * codes.shape[2] % scales.shape[2] == 0):
         _refuse("mt_quant_pack")
@@ -488,12 +519,15 @@ class QuantBank:
 
     def __init__(self, codes, scales, bias=None, stream=None):
         import torch
-        t, n, half = codes.shape
+        try:
+            t, n, half = codes.shape
+        except ValueError:
+            _refuse("QuantBank")
         k = 2 * half
-        if scales.dim() != 3 or scales.shape[2] <= 0 or k % scales.shape[2]:
+        if codes.get_device() != _place(codes) or scales.dim() != 3 or scales.shape[2] <= 0 or k % scales.shape[2]:
             _refuse("QuantBank")
         group = k // scales.shape[2]
-        if bias is not None and not (bias.dtype is torch.float32 and bias.is_cuda and bias.is_contiguous() and tuple(bias.shape) == (t, n)):
+        if bias is not None and not (bias.dtype is torch.float32 and bias.is_cuda and bias.get_device() == codes.get_device() and bias.is_contiguous() and tuple(bias.shape) == (t, n)):
             _refuse("QuantBank")
         self.packed = torch.empty((t, mt_quant_packed_bytes(k, n, group)), dtype=torch.uint8, device=codes.device)
         mt_quant_pack(codes, scales, self.packed, stream)
@@ -504,13 +538,17 @@ class QuantBank:
 
 def mt_quant_linear(x, ids, bank: QuantBank, y, stream=None) -> None:
     """y[i] = weight[ids[i]] x[i] + bias[ids[i]]: x bf16 [n, in] (any row stride), ids int32 [n], y bf16 or fp32 [n, out]."""
-    T = _types()
-    n, k = x.shape
-    rows, out = y.shape
-    x0, x1 = x.stride()
-    y0, y1 = y.stride()
+    T, at = _types(), _place(x)
+    try:
+        n, k = x.shape
+        rows, out = y.shape
+        x0, x1 = x.stride()
+        y0, y1 = y.stride()
+    except ValueError:
+        _refuse("mt_quant_linear")
     wide = y.dtype is T.f32
-    if not (x.dtype is T.bf16 and ids.dtype is T.i32 and (wide or y.dtype is T.bf16) and x.is_cuda and ids.is_cuda and y.is_cuda and
+    if not (x.dtype is T.bf16 and ids.dtype is T.i32 and (wide or y.dtype is T.bf16) and x.is_cuda and
+            x.get_device() == ids.get_device() == y.get_device() == at and
             k == bank.in_features and rows == n and out == bank.out_features and ids.dim() == 1 and ids.numel() == n and
             ids.is_contiguous() and (n == 0 or (x1 == 1 and (y1 == 1 or out == 1)))):
         _refuse("mt_quant_linear")
@@ -523,18 +561,21 @@ def mt_token_logprobs(logits, tokens, logprobs, entropies=None, top_ids=None, to
     """logits bf16 or fp32 [n, vocab] (any row stride), tokens int32 [n] -> logprobs fp32 [n], entropies fp32 [n] (or None),
     top_ids int32 [n, top] and top_logprobs fp32 [n, top] (or None)."""
     T = _types()
-    f32, top = T.f32, 0
-    n, vocab = logits.shape
-    s0, s1 = logits.stride()
+    f32, top, at = T.f32, 0, _place(logits)
+    try:
+        n, vocab = logits.shape
+        s0, s1 = logits.stride()
+    except ValueError:
+        _refuse("mt_token_logprobs")
     wide = logits.dtype is f32
-    ok = (wide or logits.dtype is T.bf16) and tokens.dtype is T.i32 and logprobs.dtype is f32 and logits.is_cuda and tokens.is_cuda and \
-        logprobs.is_cuda and tokens.dim() == 1 and tokens.numel() == n and logprobs.dim() == 1 and logprobs.numel() == n and \
+    ok = (wide or logits.dtype is T.bf16) and tokens.dtype is T.i32 and logprobs.dtype is f32 and logits.is_cuda and \
+        logits.get_device() == tokens.get_device() == logprobs.get_device() == at and tokens.dim() == 1 and tokens.numel() == n and logprobs.dim() == 1 and logprobs.numel() == n and \
         tokens.is_contiguous() and logprobs.is_contiguous() and (n == 0 or vocab <= 1 or s1 == 1)
     if entropies is not None:
-        ok = ok and entropies.dtype is f32 and entropies.is_cuda and entropies.dim() == 1 and entropies.numel() == n and entropies.is_contiguous()
+        ok = ok and entropies.dtype is f32 and entropies.get_device() == at and entropies.dim() == 1 and entropies.numel() == n and entropies.is_contiguous()
     if ok and (top_ids is not None or top_logprobs is not None):
         ok = top_ids is not None and top_logprobs is not None and top_ids.dtype is T.i32 and top_logprobs.dtype is f32 and \
-            top_ids.is_cuda and top_logprobs.is_cuda and top_ids.dim() == 2 and top_ids.shape[0] == n and \
+            top_ids.get_device() == top_logprobs.get_device() == at and top_ids.dim() == 2 and top_ids.shape[0] == n and \
             top_ids.shape == top_logprobs.shape and top_ids.is_contiguous() and top_logprobs.is_contiguous()
         top = top_ids.shape[1] if ok else 0
     if not ok:
