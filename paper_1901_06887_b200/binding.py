@@ -376,6 +376,9 @@ def _refuse(where: str) -> None:
     raise MtError(1, where) from None
 
 
+_MOST = 0x7fffffff       # of sizes: C's int32, which ctypes would cut larger numbers to
+
+
 def _place(t) -> int:
     """Where a call's tensors have to be: on the context's device (without a context, together; the library then says so)."""
     return t.get_device() if _device is None else _device
@@ -400,7 +403,10 @@ def mt_prompt_attention(q, k, v, offsets, out, scale: Optional[float] = None, st
             out.shape == shape and out.is_contiguous() and offsets.dim() == 1 and offsets.is_contiguous() and offsets.numel() > 0 and
             (n == 0 or q2 == k2 == v2 == 1)):
         _refuse("mt_prompt_attention")
-    desc = _prompt_desc(n, offsets.numel() - 1, hq, hk, d, d ** -0.5 if scale is None else scale, q0, q1, k0, k1, v0, v1)
+    try:
+        desc = _prompt_desc(n, offsets.numel() - 1, hq, hk, d, d ** -0.5 if scale is None else scale, q0, q1, k0, k1, v0, v1)
+    except (struct.error, OverflowError, ZeroDivisionError):       # a number that the description does not hold; a head of no elements
+        _refuse("mt_prompt_attention")
     code = (_lib or lib()).mt_prompt_attention(desc, q.data_ptr(), k.data_ptr(), v.data_ptr(), offsets.data_ptr(), out.data_ptr(),
                                                _stream_handle(stream))
     if code:
@@ -418,7 +424,7 @@ class KvCache:
         except ValueError:
             _refuse("KvCache")
         for c, p in ((k_codes, k_params), (v_codes, v_params)):
-            if not (c.dtype is T.u8 and p.dtype is T.bf16 and c.is_cuda and c.get_device() == p.get_device() == at and c.is_contiguous() and p.is_contiguous() and
+            if not (c.dtype is T.u8 and p.dtype is T.bf16 and c.is_cuda and pages <= _MOST and heads <= _MOST and c.get_device() == p.get_device() == at and c.is_contiguous() and p.is_contiguous() and
                     tuple(c.shape) == (pages, heads, page, half) and tuple(p.shape) == (pages, heads, page, 2)):
                 _refuse("KvCache")
         self.tensors = (k_codes, k_params, v_codes, v_params)
@@ -449,7 +455,7 @@ def mt_kv_append(cache: KvCache, k, v, slots, stream=None) -> None:
     if not (k.dtype is T.bf16 and v.dtype is T.bf16 and slots.dtype is T.i64 and k.is_cuda and
             k.get_device() == v.get_device() == slots.get_device() == at and
             v.shape == shape and h == cache.heads and d == cache.dim and slots.dim() == 1 and slots.numel() == n and slots.is_contiguous() and
-            (n == 0 or k2 == v2 == 1)):
+            (n == 0 or k2 == v2 == 1) and n <= _MOST):
         _refuse("mt_kv_append")
     code = (_lib or lib()).mt_kv_append(cache.ref, k.data_ptr(), k0, k1, v.data_ptr(), v0, v1, slots.data_ptr(), n, _stream_handle(stream))
     if code:
@@ -465,7 +471,7 @@ def mt_kv_read(cache: KvCache, slots, k_out, v_out, stream=None) -> None:
         _refuse("mt_kv_read")
     if not (k_out.dtype is T.bf16 and v_out.dtype is T.bf16 and slots.dtype is T.i64 and slots.dim() == 1 and slots.numel() == n and
             k_out.is_cuda and k_out.get_device() == v_out.get_device() == slots.get_device() == at and v_out.shape == shape and h == cache.heads and d == cache.dim and
-            k_out.is_contiguous() and v_out.is_contiguous() and slots.is_contiguous()):
+            k_out.is_contiguous() and v_out.is_contiguous() and slots.is_contiguous() and n <= _MOST):
         _refuse("mt_kv_read")
     code = (_lib or lib()).mt_kv_read(cache.ref, slots.data_ptr(), n, k_out.data_ptr(), v_out.data_ptr(), _stream_handle(stream))
     if code:
@@ -484,7 +490,8 @@ def mt_kv_attention(cache: KvCache, q, tables, lengths, out, scale: Optional[flo
         _refuse("mt_kv_attention")
     if not (q.dtype is T.bf16 and out.dtype is T.bf16 and tables.dtype is T.i32 and lengths.dtype is T.i32 and q.is_cuda and
             q.get_device() == out.get_device() == tables.get_device() == lengths.get_device() == at and d == cache.dim and out.shape == shape and rows == n and lengths.dim() == 1 and
-            lengths.numel() == n and out.is_contiguous() and tables.is_contiguous() and lengths.is_contiguous() and (n == 0 or q2 == 1)):
+            lengths.numel() == n and out.is_contiguous() and tables.is_contiguous() and lengths.is_contiguous() and (n == 0 or q2 == 1) and
+            n <= _MOST and hq <= _MOST and width <= _MOST):
         _refuse("mt_kv_attention")
     code = (_lib or lib()).mt_kv_attention(cache.ref, q.data_ptr(), q0, q1, tables.data_ptr(), width, lengths.data_ptr(), n, hq,
                                            d ** -0.5 if scale is None else scale, out.data_ptr(), _stream_handle(stream))
@@ -495,6 +502,8 @@ def mt_kv_attention(cache: KvCache, q, tables, lengths, out, scale: Optional[flo
 def mt_quant_packed_bytes(in_features: int, out_features: int, group: int) -> int:
     """Bytes of one tenant's packed weights (host code only; needs no GPU)."""
     b = ctypes.c_size_t(0)
+    if not -_MOST <= min(in_features, out_features, group) <= max(in_features, out_features, group) <= _MOST:
+        _refuse("mt_quant_packed_bytes")
     _check(lib().mt_quant_packed_bytes(int(in_features), int(out_features), int(group), ctypes.byref(b)), "mt_quant_packed_bytes")
     return int(b.value)
 
@@ -509,7 +518,7 @@ def mt_quant_pack(codes, scales, packed, stream=None) -> None:
         _refuse("mt_quant_pack")
     t, n, half = codes.shape
     group = 2 * half // scales.shape[2]
-    if packed.numel() < t * mt_quant_packed_bytes(2 * half, n, group):
+    if t > _MOST or packed.numel() < t * mt_quant_packed_bytes(2 * half, n, group):
         _refuse("mt_quant_pack")
     _check(lib().mt_quant_pack(codes.data_ptr(), scales.data_ptr(), t, 2 * half, n, group, packed.data_ptr(), _stream_handle(stream)), "mt_quant_pack")
 
@@ -550,7 +559,7 @@ def mt_quant_linear(x, ids, bank: QuantBank, y, stream=None) -> None:
     if not (x.dtype is T.bf16 and ids.dtype is T.i32 and (wide or y.dtype is T.bf16) and x.is_cuda and
             x.get_device() == ids.get_device() == y.get_device() == at and
             k == bank.in_features and rows == n and out == bank.out_features and ids.dim() == 1 and ids.numel() == n and
-            ids.is_contiguous() and (n == 0 or (x1 == 1 and (y1 == 1 or out == 1)))):
+            ids.is_contiguous() and (n == 0 or (x1 == 1 and (y1 == 1 or out == 1))) and n <= _MOST):
         _refuse("mt_quant_linear")
     code = (_lib or lib()).mt_quant_linear(bank.ref, x.data_ptr(), x0, ids.data_ptr(), n, y.data_ptr(), y0, 1 if wide else 0, _stream_handle(stream))
     if code:
@@ -570,14 +579,15 @@ def mt_token_logprobs(logits, tokens, logprobs, entropies=None, top_ids=None, to
     wide = logits.dtype is f32
     ok = (wide or logits.dtype is T.bf16) and tokens.dtype is T.i32 and logprobs.dtype is f32 and logits.is_cuda and \
         logits.get_device() == tokens.get_device() == logprobs.get_device() == at and tokens.dim() == 1 and tokens.numel() == n and logprobs.dim() == 1 and logprobs.numel() == n and \
-        tokens.is_contiguous() and logprobs.is_contiguous() and (n == 0 or vocab <= 1 or s1 == 1)
+        tokens.is_contiguous() and logprobs.is_contiguous() and (n == 0 or vocab <= 1 or s1 == 1) and \
+        n <= _MOST and vocab <= _MOST
     if entropies is not None:
         ok = ok and entropies.dtype is f32 and entropies.get_device() == at and entropies.dim() == 1 and entropies.numel() == n and entropies.is_contiguous()
     if ok and (top_ids is not None or top_logprobs is not None):
         ok = top_ids is not None and top_logprobs is not None and top_ids.dtype is T.i32 and top_logprobs.dtype is f32 and \
             top_ids.get_device() == top_logprobs.get_device() == at and top_ids.dim() == 2 and top_ids.shape[0] == n and \
             top_ids.shape == top_logprobs.shape and top_ids.is_contiguous() and top_logprobs.is_contiguous()
-        top = top_ids.shape[1] if ok else 0
+        top = min(top_ids.shape[1], _MOST) if ok else 0
     if not ok:
         _refuse("mt_token_logprobs")
     code = (_lib or lib()).mt_token_logprobs(logits.data_ptr(), 1 if wide else 0, s0, n, vocab, tokens.data_ptr(), top, logprobs.data_ptr(),

@@ -1,5 +1,5 @@
-"""What the binding's calls of the language-model operators refuse before the library sees it: tensors of another rank or on
-another device.  Always MtError with MT_ERR_INVALID_ARG."""
+"""What the binding's calls of the language-model operators refuse before the library sees it: tensors of another rank, on
+another device, sizes and numbers that the C interface cannot take.  Always MtError with MT_ERR_INVALID_ARG."""
 import pytest
 import torch
 
@@ -25,6 +25,20 @@ class Elsewhere:
 
     def __getattr__(self, name):
         return getattr(self.t, name)
+
+
+class Huge(Elsewhere):
+    """A tensor that says it has 2^32 rows more than it has."""
+
+    def get_device(self):
+        return self.t.get_device()
+
+    @property
+    def shape(self):
+        return torch.Size([self.t.shape[0] + (1 << 32), *self.t.shape[1:]])
+
+    def numel(self):
+        return self.t.numel() // self.t.shape[0] * self.shape[0]
 
 
 def calls():
@@ -62,3 +76,26 @@ def test_rank_and_place(name):
         for other in (*ranks, t.cpu(), Elsewhere(t)):
             assert code_of(f, *args[:i], other, *args[i + 1:]) == 1, (i, type(other), other.shape)
     assert mt.mt_get_async_status() == (0, -1)
+
+
+@pytest.mark.parametrize("name", ["prompt", "append", "read", "attention", "linear", "logprobs"])
+def test_sizes_beyond_32_bits(name):
+    """Never cut to their low 32 bits."""
+    f, args = calls()[name]
+    huge = [Huge(t) if isinstance(t, torch.Tensor) and t.dim() and t.shape[0] == 3 else t for t in args]
+    assert code_of(f, *huge) == 1
+
+
+@pytest.mark.parametrize("scale", [float("nan"), float("inf"), float("-inf"), 1e39])
+@pytest.mark.parametrize("name", ["prompt", "attention"])
+def test_scales_that_are_no_numbers(name, scale):
+    f, args = calls()[name]
+    assert code_of(f, *args, scale=scale) == 1
+    f(*args, scale=-3e38)
+
+
+def test_a_head_dimension_of_zero():
+    for name in ("prompt", "append", "read", "attention"):
+        f, args = calls()[name]
+        args = [t[..., :0] if isinstance(t, torch.Tensor) and t.dim() == 3 else t for t in args]
+        assert code_of(f, *args) in (1, 4)

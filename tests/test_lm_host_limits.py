@@ -34,3 +34,10 @@ def test_layers_too_wide(lib, n):
 def test_the_widest_layer(lib):
     n = (1 << 31) - (1 << 20) - 1
     assert mt.mt_quant_packed_bytes(128, n, 64) == (n + 1) * 64 + (n + 1) * 4
+
+
+def test_sizes_beyond_32_bits_are_not_cut(lib):
+    for i in range(3):
+        args = [64, 16, 64]
+        args[i] += 1 << 32
+        assert code_of(mt.mt_quant_packed_bytes, *args) == 1
