@@ -524,7 +524,7 @@ def mt_quant_pack(codes, scales, packed, stream=None) -> None:
 
 
 class QuantBank:
-    """The packed 4-bit weights of several tenants' layer, with an optional fp32 bias [tenants, out]."""
+    """The packed 4-bit weights of several tenants' layer, with an optional fp32 bias [tenants, out].  Packed on `stream`."""
 
     def __init__(self, codes, scales, bias=None, stream=None):
         import torch
@@ -538,7 +538,11 @@ class QuantBank:
         group = k // scales.shape[2]
         if bias is not None and not (bias.dtype is torch.float32 and bias.is_cuda and bias.get_device() == codes.get_device() and bias.is_contiguous() and tuple(bias.shape) == (t, n)):
             _refuse("QuantBank")
-        self.packed = torch.empty((t, mt_quant_packed_bytes(k, n, group)), dtype=torch.uint8, device=codes.device)
+        # (memory of the stream that writes it: the current stream's may still be in use there)
+        if isinstance(stream, int):
+            stream = torch.cuda.ExternalStream(stream, device=codes.device)
+        with torch.cuda.stream(stream):
+            self.packed = torch.empty((t, mt_quant_packed_bytes(k, n, group)), dtype=torch.uint8, device=codes.device)
         mt_quant_pack(codes, scales, self.packed, stream)
         self.bias, self.in_features, self.out_features = bias, k, n
         self.desc = QuantBankDesc(t, k, n, group, self.packed.data_ptr(), _ptr(bias))
