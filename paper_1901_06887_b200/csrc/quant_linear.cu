@@ -73,6 +73,10 @@ constexpr int kCodes = 1024, kStageBytes = kCodes + 128;        // a block's cod
 // (4096 x 4096, one row: 7.9 us against 10.1 with four); four where the columns' partial sums need the memory.
 __host__ __device__ constexpr int stages(int maxt) { return maxt == 1 ? 8 : 4; }
 
+// CTAs of an SM at once, which is also what a launch has of them: a further one would start when another has ended, sort the ids again and
+// fill its ring from nothing (three for calls of few rows, of which two fit: one row of 4096 -> 16384 17.8 us against 16.5, 8 tenants 94 against 86).
+__host__ __device__ constexpr int resident(int maxt) { return maxt == 2 ? 3 : maxt <= 4 ? 2 : 1; }
+
 struct Shared {
     int ids[kQuantRowsPerLaunch], slot[kQuantRowsPerLaunch], order[kQuantRowsPerLaunch];
     int tenant[kQuantRowsPerLaunch], begin[kQuantRowsPerLaunch + 1];
@@ -214,7 +218,7 @@ __device__ __forceinline__ void unit(const QuantLinearArgs& a, const Shared& s, 
 
 // MAXT: largest number of column tiles a pass may take (a launch of n rows never needs more than n of them).
 template <int MAXT, bool G32>
-__global__ void __launch_bounds__(kThreads, MAXT <= 2 ? 3 : MAXT == 4 ? 2 : 1) quant_linear_kernel(const QuantLinearArgs a) {
+__global__ void __launch_bounds__(kThreads, resident(MAXT)) quant_linear_kernel(const QuantLinearArgs a) {
     constexpr int kStages = stages(MAXT);
     __shared__ Shared s;
     extern __shared__ __align__(128) uint8_t s_bytes[];          // the warps' rings, then the join
@@ -299,6 +303,8 @@ __global__ void __launch_bounds__(kThreads, MAXT <= 2 ? 3 : MAXT == 4 ? 2 : 1) q
 }
 
 constexpr int shared_bytes(int maxt) { return kWarps * stages(maxt) * kStageBytes + kWarps * maxt * 8 * 36 * 4; }
+constexpr bool fits(int maxt) { return resident(maxt) * (shared_bytes(maxt) + (int)sizeof(Shared) + 1024) <= 228 * 1024; }     // 1 KB a CTA is the system's
+static_assert(fits(1) && fits(2) && fits(4) && fits(8), "the CTAs that a launch counts on do not fit an SM's shared memory");
 typedef void (*Kernel)(QuantLinearArgs);
 const Kernel kKernels[2][4] = {
     {quant_linear_kernel<1, false>, quant_linear_kernel<2, false>, quant_linear_kernel<4, false>, quant_linear_kernel<8, false>},
@@ -330,7 +336,7 @@ cudaError_t launch_quant_linear(const QuantLinearArgs& a, int sm_count, cudaStre
     const int most_slots = a.n < a.tenants ? a.n : a.tenants;
     const int64_t units = (int64_t)((a.N + 31) / 32) * most_slots;      // (more groups only where a tenant has over 64 rows)
     const int v = a.n <= 8 ? 0 : a.n <= 16 ? 1 : a.n <= 32 ? 2 : 3;       // up to 8 << v rows of a tenant
-    int64_t grid = (int64_t)sm_count * (v <= 1 ? 3 : v == 2 ? 2 : 1);
+    int64_t grid = (int64_t)sm_count * resident(1 << v);
     if (grid > units) grid = units;
     QuantLinearArgs b = a;
     b.codes_bytes = quant_codes_bytes(a.K, a.N);
