@@ -168,7 +168,7 @@ int log2_of(int x) {
 }
 
 // Runs of tokens per CTA: four where that leaves two CTAs for every SM.
-int items_for(int64_t n, int heads, int d) { return n * heads * 2 * (d / 8) / kThreads >= 4 * 2 * 148 ? 4 : 1; }
+int items_for(int64_t n, int heads, int d, int sm_count) { return n * heads * 2 * (d / 8) / kThreads >= 4LL * 2 * sm_count ? 4 : 1; }
 constexpr int kMaxRuns = 65535;                  // rows of a grid
 int tokens_of(int d, int items) { return kThreads / (d / 8) * items; }
 int runs_of(int n, int tokens) { return (int)((n + (int64_t)tokens - 1) / tokens); }
@@ -176,10 +176,10 @@ int runs_of(int n, int tokens) { return (int)((n + (int64_t)tokens - 1) / tokens
 }  // namespace
 
 cudaError_t launch_kv_append(const mt_kv_cache& c, const KvRows& k, const KvRows& v, const int64_t* slots, int n, const OpStatus& status,
-                             cudaStream_t s) {
+                             int sm_count, cudaStream_t s) {
     const CachePtrs kc = {static_cast<uint8_t*>(c.k_codes), static_cast<uint32_t*>(c.k_params)};
     const CachePtrs vc = {static_cast<uint8_t*>(c.v_codes), static_cast<uint32_t*>(c.v_params)};
-    const int items = items_for(n, c.kv_heads, c.head_dim);
+    const int items = items_for(n, c.kv_heads, c.head_dim, sm_count);
     auto* const f = c.head_dim == 64 ? (items == 1 ? kv_append_kernel<64, 1> : kv_append_kernel<64, 4>)
                                      : (items == 1 ? kv_append_kernel<128, 1> : kv_append_kernel<128, 4>);
     const int tokens = tokens_of(c.head_dim, items), most = kMaxRuns * tokens;
@@ -194,10 +194,10 @@ cudaError_t launch_kv_append(const mt_kv_cache& c, const KvRows& k, const KvRows
 }
 
 cudaError_t launch_kv_read(const mt_kv_cache& c, const int64_t* slots, int n, uint16_t* k_out, uint16_t* v_out, const OpStatus& status,
-                           cudaStream_t s) {
+                           int sm_count, cudaStream_t s) {
     const CachePtrs kc = {static_cast<uint8_t*>(c.k_codes), static_cast<uint32_t*>(c.k_params)};
     const CachePtrs vc = {static_cast<uint8_t*>(c.v_codes), static_cast<uint32_t*>(c.v_params)};
-    const int items = items_for(n, c.kv_heads, c.head_dim);
+    const int items = items_for(n, c.kv_heads, c.head_dim, sm_count);
     auto* const f = c.head_dim == 64 ? (items == 1 ? kv_read_kernel<64, 1> : kv_read_kernel<64, 4>)
                                      : (items == 1 ? kv_read_kernel<128, 1> : kv_read_kernel<128, 4>);
     const int tokens = tokens_of(c.head_dim, items), most = kMaxRuns * tokens;

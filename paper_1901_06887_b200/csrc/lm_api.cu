@@ -235,7 +235,7 @@ mt_status mt_kv_append(const mt_kv_cache* cache, const void* k, int64_t k_token_
     if (!k || !v || !slots || misaligned(k) || misaligned(v) || misaligned(slots, 8)) return MT_ERR_INVALID_ARG;
     const KvRows kr = {static_cast<const uint16_t*>(k), k_token_stride, k_head_stride};
     const KvRows vr = {static_cast<const uint16_t*>(v), v_token_stride, v_head_stride};
-    return to_status(launch_kv_append(*cache, kr, vr, slots, n, c.status, static_cast<cudaStream_t>(stream)));
+    return to_status(launch_kv_append(*cache, kr, vr, slots, n, c.status, c.sm_count, static_cast<cudaStream_t>(stream)));
 }
 
 mt_status mt_kv_read(const mt_kv_cache* cache, const int64_t* slots, int32_t n, void* k_out, void* v_out, void* stream) {
@@ -248,7 +248,7 @@ mt_status mt_kv_read(const mt_kv_cache* cache, const int64_t* slots, int32_t n, 
     if (st != MT_OK || n == 0) return st;
     if (!slots || !k_out || !v_out || misaligned(k_out) || misaligned(v_out) || misaligned(slots, 8)) return MT_ERR_INVALID_ARG;
     return to_status(launch_kv_read(*cache, slots, n, static_cast<uint16_t*>(k_out), static_cast<uint16_t*>(v_out), c.status,
-                                    static_cast<cudaStream_t>(stream)));
+                                    c.sm_count, static_cast<cudaStream_t>(stream)));
 }
 
 mt_status mt_kv_attention(const mt_kv_cache* cache, const void* q, int64_t q_seq_stride, int64_t q_head_stride,

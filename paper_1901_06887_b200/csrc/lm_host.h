@@ -25,9 +25,9 @@ struct KvRows {                     // rows [n][heads][head_dim] bf16 with strid
     int64_t token_stride, head_stride;
 };
 cudaError_t launch_kv_append(const mt_kv_cache& c, const KvRows& k, const KvRows& v, const int64_t* slots, int n,
-                             const OpStatus& status, cudaStream_t s);
+                             const OpStatus& status, int sm_count, cudaStream_t s);
 cudaError_t launch_kv_read(const mt_kv_cache& c, const int64_t* slots, int n, uint16_t* k_out, uint16_t* v_out,
-                           const OpStatus& status, cudaStream_t s);
+                           const OpStatus& status, int sm_count, cudaStream_t s);
 
 struct KvAttentionArgs {
     mt_kv_cache c;
