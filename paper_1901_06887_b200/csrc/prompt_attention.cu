@@ -502,6 +502,12 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
                 ++n_o;
             }
             if (!ok) break;
+            // A tile without rows waits for nothing else, and must not run ahead: it would arrive on epi_done twice in one phase, in the place of
+            // the other tile.  (A tile with rows ends its round behind the cleaners, who have waited for the same phase.)
+            if (nb == 0 && round >= 2) {
+                ok = mbar_wait(bar(s.epi_done[buf]), ((round >> 1) - 1) & 1, abort_flag, p.status.word, 233);
+                if (!ok) break;
+            }
             if (nb > 0) {
                 ok = mbar_wait(bar(s.o_ready[i]), (n_o - 1) & 1, abort_flag, p.status.word, 232);
                 if (!ok) break;
