@@ -1,9 +1,9 @@
-"""Batches beyond what one table of the kernels holds: more tiles a CTA than are looked up at once."""
+"""Batches beyond what one table of the kernels holds: more tiles a CTA than are looked up at once, more rows than a launch."""
 import numpy as np
 import pytest
 import torch
 
-from lm_util import attention_bound, init, to_np
+from lm_util import attention_bound, init, linear_bound, linear_reference, to_np
 from paper_1901_06887_b200 import binding as mt
 
 pytestmark = pytest.mark.gpu
@@ -57,3 +57,22 @@ def test_many_prompts_of_one_tile(count, hq, hkv, dim):
         vv = v[a:b].double().repeat_interleave(hq // hkv, 1)
         o, size = (torch.einsum("hij,jhd->ihd", p, x) for x in (vv, vv.abs()))
         assert ((out[a:b].double() - o).abs() <= torch.from_numpy(attention_bound(o.cpu().numpy(), size.cpu().numpy())).cuda()).all()
+
+
+@pytest.mark.parametrize("rows,tenants", [(601, 1), (1025, 7), (3000, 300)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_prompt_rows_through_a_layer(rows, tenants, dtype):
+    init()
+    g = torch.Generator(device="cuda").manual_seed(rows)
+    k, n = 256, 50
+    codes = torch.randint(0, 256, (tenants, n, k // 2), generator=g, device="cuda", dtype=torch.uint8)
+    scales = ((0.5 + torch.rand((tenants, n, k // 64), generator=g, device="cuda")) / 16).to(torch.bfloat16)
+    bias = torch.randn((tenants, n), generator=g, device="cuda")
+    x = torch.randn((rows, k), generator=g, device="cuda").to(torch.bfloat16)
+    ids = np.random.default_rng(rows).integers(0, tenants, rows)
+    ids.sort()                                                   # prompts one behind the other
+    y = torch.full((rows, n), 7.0, dtype=dtype, device="cuda")
+    mt.mt_quant_linear(x, torch.tensor(ids, dtype=torch.int32, device="cuda"), mt.QuantBank(codes, scales, bias), y)
+    assert mt.mt_get_async_status() == (0, -1)
+    want, a = linear_reference(x, ids.tolist(), codes, scales, bias)
+    assert (np.abs(to_np(y) - want) <= linear_bound(want, a, k, dtype == torch.bfloat16)).all()
