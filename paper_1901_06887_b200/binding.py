@@ -372,15 +372,15 @@ def _types():
     return _Types
 
 
-def _refuse(where: str) -> None:
-    raise MtError(1, where) from None
+def _refuse(where: str, needs_context: bool = True) -> None:
+    raise MtError(9 if needs_context and _device is None else 1, where) from None      # without a context no tensor is in the right place
 
 
 _MOST = 0x7fffffff       # of sizes: C's int32, which ctypes would cut larger numbers to
 
 
 def _place(t) -> int:
-    """Where a call's tensors have to be: on the context's device (without a context, together; the library then says so)."""
+    """Where the tensors of a cache or a bank have to be: on the context's device (a cache may be put together before there is one)."""
     return t.get_device() if _device is None else _device
 
 
@@ -388,7 +388,7 @@ def mt_prompt_attention(q, k, v, offsets, out, scale: Optional[float] = None, st
     """Causal attention over packed prompts: q bf16 [n, q_heads, dim], k and v [n, kv_heads, dim] (any token and head strides),
     offsets int32 [sequences + 1], out bf16 [n, q_heads, dim] contiguous.  scale: 1 / sqrt(dim) if None."""
     T = _types()
-    bf16, at = T.bf16, _place(q)
+    bf16 = T.bf16
     try:
         n, hq, d = shape = q.shape
         nk, hk, dk = kshape = k.shape
@@ -398,8 +398,8 @@ def mt_prompt_attention(q, k, v, offsets, out, scale: Optional[float] = None, st
     except ValueError:
         _refuse("mt_prompt_attention")
     if not (q.dtype is bf16 and k.dtype is bf16 and v.dtype is bf16 and out.dtype is bf16 and offsets.dtype is T.i32 and
-            q.get_device() == k.get_device() == v.get_device() == out.get_device() == offsets.get_device() == at and
-            q.is_cuda and nk == n and dk == d and v.shape == kshape and
+            q.get_device() == k.get_device() == v.get_device() == out.get_device() == offsets.get_device() == _device and
+            nk == n and dk == d and v.shape == kshape and
             out.shape == shape and out.is_contiguous() and offsets.dim() == 1 and offsets.is_contiguous() and offsets.numel() > 0 and
             (n == 0 or q2 == k2 == v2 == 1)):
         _refuse("mt_prompt_attention")
@@ -422,11 +422,11 @@ class KvCache:
         try:
             pages, heads, page, half = k_codes.shape
         except ValueError:
-            _refuse("KvCache")
+            _refuse("KvCache", False)
         for c, p in ((k_codes, k_params), (v_codes, v_params)):
             if not (c.dtype is T.u8 and p.dtype is T.bf16 and c.is_cuda and pages <= _MOST and heads <= _MOST and c.get_device() == p.get_device() == at and c.is_contiguous() and p.is_contiguous() and
                     tuple(c.shape) == (pages, heads, page, half) and tuple(p.shape) == (pages, heads, page, 2)):
-                _refuse("KvCache")
+                _refuse("KvCache", False)
         self.tensors = (k_codes, k_params, v_codes, v_params)
         self.heads, self.dim = heads, 2 * half
         self.desc = KvCacheDesc(pages, page, heads, 2 * half, *[x.data_ptr() for x in self.tensors])
@@ -445,15 +445,15 @@ class KvCache:
 
 def mt_kv_append(cache: KvCache, k, v, slots, stream=None) -> None:
     """Round k and v, bf16 [n, kv_heads, dim] (any token and head strides), to 4 bits and write token i to slot slots[i] (int64 [n])."""
-    T, at = _types(), _place(k)
+    T = _types()
     try:
         n, h, d = shape = k.shape
         k0, k1, k2 = k.stride()
         v0, v1, v2 = v.stride()
     except ValueError:
         _refuse("mt_kv_append")
-    if not (k.dtype is T.bf16 and v.dtype is T.bf16 and slots.dtype is T.i64 and k.is_cuda and
-            k.get_device() == v.get_device() == slots.get_device() == at and
+    if not (k.dtype is T.bf16 and v.dtype is T.bf16 and slots.dtype is T.i64 and
+            k.get_device() == v.get_device() == slots.get_device() == _device and
             v.shape == shape and h == cache.heads and d == cache.dim and slots.dim() == 1 and slots.numel() == n and slots.is_contiguous() and
             (n == 0 or k2 == v2 == 1) and n <= _MOST):
         _refuse("mt_kv_append")
@@ -464,13 +464,13 @@ def mt_kv_append(cache: KvCache, k, v, slots, stream=None) -> None:
 
 def mt_kv_read(cache: KvCache, slots, k_out, v_out, stream=None) -> None:
     """The cached values of slots (int64 [n]) as bf16 [n, kv_heads, dim]."""
-    T, at = _types(), _place(k_out)
+    T = _types()
     try:
         n, h, d = shape = k_out.shape
     except ValueError:
         _refuse("mt_kv_read")
     if not (k_out.dtype is T.bf16 and v_out.dtype is T.bf16 and slots.dtype is T.i64 and slots.dim() == 1 and slots.numel() == n and
-            k_out.is_cuda and k_out.get_device() == v_out.get_device() == slots.get_device() == at and v_out.shape == shape and h == cache.heads and d == cache.dim and
+            k_out.get_device() == v_out.get_device() == slots.get_device() == _device and v_out.shape == shape and h == cache.heads and d == cache.dim and
             k_out.is_contiguous() and v_out.is_contiguous() and slots.is_contiguous() and n <= _MOST):
         _refuse("mt_kv_read")
     code = (_lib or lib()).mt_kv_read(cache.ref, slots.data_ptr(), n, k_out.data_ptr(), v_out.data_ptr(), _stream_handle(stream))
@@ -481,15 +481,15 @@ def mt_kv_read(cache: KvCache, slots, k_out, v_out, stream=None) -> None:
 def mt_kv_attention(cache: KvCache, q, tables, lengths, out, scale: Optional[float] = None, stream=None) -> None:
     """One new token per sequence over its cached tokens: q bf16 [sequences, q_heads, dim] (any strides), tables int32
     [sequences, width], lengths int32 [sequences], out bf16 like q, contiguous.  scale: 1 / sqrt(dim) if None."""
-    T, at = _types(), _place(q)
+    T = _types()
     try:
         n, hq, d = shape = q.shape
         q0, q1, q2 = q.stride()
         rows, width = tables.shape
     except ValueError:
         _refuse("mt_kv_attention")
-    if not (q.dtype is T.bf16 and out.dtype is T.bf16 and tables.dtype is T.i32 and lengths.dtype is T.i32 and q.is_cuda and
-            q.get_device() == out.get_device() == tables.get_device() == lengths.get_device() == at and d == cache.dim and out.shape == shape and rows == n and lengths.dim() == 1 and
+    if not (q.dtype is T.bf16 and out.dtype is T.bf16 and tables.dtype is T.i32 and lengths.dtype is T.i32 and
+            q.get_device() == out.get_device() == tables.get_device() == lengths.get_device() == _device and d == cache.dim and out.shape == shape and rows == n and lengths.dim() == 1 and
             lengths.numel() == n and out.is_contiguous() and tables.is_contiguous() and lengths.is_contiguous() and (n == 0 or q2 == 1) and
             n <= _MOST and hq <= _MOST and width <= _MOST):
         _refuse("mt_kv_attention")
@@ -503,7 +503,7 @@ def mt_quant_packed_bytes(in_features: int, out_features: int, group: int) -> in
     """Bytes of one tenant's packed weights (host code only; needs no GPU)."""
     b = ctypes.c_size_t(0)
     if not -_MOST <= min(in_features, out_features, group) <= max(in_features, out_features, group) <= _MOST:
-        _refuse("mt_quant_packed_bytes")
+        _refuse("mt_quant_packed_bytes", False)
     _check(lib().mt_quant_packed_bytes(int(in_features), int(out_features), int(group), ctypes.byref(b)), "mt_quant_packed_bytes")
     return int(b.value)
 
@@ -515,11 +515,11 @@ def mt_quant_pack(codes, scales, packed, stream=None) -> None:
             codes.get_device() == scales.get_device() == packed.get_device() == at and
             codes.dim() == 3 and scales.dim() == 3 and codes.shape[:2] == scales.shape[:2] and codes.is_contiguous() and
             scales.is_contiguous() and packed.is_contiguous() and scales.shape[2] > 0 and 2 * codes.shape[2] % scales.shape[2] == 0):
-        _refuse("mt_quant_pack")
+        _refuse("mt_quant_pack", False)
     t, n, half = codes.shape
     group = 2 * half // scales.shape[2]
     if t > _MOST or packed.numel() < t * mt_quant_packed_bytes(2 * half, n, group):
-        _refuse("mt_quant_pack")
+        _refuse("mt_quant_pack", False)
     _check(lib().mt_quant_pack(codes.data_ptr(), scales.data_ptr(), t, 2 * half, n, group, packed.data_ptr(), _stream_handle(stream)), "mt_quant_pack")
 
 
@@ -531,13 +531,13 @@ class QuantBank:
         try:
             t, n, half = codes.shape
         except ValueError:
-            _refuse("QuantBank")
+            _refuse("QuantBank", False)
         k = 2 * half
         if codes.get_device() != _place(codes) or scales.dim() != 3 or scales.shape[2] <= 0 or k % scales.shape[2]:
-            _refuse("QuantBank")
+            _refuse("QuantBank", False)
         group = k // scales.shape[2]
         if bias is not None and not (bias.dtype is torch.float32 and bias.is_cuda and bias.get_device() == codes.get_device() and bias.is_contiguous() and tuple(bias.shape) == (t, n)):
-            _refuse("QuantBank")
+            _refuse("QuantBank", False)
         # (memory of the stream that writes it: the current stream's may still be in use there)
         if isinstance(stream, int):
             stream = torch.cuda.ExternalStream(stream, device=codes.device)
@@ -551,7 +551,7 @@ class QuantBank:
 
 def mt_quant_linear(x, ids, bank: QuantBank, y, stream=None) -> None:
     """y[i] = weight[ids[i]] x[i] + bias[ids[i]]: x bf16 [n, in] (any row stride), ids int32 [n], y bf16 or fp32 [n, out]."""
-    T, at = _types(), _place(x)
+    T = _types()
     try:
         n, k = x.shape
         rows, out = y.shape
@@ -560,8 +560,8 @@ def mt_quant_linear(x, ids, bank: QuantBank, y, stream=None) -> None:
     except ValueError:
         _refuse("mt_quant_linear")
     wide = y.dtype is T.f32
-    if not (x.dtype is T.bf16 and ids.dtype is T.i32 and (wide or y.dtype is T.bf16) and x.is_cuda and
-            x.get_device() == ids.get_device() == y.get_device() == at and
+    if not (x.dtype is T.bf16 and ids.dtype is T.i32 and (wide or y.dtype is T.bf16) and
+            x.get_device() == ids.get_device() == y.get_device() == _device and
             k == bank.in_features and rows == n and out == bank.out_features and ids.dim() == 1 and ids.numel() == n and
             ids.is_contiguous() and (n == 0 or (x1 == 1 and (y1 == 1 or out == 1))) and n <= _MOST):
         _refuse("mt_quant_linear")
@@ -574,22 +574,22 @@ def mt_token_logprobs(logits, tokens, logprobs, entropies=None, top_ids=None, to
     """logits bf16 or fp32 [n, vocab] (any row stride), tokens int32 [n] -> logprobs fp32 [n], entropies fp32 [n] (or None),
     top_ids int32 [n, top] and top_logprobs fp32 [n, top] (or None)."""
     T = _types()
-    f32, top, at = T.f32, 0, _place(logits)
+    f32, top = T.f32, 0
     try:
         n, vocab = logits.shape
         s0, s1 = logits.stride()
     except ValueError:
         _refuse("mt_token_logprobs")
     wide = logits.dtype is f32
-    ok = (wide or logits.dtype is T.bf16) and tokens.dtype is T.i32 and logprobs.dtype is f32 and logits.is_cuda and \
-        logits.get_device() == tokens.get_device() == logprobs.get_device() == at and tokens.dim() == 1 and tokens.numel() == n and logprobs.dim() == 1 and logprobs.numel() == n and \
+    ok = (wide or logits.dtype is T.bf16) and tokens.dtype is T.i32 and logprobs.dtype is f32 and \
+        logits.get_device() == tokens.get_device() == logprobs.get_device() == _device and tokens.dim() == 1 and tokens.numel() == n and logprobs.dim() == 1 and logprobs.numel() == n and \
         tokens.is_contiguous() and logprobs.is_contiguous() and (n == 0 or vocab <= 1 or s1 == 1) and \
         n <= _MOST and vocab <= _MOST
     if entropies is not None:
-        ok = ok and entropies.dtype is f32 and entropies.get_device() == at and entropies.dim() == 1 and entropies.numel() == n and entropies.is_contiguous()
+        ok = ok and entropies.dtype is f32 and entropies.get_device() == _device and entropies.dim() == 1 and entropies.numel() == n and entropies.is_contiguous()
     if ok and (top_ids is not None or top_logprobs is not None):
         ok = top_ids is not None and top_logprobs is not None and top_ids.dtype is T.i32 and top_logprobs.dtype is f32 and \
-            top_ids.get_device() == top_logprobs.get_device() == at and top_ids.dim() == 2 and top_ids.shape[0] == n and \
+            top_ids.get_device() == top_logprobs.get_device() == _device and top_ids.dim() == 2 and top_ids.shape[0] == n and \
             top_ids.shape == top_logprobs.shape and top_ids.is_contiguous() and top_logprobs.is_contiguous()
         top = min(top_ids.shape[1], _MOST) if ok else 0
     if not ok:

@@ -41,3 +41,11 @@ def test_sizes_beyond_32_bits_are_not_cut(lib):
         args = [64, 16, 64]
         args[i] += 1 << 32
         assert code_of(mt.mt_quant_packed_bytes, *args) == 1
+
+
+def test_calls_without_a_context(lib):
+    import torch
+    x, i = torch.zeros((2, 2, 64), dtype=torch.bfloat16), torch.zeros(2, dtype=torch.int32)
+    assert code_of(mt.mt_prompt_attention, x, x, x, i, x) == 9
+    assert code_of(mt.mt_token_logprobs, x[:, 0], i, torch.zeros(2)) == 9
+    assert code_of(mt.KvCache, x, x, x, x) == 1
