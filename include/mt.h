@@ -316,10 +316,11 @@ mt_status mt_bucket_noalloc(const int32_t* model_ids, int32_t n, int32_t n_model
  * All scratch goes away with mt_shutdown, after which a graph with mt_kv_attention must not be replayed.
  *
  * Refusals: MT_ERR_INVALID_ARG null pointer, negative size, unknown type, misaligned pointer, a scale that is not
- * finite; MT_ERR_UNSUPPORTED a size or stride outside what the kernels take; nothing is enqueued then.  A count of zero is a no-op.  What only the
- * device can see (an id, page, slot, length or offset out of range) never faults: the rows concerned are NaN (or left
- * out, where rows are written to a cache), and the sticky status of mt_get_async_status is MT_ERR_BAD_MODEL_ID (ids) or
- * MT_ERR_INVALID_ARG, with the smallest index concerned of the first such call (mt_token_logprobs raises nothing).
+ * finite; MT_ERR_UNSUPPORTED a size or stride outside what the kernels take; nothing is enqueued then.  A count of zero is
+ * a no-op.  What only the device can see (an id, page, slot, length or offset out of range) never faults: the rows
+ * concerned are NaN (or left out, where rows are written to a cache), and the sticky status of mt_get_async_status is
+ * MT_ERR_BAD_MODEL_ID (ids) or MT_ERR_INVALID_ARG, with the smallest index concerned of the first such call
+ * (mt_token_logprobs raises nothing).
  * mt_prompt_attention, whose kernel waits on barriers, can also report MT_ERR_TIMEOUT there (a wait that gave up; its
  * output is then incomplete). */
 typedef enum { MT_BF16 = 0, MT_FP32 = 1 } mt_dtype;
@@ -363,8 +364,9 @@ mt_status mt_kv_append(const mt_kv_cache* cache_host, const void* k, int64_t k_t
                        const void* v, int64_t v_token_stride, int64_t v_head_stride, const int64_t* slots, int32_t n,
                        void* stream);
 
-/* The values of n slots, rounded to bf16: k_out and v_out [n][kv_heads][head_dim], contiguous (what a prompt that goes on
- * from cached tokens, or a move to another cache, needs).  A slot of -1 gives zeros; any other slot outside the cache gives
+/* The values of n slots, rounded to bf16: k_out and v_out [n][kv_heads][head_dim], contiguous (for a caller's own layers, for a
+ * move to another cache, for inspection; mt_prompt_attention has one length for queries and keys, so a prompt that goes on
+ * from cached tokens is not among its uses yet).  A slot of -1 gives zeros; any other slot outside the cache gives
  * NaN and sets the sticky status. */
 mt_status mt_kv_read(const mt_kv_cache* cache_host, const int64_t* slots, int32_t n, void* k_out, void* v_out, void* stream);
 

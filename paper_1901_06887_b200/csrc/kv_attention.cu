@@ -19,14 +19,16 @@
 // made of the same rounded P.  Every head of a tile of 32 tokens has a scale of P of its own; the tile is added to the running o in
 // fp32; its integer sums start at 1.5 * 2^23 as a bit pattern, so they need no conversion to be read as floats.
 //
-// Bound: memory.  head_dim + 8 bytes per cached token and head; some 500 warp instructions per 32 tokens.
+// Cost.  head_dim + 8 bytes per cached token and head, and 618 warp instructions per 32 tokens (head_dim 128, up to 8 query heads).  No unit is
+// full (4 sequences, 448 thousand tokens): 60 % of the issue slots, logic pipe 49 %, memory 51 %; what shows are the chains of dependent
+// instructions within a tile, which 4 warps a scheduler do not hide.
 //
 // Split.  The tiles (32 tokens of one (sequence, head)) of the whole batch, in order, are cut into equal contiguous shares, one per warp, so
 // ragged batches balance without a schedule from the host: every CTA adds up the lengths itself and its warps find their own starts.  A warp
-// that holds all of a (sequence, head) writes the output; else its part goes to scratch, and a second launch (a CTA per warp, most with
-// nothing to do) joins the parts in order.  A warp's stream of tiles runs on across its (sequence, head)s, so short ones cost no pause: CTAs that
+// that holds all of a (sequence, head) writes the output; else its part goes to scratch, and a second launch (its CTAs go over the sequences' query heads, most
+// with nothing to do) joins the parts in order.  A warp's stream of tiles runs on across its (sequence, head)s, so short ones cost no pause: CTAs that
 // took whole shares, joined their warps in shared memory and refilled their rings for every (sequence, head) spent 76 us on a batch of 64
-// sequences (1 to 8000 tokens), 61 us now.
+// sequences (1 to 8000 tokens), this 61 us (63 with P relative to the largest product).
 //
 // Operand layout.  The inner index of a product may be permuted freely as long as both sides agree, so a lane loads 16
 // (head_dim 128) contiguous bytes of a key row and calls them its slice of every k step; queries are permuted once to match.  For the

@@ -1,9 +1,11 @@
 // The 4-bit cache of keys and values: rounding rows into slots and reading slots back.
 //
-// A row of head_dim elements becomes bias = min, scale = bf16((max - min) / 15) and codes rint((x - bias) / scale), with
-// IEEE subtraction and division, so the stored bytes are a function of the row alone.  Both directions move
-// (2 + 1/2) bytes per element and do a handful of operations on each, so they are bound by memory, and for a step's few
-// tokens by the launch.  A row is one group of lanes, 16 bytes (8 elements) a lane: 8 lanes for head_dim 64, 16 for 128.  A CTA takes one
+// A row of head_dim elements becomes bias = min, scale = bf16((max - min) / 15) and codes rint((x - bias) / scale), as IEEE
+// subtraction and division give them (codes are found by the reciprocal and settled by exact remainders), so the stored bytes are a
+// function of the row alone.  Both directions move (2 + 1/2) bytes per element.  For a step's few tokens they are bound by the launch; for 8191
+// tokens of 8 heads of 128 they take 23 and 14 us cold, 3.3 and 2 times their bytes.  Append: 78 % of the issue slots while an SM has work, which is
+// 82 % of the time (2048 short CTAs of one load - reduce - store chain, 3.5 waves); a quarter fewer instructions left its time as it was.  Read: waits
+// on memory first (codes behind slots), SMs with work 74 % of the time.  A row is one group of lanes, 16 bytes (8 elements) a lane: 8 lanes for head_dim 64, 16 for 128.  A CTA takes one
 // head's keys or values of 16 (32) tokens, or four times as many where that still fills the GPU: then a lane has four loads in flight.
 #include "lm_device.cuh"
 #include "lm_host.h"
@@ -30,7 +32,7 @@ __device__ __forceinline__ float max_nan(float a, float b) {
 constexpr int kThreads = 256;
 
 // grid (2 heads, tokens): a CTA's tokens are ITEMS runs of kThreads / L; neighbouring CTAs take the other heads, keys and values of the same
-// tokens, which lie side by side in a projection's output (append and read of 8191 tokens of 8 heads: 29 us together, instructions bound the first, 22 us, and memory the second, 12).
+// tokens, which lie side by side in a projection's output (append and read of 8191 tokens of 8 heads: 29 us together on rotating inputs).
 template <int D, int ITEMS>
 __global__ void __launch_bounds__(kThreads) kv_append_kernel(CachePtrs kc, CachePtrs vc, int64_t n_slots, int page_shift, KvRows k, KvRows v,
                                                              const int64_t* __restrict__ slots, int n, int token0, OpStatus status) {

@@ -3,6 +3,10 @@
 // Mathematics.  o_i = sum_{j <= i} p_ij v_j / sum_{j <= i} p_ij, p_ij = 2^(c (q_i . k_j - m_i)), c = scale log2(e), in one pass over blocks of
 // 128 keys.  m_i is a running reference, not the maximum: it moves, and the sums so far are rescaled, only when a block's maximum lies
 // more than 8 above it (in log2); until then p is at most 2^8, which fp32 sums and the bf16 p hold as exactly as 1.
+// p is rounded to bf16 before it meets v: kind::f16 takes one type for both operands, and v is bf16.  The roundings (2^-8 of a p at
+// most) are independent and average out, and l sums the unrounded p: over 8192 tokens the output is 0.0021 off 64 bits (relative, root mean square)
+// where its own rounding to bf16 makes 0.0016.  P in two bf16 parts would take the difference away and double P V, half as much again of the tensor
+// pipe's time, which already bounds the kernel together with the exponentials.
 //
 // Tile.  A CTA owns two tiles of 128 rows (one tensor-memory accumulator each) and streams the keys and values that either needs.
 // A row is a (token, head) pair: R heads that share a key/value head (the largest power of two in the group) are packed into the rows, so

@@ -4,14 +4,15 @@
 // exact subtraction of 136) with the weights as the 16-row operand and up to 64 of the tenant's rows as columns; the sum over 64 (or 32)
 // inputs is multiplied with the group's scale in fp32 and added up in fp32.  Nothing is rounded but the sums.
 //
-// Bound: memory, K / 2 + 2 K / group bytes per output and tenant, whatever the number of its rows (up to some 16; beyond, the matrix
-// instructions).  The packed order makes a warp's load 512 contiguous bytes that are the operand of four instructions; the rows' slices of the
+// Cost.  K / 2 + 2 K / group bytes per output and tenant, whatever the number of its rows (up to some 16; beyond, the matrix instructions), and 113
+// warp instructions per 16 outputs x 64 inputs.  No unit is full (8 tenants of 4096 -> 16384, 24 rows): logic pipe 62 %, issue slots 63 %, memory 37 %,
+// with 16 warps an SM to hide latency.  The packed order makes a warp's load 512 contiguous bytes that are the operand of four instructions; the rows' slices of the
 // inner index are chosen so that a lane's inputs are 16 contiguous bytes too.
 //
 // Split.  A CTA takes (tenant, 32 outputs) units in turn, its eight warps every eighth block of 64 inputs; they join through shared memory.
 // Every warp copies its blocks ahead into a ring of its own (cp.async, three or seven blocks ahead, on through the units to come), so the joins and
 // the ends of units do not empty the pipe: loading into registers unit by unit left the kernel waiting for memory (93 us for 8 tenants of
-// 4096 -> 16384, 24 rows).  Two tiles of 16 outputs share the rows' loads and the loop: what is left is bound by instructions.
+// 4096 -> 16384, 24 rows).  Two tiles of 16 outputs share the rows' loads and the loop: 88 us.
 // Which tenants occur is found out by every CTA for itself from the ids (at most 256 a launch): no bucketing launch, and only tenants that
 // occur cost anything.
 #include "lm_device.cuh"
