@@ -135,6 +135,12 @@ __device__ __forceinline__ bool get_item(const Control& s, const PromptParams& p
     return it.len > 0;
 }
 
+// After an abandoned wait: a bounded time for copies and matrix instructions that are still in flight.
+__device__ __noinline__ void settle() {
+    const uint64_t t0 = global_timer_ns();
+    while (global_timer_ns() - t0 < 2000000ull) __nanosleep(1000);
+}
+
 template <int D>
 __global__ void __launch_bounds__(kThreads, 1)
 prompt_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
@@ -222,7 +228,6 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
         asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
         if (lane == 0) {
             int fill = 0;                        // operands put into the ring so far
-            uint32_t raw_phase = 0, raw_used = 0;
             bool ok = true;
             Item it;
             for (int round = 0; ok && get_item(s, p, round, it); ++round) {
@@ -247,17 +252,8 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
                     mbar_expect_tx(full, kOp);
                     for (int h = 0; h < D / 64; ++h)
                         tma_load_3d(kv_smem + slot * kOp + h * kHalf, (x & 1) ? &map_v : &map_k, h * 64, kv_head, it.start + (x >> 1) * kBlock, full);
-                    if (masked) {
-                        mbar_arrive(bar(s.kv_full[slot]));
-                        raw_phase ^= 1u << slot;
-                        raw_used |= 1u << slot;
-                    }
+                    if (masked) mbar_arrive(bar(s.kv_full[slot]));
                 }
-            }
-            if (!ok) {                           // let copies in flight land before the memory goes
-                for (int x = max(0, fill - kSlots); x < fill; ++x) mbar_wait_short(bar(s.kv_full[x % kSlots]), (x / kSlots) & 1);
-                for (int i = 0; i < kSlots; ++i)
-                    if (raw_used >> i & 1) mbar_wait_short(bar(s.v_raw[i]), (raw_phase >> i & 1) ^ 1);
             }
         }
     } else if (warp == 9) {
@@ -559,6 +555,8 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
             mbar_arrive(bar(s.epi_done[buf]));
         }
     }
+    // (every thread gets here, also after an abandoned wait)
+    if (*abort_flag) settle();
     tc_fence_before();
     __syncthreads();
     if (warp == 8) {
