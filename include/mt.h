@@ -306,14 +306,14 @@ mt_status mt_bucket_noalloc(const int32_t* model_ids, int32_t n, int32_t n_model
  *
  * They need mt_init (else MT_ERR_NOT_INIT) but no registered model: every array is the caller's.  Unless marked "host",
  * pointers are device memory of the context's device.  Each call only enqueues kernels on `stream` and returns; arrays
- * must stay valid, and unchanged where they are inputs, until the stream has passed the call.  mt_kv_attention uses
- * scratch that the library keeps PER STREAM (by the stream's id, so the per-thread default stream counts once per thread):
+ * must stay valid, and unchanged where they are inputs, until the stream has passed the call.  mt_kv_attention, mt_cross_attention,
+ * mt_kv_reserve, mt_kv_fork, mt_kv_release and mt_kv_compact use scratch that the library keeps PER STREAM (by the stream's id, so the per-thread default stream counts once per thread):
  * calls on different streams may overlap.  The first call on a stream, and one that needs more than any before, allocates
  * and may synchronise the stream.  At most 64 streams have scratch at a time; a call on another one waits for the device and
  * takes over what was used longest ago.  All of them may be captured into CUDA graphs, with no call before it.  Scratch of a
  * captured call belongs to its graph: graphs may be replayed on any stream, beside each other and beside calls (two
  * instances of one graph must not overlap); it is used again for other graphs when the graph and its instances are gone.
- * All scratch goes away with mt_shutdown, after which a graph with mt_kv_attention must not be replayed.
+ * All scratch goes away with mt_shutdown, after which a graph with such a call must not be replayed.
  *
  * Refusals: MT_ERR_INVALID_ARG null pointer, negative size, unknown type, misaligned pointer, a scale that is not
  * finite; MT_ERR_UNSUPPORTED a size or stride outside what the kernels take; nothing is enqueued then.  A count of zero is
@@ -321,7 +321,7 @@ mt_status mt_bucket_noalloc(const int32_t* model_ids, int32_t n, int32_t n_model
  * concerned are NaN (or left out, where rows are written to a cache), and the sticky status of mt_get_async_status is
  * MT_ERR_BAD_MODEL_ID (ids) or MT_ERR_INVALID_ARG, with the smallest index concerned of the first such call
  * (mt_token_logprobs raises nothing).
- * mt_prompt_attention, whose kernel waits on barriers, can also report MT_ERR_TIMEOUT there (a wait that gave up; its
+ * mt_prompt_attention and mt_cross_attention, whose kernels wait on barriers, can also report MT_ERR_TIMEOUT there (a wait that gave up; its
  * output is then incomplete). */
 typedef enum { MT_BF16 = 0, MT_FP32 = 1 } mt_dtype;
 
@@ -421,6 +421,95 @@ mt_status mt_quant_linear(const mt_quant_bank* bank_host, const void* x, int64_t
 mt_status mt_token_logprobs(const void* logits, int32_t dtype, int64_t row_stride, int32_t n, int32_t vocab,
                             const int32_t* tokens, int32_t top, float* logprobs, float* entropies, int32_t* top_ids,
                             float* top_logprobs, void* stream);
+
+/* Attention of packed queries to an encoder's states, of another length and without a causal mask:
+ *   out[i][h] = sum over the states j of i's sequence of softmax_j(scale * q[i][h] . k[j][h / g]) v[j][h / g],  g = q_heads / kv_heads.
+ * Sequence s has the tokens offsets[s] .. offsets[s+1]-1 (one token each in a token step) and the states ranges[s][0] .. ranges[s][1]-1, so sequences may
+ * share states (several answers about one image) and states may lie in padded rows.  q [n_tokens][q_heads][head_dim], k and v
+ * [n_states][kv_heads][head_dim], bf16, each with its own strides (elements) between tokens and heads and head_dim contiguous; out bf16, contiguous,
+ * must not overlap the inputs.  offsets int32 [n_seqs + 1], not decreasing, between 0 and n_tokens; ranges int32 [n_seqs][2], 0 <= first <= end <= n_states;
+ * rows outside every sequence are not written.  A sequence without states gives zeros.  A sequence whose offsets or range break this is not computed
+ * (its rows are left as they were; sticky status, index of the sequence).  Scores and sums are fp32; the probabilities are rounded to bf16 before they
+ * meet v.  States outside a sequence's range never show, whatever they hold.  (An infinity of v in a state that IS seen may come out as NaN.)
+ * May report MT_ERR_TIMEOUT and uses scratch, see above.  Limits as mt_prompt_attention; n_tokens and n_states at most 2^30. */
+typedef struct {
+    int32_t n_tokens, n_states, n_seqs, q_heads, kv_heads, head_dim;
+    float scale;
+    int64_t q_token_stride, q_head_stride, k_token_stride, k_head_stride, v_token_stride, v_head_stride;
+} mt_cross_desc;
+mt_status mt_cross_attention(const mt_cross_desc* desc_host, const void* q, const void* k, const void* v, const int32_t* offsets,
+                             const int32_t* ranges, void* out, void* stream);
+
+/* Rotary positions: turns pairs of channels of n tokens' heads by position times frequency,
+ *   (x, y) -> (x cos a - y sin a, x sin a + y cos a),   a = positions[i][axis of c] * frequencies[c],   c = 0 .. rotary_dim / 2 - 1,
+ * back with inverse != 0 (which is also the gradient).  Pair c is channels c and c + rotary_dim / 2, or with neighbours != 0 channels 2 c and 2 c + 1; channels
+ * from rotary_dim on are copied.  axes (1 to 4) positions a token, positions int32 [n][axes]: the first sections[0] pairs turn by the first, the next
+ * sections[1] by the second, ..; the sections add up to rotary_dim / 2.  frequencies fp32 [rotary_dim / 2], radians a step.  Angles are formed and
+ * reduced in 64 bits, so far positions lose nothing.  x and out: bf16 or fp32 by dtype, [n][heads][head_dim] with strides (elements, multiples of
+ * 8) between tokens and heads, 16-byte aligned; out may be x with the same strides, and must not overlap it otherwise.
+ * Limits: head_dim a multiple of 8, at most 512; rotary_dim a multiple of 16, at most head_dim. */
+typedef struct {
+    int32_t n, heads, head_dim, rotary_dim, axes;
+    int32_t sections[4];
+    int32_t neighbours, inverse, dtype;
+    int64_t x_token_stride, x_head_stride, out_token_stride, out_head_stride;
+} mt_rotate_desc;
+mt_status mt_rotate(const mt_rotate_desc* desc_host, const void* x, const int32_t* positions, const float* frequencies, void* out, void* stream);
+
+/* Who has which page of a cache: rows of tables and their lengths, as mt_kv_attention takes them, and how many rows hold each page.
+ *   refs     int32 [n_pages], 16-byte aligned; 0: free
+ *   tables   int32 [n_rows][table_width]; entries past a row's last page mean nothing and are left as they are
+ *   lengths  int32 [n_rows], tokens; a row of 0 tokens holds no page
+ * All caches of a model (one a layer) go by one of these.  The calls below change it on the device, in stream order, without the host seeing it; they are
+ * deterministic: pages are handed out lowest first, in the order of the call.  A shared page is always full, so appending to a row never shows in
+ * another.  A row index outside [0, n_rows), one that an earlier place of the same call names, a length that is negative or passes the table, or a page outside
+ * the cache: that place of the call is left out (sticky status MT_ERR_INVALID_ARG, its index).  A place for which no free page is left is left out
+ * too (MT_ERR_OOM); places behind it that need pages then are as well.  They use scratch, see above.
+ * Limits: page_tokens 16, 32, 64, 128 or 256; table_width * page_tokens below 2^31 - 64. */
+typedef struct {
+    int32_t n_pages, page_tokens, n_rows, table_width;
+    int32_t *refs, *tables, *lengths;
+} mt_kv_pages;
+
+/* Makes room for counts[i] more tokens in row rows[i]: new pages where the last one is full, lengths[rows[i]] += counts[i].  slots int64 [n_slots]: the
+ * slots of the new tokens, as mt_kv_append takes them, of all places one behind the other; -1 for the tokens of a place that is left out, and behind the last.  A place
+ * whose tokens pass n_slots is left out (MT_ERR_INVALID_ARG), and so is one with a negative count, which takes no slots. */
+mt_status mt_kv_reserve(const mt_kv_pages* pages_host, const int32_t* rows, const int32_t* counts, int32_t n, int64_t* slots, int64_t n_slots,
+                        void* stream);
+
+/* Row children[i] becomes what row parents[i] was before the call: the parent's full pages are shared, a partly filled last page is to be copied to a free one, and
+ * the pages that the child held are given back.  copies int32 [n][3]: page from, page to, tokens; -1, -1, 0 where there is nothing to copy.  Give them to mt_kv_copy
+ * before anything is appended.  A row may be a parent several times, and parent and child at once (beams that change places); a row that is its own parent stays
+ * as it is.  Pages that the call gives back are not handed out by the same call, so no page is both copied from and copied to. */
+mt_status mt_kv_fork(const mt_kv_pages* pages_host, const int32_t* parents, const int32_t* children, int32_t n, int32_t* copies, void* stream);
+
+/* Rows that have ended: their pages are given back, their lengths become 0. */
+mt_status mt_kv_release(const mt_kv_pages* pages_host, const int32_t* rows, int32_t n, void* stream);
+
+/* Moves used pages to the front: of U used pages those at U and above go to the free ones below U, the i-th to the i-th, at most n of them; tables and refs follow, for
+ * all rows.  copies as above, one a page moved, full pages; behind the last -1, -1, 0.  (n of half the pages is always enough.)  A row whose length is out of
+ * range is not looked at (MT_ERR_INVALID_ARG, the row). */
+mt_status mt_kv_compact(const mt_kv_pages* pages_host, int32_t* copies, int32_t n, void* stream);
+
+/* Copies the first tokens' rows of pages, codes and parameters of keys and values, in each of n_caches caches with the same n_pages and page_tokens: copies int32
+ * [n][3], page from, page to, tokens; -1, -1 is left out.  Anything else outside the cache, or a number of tokens outside [0, page_tokens], is left out and sets the
+ * sticky status.  No page may be copied to twice, or be copied from and to. */
+mt_status mt_kv_copy(const mt_kv_cache* const* caches_host, int32_t n_caches, const int32_t* copies, int32_t n, void* stream);
+
+/* Draws a token from each of n rows of `vocab` logits (bf16 or fp32 by dtype, row_stride elements apart, any alignment of whole elements).
+ *   w_i = exp((x_i - max x) / temperature); in the order of falling logits, equal ones by rising index, those are kept that pass all of
+ *   top_k > 0    the first top_k
+ *   top_p < 1    the fewest whose mass reaches top_p times that of the whole row
+ *   min_p > 0    w_i >= min_p
+ * and the first in any case.  ids[i] is the first token, in the order of the vocabulary, at which the sum of kept w exceeds uniform[i] (in [0, 1)) times all of it;
+ * logprobs[i] its log probability among the kept (may be NULL).  temperature, top_k, top_p, min_p and uniform are arrays of n; NULL: 1, none, none, none.  Temperature 0, or a
+ * min_p above 1, takes the first.  Weights are 64-bit whole numbers, the largest 2^46 (fewer in rows of more than 2^16 logits), so draws do not depend on the
+ * order of summing; what is below one of those units is never drawn.  A row without a distribution (nothing but minus infinity, a NaN or plus infinity) gives id -1 and NaN;
+ * so does one with a negative, infinite or NaN temperature, a NaN limit or a uniform number outside [0, 1), with the sticky status MT_ERR_INVALID_ARG.
+ * Limits: vocab below 2^30. */
+mt_status mt_token_sample(const void* logits, int32_t dtype, int64_t row_stride, int32_t n, int32_t vocab, const float* temperature,
+                          const int32_t* top_k, const float* top_p, const float* min_p, const float* uniform, int32_t* ids, float* logprobs,
+                          void* stream);
 
 #ifdef __cplusplus
 }

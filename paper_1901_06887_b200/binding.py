@@ -27,7 +27,8 @@ EXPORTS = ["mt_init", "mt_shutdown", "mt_register_model", "mt_infer", "mt_infer_
            "mt_debug_schedule_balance", "mt_set_cache_bytes", "mt_prefetch", "mt_get_cache_stats", "mt_cache_sim_create",
            "mt_cache_sim_access", "mt_cache_sim_release", "mt_cache_sim_stats", "mt_cache_sim_destroy", "mt_output_elems", "mt_input_elems",
            "mt_prompt_attention", "mt_kv_append", "mt_kv_read", "mt_kv_attention", "mt_quant_packed_bytes", "mt_quant_pack",
-           "mt_quant_linear", "mt_token_logprobs"]
+           "mt_quant_linear", "mt_token_logprobs", "mt_cross_attention", "mt_rotate", "mt_kv_reserve", "mt_kv_fork", "mt_kv_release",
+           "mt_kv_compact", "mt_kv_copy", "mt_token_sample"]
 
 
 class MtError(RuntimeError):
@@ -52,11 +53,20 @@ class LayerDesc(ctypes.Structure):
 
 # mt_prompt_desc as bytes: n_tokens, n_seqs, q_heads, kv_heads, head_dim, scale, then token and head strides of q, k, v
 _prompt_desc = struct.Struct("=5if6q").pack
+# mt_cross_desc: n_tokens, n_states, n_seqs, q_heads, kv_heads, head_dim, scale, four bytes of padding, strides of q, k, v
+_cross_desc = struct.Struct("=6if4x6q").pack
+# mt_rotate_desc: n, heads, head_dim, rotary_dim, axes, four sections, neighbours, inverse, dtype, token and head strides of x and out
+_rotate_desc = struct.Struct("=12i4q").pack
 
 
 class KvCacheDesc(ctypes.Structure):
     _fields_ = [(k, ctypes.c_int32) for k in ("n_pages", "page_tokens", "kv_heads", "head_dim")] + \
                [(k, ctypes.c_void_p) for k in ("k_codes", "k_params", "v_codes", "v_params")]
+
+
+class KvPagesDesc(ctypes.Structure):
+    _fields_ = [(k, ctypes.c_int32) for k in ("n_pages", "page_tokens", "n_rows", "table_width")] + \
+               [(k, ctypes.c_void_p) for k in ("refs", "tables", "lengths")]
 
 
 class QuantBankDesc(ctypes.Structure):
@@ -116,6 +126,14 @@ def lib() -> ctypes.CDLL:
         l.mt_quant_pack.argtypes = [vp, vp, i32, i32, i32, i32, vp, vp]
         l.mt_quant_linear.argtypes = [vp, vp, i64, vp, i32, vp, i64, i32, vp]
         l.mt_token_logprobs.argtypes = [vp, i32, i64, i32, i32, vp, i32, vp, vp, vp, vp, vp]
+        l.mt_cross_attention.argtypes = [vp] * 8
+        l.mt_rotate.argtypes = [vp] * 6
+        l.mt_kv_reserve.argtypes = [vp, vp, vp, i32, vp, i64, vp]
+        l.mt_kv_fork.argtypes = [vp, vp, vp, i32, vp, vp]
+        l.mt_kv_release.argtypes = [vp, vp, i32, vp]
+        l.mt_kv_compact.argtypes = [vp, vp, i32, vp]
+        l.mt_kv_copy.argtypes = [vp, i32, vp, i32, vp]
+        l.mt_token_sample.argtypes = [vp, i32, i64, i32, i32] + [vp] * 8
         for name in EXPORTS:
             if name != "mt_status_string":
                 getattr(l, name).restype = ctypes.c_int
@@ -599,3 +617,182 @@ def mt_token_logprobs(logits, tokens, logprobs, entropies=None, top_ids=None, to
                                              None if top_logprobs is None else top_logprobs.data_ptr(), _stream_handle(stream))
     if code:
         raise MtError(code, "mt_token_logprobs")
+
+
+def mt_cross_attention(q, k, v, offsets, ranges, out, scale: Optional[float] = None, stream=None) -> None:
+    """Attention to an encoder's states: q bf16 [n, q_heads, dim], k and v [states, kv_heads, dim] (any token and head strides), offsets int32
+    [sequences + 1] of the queries, ranges int32 [sequences, 2] (first state, end), out bf16 like q, contiguous.  scale: 1 / sqrt(dim) if None."""
+    T = _types()
+    bf16, i32 = T.bf16, T.i32
+    try:
+        n, hq, d = shape = q.shape
+        m, hk, dk = kshape = k.shape
+        q0, q1, q2 = q.stride()
+        k0, k1, k2 = k.stride()
+        v0, v1, v2 = v.stride()
+        seqs, two = ranges.shape
+    except ValueError:
+        _refuse("mt_cross_attention")
+    if not (q.dtype is bf16 and k.dtype is bf16 and v.dtype is bf16 and out.dtype is bf16 and offsets.dtype is i32 and ranges.dtype is i32 and
+            q.get_device() == k.get_device() == v.get_device() == out.get_device() == offsets.get_device() == ranges.get_device() == _device and
+            dk == d and v.shape == kshape and out.shape == shape and out.is_contiguous() and offsets.dim() == 1 and offsets.is_contiguous() and
+            offsets.numel() == seqs + 1 and two == 2 and ranges.is_contiguous() and (n == 0 or q2 == 1) and (m == 0 or k2 == v2 == 1)):
+        _refuse("mt_cross_attention")
+    if m == 0:
+        k0 = v0 = hk * d               # (strides of what holds nothing)
+        k1 = v1 = d
+    try:
+        desc = _cross_desc(n, m, seqs, hq, hk, d, d ** -0.5 if scale is None else scale, q0, q1, k0, k1, v0, v1)
+    except (struct.error, OverflowError, ZeroDivisionError):
+        _refuse("mt_cross_attention")
+    code = (_lib or lib()).mt_cross_attention(desc, q.data_ptr(), k.data_ptr(), v.data_ptr(), offsets.data_ptr(), ranges.data_ptr(),
+                                              out.data_ptr(), _stream_handle(stream))
+    if code:
+        raise MtError(code, "mt_cross_attention")
+
+
+def mt_rotate(x, positions, frequencies, out, sections: Optional[Sequence[int]] = None, neighbours: bool = False, inverse: bool = False,
+              stream=None) -> None:
+    """Rotary positions: x bf16 or fp32 [n, heads, dim] (any token and head strides), positions int32 [n] or [n, axes], frequencies fp32
+    [rotary / 2], out like x (or x itself).  sections: pairs of each axis, adding up to rotary / 2 (None: one axis has them all)."""
+    T = _types()
+    wide = x.dtype is T.f32
+    try:
+        n, h, d = shape = x.shape
+        x0, x1, x2 = x.stride()
+        o0, o1, o2 = out.stride()
+    except ValueError:
+        _refuse("mt_rotate")
+    half = frequencies.numel()
+    axes = 1 if positions.dim() == 1 else positions.shape[-1]
+    cut = (half,) if sections is None else tuple(sections)
+    if not ((wide or x.dtype is T.bf16) and out.dtype is x.dtype and positions.dtype is T.i32 and frequencies.dtype is T.f32 and
+            x.get_device() == out.get_device() == positions.get_device() == frequencies.get_device() == _device and out.shape == shape and
+            0 < positions.dim() <= 2 and positions.shape[0] == n and positions.is_contiguous() and frequencies.dim() == 1 and
+            frequencies.is_contiguous() and len(cut) == axes <= 4 and (n == 0 or d <= 1 or x2 == o2 == 1)):
+        _refuse("mt_rotate")
+    try:
+        desc = _rotate_desc(n, h, d, 2 * half, axes, *cut, *(0,) * (4 - axes), bool(neighbours), bool(inverse), 1 if wide else 0, x0, x1, o0, o1)
+    except struct.error:
+        _refuse("mt_rotate")
+    code = (_lib or lib()).mt_rotate(desc, x.data_ptr(), positions.data_ptr(), frequencies.data_ptr(), out.data_ptr(), _stream_handle(stream))
+    if code:
+        raise MtError(code, "mt_rotate")
+
+
+class KvPages:
+    """The caller's tensors as the book of a cache's pages: refs int32 [pages], tables int32 [rows, width], lengths int32 [rows], contiguous.  Keeps them
+    alive; allocates nothing."""
+
+    def __init__(self, refs, tables, lengths, page_tokens: int):
+        T, at = _types(), _place(refs)
+        if not (refs.dtype is T.i32 and tables.dtype is T.i32 and lengths.dtype is T.i32 and refs.is_cuda and
+                refs.get_device() == tables.get_device() == lengths.get_device() == at and refs.dim() == 1 and tables.dim() == 2 and
+                lengths.dim() == 1 and lengths.numel() == tables.shape[0] and refs.is_contiguous() and tables.is_contiguous() and
+                lengths.is_contiguous() and max(refs.numel(), *tables.shape) <= _MOST and 0 <= page_tokens <= _MOST):
+            _refuse("KvPages", False)
+        self.refs, self.tables, self.lengths, self.page_tokens = refs, tables, lengths, page_tokens
+        self.desc = KvPagesDesc(refs.numel(), page_tokens, *tables.shape, refs.data_ptr(), tables.data_ptr(), lengths.data_ptr())
+        self.ref = ctypes.byref(self.desc)
+
+    @classmethod
+    def empty(cls, n_pages: int, page_tokens: int, rows: int, table_width: int, device="cuda"):
+        """A new book: every page free, every row without tokens."""
+        import torch
+        zeros = lambda *shape: torch.zeros(shape, dtype=torch.int32, device=device)
+        return cls(zeros(n_pages), zeros(rows, table_width), zeros(rows), page_tokens)
+
+
+def _is_ints(t, n: int) -> bool:
+    return t.dtype is _Types.i32 and t.get_device() == _device and t.dim() == 1 and t.numel() == n and t.is_contiguous() and n <= _MOST
+
+
+def _is_copies(t) -> bool:
+    return t.dtype is _Types.i32 and t.get_device() == _device and t.dim() == 2 and t.shape[1] == 3 and t.is_contiguous() and t.shape[0] <= _MOST
+
+
+def mt_kv_reserve(pages: KvPages, rows, counts, slots, stream=None) -> None:
+    """Room for counts[i] more tokens in row rows[i] (int32); slots int64 (at least sum(counts)): where they go, for mt_kv_append."""
+    T, n = _types(), rows.numel()
+    if not (_is_ints(rows, n) and _is_ints(counts, n) and slots.dtype is T.i64 and slots.get_device() == _device and slots.dim() == 1 and slots.is_contiguous()):
+        _refuse("mt_kv_reserve")
+    code = (_lib or lib()).mt_kv_reserve(pages.ref, rows.data_ptr(), counts.data_ptr(), n, slots.data_ptr(), slots.numel(), _stream_handle(stream))
+    if code:
+        raise MtError(code, "mt_kv_reserve")
+
+
+def mt_kv_fork(pages: KvPages, parents, children, copies, stream=None) -> None:
+    """Row children[i] becomes what row parents[i] was (int32); copies int32 [n, 3]: what mt_kv_copy has to copy."""
+    _types()
+    n = parents.numel()
+    if not (_is_ints(parents, n) and _is_ints(children, n) and _is_copies(copies) and copies.shape[0] == n):
+        _refuse("mt_kv_fork")
+    code = (_lib or lib()).mt_kv_fork(pages.ref, parents.data_ptr(), children.data_ptr(), n, copies.data_ptr(), _stream_handle(stream))
+    if code:
+        raise MtError(code, "mt_kv_fork")
+
+
+def mt_kv_release(pages: KvPages, rows, stream=None) -> None:
+    """Gives the pages of rows (int32) back; their lengths become 0."""
+    _types()
+    n = rows.numel()
+    if not _is_ints(rows, n):
+        _refuse("mt_kv_release")
+    code = (_lib or lib()).mt_kv_release(pages.ref, rows.data_ptr(), n, _stream_handle(stream))
+    if code:
+        raise MtError(code, "mt_kv_release")
+
+
+def mt_kv_compact(pages: KvPages, copies, stream=None) -> None:
+    """Moves used pages to the front, at most copies.shape[0] of them; copies int32 [n, 3]: what mt_kv_copy has to copy."""
+    _types()
+    if not _is_copies(copies):
+        _refuse("mt_kv_compact")
+    code = (_lib or lib()).mt_kv_compact(pages.ref, copies.data_ptr(), copies.shape[0], _stream_handle(stream))
+    if code:
+        raise MtError(code, "mt_kv_compact")
+
+
+class KvCopier:
+    """The caches of a model (one a layer, with the same pages) that mt_kv_copy copies in.  Keeps them alive."""
+
+    def __init__(self, caches: Sequence[KvCache]):
+        self.caches = list(caches)
+        self.array = (ctypes.POINTER(KvCacheDesc) * len(self.caches))(*[ctypes.pointer(c.desc) for c in self.caches])
+        self.n = len(self.caches)
+
+
+def mt_kv_copy(copier: KvCopier, copies, stream=None) -> None:
+    """Copies pages in every cache: copies int32 [n, 3], page from, page to, tokens; -1, -1 is left out."""
+    _types()
+    if not _is_copies(copies):
+        _refuse("mt_kv_copy")
+    code = (_lib or lib()).mt_kv_copy(copier.array, copier.n, copies.data_ptr(), copies.shape[0], _stream_handle(stream))
+    if code:
+        raise MtError(code, "mt_kv_copy")
+
+
+def mt_token_sample(logits, uniform, ids, logprobs=None, temperature=None, top_k=None, top_p=None, min_p=None, stream=None) -> None:
+    """logits bf16 or fp32 [n, vocab] (any row stride), uniform fp32 [n] in [0, 1) -> ids int32 [n], logprobs fp32 [n] (or None).  temperature, top_p and
+    min_p fp32 [n], top_k int32 [n], or None."""
+    T = _types()
+    f32 = T.f32
+    try:
+        n, vocab = logits.shape
+        s0, s1 = logits.stride()
+    except ValueError:
+        _refuse("mt_token_sample")
+    wide = logits.dtype is f32
+    ok = (wide or logits.dtype is T.bf16) and logits.get_device() == _device and (n == 0 or vocab <= 1 or s1 == 1) and n <= _MOST and vocab <= _MOST and \
+        _is_ints(ids, n) and (top_k is None or _is_ints(top_k, n))
+    for x in (uniform, logprobs, temperature, top_p, min_p):
+        if x is not None:
+            ok = ok and x.dtype is f32 and x.get_device() == _device and x.dim() == 1 and x.numel() == n and x.is_contiguous()
+    if not ok:
+        _refuse("mt_token_sample")
+    code = (_lib or lib()).mt_token_sample(logits.data_ptr(), 1 if wide else 0, s0, n, vocab, None if temperature is None else temperature.data_ptr(),
+                                           None if top_k is None else top_k.data_ptr(), None if top_p is None else top_p.data_ptr(),
+                                           None if min_p is None else min_p.data_ptr(), uniform.data_ptr(), ids.data_ptr(),
+                                           None if logprobs is None else logprobs.data_ptr(), _stream_handle(stream))
+    if code:
+        raise MtError(code, "mt_token_sample")

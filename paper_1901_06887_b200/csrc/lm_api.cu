@@ -71,6 +71,15 @@ mt_status check_cache(const mt_kv_cache* c) {
     return MT_OK;
 }
 
+mt_status check_pages(const mt_kv_pages* p) {
+    if (!p || p->n_pages < 0 || p->n_rows < 0 || p->table_width < 0) return MT_ERR_INVALID_ARG;
+    if (p->page_tokens < 16 || p->page_tokens > 256 || (p->page_tokens & (p->page_tokens - 1))) return MT_ERR_UNSUPPORTED;
+    if (p->n_pages > INT_MAX - 256 || (int64_t)p->table_width * p->page_tokens > INT_MAX - 64) return MT_ERR_UNSUPPORTED;
+    if ((p->n_pages > 0 && !p->refs) || (p->n_rows > 0 && (!p->lengths || (p->table_width > 0 && !p->tables)))) return MT_ERR_INVALID_ARG;
+    if (misaligned(p->refs) || misaligned(p->tables, 4) || misaligned(p->lengths, 4)) return MT_ERR_INVALID_ARG;
+    return MT_OK;
+}
+
 mt_status check_quant(int K, int N, int group) {
     if (K <= 0 || N <= 0 || group <= 0) return MT_ERR_INVALID_ARG;
     if (N > INT_MAX - (1 << 20)) return MT_ERR_UNSUPPORTED;         // the kernels round N up, and step past it
@@ -191,6 +200,7 @@ cudaError_t configure_operators() {
     if (e == cudaSuccess) e = configure_kv_attention();
     if (e == cudaSuccess) e = configure_quant_linear();
     if (e == cudaSuccess) e = configure_token_logprobs();
+    if (e == cudaSuccess) e = configure_cross_attention();
     return e;
 }
 
@@ -343,6 +353,141 @@ mt_status mt_token_logprobs(const void* logits, int32_t dtype, int64_t row_strid
     a.logits = logits; a.fp32 = dtype == MT_FP32; a.row_stride = row_stride; a.n = n; a.vocab = vocab; a.tokens = tokens; a.top = top;
     a.logprobs = logprobs; a.entropies = entropies; a.top_ids = top_ids; a.top_logprobs = top_logprobs;
     return launch_token_logprobs(a, c, static_cast<cudaStream_t>(stream));
+}
+
+mt_status mt_cross_attention(const mt_cross_desc* d, const void* q, const void* k, const void* v, const int32_t* offsets,
+                             const int32_t* ranges, void* out, void* stream) {
+    if (!d || d->n_tokens < 0 || d->n_states < 0 || d->n_seqs < 0 || d->q_heads <= 0 || d->kv_heads <= 0 || !std::isfinite(d->scale)) return MT_ERR_INVALID_ARG;
+    if (!(d->head_dim == 64 || d->head_dim == 128) || d->q_heads % d->kv_heads || d->q_heads > 65535) return MT_ERR_UNSUPPORTED;
+    if (d->n_tokens > (1 << 30) || d->n_states > (1 << 30)) return MT_ERR_UNSUPPORTED;
+    const int64_t hd = d->head_dim;
+    if (bad_stride(d->q_token_stride, hd) || bad_stride(d->k_token_stride, hd) || bad_stride(d->v_token_stride, hd) ||
+        bad_stride(d->q_head_stride, hd) || bad_stride(d->k_head_stride, hd) || bad_stride(d->v_head_stride, hd))
+        return MT_ERR_UNSUPPORTED;
+    std::unique_lock<std::mutex> lk;
+    OpContext c;
+    mt_status st = op_begin(&lk, &c);
+    if (st != MT_OK) return st;
+    if (d->n_tokens == 0 || d->n_seqs == 0) return MT_OK;
+    if (!q || (d->n_states > 0 && (!k || !v)) || !offsets || !ranges || !out) return MT_ERR_INVALID_ARG;
+    if (misaligned(q) || misaligned(k) || misaligned(v) || misaligned(out) || misaligned(offsets, 4) || misaligned(ranges, 4)) return MT_ERR_INVALID_ARG;
+    CrossArgs a;
+    a.d = *d;
+    a.q = static_cast<const uint16_t*>(q); a.k = static_cast<const uint16_t*>(k); a.v = static_cast<const uint16_t*>(v);
+    a.offsets = offsets; a.ranges = ranges; a.out = static_cast<uint16_t*>(out); a.status = c.status;
+    return launch_cross_attention(a, c, static_cast<cudaStream_t>(stream));
+}
+
+mt_status mt_rotate(const mt_rotate_desc* d, const void* x, const int32_t* positions, const float* frequencies, void* out, void* stream) {
+    if (!d || d->n < 0 || d->heads <= 0 || d->head_dim <= 0 || d->rotary_dim <= 0 || (d->dtype != MT_BF16 && d->dtype != MT_FP32)) return MT_ERR_INVALID_ARG;
+    if (d->axes < 1 || d->axes > 4) return MT_ERR_INVALID_ARG;
+    int64_t pairs = 0;
+    for (int i = 0; i < d->axes; ++i) {
+        if (d->sections[i] < 0) return MT_ERR_INVALID_ARG;
+        pairs += d->sections[i];
+    }
+    if (pairs * 2 != d->rotary_dim || d->rotary_dim > d->head_dim) return MT_ERR_INVALID_ARG;
+    if (d->head_dim % 8 || d->head_dim > 512 || d->rotary_dim % 16 || d->heads > 65535) return MT_ERR_UNSUPPORTED;
+    if (bad_stride(d->x_token_stride, 0) || bad_stride(d->x_head_stride, 0) || bad_stride(d->out_token_stride, 0) || bad_stride(d->out_head_stride, 0))
+        return MT_ERR_UNSUPPORTED;
+    if ((d->n > 1 && d->out_token_stride < d->head_dim) || (d->heads > 1 && d->out_head_stride < d->head_dim)) return MT_ERR_INVALID_ARG;
+    std::unique_lock<std::mutex> lk;
+    OpContext c;
+    mt_status st = op_begin(&lk, &c);
+    if (st != MT_OK || d->n == 0) return st;
+    if (!x || !positions || !frequencies || !out || misaligned(x) || misaligned(out) || misaligned(positions, 4) || misaligned(frequencies, 4))
+        return MT_ERR_INVALID_ARG;
+    RotateArgs a;
+    a.n = d->n; a.heads = d->heads; a.head_dim = d->head_dim; a.rotary_dim = d->rotary_dim; a.axes = d->axes;
+    for (int i = 0; i < 4; ++i) a.sections[i] = d->sections[i];
+    a.neighbours = d->neighbours != 0; a.inverse = d->inverse != 0; a.fp32 = d->dtype == MT_FP32;
+    a.x = x; a.x_token_stride = d->x_token_stride; a.x_head_stride = d->x_head_stride;
+    a.positions = positions; a.frequencies = frequencies;
+    a.out = out; a.out_token_stride = d->out_token_stride; a.out_head_stride = d->out_head_stride;
+    return to_status(launch_rotate(a, static_cast<cudaStream_t>(stream)));
+}
+
+mt_status mt_kv_reserve(const mt_kv_pages* pages, const int32_t* rows, const int32_t* counts, int32_t n, int64_t* slots, int64_t n_slots, void* stream) {
+    mt_status st = check_pages(pages);
+    if (st != MT_OK) return st;
+    if (n < 0 || n_slots < 0) return MT_ERR_INVALID_ARG;
+    std::unique_lock<std::mutex> lk;
+    OpContext c;
+    st = op_begin(&lk, &c);
+    if (st != MT_OK || (n == 0 && n_slots == 0)) return st;
+    if ((n > 0 && (!rows || !counts)) || (n_slots > 0 && !slots) || misaligned(rows, 4) || misaligned(counts, 4) || misaligned(slots, 8)) return MT_ERR_INVALID_ARG;
+    return launch_kv_pages({KvPagesArgs::kReserve, *pages, n, rows, counts, nullptr, slots, n_slots, c.status}, static_cast<cudaStream_t>(stream));
+}
+
+mt_status mt_kv_fork(const mt_kv_pages* pages, const int32_t* parents, const int32_t* children, int32_t n, int32_t* copies, void* stream) {
+    mt_status st = check_pages(pages);
+    if (st != MT_OK) return st;
+    if (n < 0) return MT_ERR_INVALID_ARG;
+    std::unique_lock<std::mutex> lk;
+    OpContext c;
+    st = op_begin(&lk, &c);
+    if (st != MT_OK || n == 0) return st;
+    if (!parents || !children || !copies || misaligned(parents, 4) || misaligned(children, 4) || misaligned(copies, 4)) return MT_ERR_INVALID_ARG;
+    return launch_kv_pages({KvPagesArgs::kFork, *pages, n, children, parents, copies, nullptr, 0, c.status}, static_cast<cudaStream_t>(stream));
+}
+
+mt_status mt_kv_release(const mt_kv_pages* pages, const int32_t* rows, int32_t n, void* stream) {
+    mt_status st = check_pages(pages);
+    if (st != MT_OK) return st;
+    if (n < 0) return MT_ERR_INVALID_ARG;
+    std::unique_lock<std::mutex> lk;
+    OpContext c;
+    st = op_begin(&lk, &c);
+    if (st != MT_OK || n == 0) return st;
+    if (!rows || misaligned(rows, 4)) return MT_ERR_INVALID_ARG;
+    return launch_kv_pages({KvPagesArgs::kRelease, *pages, n, rows, nullptr, nullptr, nullptr, 0, c.status}, static_cast<cudaStream_t>(stream));
+}
+
+mt_status mt_kv_compact(const mt_kv_pages* pages, int32_t* copies, int32_t n, void* stream) {
+    mt_status st = check_pages(pages);
+    if (st != MT_OK) return st;
+    if (n < 0) return MT_ERR_INVALID_ARG;
+    std::unique_lock<std::mutex> lk;
+    OpContext c;
+    st = op_begin(&lk, &c);
+    if (st != MT_OK || n == 0) return st;
+    if (!copies || misaligned(copies, 4)) return MT_ERR_INVALID_ARG;
+    return launch_kv_pages({KvPagesArgs::kCompact, *pages, n, nullptr, nullptr, copies, nullptr, 0, c.status}, static_cast<cudaStream_t>(stream));
+}
+
+mt_status mt_kv_copy(const mt_kv_cache* const* caches, int32_t n_caches, const int32_t* copies, int32_t n, void* stream) {
+    if (n_caches < 0 || n < 0 || (n_caches > 0 && !caches)) return MT_ERR_INVALID_ARG;
+    for (int i = 0; i < n_caches; ++i) {
+        const mt_status st = check_cache(caches[i]);
+        if (st != MT_OK) return st;
+        if (caches[i]->n_pages != caches[0]->n_pages || caches[i]->page_tokens != caches[0]->page_tokens) return MT_ERR_INVALID_ARG;
+    }
+    std::unique_lock<std::mutex> lk;
+    OpContext c;
+    mt_status st = op_begin(&lk, &c);
+    if (st != MT_OK || n == 0 || n_caches == 0) return st;
+    if (!copies || misaligned(copies, 4)) return MT_ERR_INVALID_ARG;
+    return to_status(launch_kv_copy(caches, n_caches, copies, n, c.status, static_cast<cudaStream_t>(stream)));
+}
+
+mt_status mt_token_sample(const void* logits, int32_t dtype, int64_t row_stride, int32_t n, int32_t vocab, const float* temperature,
+                          const int32_t* top_k, const float* top_p, const float* min_p, const float* uniform, int32_t* ids, float* logprobs,
+                          void* stream) {
+    if (n < 0 || vocab <= 0 || (dtype != MT_BF16 && dtype != MT_FP32)) return MT_ERR_INVALID_ARG;
+    if (vocab >= (1 << 30) || row_stride < 0 || row_stride >= (int64_t(1) << 36)) return MT_ERR_UNSUPPORTED;
+    std::unique_lock<std::mutex> lk;
+    OpContext c;
+    mt_status st = op_begin(&lk, &c);
+    if (st != MT_OK || n == 0) return st;
+    if (!logits || !uniform || !ids) return MT_ERR_INVALID_ARG;
+    if (misaligned(logits, dtype == MT_FP32 ? 4 : 2) || misaligned(temperature, 4) || misaligned(top_k, 4) || misaligned(top_p, 4) ||
+        misaligned(min_p, 4) || misaligned(uniform, 4) || misaligned(ids, 4) || misaligned(logprobs, 4))
+        return MT_ERR_INVALID_ARG;
+    SampleArgs a;
+    a.logits = logits; a.fp32 = dtype == MT_FP32; a.row_stride = row_stride; a.n = n; a.vocab = vocab;
+    a.temperature = temperature; a.top_k = top_k; a.top_p = top_p; a.min_p = min_p; a.uniform = uniform;
+    a.ids = ids; a.logprobs = logprobs; a.status = c.status;
+    return launch_token_sample(a, c, static_cast<cudaStream_t>(stream));
 }
 
 }  // extern "C"

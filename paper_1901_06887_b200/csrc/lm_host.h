@@ -1,5 +1,5 @@
-// Launchers of the language-model operators (prompt_attention.cu, kv_cache.cu, kv_attention.cu, quant_linear.cu,
-// token_logprobs.cu), called by lm_api.cu after it has checked the arguments.
+// Launchers of the language-model operators (prompt_attention.cu, cross_attention.cu, rotate.cu, kv_cache.cu, kv_pages.cu, kv_attention.cu,
+// quant_linear.cu, token_logprobs.cu, token_sample.cu), called by lm_api.cu after it has checked the arguments.
 #pragma once
 
 #include <cuda_runtime.h>
@@ -93,6 +93,56 @@ struct LogprobArgs {
 };
 cudaError_t configure_token_logprobs();
 mt_status launch_token_logprobs(const LogprobArgs& a, const OpContext& c, cudaStream_t s);
+
+struct CrossArgs {
+    mt_cross_desc d;
+    const uint16_t *q, *k, *v;
+    const int32_t *offsets, *ranges;
+    uint16_t* out;
+    OpStatus status;
+};
+cudaError_t configure_cross_attention();
+mt_status launch_cross_attention(const CrossArgs& a, const OpContext& c, cudaStream_t s);
+
+struct RotateArgs {
+    int n, heads, head_dim, rotary_dim, axes;
+    int sections[4];
+    int neighbours, inverse, fp32;
+    const void* x;
+    int64_t x_token_stride, x_head_stride;
+    const int32_t* positions;
+    const float* frequencies;
+    void* out;
+    int64_t out_token_stride, out_head_stride;
+};
+cudaError_t launch_rotate(const RotateArgs& a, cudaStream_t s);
+
+struct KvPagesArgs {
+    enum What { kReserve, kFork, kRelease, kCompact } what;
+    mt_kv_pages k;
+    int n;
+    const int32_t *rows, *other;    // reserve: rows, counts; fork: children, parents; release: rows
+    int32_t* copies;
+    int64_t* slots;
+    int64_t n_slots;
+    OpStatus status;
+};
+mt_status launch_kv_pages(const KvPagesArgs& a, cudaStream_t s);
+cudaError_t launch_kv_copy(const mt_kv_cache* const* caches, int n_caches, const int32_t* copies, int n, const OpStatus& status, cudaStream_t s);
+
+struct SampleArgs {
+    const void* logits;
+    int fp32;
+    int64_t row_stride;
+    int n, vocab;
+    const float* temperature;
+    const int32_t* top_k;
+    const float *top_p, *min_p, *uniform;
+    int32_t* ids;
+    float* logprobs;
+    OpStatus status;
+};
+mt_status launch_token_sample(const SampleArgs& a, const OpContext& c, cudaStream_t s);
 
 // Scratch of at least `bytes` (256-byte aligned, contents left over from earlier calls) for work on stream `s`: the stream's, or the
 // graph's that `s` is captured into.  (Mutex held.)
