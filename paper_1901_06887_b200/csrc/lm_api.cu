@@ -201,6 +201,7 @@ cudaError_t configure_operators() {
     if (e == cudaSuccess) e = configure_quant_linear();
     if (e == cudaSuccess) e = configure_token_logprobs();
     if (e == cudaSuccess) e = configure_cross_attention();
+    if (e == cudaSuccess) e = configure_token_sample();
     return e;
 }
 

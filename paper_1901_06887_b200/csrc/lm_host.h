@@ -142,6 +142,7 @@ struct SampleArgs {
     float* logprobs;
     OpStatus status;
 };
+cudaError_t configure_token_sample();
 mt_status launch_token_sample(const SampleArgs& a, const OpContext& c, cudaStream_t s);
 
 // Scratch of at least `bytes` (256-byte aligned, contents left over from earlier calls) for work on stream `s`: the stream's, or the

@@ -20,10 +20,13 @@ namespace mt {
 namespace {
 
 constexpr int kThreads = 512, kWarps = kThreads / 32;
-constexpr int kBins = 1024;
-constexpr int kList = 1024;
+constexpr int kBins = 2 * kThreads;
+constexpr int kFine = 16, kCoarse = kBins / kFine;
+constexpr int kList = kThreads;
 constexpr int kMaxParts = 8;
-constexpr int kMinPart = 4096;                // logits of a part, at least
+static_assert(kBins == 2 * kThreads && kThreads == kMaxParts * kCoarse && kFine == 16, "");
+constexpr int kMinPart = 2048;                // logits of a part, at least
+constexpr int kHeldBytes = 65536;             // of a part that stays in shared memory, at most: two CTAs an SM
 using u64 = unsigned long long;
 
 struct Params {
@@ -34,28 +37,20 @@ struct Params {
 };
 
 struct Shared {
-    uint32_t count[kBins], lo[kBins], hi[kBins];
-    uint32_t key[kList];
-    int32_t index[kList];
-    uint32_t part_key[kList];                 // this part's share of the list
-    int32_t part_index[kList];
-    u64 sorted[kList];
-    int32_t order[kList];
-    u64 warp_sum[kWarps];
-    u64 scan[kWarps], scan2[kWarps];
-    float warp_max[kWarps];
-    uint32_t warp_lo[kWarps], warp_hi[kWarps];
-    u64 sum;
+    uint2 count[kThreads], lo[kThreads], hi[kThreads];       // bins 2 t and 2 t + 1: entries, and mass in two words
+    u64 entry[kList], part_entry[kList], sorted[kList];      // the list, this part's share of it (ordered logit, rising as the index falls), weights in order
+    u64 coarse_mass[kCoarse];                 // sixteen bins each
+    uint32_t coarse_count[kCoarse];
+    double table[16];
+    u64 warp_sum[kWarps], scan[kWarps], scan2[kWarps];
+    uint32_t warp_a[kWarps], warp_b[kWarps];
     float max;
-    int bad;
-    uint32_t key_lo, key_hi;
-    int n_list;
-    uint32_t ties;
-    int32_t found;                            // of the r-th tie, by its part
-    int bin;
-    u64 above_mass, bin_mass;
-    uint32_t above_count, bin_count;
-    int pick;
+    u64 sum;
+    uint32_t key_lo, key_hi, ties;
+    int n_list, found;
+    int bin, pick;
+    u64 above_mass;
+    uint32_t above_count;
 };
 
 __device__ __forceinline__ uint32_t ordered(float x) {        // grows with the value; minus zero counts as zero
@@ -65,14 +60,35 @@ __device__ __forceinline__ uint32_t ordered(float x) {        // grows with the 
 __device__ __forceinline__ float unordered(uint32_t o) {
     return __uint_as_float(o & 0x80000000u ? o ^ 0x80000000u : ~o);
 }
+// Loads from the shared memory of CTA `rank` of the cluster.  (Volatile keeps them behind the barrier in front; without a clobber several are under way
+// at once.)
 __device__ __forceinline__ uint32_t remote_u32(const void* p, uint32_t rank) {
     uint32_t v;
-    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(map_to_cta(smem_u32(p), rank)) : "memory");
+    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(map_to_cta(smem_u32(p), rank)));
+    return v;
+}
+__device__ __forceinline__ uint2 remote_u32x2(const void* p, uint32_t rank) {
+    uint2 v;
+    asm volatile("ld.shared::cluster.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(map_to_cta(smem_u32(p), rank)));
     return v;
 }
 __device__ __forceinline__ u64 remote_u64(const void* p, uint32_t rank) {
     u64 v;
-    asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(map_to_cta(smem_u32(p), rank)) : "memory");
+    asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(map_to_cta(smem_u32(p), rank)));
+    return v;
+}
+__device__ __forceinline__ u64 warp_sum_u64(u64 v) {
+#pragma unroll
+    for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+}
+template <class T>
+__device__ __forceinline__ T warp_scan(T v, int lane) {       // with its own
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        const T y = __shfl_up_sync(0xffffffffu, v, d);
+        if (lane >= d) v += y;
+    }
     return v;
 }
 
@@ -92,55 +108,117 @@ struct Row {
         n_vec = (int)(((int64_t)v + skew + kVec<FP32> - 1) / kVec<FP32>);
     }
     // minus infinity outside the row
-    __device__ __forceinline__ void load(int j, float (&x)[kVec<FP32>]) const {
+    __device__ __forceinline__ uint4 load(int j) const {
         constexpr int N = kVec<FP32>;
         const int first = j * N - skew;
-        if (first >= 0 && first + N <= vocab) {
-            const uint4 v = *reinterpret_cast<const uint4*>(base + (int64_t)j * 16);
-            if (FP32) {
-                x[0] = __uint_as_float(v.x); x[1] = __uint_as_float(v.y); x[2] = __uint_as_float(v.z); x[3] = __uint_as_float(v.w);
-            } else {
-                x[0] = bf16_lo(v.x); x[1] = bf16_hi(v.x); x[2] = bf16_lo(v.y); x[3] = bf16_hi(v.y);
-                x[N - 4] = bf16_lo(v.z); x[N - 3] = bf16_hi(v.z); x[N - 2] = bf16_lo(v.w); x[N - 1] = bf16_hi(v.w);
-            }
-        } else {
+        if (first >= 0 && first + N <= vocab) return *reinterpret_cast<const uint4*>(base + (int64_t)j * 16);
+        uint32_t w[4];
 #pragma unroll
-            for (int e = 0; e < N; ++e) {
-                const int i = first + e;
-                x[e] = i < 0 || i >= vocab ? -INFINITY
-                     : FP32 ? reinterpret_cast<const float*>(base)[(int64_t)j * N + e] : bf16_to_f(reinterpret_cast<const uint16_t*>(base)[(int64_t)j * N + e]);
+        for (int q = 0; q < 4; ++q) {
+            w[q] = FP32 ? 0xff800000u : 0xff80ff80u;
+#pragma unroll
+            for (int h = 0; h < (FP32 ? 1 : 2); ++h) {
+                const int e = FP32 ? q : 2 * q + h, i = first + e;
+                if (i < 0 || i >= vocab) continue;
+                if (FP32) w[q] = reinterpret_cast<const uint32_t*>(base)[(int64_t)j * N + e];
+                else w[q] = __byte_perm(w[q], reinterpret_cast<const uint16_t*>(base)[(int64_t)j * N + e], h ? 0x5410 : 0x3254);
             }
         }
+        return make_uint4(w[0], w[1], w[2], w[3]);
     }
 };
-
-struct Weights {
-    double max, c, scale;
-    __device__ __forceinline__ double real(float x) const { return exp2(((double)x - max) * c); }
-    __device__ __forceinline__ u64 whole(double w) const { return __double2ull_rn(w * scale); }
-};
+template <bool FP32>
+__device__ __forceinline__ void decode(const uint4& v, float (&x)[kVec<FP32>]) {
+    constexpr int N = kVec<FP32>;
+    if (FP32) {
+        x[0] = __uint_as_float(v.x); x[1] = __uint_as_float(v.y); x[2] = __uint_as_float(v.z); x[3] = __uint_as_float(v.w);
+    } else {
+        x[0] = bf16_lo(v.x); x[1] = bf16_hi(v.x); x[2] = bf16_lo(v.y); x[3] = bf16_hi(v.y);
+        x[N - 4] = bf16_lo(v.z); x[N - 3] = bf16_hi(v.z); x[N - 2] = bf16_lo(v.w); x[N - 1] = bf16_hi(v.w);
+    }
+}
 
 template <bool FP32>
-__global__ void __launch_bounds__(kThreads) token_sample_kernel(const Params p) {
+__device__ __forceinline__ float element(const void* p, int64_t i) {
+    return FP32 ? static_cast<const float*>(p)[i] : bf16_to_f(static_cast<const uint16_t*>(p)[i]);
+}
+
+// Weights as whole numbers, 2^y 2^shift with y = c (x - max).  y = n / 16 + r: 2^(n / 16) comes from a table of 16 (two banks each: no conflicts), 2^r, |r| <= 1/32,
+// from its series to r^5, off by 2^-42.  Adding 2^52 + 2^51 over 16 rounds to sixteenths and leaves n in the low word; adding 2^52 rounds to a whole number
+// and leaves it there.  Nine operations of 64 bits; the weight of x = max is exact.  What lies 100 powers of two and more below the maximum goes
+// through as the maximum, so that n stays small, and gets a factor next to zero.
+constexpr u64 kWhole = 0x4330000000000000ull;          // 2^52
+struct Weights {
+    double max, c;
+    float top, far;                           // the maximum, and a distance of 100 powers of two below it
+    const double* table;                      // 2^(i / 16) 2^shift
+    // with 2^52 in front
+    __device__ __forceinline__ u64 raw(float x) const {
+        const bool none = x - top < far;
+        const double d = (double)(none ? top : x) - max, magic = 422212465065984.0;
+        const double t = fma(d, c, magic), r = fma(d, c, magic - t);
+        const int n = __double2loint(t);
+        double p = fma(r, 1.3333558146428443e-3, 9.6181291076284771e-3);
+        p = fma(r, p, 5.5504108664821579e-2);
+        p = fma(r, p, 2.4022650695910071e-1);
+        p = fma(r, p, 6.9314718055994530e-1);
+        p = fma(r, p, 1.0);
+        const double e = table[n & 15];
+        const int hi = __double2hiint(e) + ((n >> 4) << 20);
+        const double scaled = __hiloint2double(none ? 0 : hi, __double2loint(e));
+        return (u64)__double_as_longlong(fma(p, scaled, 4503599627370496.0));
+    }
+    __device__ __forceinline__ u64 operator()(float x) const { return raw(x) - kWhole; }
+};
+
+template <bool FP32, bool HOLD>
+__global__ void __launch_bounds__(kThreads, 2) token_sample_kernel(const Params p) {
     __shared__ Shared s;
+    extern __shared__ uint4 held[];           // this part's vectors, where they fit
     constexpr int N = kVec<FP32>;
     const SampleArgs& a = p.a;
     const int t = threadIdx.x, warp = t >> 5, lane = t & 31;
     const int64_t row_i = blockIdx.x / p.parts;
-    const int part = (int)(blockIdx.x - row_i * p.parts);
+    const int part = (int)(blockIdx.x - row_i * p.parts), parts = p.parts;
     pdl_launch_dependents();
     pdl_wait();
 
     const Row<FP32> row(a.logits, row_i * a.row_stride, a.vocab);
     const int vec0 = (int)min((int64_t)(part * kWarps + warp) * p.vecs, (int64_t)row.n_vec), vec1 = min(vec0 + p.vecs, row.n_vec);
-    auto team_sync = [&]() { if (p.parts > 1) cluster_sync_all(); else __syncthreads(); };
+    auto team_sync = [&]() { if (parts > 1) cluster_sync_all(); else __syncthreads(); };
+    // what every part has, in lane r for part r (behind a team_sync)
+    auto of_parts_u64 = [&](const u64& x) { return parts == 1 ? (lane == 0 ? x : 0) : lane < parts ? remote_u64(&x, lane) : 0; };
+    auto of_parts_u32 = [&](const void* x) { return parts == 1 ? (lane == 0 ? *static_cast<const uint32_t*>(x) : 0) : lane < parts ? remote_u32(x, lane) : 0; };
+    const int held0 = part * kWarps * p.vecs;
+    auto vec_at = [&](int j) { return HOLD ? held[j - held0] : row.load(j); };
     // f(value, index) for this lane's elements of its warp's stretch (minus infinity outside the row)
     auto for_lane = [&](auto f) {
         for (int j = vec0 + lane; j < vec1; j += 32) {
             float x[N];
-            row.load(j, x);
+            decode<FP32>(vec_at(j), x);
 #pragma unroll
             for (int e = 0; e < N; ++e) f(x[e], j * N - row.skew + e);
+        }
+    };
+
+    // The same for the elements that pass a test, which is made of 32 elements of the lane at a time: the lanes of a warp then call f as often as the one
+    // with most of them, not for every element that any lane has.
+    auto for_passing = [&](auto passes, auto f) {
+        constexpr int kVecs = 32 / N;
+        for (int j0 = vec0 + lane; j0 < vec1; j0 += 32 * kVecs) {
+            uint32_t m = 0;
+#pragma unroll
+            for (int h = 0; h < kVecs; ++h) {
+                if (j0 + 32 * h >= vec1) break;
+                float x[N];
+                decode<FP32>(vec_at(j0 + 32 * h), x);
+#pragma unroll
+                for (int e = 0; e < N; ++e) m |= passes(x[e]) ? 1u << (h * N + e) : 0u;
+            }
+            for (; m; m &= m - 1) {
+                const int bit = __ffs(m) - 1, j = j0 + 32 * (bit / N), e = bit % N, i = j * N - row.skew + e;
+                f(HOLD ? element<FP32>(held + (j - held0), e) : element<FP32>(row.base, (int64_t)j * N + e), i);
+            }
         }
     };
 
@@ -150,27 +228,44 @@ __global__ void __launch_bounds__(kThreads) token_sample_kernel(const Params p) 
     int top_k = a.top_k ? a.top_k[row_i] : 0;
     const bool refused = !(temperature >= 0.f && temperature < INFINITY) || top_p != top_p || min_p != min_p || !(u >= 0.f && u < 1.f);
     if (temperature == 0.f || min_p > 1.f) { top_k = 1; min_p = 0.f; }
-    if (temperature == 0.f) temperature = 1.f;
+    temperature = temperature == 0.f ? 1.f : fmaxf(temperature, 0x1p-126f);
     if (top_k <= 0 || top_k > a.vocab) top_k = a.vocab;
 
     // --- the maximum
     {
         float m = -INFINITY;
         bool bad = false;
-        for_lane([&](float x, int) { m = fmaxf(m, x); bad |= x != x; });
+        constexpr int kAhead = 4;
+        for (int j0 = vec0 + lane; j0 < vec1; j0 += 32 * kAhead) {
+            uint4 v[kAhead];
+#pragma unroll
+            for (int h = 0; h < kAhead; ++h)
+                if (j0 + 32 * h < vec1) v[h] = row.load(j0 + 32 * h);
+#pragma unroll
+            for (int h = 0; h < kAhead; ++h) {
+                if (j0 + 32 * h >= vec1) break;
+                if (HOLD) held[j0 + 32 * h - held0] = v[h];
+                float x[N];
+                decode<FP32>(v[h], x);
+#pragma unroll
+                for (int e = 0; e < N; ++e) { m = fmaxf(m, x[e]); bad |= x[e] != x[e]; }
+            }
+        }
+        if (t < 16) s.table[t] = exp2(t / 16.0) * (double)(1ull << p.shift);
+        s.count[t] = s.lo[t] = s.hi[t] = make_uint2(0, 0);
+        if (t == 0) s.n_list = 0;
         m = warp_max(m);
         bad = __any_sync(0xffffffffu, bad);
-        if (lane == 0) s.warp_max[warp] = bad ? INFINITY : m;      // plus infinity is no distribution either
+        if (lane == 0) s.warp_a[warp] = __float_as_uint(bad ? INFINITY : m);      // plus infinity is no distribution either
         __syncthreads();
-        if (t == 0) {
-            float all = s.warp_max[0];
-            for (int w = 1; w < kWarps; ++w) all = fmaxf(all, s.warp_max[w]);
-            s.max = all;
+        if (warp == 0) {
+            m = warp_max(lane < kWarps ? __uint_as_float(s.warp_a[lane]) : -INFINITY);
+            if (lane == 0) s.max = m;
         }
     }
     team_sync();
-    float top = s.max;
-    for (int r = 0; r < (p.parts > 1 ? p.parts : 0); ++r) top = fmaxf(top, __uint_as_float(remote_u32(&s.max, r)));
+    const uint32_t top_bits = of_parts_u32(&s.max);
+    const float top = warp_max(lane < parts ? __uint_as_float(top_bits) : -INFINITY);
     if (refused || !(top > -INFINITY && top < INFINITY)) {
         if (part == 0 && t == 0) {
             a.ids[row_i] = -1;
@@ -180,202 +275,208 @@ __global__ void __launch_bounds__(kThreads) token_sample_kernel(const Params p) 
         team_sync();
         return;
     }
+    const double scale = (double)(1ull << p.shift);
     Weights wt;
     wt.max = top;
     wt.c = 1.4426950408889634074 / (double)temperature;
-    wt.scale = (double)(1ull << p.shift);
+    wt.top = top;
+    wt.far = -(float)fmin(100.0 / wt.c, 3.402823466e38);
+    wt.table = s.table;
+    const u64 least = min_p > 0.f ? (u64)ceil((double)min_p * scale) : 0;
 
-    auto block_sum = [&](u64 v) {             // of every thread, in every thread
-#pragma unroll
-        for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-        __syncthreads();
-        if (lane == 0) s.scan[warp] = v;
-        __syncthreads();
-        u64 all = 0;
-        for (int w = 0; w < kWarps; ++w) all += s.scan[w];
-        return all;
-    };
-
-    // --- the last entry kept: all, unless a limit is reached
-    uint32_t cut_key = 0;
-    int cut_index = 0x7fffffff;
-    const bool by_mass = top_p < 1.f;
+    // --- the last entry kept: all, unless a limit is reached.  An entry is (ordered logit, ~index): the larger comes first.
+    u64 cut = 0;
+    const bool by_mass = top_p < 1.f && top_k > 1;
     if (top_k < a.vocab || by_mass) {
         u64 target = ~0ull;                   // mass at which top-p is reached
         float range = (float)p.shift + 2.f;   // in powers of two below the maximum
-        uint32_t key_lo = 0, key_hi = 0xffffffffu, above_count = 0;
-        u64 above_mass = 0;
-        int bin1 = -1;
-        bool ties = false, none = false;
-        uint32_t n_in = 0;                    // entries among which the last one is
-        if (by_mass && top_k > 1) {
-            u64 mine = 0;
-            for_lane([&](float x, int) { mine += wt.whole(wt.real(x)); });
-            const u64 sum = block_sum(mine);
-            if (t == 0) s.sum = sum;
-            team_sync();
-            u64 all = sum;
-            if (p.parts > 1) {
-                all = 0;
-                for (int r = 0; r < p.parts; ++r) all += remote_u64(&s.sum, r);
-            }
-            target = top_p > 0.f ? (u64)ceil((double)top_p * (double)all) : 0;
-            const float tail = log2f((float)a.vocab / (fmaxf(1.f - top_p, 1e-7f) * (float)((double)all / wt.scale))) + 1.f;
-            range = fminf(range, fmaxf(tail, 1.f));
-        }
-        const float cf = (float)fmin(wt.c, 1e30), bins = (float)(kBins - 1) / range;
+        if (by_mass) range = fminf(range, log2f((float)a.vocab / fmaxf(1.f - top_p, 1e-7f)) + 1.f);
+        const float per = fminf((float)wt.c * ((float)(kBins - 1) / range), 3.402823466e38f);
         auto first_bin = [&](float x) {       // falls with the value
-            const float b = (top - x) * cf * bins;
+            const float b = (top - x) * per;
             return b < (float)kBins ? (int)b : kBins;
         };
-        if (top_k == 1) { ties = true; key_lo = key_hi = ordered(top); }
-
-        for (int level = 0; !ties && !none; ++level) {
-            // histogram of what is left
-            int down = 0;
-            if (level > 0) while ((key_hi - key_lo) >> down >= (uint32_t)kBins) ++down;
+        uint32_t* const counts = reinterpret_cast<uint32_t*>(s.count);
+        uint32_t* const los = reinterpret_cast<uint32_t*>(s.lo);
+        uint32_t* const his = reinterpret_cast<uint32_t*>(s.hi);
+        auto into_bin = [&](int b, u64 w) {
+            atomicAdd(counts + b, 1u);
+            if (by_mass) {
+                const uint32_t lo = (uint32_t)w, old = atomicAdd(los + b, lo), hi = (uint32_t)(w >> 32) + (old + lo < old ? 1u : 0u);
+                if (hi) atomicAdd(his + b, hi);
+            }
+        };
+        uint32_t key_lo = 0, key_hi = 0xffffffffu, above_count = 0, n_in = 0;
+        u64 above_mass = 0;
+        int bin1 = -1, bin = -1;
+        // The bin, of all parts' added up, where a limit is reached: s.bin, -1 if none.  Every CTA finds it for itself: first among the parts' sums of
+        // sixteen bins, then among these sixteen, so little is read from other CTAs (all 1024 bins took 9000 cycles).
+        auto find_bin = [&](bool first) {
             __syncthreads();
-            for (int b = t; b < kBins; b += kThreads) s.count[b] = s.lo[b] = s.hi[b] = 0;
-            __syncthreads();
-            for_lane([&](float x, int) {
-                if (x == -INFINITY) return;
-                const int b1 = first_bin(x);
-                int b;
-                if (level == 0) {
-                    b = b1;
-                    if (b >= kBins) return;
-                } else {
-                    const uint32_t key = ordered(x);
-                    if (b1 != bin1 || key < key_lo || key > key_hi) return;
-                    b = (int)((key_hi - key) >> down);
-                }
-                atomicAdd(&s.count[b], 1u);
-                if (by_mass) {
-                    const u64 w = wt.whole(wt.real(x));
-                    const uint32_t lo = (uint32_t)w, old = atomicAdd(&s.lo[b], lo), hi = (uint32_t)(w >> 32) + (old + lo < old ? 1u : 0u);
-                    if (hi) atomicAdd(&s.hi[b], hi);
-                }
-            });
+            {
+                const uint2 count = s.count[t], lo = s.lo[t], hi = s.hi[t];
+                uint32_t n = count.x + count.y;
+                u64 m = ((u64)hi.x << 32) + lo.x + ((u64)hi.y << 32) + lo.y;
+#pragma unroll
+                for (int o = kFine / 4; o; o >>= 1) { n += __shfl_xor_sync(0xffffffffu, n, o); m += __shfl_xor_sync(0xffffffffu, m, o); }
+                if (t % (kFine / 2) == 0) { s.coarse_count[t / (kFine / 2)] = n; s.coarse_mass[t / (kFine / 2)] = m; }
+                if (t == 0) s.bin = -1;
+            }
             team_sync();
-            // every CTA adds all parts up; a thread has two bins
-            uint32_t count[2];
-            u64 mass[2];
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const int b = 2 * t + e;
-                count[e] = 0;
-                mass[e] = 0;
-                for (int r = 0; r < p.parts; ++r) {
-                    if (p.parts > 1) {
-                        count[e] += remote_u32(&s.count[b], r);
-                        if (by_mass) mass[e] += ((u64)remote_u32(&s.hi[b], r) << 32) + remote_u32(&s.lo[b], r);
-                    } else {
-                        count[e] += s.count[b];
-                        mass[e] += ((u64)s.hi[b] << 32) + s.lo[b];
-                    }
-                }
+            // a limit is reached among n entries of mass m behind c_before of m_before?  (A target of zero is reached by the first entry, not before it.)
+            auto reached = [&](u64 c_before, u64 m_before, uint32_t n, u64 m) {
+                const bool was = c_before >= (u64)top_k || m_before >= target, is = c_before + n >= (u64)top_k || m_before + m >= target;
+                return n > 0 && is && (!was || c_before == 0);
+            };
+            const int group = t / kMaxParts, r = t % kMaxParts;
+            uint32_t n = 0;
+            u64 m = 0, whole = 0;
+            if (r < parts) {
+                n = parts > 1 ? remote_u32(&s.coarse_count[group], r) : s.coarse_count[group];
+                m = parts > 1 ? remote_u64(&s.coarse_mass[group], r) : s.coarse_mass[group];
             }
-            u64 c_incl = count[0] + count[1], m_incl = mass[0] + mass[1];
-#pragma unroll
-            for (int d = 1; d < 32; d <<= 1) {
-                const u64 cy = __shfl_up_sync(0xffffffffu, c_incl, d), my = __shfl_up_sync(0xffffffffu, m_incl, d);
-                if (lane >= d) { c_incl += cy; m_incl += my; }
+            if (first && by_mass) {
+                whole = warp_sum_u64(of_parts_u64(s.sum));
+                target = top_p > 0.f ? (u64)ceil((double)top_p * (double)whole) : 0;
             }
+#pragma unroll
+            for (int o = kMaxParts / 2; o; o >>= 1) { n += __shfl_xor_sync(0xffffffffu, n, o); m += __shfl_xor_sync(0xffffffffu, m, o); }
+            const u64 c_incl = warp_scan(r == 0 ? (u64)n : 0, lane), m_incl = warp_scan(r == 0 ? m : 0, lane);
             if (lane == 31) { s.scan[warp] = c_incl; s.scan2[warp] = m_incl; }
-            if (t == 0) s.bin = -1;
             __syncthreads();
-            u64 c_before = above_count + c_incl - count[0] - count[1], m_before = above_mass + m_incl - mass[0] - mass[1];
+            u64 c_before = above_count + c_incl - n, m_before = above_mass + m_incl - m;
             for (int w = 0; w < warp; ++w) { c_before += s.scan[w]; m_before += s.scan2[w]; }
+            if (r == 0 && reached(c_before, m_before, n, m)) { s.bin = group; s.above_count = (uint32_t)c_before; s.above_mass = m_before; }
+            __syncthreads();
+            const int coarse = s.bin;
+            if (coarse >= 0) {                // every warp: bin lane % 16 of parts lane / 16, + 2, ..
+                const int b = coarse * kFine + lane % kFine;
+                n = 0;
+                m = 0;
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const bool was = c_before >= (u64)top_k || m_before >= target;
-                const u64 c_after = c_before + count[e], m_after = m_before + mass[e];
-                const bool is = c_after >= (u64)top_k || m_after >= target;
-                // (a target of zero is reached by the first entry, not before it)
-                if (count[e] > 0 && is && (!was || c_before == 0)) {
-                    s.bin = 2 * t + e;
-                    s.above_count = (uint32_t)c_before; s.above_mass = m_before;
-                    s.bin_count = count[e]; s.bin_mass = mass[e];
+                for (int q = 0; q < kMaxParts; q += 2) {
+                    const int of = q + lane / kFine;
+                    if (of >= parts) continue;
+                    n += parts > 1 ? remote_u32(counts + b, of) : counts[b];
+                    m += parts > 1 ? ((u64)remote_u32(his + b, of) << 32) + remote_u32(los + b, of) : ((u64)his[b] << 32) + los[b];
                 }
-                c_before = c_after; m_before = m_after;
-            }
-            team_sync();                      // (the histogram may be cleared again)
-            if (s.bin < 0) { none = true; break; }
-            above_count = s.above_count;
-            above_mass = s.above_mass;
-            n_in = s.bin_count;
-            if (level == 0) {
-                bin1 = s.bin;
+                n += __shfl_xor_sync(0xffffffffu, n, kFine);
+                m += __shfl_xor_sync(0xffffffffu, m, kFine);
+                const u64 c = s.above_count + warp_scan(lane < kFine ? (u64)n : 0, lane) - n, before = s.above_mass + warp_scan(lane < kFine ? m : 0, lane) - m;
+                const uint32_t hit = __ballot_sync(0xffffffffu, lane < kFine && reached(c, before, n, m));
+                const int at = __ffs(hit) - 1;
+                above_count = (uint32_t)__shfl_sync(0xffffffffu, c, at);
+                above_mass = __shfl_sync(0xffffffffu, before, at);
+                n_in = __shfl_sync(0xffffffffu, n, at);
+                bin = coarse * kFine + at;
             } else {
-                const uint32_t hi = key_hi - ((uint32_t)s.bin << down);
-                const uint32_t span = (1u << down) - 1u;
-                key_lo = hi - key_lo > span ? hi - span : key_lo;
-                key_hi = hi;
+                bin = -1;
             }
-            if (n_in <= (uint32_t)kList) break;
-            if (level == 0) {                 // the keys of the bin
-                uint32_t lo = 0xffffffffu, hi = 0;
+            team_sync();                      // (the bins may be cleared again)
+        };
+        bool ties = top_k == 1, none = false;
+        if (ties) {
+            key_lo = key_hi = ordered(top);
+        } else {
+            u64 mine = 0;
+            if (by_mass) {                    // the row's mass and the first histogram in one pass
                 for_lane([&](float x, int) {
-                    if (x == -INFINITY || first_bin(x) != bin1) return;
-                    const uint32_t key = ordered(x);
-                    lo = min(lo, key);
-                    hi = max(hi, key);
+                    const u64 w = wt(x);
+                    mine += w;
+                    const int b = first_bin(x);
+                    if (b < kBins) into_bin(b, w);
                 });
-                lo = __reduce_min_sync(0xffffffffu, lo);
-                hi = __reduce_max_sync(0xffffffffu, hi);
-                if (lane == 0) { s.warp_lo[warp] = lo; s.warp_hi[warp] = hi; }
-                __syncthreads();
-                if (t == 0) {
-                    for (int w = 1; w < kWarps; ++w) { lo = min(lo, s.warp_lo[w]); hi = max(hi, s.warp_hi[w]); }
-                    s.key_lo = lo; s.key_hi = hi;
-                }
-                team_sync();
-                key_lo = s.key_lo;
-                key_hi = s.key_hi;
-                for (int r = 0; r < (p.parts > 1 ? p.parts : 0); ++r) { key_lo = min(key_lo, remote_u32(&s.key_lo, r)); key_hi = max(key_hi, remote_u32(&s.key_hi, r)); }
+            } else {
+                for_lane([&](float x, int) {
+                    const int b = first_bin(x);
+                    if (b < kBins) atomicAdd(counts + b, 1u);
+                });
             }
-            if (key_lo == key_hi) ties = true;
+            if (by_mass) {
+                mine = warp_sum_u64(mine);
+                if (lane == 0) s.warp_sum[warp] = mine;
+                __syncthreads();
+                if (warp == 0) {
+                    const u64 all = warp_sum_u64(lane < kWarps ? s.warp_sum[lane] : 0);
+                    if (lane == 0) s.sum = all;
+                }
+            }
+            find_bin(true);
+            none = bin < 0;
+            bin1 = bin;
+        }
+        if (!ties && !none && n_in > (uint32_t)kList) {       // too many: on by the bits of the bin's keys
+            uint32_t lo = 0xffffffffu, hi = 0;
+            for_lane([&](float x, int) {
+                if (first_bin(x) != bin1) return;
+                const uint32_t key = ordered(x);
+                lo = min(lo, key);
+                hi = max(hi, key);
+            });
+            lo = __reduce_min_sync(0xffffffffu, lo);
+            hi = __reduce_max_sync(0xffffffffu, hi);
+            if (lane == 0) { s.warp_a[warp] = lo; s.warp_b[warp] = hi; }
+            __syncthreads();
+            if (warp == 0) {
+                lo = __reduce_min_sync(0xffffffffu, lane < kWarps ? s.warp_a[lane] : 0xffffffffu);
+                hi = __reduce_max_sync(0xffffffffu, lane < kWarps ? s.warp_b[lane] : 0);
+                if (lane == 0) { s.key_lo = lo; s.key_hi = hi; }
+            }
+            team_sync();
+            lo = of_parts_u32(&s.key_lo);
+            hi = of_parts_u32(&s.key_hi);
+            key_lo = __reduce_min_sync(0xffffffffu, lane < parts ? lo : 0xffffffffu);
+            key_hi = __reduce_max_sync(0xffffffffu, lane < parts ? hi : 0);
+            while (key_lo != key_hi && n_in > (uint32_t)kList) {
+                int down = 0;
+                while ((key_hi - key_lo) >> down >= (uint32_t)kBins) ++down;
+                s.count[t] = s.lo[t] = s.hi[t] = make_uint2(0, 0);
+                __syncthreads();
+                for_passing([&](float x) { return first_bin(x) == bin1; }, [&](float x, int) {
+                    const uint32_t key = ordered(x);
+                    if (key >= key_lo && key <= key_hi) into_bin((int)((key_hi - key) >> down), by_mass ? wt(x) : 0);
+                });
+                find_bin(false);
+                const uint32_t end = key_hi - ((uint32_t)bin << down), span = (1u << down) - 1u;
+                key_lo = end - key_lo > span ? end - span : key_lo;
+                key_hi = end;
+            }
+            ties = key_lo == key_hi;
         }
 
         if (ties) {                           // one value: its r first
-            const u64 w = wt.whole(wt.real(unordered(key_lo)));
+            const u64 w = wt(unordered(key_lo));
             u64 r = (u64)top_k - above_count;
-            if (by_mass && top_k > 1 && w > 0) {
+            if (by_mass && w > 0) {
                 const u64 need = target > above_mass ? (target - above_mass + w - 1) / w : 1;
                 if (need < r) r = need;
             }
             if (r < 1) r = 1;
             uint32_t n = 0;
-            for_lane([&](float x, int) { n += x > -INFINITY && ordered(x) == key_lo ? 1u : 0u; });
+            for_lane([&](float x, int) { n += ordered(x) == key_lo ? 1u : 0u; });
             n = __reduce_add_sync(0xffffffffu, n);
-            __syncthreads();
-            if (lane == 0) s.warp_lo[warp] = n;
+            if (lane == 0) s.warp_a[warp] = n;
             if (t == 0) s.found = -1;
             __syncthreads();
-            uint32_t before = 0, all = 0;
-            for (int v = 0; v < kWarps; ++v) { const uint32_t x = s.warp_lo[v]; if (v < warp) before += x; all += x; }
-            if (t == 0) s.ties = all;
+            const uint32_t in_warp = lane < kWarps ? s.warp_a[lane] : 0;
+            if (t == 0) s.ties = 0;
+            const uint32_t in_part = __reduce_add_sync(0xffffffffu, in_warp);
+            if (t == 0) s.ties = in_part;
             team_sync();
-            for (int q = 0; q < part; ++q) before += remote_u32(&s.ties, q);
+            const uint32_t of_part = of_parts_u32(&s.ties);
+            const uint32_t before = __reduce_add_sync(0xffffffffu, (lane < part ? of_part : 0) + (lane < warp ? in_warp : 0));
             if (r > before && r <= (u64)before + n) {             // the warp that has it
                 uint32_t left = (uint32_t)(r - before);
                 for (int j0 = vec0; j0 < vec1 && left > 0; j0 += 32) {
                     const int j = j0 + lane;
-                    float x[N];
                     uint32_t m = 0;
                     if (j < vec1) {
-                        row.load(j, x);
+                        float x[N];
+                        decode<FP32>(vec_at(j), x);
 #pragma unroll
-                        for (int e = 0; e < N; ++e) if (x[e] > -INFINITY && ordered(x[e]) == key_lo) m |= 1u << e;
+                        for (int e = 0; e < N; ++e) if (ordered(x[e]) == key_lo) m |= 1u << e;
                     }
-                    const uint32_t here = __popc(m);
-                    uint32_t incl = here;
-#pragma unroll
-                    for (int d = 1; d < 32; d <<= 1) {
-                        const uint32_t y = __shfl_up_sync(0xffffffffu, incl, d);
-                        if (lane >= d) incl += y;
-                    }
-                    const uint32_t total = __shfl_sync(0xffffffffu, incl, 31);
+                    const uint32_t here = __popc(m), incl = warp_scan(here, lane), total = __shfl_sync(0xffffffffu, incl, 31);
                     if (left > incl - here && left <= incl) {
                         for (uint32_t k = left - (incl - here); k > 1; --k) m &= m - 1;
                         s.found = j * N - row.skew + __ffs(m) - 1;
@@ -384,96 +485,79 @@ __global__ void __launch_bounds__(kThreads) token_sample_kernel(const Params p) 
                 }
             }
             team_sync();
-            cut_key = key_lo;
-            cut_index = s.found;
-            for (int q = 0; q < (p.parts > 1 ? p.parts : 0); ++q) cut_index = max(cut_index, (int)remote_u32(&s.found, q));
-            if (cut_index < 0) cut_index = 0x7fffffff;            // fewer than that: all
+            const int at_part = (int)of_parts_u32(&s.found);
+            const int index = __reduce_max_sync(0xffffffffu, lane < parts ? at_part : -1);
+            cut = (u64)key_lo << 32 | (index < 0 ? 0x80000000u : (uint32_t)~index);         // (fewer than that: all)
         } else if (!none) {                   // a list
-            if (t == 0) s.n_list = 0;
-            __syncthreads();
-            const bool keys = key_hi != 0xffffffffu || key_lo != 0;
-            for_lane([&](float x, int i) {
-                if (x == -INFINITY || first_bin(x) != bin1) return;
+            for_passing([&](float x) { return first_bin(x) == bin1; }, [&](float x, int i) {
                 const uint32_t key = ordered(x);
-                if (keys && (key < key_lo || key > key_hi)) return;
-                const int at = atomicAdd(&s.n_list, 1);
-                s.part_key[at] = key;
-                s.part_index[at] = i;
+                if (key < key_lo || key > key_hi) return;
+                s.part_entry[atomicAdd(&s.n_list, 1)] = (u64)key << 32 | (uint32_t)~i;
             });
             team_sync();
-            int n = 0;
-            for (int r = 0; r < p.parts; ++r) {
-                const int m = p.parts > 1 ? (int)remote_u32(&s.n_list, r) : s.n_list;
-                for (int i = t; i < m; i += kThreads) {
-                    s.key[n + i] = p.parts > 1 ? remote_u32(&s.part_key[i], r) : s.part_key[i];
-                    s.index[n + i] = p.parts > 1 ? (int32_t)remote_u32(&s.part_index[i], r) : s.part_index[i];
-                }
-                n += m;
+            const int in_part = (int)of_parts_u32(&s.n_list), n = (int)n_in;
+            const int upto = warp_scan(in_part, lane);
+            int from = 0, first = 0;          // entry t: of which part, and that part's first
+#pragma unroll
+            for (int r = 0; r < kMaxParts - 1; ++r) {
+                const int end = __shfl_sync(0xffffffffu, upto, r);
+                if (r + 1 < parts && t >= end) { from = r + 1; first = end; }
             }
+            if (t < n) s.entry[t] = parts > 1 ? remote_u64(&s.part_entry[t - first], from) : s.part_entry[t];
             if (t == 0) s.pick = n - 1;
             __syncthreads();
-            for (int i = t; i < n; i += kThreads) {
-                const uint32_t key = s.key[i];
-                const int at = s.index[i];
-                int rank = 0;
-                for (int j = 0; j < n; ++j) rank += (s.key[j] > key || (s.key[j] == key && s.index[j] < at)) ? 1 : 0;
-                s.order[rank] = i;
-                s.sorted[rank] = by_mass ? wt.whole(wt.real(unordered(key))) : 0;
-            }
+            // an entry's rank, counted by 1 to 32 threads
+            int each = 1;
+            while (each < 32 && n * each * 2 <= kThreads) each *= 2;
+            const int i = t / each;
+            const u64 mine = i < n ? s.entry[i] : 0;
+            int rank = 0;
+            if (i < n) for (int j = t & (each - 1); j < n; j += each) rank += s.entry[j] > mine ? 1 : 0;
+            for (int o = each / 2; o; o >>= 1) rank += __shfl_xor_sync(0xffffffffu, rank, o);
+            if (i < n && (t & (each - 1)) == 0) s.sorted[rank] = mine;
             __syncthreads();
-            u64 v[2], incl = 0;
-#pragma unroll
-            for (int e = 0; e < 2; ++e) { v[e] = 2 * t + e < n ? s.sorted[2 * t + e] : 0; incl += v[e]; }
-            const u64 own = incl;
-#pragma unroll
-            for (int d = 1; d < 32; d <<= 1) {
-                const u64 y = __shfl_up_sync(0xffffffffu, incl, d);
-                if (lane >= d) incl += y;
-            }
+            const u64 x = t < n ? s.sorted[t] : 0;
+            const u64 incl = warp_scan(by_mass && t < n ? wt(unordered((uint32_t)(x >> 32))) : 0, lane);
             if (lane == 31) s.scan[warp] = incl;
             __syncthreads();
-            u64 mass = above_mass + incl - own;
+            u64 mass = above_mass + incl;
             for (int w = 0; w < warp; ++w) mass += s.scan[w];
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                mass += v[e];
-                const int j = 2 * t + e;
-                if (j < n && ((u64)above_count + j + 1 >= (u64)top_k || mass >= target)) atomicMin(&s.pick, j);
-            }
+            if (t < n && ((u64)above_count + t + 1 >= (u64)top_k || mass >= target)) atomicMin(&s.pick, t);
             __syncthreads();
-            const int last = s.order[s.pick];
-            cut_key = s.key[last];
-            cut_index = s.index[last];
+            cut = s.sorted[s.pick];
         }
     }
 
     // --- the kept mass, stretch by stretch, and the token
+    const uint32_t cut_key = (uint32_t)(cut >> 32);
+    const int cut_index = (int)~(uint32_t)cut;
+    const bool all_kept = cut == 0 && least == 0;
     auto weight = [&](float x, int i) -> u64 {
+        const u64 w = wt(x);
         const uint32_t key = ordered(x);
-        if (x == -INFINITY || key < cut_key || (key == cut_key && i > cut_index)) return 0;
-        const double w = wt.real(x);
-        return min_p > 0.f && w < (double)min_p ? 0 : wt.whole(w);
+        return w < least || key < cut_key || (key == cut_key && i > cut_index) ? 0 : w;
     };
+    // (a float that lies below the last one kept needs no weight)
+    const float floor_x = cut == 0 ? -INFINITY : unordered(cut_key);
     u64 mine = 0;
-    for_lane([&](float x, int i) { mine += weight(x, i); });
-    u64 stretch = mine;
-#pragma unroll
-    for (int o = 16; o; o >>= 1) stretch += __shfl_xor_sync(0xffffffffu, stretch, o);
-    __syncthreads();
+    if (all_kept) {
+        int n = 0;
+        for_lane([&](float x, int) { mine += wt.raw(x); ++n; });
+        mine -= (u64)n * kWhole;
+    } else {
+        for_passing([&](float x) { return x >= floor_x; }, [&](float x, int i) { mine += weight(x, i); });
+    }
+    const u64 stretch = warp_sum_u64(mine);
     if (lane == 0) s.warp_sum[warp] = stretch;
     __syncthreads();
-    u64 before = 0, sum = 0;
-    for (int w = 0; w < kWarps; ++w) { const u64 x = s.warp_sum[w]; if (w < warp) before += x; sum += x; }
-    u64 all = sum;
-    if (p.parts > 1) {
-        if (t == 0) s.sum = sum;
+    const u64 in_warp = lane < kWarps ? s.warp_sum[lane] : 0;
+    u64 before = warp_sum_u64(lane < warp ? in_warp : 0), all = warp_sum_u64(in_warp);
+    if (parts > 1) {
+        if (t == 0) s.sum = all;
         team_sync();
-        all = 0;
-        for (int r = 0; r < p.parts; ++r) {
-            const u64 x = remote_u64(&s.sum, r);
-            if (r < part) before += x;
-            all += x;
-        }
+        const u64 of_part = of_parts_u64(s.sum);
+        before += warp_sum_u64(lane < part ? of_part : 0);
+        all = warp_sum_u64(of_part);
     }
     u64 at = (u64)((double)u * (double)all);
     if (at >= all) at = all - 1;
@@ -486,47 +570,52 @@ __global__ void __launch_bounds__(kThreads) token_sample_kernel(const Params p) 
 #pragma unroll
             for (int e = 0; e < N; ++e) w[e] = 0;
             if (j < vec1) {
-                row.load(j, x);
+                decode<FP32>(vec_at(j), x);
 #pragma unroll
                 for (int e = 0; e < N; ++e) { w[e] = weight(x[e], j * N - row.skew + e); own += w[e]; }
             }
-            u64 incl = own;
-#pragma unroll
-            for (int d = 1; d < 32; d <<= 1) {
-                const u64 y = __shfl_up_sync(0xffffffffu, incl, d);
-                if (lane >= d) incl += y;
-            }
+            const u64 incl = warp_scan(own, lane);
             u64 sofar = run + incl - own;
             if (at >= sofar && at < sofar + own) {
 #pragma unroll
                 for (int e = 0; e < N; ++e) {
                     if (at >= sofar && at < sofar + w[e]) {
                         a.ids[row_i] = j * N - row.skew + e;
-                        if (a.logprobs) a.logprobs[row_i] = (float)(((double)x[e] - wt.max) / (double)temperature - log((double)all / wt.scale));
+                        if (a.logprobs) a.logprobs[row_i] = (float)(((double)x[e] - wt.max) / (double)temperature - log((double)all / scale));
                     }
                     sofar += w[e];
                 }
             }
             run += __shfl_sync(0xffffffffu, incl, 31);
+            if (run > at) break;
         }
     }
-    team_sync();                              // nobody's shared memory goes before it has been read
+    if (parts > 1) cluster_sync_all();        // nobody's shared memory goes before it has been read
 }
 
 }  // namespace
 
+cudaError_t configure_token_sample() {
+    const cudaError_t e = cudaFuncSetAttribute(token_sample_kernel<true, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kHeldBytes);
+    return e == cudaSuccess ? cudaFuncSetAttribute(token_sample_kernel<false, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kHeldBytes) : e;
+}
+
 mt_status launch_token_sample(const SampleArgs& a, const OpContext& c, cudaStream_t s) {
     Params p;
     p.a = a;
+    const int vec = a.fp32 ? 4 : 8, most = (a.vocab + 2 * vec - 2) / vec;          // vectors of a row that starts anywhere
+    auto vecs = [&](int parts) { return (most + parts * kWarps - 1) / (parts * kWarps); };
+    auto fits = [&](int parts) { return vecs(parts) * kWarps * 16 <= kHeldBytes; };
     p.parts = 1;
-    while (p.parts < kMaxParts && (int64_t)a.n * p.parts * 2 <= 2LL * c.sm_count && a.vocab / (p.parts * 2) >= kMinPart) p.parts *= 2;
+    while (p.parts < kMaxParts && a.vocab / (p.parts * 2) >= kMinPart && (!fits(p.parts) || (int64_t)a.n * p.parts * 2 <= 2LL * c.sm_count)) p.parts *= 2;
+    p.vecs = vecs(p.parts);
+    const bool hold = fits(p.parts);
     p.shift = 46;
     while (p.shift > 0 && ((int64_t)a.vocab << p.shift) > (1ll << 62)) --p.shift;
-    const int vec = a.fp32 ? 4 : 8, most = (a.vocab + 2 * vec - 2) / vec;          // vectors of a row that starts anywhere
-    p.vecs = (most + p.parts * kWarps - 1) / (p.parts * kWarps);
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)((int64_t)a.n * p.parts));
     cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = hold ? p.vecs * kWarps * 16 : 0;
     cfg.stream = s;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -537,7 +626,8 @@ mt_status launch_token_sample(const SampleArgs& a, const OpContext& c, cudaStrea
     cfg.attrs = attr;
     cfg.numAttrs = p.parts > 1 ? 2 : 1;
     ++g_kernel_launches;
-    const cudaError_t e = a.fp32 ? cudaLaunchKernelEx(&cfg, token_sample_kernel<true>, p) : cudaLaunchKernelEx(&cfg, token_sample_kernel<false>, p);
+    const cudaError_t e = a.fp32 ? (hold ? cudaLaunchKernelEx(&cfg, token_sample_kernel<true, true>, p) : cudaLaunchKernelEx(&cfg, token_sample_kernel<true, false>, p))
+                                 : (hold ? cudaLaunchKernelEx(&cfg, token_sample_kernel<false, true>, p) : cudaLaunchKernelEx(&cfg, token_sample_kernel<false, false>, p));
     return e == cudaSuccess ? MT_OK : MT_ERR_CUDA;
 }
 
