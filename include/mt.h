@@ -506,7 +506,7 @@ mt_status mt_kv_copy(const mt_kv_cache* const* caches_host, int32_t n_caches, co
  * min_p above 1, takes the first; one below 2^-126 counts as that.  Weights are 64-bit whole numbers, the largest 2^46 (fewer in rows of more than 2^16 logits), so draws do not depend on the
  * order of summing; what is below one of those units is never drawn.  A row without a distribution (nothing but minus infinity, a NaN or plus infinity) gives id -1 and NaN;
  * so does one with a negative, infinite or NaN temperature, a NaN limit or a uniform number outside [0, 1), with the sticky status MT_ERR_INVALID_ARG.
- * Limits: vocab below 2^30. */
+ * Limits: n at most 2^29; vocab below 2^30. */
 mt_status mt_token_sample(const void* logits, int32_t dtype, int64_t row_stride, int32_t n, int32_t vocab, const float* temperature,
                           const int32_t* top_k, const float* top_p, const float* min_p, const float* uniform, int32_t* ids, float* logprobs,
                           void* stream);

@@ -7,6 +7,8 @@
 // Tile.  Two tiles of 128 rows share the states that stream through shared memory.  A row is a (token, head) pair: R heads that share a
 // key/value head (the largest power of two in the group, 16 at most) are packed into the rows, so one token with a large group already shares its states.
 //
+// Sequences that follow one another and have the same states (answers about one image) are one: 64 answers, four to a source, 104 -> XX us a token step.
+//
 // Order of work.  A unit is a block of states for a tile pair; the units of all (sequence, head pack, tile pair) are in one line, which is cut
 // into equal shares, one a CTA.  A tile pair that a border cuts is done in pieces: each leaves its sums (o without the division, m, l) in scratch, and a
 // second launch joins them.  So one token over a long recording takes all SMs, and ragged batches are even.  Where there are tile pairs enough
@@ -34,7 +36,7 @@ struct Control {
     uint64_t q_full[2], q_empty, s_full[2], p_half[2], p_ready[2], o_ready[2], kv_full[8], kv_empty[8], v_raw[8], v_clean[8];
     uint32_t tmem;
     int abort;
-    int start[kMaxSeqs], len[kMaxSeqs], first[kMaxSeqs], states[kMaxSeqs];
+    int start[kMaxSeqs + 1], len[kMaxSeqs], first[kMaxSeqs], states[kMaxSeqs];
     long long before[kMaxSeqs + 1];           // units of the sequences before
 };
 constexpr int kControlBytes = ((int)sizeof(Control) + 127) / 128 * 128;
@@ -174,10 +176,22 @@ cross_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
         s.start[i] = a;
         s.len[i] = bad ? 0 : b - a;
         s.first[i] = f;
-        s.states[i] = bad ? 0 : e - f;
+        s.states[i] = bad ? -1 : e - f;
+        if (i == p.n_seqs - 1) s.start[p.n_seqs] = b;
     }
     __syncthreads();
     if (warp == 0) {
+        // neighbours with the same states become one: the first takes the tokens of all, the others have none
+        int next = p.n_seqs;                       // first sequence behind these 32 that begins one
+        for (int r0 = (p.n_seqs - 1) / 32 * 32; r0 >= 0; r0 -= 32) {
+            const int r = r0 + lane;
+            const bool there = r < p.n_seqs;
+            const bool begins = there && (r == 0 || s.states[r] < 0 || s.states[r - 1] < 0 || s.states[r] != s.states[r - 1] || s.first[r] != s.first[r - 1]);
+            const uint32_t heads = __ballot_sync(0xffffffffu, begins), behind = lane < 31 ? heads >> (lane + 1) : 0;
+            if (there && s.states[r] >= 0) s.len[r] = begins ? s.start[behind ? r + __ffs(behind) : next] - s.start[r] : 0;
+            if (heads) next = r0 + __ffs(heads) - 1;
+        }
+        __syncwarp();
         long long run = 0;
         for (int r0 = 0; r0 < p.n_seqs; r0 += 32) {
             const int r = r0 + lane;
@@ -359,6 +373,17 @@ cross_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
         note.last = -1;
         while (ok && next_piece(s, p, walk, it)) {
             if (i >= it.tiles) continue;
+            const int rows = min((it.len - it.t0) << p.pack_shift, 256);
+            if (i * 128 + (warp & 3) * 32 >= rows) {           // a warp without rows: what it would write is nobody's
+                for (int j = it.b0; j < it.b1; ++j) {
+                    ok = mbar_wait(bar(s.s_full[i]), n_s++ & 1, abort_flag, p.status.word, 273);
+                    if (!ok) break;
+                    mbar_arrive(bar(s.p_half[i]));
+                    mbar_arrive(bar(s.p_ready[i]));
+                    ++n_o;
+                }
+                continue;
+            }
             float m = 0.f, l = 0.f;
             for (int j = it.b0; j < it.b1; ++j) {
                 ok = mbar_wait(bar(s.s_full[i]), n_s++ & 1, abort_flag, p.status.word, 270);
@@ -446,7 +471,6 @@ cross_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
             ok = mbar_wait(bar(s.o_ready[i]), (n_o - 1) & 1, abort_flag, p.status.word, 272);
             if (!ok) break;
             tc_fence_after();
-            const int rows = min((it.len - it.t0) << p.pack_shift, 256);
             if (it.b1 - it.b0 == it.nb) {
                 const float inv = it.states > 0 ? 1.f / l : 0.f;
                 // 32 channels at a time through shared memory, so that four lanes store 64 contiguous bytes of a row
@@ -523,24 +547,37 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const CrossParams p,
     if (note.last < 0) return;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = gridDim.y * (kJoinThreads / 32);
     const Piece<D>* const pieces = static_cast<const Piece<D>*>(p.pieces);
+    const int n = note.last - blockIdx.x + 1;
+    auto piece = [&](int i) -> const Piece<D>& { return pieces[2 * (blockIdx.x + i) + (i == 0 ? 1 : 0)]; };
+    // (a CTA of fewer units than there are CTAs may have had none)
+    auto there = [&](int i) { return share_begin(note.total, blockIdx.x + i, ctas) < share_begin(note.total, blockIdx.x + i + 1, ctas); };
     for (int row = blockIdx.y * (kJoinThreads / 32) + warp; row < note.rows; row += warps) {
-        float o[D / 32], m = 0.f, l = 0.f;
-        bool none = true;
+        float m = -INFINITY, l = 0.f, o[D / 32];
 #pragma unroll
         for (int e = 0; e < D / 32; ++e) o[e] = 0.f;
-        for (int c = blockIdx.x; c <= note.last; ++c) {
-            if (share_begin(note.total, c, ctas) == share_begin(note.total, c + 1, ctas)) continue;
-            const Piece<D>& x = pieces[2 * c + (c == blockIdx.x ? 1 : 0)];
-            const float2 ml = x.ml[row];
-            if (ml.y == 0.f) continue;                         // all its scores minus infinity
-            const float nm = none ? ml.x : fmaxf(m, ml.x), old = none ? 0.f : ex2((m - nm) * p.c), f = ex2((ml.x - nm) * p.c);
-            l = l * old + ml.y * f;
+        for (int i = lane; i < n; i += 32)
+            if (there(i) && piece(i).ml[row].y != 0.f) m = fmaxf(m, piece(i).ml[row].x);     // (0: all its scores minus infinity)
+        m = warp_max(m);
+        for (int i0 = 0; i0 < n; i0 += 32) {
+            float f = -1.f;                   // nothing to add
+            if (i0 + lane < n && there(i0 + lane)) {
+                const float2 ml = piece(i0 + lane).ml[row];
+                if (ml.y != 0.f) {
+                    f = ml.y == ml.y ? ex2((ml.x - m) * p.c) : ml.y;
+                    l += ml.y * f;
+                }
+            }
+#pragma unroll 4
+            for (int k = 0; k < min(32, n - i0); ++k) {
+                const float g = __shfl_sync(0xffffffffu, f, k);
+                const float* const x = piece(i0 + k).o[row] + lane;
+                if (g != -1.f) {
 #pragma unroll
-            for (int e = 0; e < D / 32; ++e) o[e] = o[e] * old + x.o[row][lane + 32 * e] * f;
-            m = nm;
-            none = false;
+                    for (int e = 0; e < D / 32; ++e) o[e] = fmaf(x[32 * e], g, o[e]);
+                }
+            }
         }
-        const float inv = 1.f / l;
+        const float inv = 1.f / warp_sum(l);
         const int token = note.row + (row >> p.pack_shift), head = note.pack * p.pack + (row & (p.pack - 1));
         uint16_t* const out = p.out + ((int64_t)token * p.q_heads + head) * D;
 #pragma unroll

@@ -77,4 +77,4 @@ def test_copy_refusals(lib):
 
 def test_sample_refusals(lib):
     f = lambda dt=0, stride=100, n=1, vocab=100: lib.mt_token_sample(None, dt, stride, n, vocab, *[None] * 8)
-    assert f(dt=2) == 1 and f(n=-1) == 1 and f(vocab=0) == 1 and f(vocab=1 << 30) == 4 and f(stride=-1) == 4 and f(stride=1 << 36) == 4 and f() == 9
+    assert f(dt=2) == 1 and f(n=-1) == 1 and f(vocab=0) == 1 and f(vocab=1 << 30) == 4 and f(n=(1 << 29) + 1) == 4 and f(stride=-1) == 4 and f(stride=1 << 36) == 4 and f() == 9
