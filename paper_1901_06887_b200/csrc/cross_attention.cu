@@ -7,7 +7,7 @@
 // Tile.  Two tiles of 128 rows share the states that stream through shared memory.  A row is a (token, head) pair: R heads that share a
 // key/value head (the largest power of two in the group, 16 at most) are packed into the rows, so one token with a large group already shares its states.
 //
-// Sequences that follow one another and have the same states (answers about one image) are one: 64 answers, four to a source, 104 -> XX us a token step.
+// Sequences that follow one another and have the same states (answers about one image) are one: 64 answers, four to a source, 104 -> 39 us a token step.
 //
 // Order of work.  A unit is a block of states for a tile pair; the units of all (sequence, head pack, tile pair) are in one line, which is cut
 // into equal shares, one a CTA.  A tile pair that a border cuts is done in pieces: each leaves its sums (o without the division, m, l) in scratch, and a
@@ -27,20 +27,38 @@ constexpr int kThreads = 384;
 constexpr int kMaxSeqs = 512;                 // sequences of one launch
 constexpr float kSlack = 8.f;
 constexpr int kEnough = 8;                    // tile pairs an SM, from which shares end at tile pairs
+constexpr int kUneven = 20;                   // units that the longest such share may have above the mean: what pieces and their joins cost
 constexpr int kJoinThreads = 256;
 
 template <int D> __host__ __device__ constexpr int slots() { return D == 128 ? 4 : 8; }
 template <int D> __host__ __device__ constexpr int operand_bytes() { return kHalf * (D / 64); }
 
+// A share of the line of units, piece by piece.
+struct Walk {
+    int left;                                 // units (of queries that fit in memory a CTA has fewer than 2^31)
+    int seq, pack, tile, block;               // where the next one is
+};
+struct Work {
+    int seq, t0, pack;                        // first token of the tile pair, head pack
+    int states;
+    int b0, b1, nb;                           // blocks of the piece, and of the tile pair
+    int tiles;                                // tiles with rows
+};
 struct Control {
-    uint64_t q_full[2], q_empty, s_full[2], p_half[2], p_ready[2], o_ready[2], kv_full[8], kv_empty[8], v_raw[8], v_clean[8];
+    uint64_t q_full[2], q_empty, s_full[2], s_free[2], p_half[2], p_ready[2], o_ready[2], kv_full[8], kv_empty[8], v_raw[8], v_clean[8];
     uint32_t tmem;
-    int abort;
+    int abort, whole;
+    unsigned long long longest;
     int start[kMaxSeqs + 1], len[kMaxSeqs], first[kMaxSeqs], states[kMaxSeqs];
     long long before[kMaxSeqs + 1];           // units of the sequences before
+    Walk walk[8];                             // of the softmax warps, while a piece is under way: the registers are needed
+    Work work[8];
 };
 constexpr int kControlBytes = ((int)sizeof(Control) + 127) / 128 * 128;
 constexpr int kStageBytes = 8 * 2048;           // output staging of the eight softmax warps
+// P lies over the columns of S, or, where tensor memory has room, behind O: then the next S is made while the exponentials of this one run.  (16 heads of 64, 11 001
+// queries, 4500 to 6000 states: 321 against 342 us.)
+template <int D> __host__ __device__ constexpr bool apart() { return 256 + 2 * D + 2 * 64 <= 512; }
 template <int D> constexpr int shared_bytes() { return 1024 + (2 + slots<D>()) * operand_bytes<D>() + kControlBytes + kStageBytes; }
 
 // What a CTA leaves behind of a tile pair that a border cuts: two such places a CTA, the piece that ends a tile pair begun by others, and the one
@@ -60,7 +78,7 @@ struct CrossParams {
     const int32_t *offsets, *ranges;
     int n_seqs, seq0, n_tokens, n_states;
     int q_heads, group, pack, pack_shift;     // pack: heads packed into a tile's rows
-    int whole;                                // shares end at tile pairs
+    int whole;                                // shares end at tile pairs: 0 no, 1 yes, 2 if that is even enough
     float c;                                  // |scale| log2(e)
     int negate;                               // scale < 0
     uint16_t* out;
@@ -69,17 +87,6 @@ struct CrossParams {
     OpStatus status;
 };
 
-// A share of the line of units, piece by piece.
-struct Walk {
-    long long at, end;
-    int seq, pack, tile, block;               // where `at` is
-};
-struct Work {
-    int start, len, t0, pack;                 // first row of the sequence, its length, first token of the tile pair, head pack
-    int first, states;                        // the sequence's states
-    int b0, b1, nb;                           // blocks of the piece, and of the tile pair
-    int tiles;                                // tiles with rows
-};
 __device__ __forceinline__ int blocks_of(int states) { return states > 0 ? (states + kBlock - 1) / kBlock : 1; }
 __device__ __forceinline__ long long share_begin(long long total, int cta, int ctas) { return total * cta / ctas; }
 
@@ -96,41 +103,43 @@ __device__ __forceinline__ void locate(const Control& s, const CrossParams& p, l
     w.pack = (int)(item / tiles);
     w.tile = (int)(item - (long long)w.pack * tiles);
 }
-__device__ __forceinline__ Walk begin_share(const Control& s, const CrossParams& p) {
+// First unit of a CTA's share.
+__device__ __forceinline__ long long share_edge(const Control& s, const CrossParams& p, int cta, bool whole) {
     const long long total = s.before[p.n_seqs];
-    long long edge[2];
-#pragma unroll
-    for (int e = 0; e < 2; ++e) {
-        long long x = share_begin(total, blockIdx.x + e, gridDim.x);
-        if (p.whole && x < total) {
-            Walk w;
-            locate(s, p, x, w);
-            if (w.block > 0) x += blocks_of(s.states[w.seq]) - w.block;
-        }
-        edge[e] = x;
+    long long x = share_begin(total, cta, gridDim.x);
+    if (whole && x < total) {
+        Walk w;
+        locate(s, p, x, w);
+        if (w.block > 0) x += blocks_of(s.states[w.seq]) - w.block;
     }
+    return x;
+}
+__device__ __forceinline__ Walk begin_share(const Control& s, const CrossParams& p) {
+    const bool whole = s.whole != 0;
+    const long long edge[2] = {share_edge(s, p, blockIdx.x, whole), share_edge(s, p, blockIdx.x + 1, whole)};
     Walk w;
-    w.at = edge[0];
-    w.end = edge[1];
+    w.left = (int)(edge[1] - edge[0]);
     w.seq = w.pack = w.tile = w.block = 0;
-    if (w.at < w.end) locate(s, p, w.at, w);
+    if (w.left > 0) locate(s, p, edge[0], w);
     return w;
 }
 // The next piece of the share.
 __device__ __forceinline__ bool next_piece(const Control& s, const CrossParams& p, Walk& w, Work& k) {
-    if (w.at >= w.end) return false;
-    const int tokens = 256 >> p.pack_shift;
-    while (s.before[w.seq + 1] <= w.at) { ++w.seq; w.pack = w.tile = w.block = 0; }      // (sequences without rows have no units)
-    k.start = s.start[w.seq]; k.len = s.len[w.seq]; k.first = s.first[w.seq]; k.states = s.states[w.seq];
+    if (w.left <= 0) return false;
+    const int tokens = 256 >> p.pack_shift, packs = p.q_heads >> p.pack_shift;
+    while (w.pack == packs || s.len[w.seq] == 0) { ++w.seq; w.pack = w.tile = w.block = 0; }
+    const int len = s.len[w.seq];
+    k.seq = w.seq;
+    k.states = s.states[w.seq];
     k.pack = w.pack;
     k.t0 = w.tile * tokens;
     k.nb = blocks_of(k.states);
     k.b0 = w.block;
-    k.b1 = (int)min((long long)k.nb, w.block + (w.end - w.at));
-    k.tiles = k.t0 + tokens / 2 < k.len ? 2 : 1;
-    w.at += k.b1 - k.b0;
+    k.b1 = min(k.nb, w.block + w.left);
+    k.tiles = k.t0 + tokens / 2 < len ? 2 : 1;
+    w.left -= k.b1 - k.b0;
     w.block = 0;
-    if (++w.tile * tokens >= k.len) { w.tile = 0; ++w.pack; }
+    if (++w.tile * tokens >= len) { w.tile = 0; ++w.pack; }
     return true;
 }
 
@@ -140,6 +149,8 @@ cross_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
                        const __grid_constant__ CUtensorMap map_v, const CrossParams p) {
     extern __shared__ uint8_t smem_raw[];
     constexpr int kSlots = slots<D>(), kOp = operand_bytes<D>();
+    constexpr bool kApart = apart<D>();
+    constexpr int kP0 = kApart ? 256 + 2 * D : 0, kPStep = kApart ? 64 : 128;  // columns of P
     const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
     uint8_t* const smem = smem_raw + (base - raw);
     Control& s = *reinterpret_cast<Control*>(smem + (2 + kSlots) * kOp);
@@ -150,7 +161,7 @@ cross_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < 2; ++i) {
-            mbar_init(bar(s.q_full[i]), 1); mbar_init(bar(s.s_full[i]), 1); mbar_init(bar(s.p_half[i]), 128); mbar_init(bar(s.p_ready[i]), 128);
+            mbar_init(bar(s.q_full[i]), 1); mbar_init(bar(s.s_full[i]), 1); mbar_init(bar(s.s_free[i]), 128); mbar_init(bar(s.p_half[i]), 128); mbar_init(bar(s.p_ready[i]), 128);
             mbar_init(bar(s.o_ready[i]), 1);
         }
         mbar_init(bar(s.q_empty), 1);
@@ -205,20 +216,27 @@ cross_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
             if (r < p.n_seqs) s.before[r] = run + incl - v;
             run += __shfl_sync(0xffffffffu, incl, 31);
         }
-        if (lane == 0) s.before[p.n_seqs] = run;
+        if (lane == 0) { s.before[p.n_seqs] = run; s.whole = p.whole == 1; s.longest = 0; }
+    }
+    if (p.whole == 2) {
+        __syncthreads();
+        for (int i = threadIdx.x; i < gridDim.x; i += kThreads)
+            atomicMax(&s.longest, (unsigned long long)(share_edge(s, p, i + 1, true) - share_edge(s, p, i, true)));
+        __syncthreads();
+        if (threadIdx.x == 0) s.whole = (long long)s.longest <= s.before[p.n_seqs] / gridDim.x + kUneven;
     }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     pdl_launch_dependents();
     const uint32_t tmem = s.tmem;
-    const uint32_t tmem_s = tmem, tmem_o = tmem + 256;         // S (and P) of tile i: + 128 i; O: + D i
+    const uint32_t tmem_s = tmem, tmem_o = tmem + 256;         // S of tile i: + 128 i; O: + D i; P: see kApart
     Walk walk = begin_share(s, p);
     Work it;
 
     if (warp == 8) {
         // ------------------------------------------------------------------------------------------ copies
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 120;");
         if (lane == 0) {
             int fill = 0, rounds = 0;            // operands put into the ring so far; pieces
             bool ok = true;
@@ -228,7 +246,7 @@ cross_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
                 for (int i = 0; i < it.tiles; ++i) {
                     mbar_expect_tx(bar(s.q_full[i]), kOp);
                     for (int h = 0; h < D / 64; ++h)
-                        tma_load_3d(q_smem + i * kOp + h * kHalf, &map_q, h * 64, it.pack * p.pack, it.start + it.t0 + i * (tokens / 2), bar(s.q_full[i]));
+                        tma_load_3d(q_smem + i * kOp + h * kHalf, &map_q, h * 64, it.pack * p.pack, s.start[it.seq] + it.t0 + i * (tokens / 2), bar(s.q_full[i]));
                 }
                 const int kv_head = it.pack * p.pack / p.group;
                 for (int x = 2 * it.b0; ok && x < 2 * it.b1; ++x, ++fill) {
@@ -240,14 +258,14 @@ cross_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
                     const uint32_t full = ragged ? bar(s.v_raw[slot]) : bar(s.kv_full[slot]);
                     mbar_expect_tx(full, kOp);
                     for (int h = 0; h < D / 64; ++h)
-                        tma_load_3d(kv_smem + slot * kOp + h * kHalf, (x & 1) ? &map_v : &map_k, h * 64, kv_head, it.first + (x >> 1) * kBlock, full);
+                        tma_load_3d(kv_smem + slot * kOp + h * kHalf, (x & 1) ? &map_v : &map_k, h * 64, kv_head, s.first[it.seq] + (x >> 1) * kBlock, full);
                     if (ragged) mbar_arrive(bar(s.kv_full[slot]));
                 }
             }
         }
     } else if (warp == 9) {
         // ------------------------------------------------------------------------------------------ matrix instructions
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 120;");
         // the whole warp walks the loop, so that addresses stay warp-uniform; one elected lane issues
         const bool leader = elect_one();
         constexpr uint32_t kIdPv = make_idesc_bf16(128, D) | (1u << 16);
@@ -255,7 +273,7 @@ cross_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
         const uint32_t q_lo = desc_lo(q_smem), k_lo = desc_lo(kv_smem), v_lo = desc_lo_values(kv_smem);
         const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
         constexpr uint32_t kOpLo = kOp >> 4;
-        uint32_t fill = 0, n_q0 = 0, n_q1 = 0, n_p0 = 0, n_p1 = 0, clean_phase = 0;
+        uint32_t fill = 0, n_q0 = 0, n_q1 = 0, n_p0 = 0, n_p1 = 0, clean_phase = 0;      // n_p: blocks of the tile so far
         bool ok = true;
         auto wait = [&](const uint64_t& b, uint32_t parity, int where) { ok = ok && mbar_wait(bar(b), parity & 1, abort_flag, p.status.word, where); };
         auto qk = [&](int i, uint32_t slot) {
@@ -272,7 +290,7 @@ cross_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
         };
         // the first 64 states go while the second half of P is still in its exponentials
         auto pv = [&](int i, uint32_t slot, bool first, uint32_t n) {
-            const uint32_t d = tm + 256 + D * i, a = tm + 128 * i, b = v_lo + slot * kOpLo;
+            const uint32_t d = tm + 256 + D * i, a = tm + kP0 + kPStep * i, b = v_lo + slot * kOpLo;
             wait(s.p_half[i], n, 254);
             if (!ok) return;
             tc_fence_after();
@@ -313,19 +331,32 @@ cross_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
             }
             for (int j = 0; ok && j < nb; ++j) {
                 const uint32_t vx = fill + 2 * j + 1, vslot = vx % kSlots, kslot = (vx + 1) % kSlots, kpar = (vx + 1) / kSlots;
+                if (kApart && j + 1 < nb) {
+                    wait(s.kv_full[kslot], kpar, 255);
+                    wait(s.s_free[0], n_p0, 257);
+                    if (!ok) break;
+                    tc_fence_after();
+                    qk(0, kslot);
+                }
                 wait(s.kv_full[vslot], vx / kSlots, 252);
                 if (j == ragged) {
                     wait(s.v_clean[vslot], clean_phase >> vslot, 253);
                     clean_phase ^= 1u << vslot;
                 }
-                if (j + 1 < nb) wait(s.kv_full[kslot], kpar, 255);
+                if (!kApart && j + 1 < nb) wait(s.kv_full[kslot], kpar, 255);
                 pv(0, vslot, j == 0, n_p0++);
                 if (!ok) break;
-                if (j + 1 < nb) qk(0, kslot);
+                if (!kApart && j + 1 < nb) qk(0, kslot);
                 if (two) {
+                    if (kApart && j + 1 < nb) {
+                        wait(s.s_free[1], n_p1, 257);
+                        if (!ok) break;
+                        tc_fence_after();
+                        qk(1, kslot);
+                    }
                     pv(1, vslot, j == 0, n_p1++);
                     if (!ok) break;
-                    if (j + 1 < nb) qk(1, kslot);
+                    if (!kApart && j + 1 < nb) qk(1, kslot);
                 }
                 if (leader) {
                     umma_commit(bar(s.kv_empty[vslot]));
@@ -337,7 +368,7 @@ cross_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
         }
     } else if (warp >= 10) {
         // ------------------------------------------------------------------------------------------ values behind the last state
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 120;");
         const int t = threadIdx.x - 320;         // rows t and t + 64
         int fill = 0;
         uint32_t raw_phase = 0;
@@ -362,30 +393,35 @@ cross_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
     } else {
         // ------------------------------------------------------------------------------------------ softmax, one row per thread
         // registers move here: 256 threads x 208 + 128 x 88 = the launch's 384 x 168
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 192;");
         const int i = warp >> 2;
         const int r = threadIdx.x & 127;
         const uint32_t lanes = (uint32_t)(warp & 3) << 21;     // tensor-memory lane of the warp's first row, in the address's upper half
-        const uint32_t my_s = tmem_s + 128 * i + lanes, my_o = tmem_o + D * i + lanes;
+        const uint32_t my_s = tmem_s + 128 * i + lanes, my_o = tmem_o + D * i + lanes, my_p = tmem + kP0 + kPStep * i + lanes;
         int n_s = 0, n_o = 0;
         bool ok = true;
-        Note note;
-        note.last = -1;
+        if (threadIdx.x == 0 && p.notes) p.notes[blockIdx.x].last = -1;
         while (ok && next_piece(s, p, walk, it)) {
             if (i >= it.tiles) continue;
-            const int rows = min((it.len - it.t0) << p.pack_shift, 256);
-            if (i * 128 + (warp & 3) * 32 >= rows) {           // a warp without rows: what it would write is nobody's
+            if (i * 128 + (warp & 3) * 32 >= min(s.len[it.seq] - it.t0, tokens) << p.pack_shift) {           // a warp without rows: what it would write is nobody's
                 for (int j = it.b0; j < it.b1; ++j) {
                     ok = mbar_wait(bar(s.s_full[i]), n_s++ & 1, abort_flag, p.status.word, 273);
                     if (!ok) break;
+                    if (kApart) {             // (not ahead of the other warps: the barriers count them all)
+                        mbar_arrive(bar(s.s_free[i]));
+                        if (j > it.b0) ok = mbar_wait(bar(s.o_ready[i]), (n_o - 1) & 1, abort_flag, p.status.word, 275);
+                        if (!ok) break;
+                    }
                     mbar_arrive(bar(s.p_half[i]));
                     mbar_arrive(bar(s.p_ready[i]));
                     ++n_o;
                 }
                 continue;
             }
+            if (lane == 0) { s.walk[warp] = walk; s.work[warp] = it; }
+            const int first = it.b0, end = it.b1, states = it.states;
             float m = 0.f, l = 0.f;
-            for (int j = it.b0; j < it.b1; ++j) {
+            for (int j = first; j < end; ++j) {
                 ok = mbar_wait(bar(s.s_full[i]), n_s++ & 1, abort_flag, p.status.word, 270);
                 if (!ok) break;
                 tc_fence_after();
@@ -393,8 +429,12 @@ cross_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
 #pragma unroll
                 for (int c = 0; c < 4; ++c) tmem_ld32(my_s + 32 * c, x[c]);
                 tmem_ld_wait();
-                if ((j + 1) * kBlock > it.states) {
-                    const int lim = it.states - j * kBlock;    // states of the block
+                if (kApart) {
+                    tc_fence_before();
+                    mbar_arrive(bar(s.s_free[i]));
+                }
+                if ((j + 1) * kBlock > states) {
+                    const int lim = states - j * kBlock;    // states of the block
 #pragma unroll
                     for (int c = 0; c < 4; ++c)
 #pragma unroll
@@ -411,16 +451,23 @@ cross_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
                 const float mx = fmaxf(max3(mx4[0], mx4[1], mx4[2]), mx4[3]);
                 // (a row without weight so far, all its scores minus infinity, starts again; m stays finite)
                 const bool move = (mx - m) * p.c > kSlack || l == 0.f;
-                if (j == it.b0) {
+                if (j == first) {
                     m = mx > -INFINITY ? mx : 0.f;
-                } else if (__any_sync(0xffffffffu, move)) {
+                } else if (kApart) {          // P of the block before has to be read before this one's is written
+                    ok = mbar_wait(bar(s.o_ready[i]), (n_o - 1) & 1, abort_flag, p.status.word, 271);
+                    if (!ok) break;
+                    tc_fence_after();
+                }
+                if (j > first && __any_sync(0xffffffffu, move)) {
                     // (a row moves on its own account only, so its bits do not depend on its neighbours)
                     const float nm = move && mx > -INFINITY ? mx : m, f = m == nm || l == 0.f ? 1.f : ex2((m - nm) * p.c);
                     m = nm;
                     l *= f;
-                    ok = mbar_wait(bar(s.o_ready[i]), (n_o - 1) & 1, abort_flag, p.status.word, 271);
-                    if (!ok) break;
-                    tc_fence_after();
+                    if (!kApart) {
+                        ok = mbar_wait(bar(s.o_ready[i]), (n_o - 1) & 1, abort_flag, p.status.word, 274);
+                        if (!ok) break;
+                        tc_fence_after();
+                    }
 #pragma unroll 1
                     for (int c = 0; c < D / 16; ++c) {
                         uint32_t y[16];
@@ -450,7 +497,7 @@ cross_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
                         sum[e & 1] = add2(sum[e & 1], pair_of(a, b));
                         w[e] = pack_bf16x2(a, b);
                     }
-                    tmem_st16(my_s + 16 * c, w);
+                    tmem_st16(my_p + 16 * c, w);
                 };
                 chunk(0);
                 chunk(1);
@@ -471,6 +518,11 @@ cross_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
             ok = mbar_wait(bar(s.o_ready[i]), (n_o - 1) & 1, abort_flag, p.status.word, 272);
             if (!ok) break;
             tc_fence_after();
+            __syncwarp();
+            walk = s.walk[warp];
+            it = s.work[warp];
+            __syncwarp();                     // (before the next piece is put there)
+            const int rows = min(s.len[it.seq] - it.t0, tokens) << p.pack_shift;
             if (it.b1 - it.b0 == it.nb) {
                 const float inv = it.states > 0 ? 1.f / l : 0.f;
                 // 32 channels at a time through shared memory, so that four lanes store 64 contiguous bytes of a row
@@ -498,7 +550,7 @@ cross_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
                         const int head = it.pack * p.pack + (of_pair & (p.pack - 1));
                         const uint4 w = stage[row * 4 + (sub ^ ((row >> 1) & 3))];
                         if (of_pair < rows)
-                            reinterpret_cast<uint4*>(p.out + ((int64_t)(it.start + it.t0 + (of_pair >> p.pack_shift)) * p.q_heads + head) * D)[c * 4 + sub] = w;
+                            reinterpret_cast<uint4*>(p.out + ((int64_t)(s.start[it.seq] + it.t0 + (of_pair >> p.pack_shift)) * p.q_heads + head) * D)[c * 4 + sub] = w;
                     }
                 }
             } else {
@@ -517,15 +569,13 @@ cross_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
                 }
                 if (row < rows) piece.ml[row] = make_float2(m, l);
                 if (it.b0 == 0) {
-                    const long long total = s.before[p.n_seqs], end = walk.at + (it.nb - it.b1);       // of the tile pair
-                    note.total = total;
-                    note.last = (int)((end * gridDim.x - 1) / total);
-                    note.row = it.start + it.t0; note.rows = rows; note.pack = it.pack;
+                    const int of_seq = (s.len[it.seq] + tokens - 1) / tokens;
+                    const long long total = s.before[p.n_seqs], last = s.before[it.seq] + ((long long)it.pack * of_seq + it.t0 / tokens + 1) * it.nb;
+                    if (threadIdx.x == 0) p.notes[blockIdx.x] = {total, (int)((last * gridDim.x - 1) / total), s.start[it.seq] + it.t0, rows, it.pack};
                 }
             }
             tc_fence_before();
         }
-        if (threadIdx.x == 0 && p.notes) p.notes[blockIdx.x] = note;
     }
     // (every thread gets here, also after an abandoned wait)
     if (*abort_flag) settle();
@@ -594,9 +644,9 @@ mt_status launch(const CrossArgs& a, CrossParams& p, const CUtensorMap& mq, cons
         p.offsets = a.offsets + seq0;
         p.ranges = a.ranges + 2 * (int64_t)seq0;
         cudaError_t e = launch_pdl(cross_attention_kernel<D>, dim3((unsigned)grid), dim3(kThreads), (size_t)shared_bytes<D>(), s, mq, mk, mv, p);
-        if (e == cudaSuccess && !p.whole) {
-            const int64_t rows = (int64_t)a.d.n_tokens * p.pack;               // of a tile pair, at most
-            e = launch_pdl(join_kernel<D>, dim3((unsigned)grid, rows > 64 ? 4 : 1), dim3(kJoinThreads), 0, s, p, grid);
+        if (e == cudaSuccess && p.whole != 1) {
+            const int64_t all = (int64_t)a.d.n_tokens * p.pack, rows = all < 256 ? all : 256;                          // of a tile pair, at most
+            e = launch_pdl(join_kernel<D>, dim3((unsigned)grid, (unsigned)((rows + 15) / 16)), dim3(kJoinThreads), 0, s, p, grid);
         }
         if (e != cudaSuccess) return MT_ERR_CUDA;
         if (a.d.n_seqs - seq0 <= kMaxSeqs) break;
@@ -629,10 +679,10 @@ mt_status launch_cross_attention(const CrossArgs& a, const OpContext& c, cudaStr
     p.status = a.status;
     // tile pairs of all sequences together, at least (where the offsets take in all tokens)
     const int64_t pairs = ((int64_t)d.n_tokens * p.pack + 255) / 256 * (d.q_heads / p.pack);
-    p.whole = pairs >= (int64_t)kEnough * c.sm_count;
+    p.whole = pairs >= (int64_t)kEnough * c.sm_count ? 1 : pairs >= c.sm_count ? 2 : 0;
     p.notes = nullptr;
     p.pieces = nullptr;
-    if (!p.whole) {
+    if (p.whole != 1) {
         const size_t notes = (sizeof(Note) * c.sm_count + 255) / 256 * 256;
         uint8_t* w;
         const mt_status st = op_scratch(s, notes + 2 * (size_t)c.sm_count * (d.head_dim == 64 ? sizeof(Piece<64>) : sizeof(Piece<128>)), &w);
