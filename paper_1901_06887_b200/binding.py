@@ -704,19 +704,19 @@ class KvPages:
 
 
 def _is_ints(t, n: int) -> bool:
-    return t.dtype is _Types.i32 and t.get_device() == _device and t.dim() == 1 and t.numel() == n and t.is_contiguous() and n <= _MOST
+    return t.dtype is _Types.i32 and t.get_device() == _device and t.shape == (n,) and t.is_contiguous() and n <= _MOST
 
 
-def _is_copies(t) -> bool:
-    return t.dtype is _Types.i32 and t.get_device() == _device and t.dim() == 2 and t.shape[1] == 3 and t.is_contiguous() and t.shape[0] <= _MOST
+def _is_copies(t, n: int) -> bool:
+    return t.dtype is _Types.i32 and t.get_device() == _device and t.shape == (n, 3) and t.is_contiguous() and n <= _MOST
 
 
 def mt_kv_reserve(pages: KvPages, rows, counts, slots, stream=None) -> None:
     """Room for counts[i] more tokens in row rows[i] (int32); slots int64 (at least sum(counts)): where they go, for mt_kv_append."""
-    T, n = _types(), rows.numel()
-    if not (_is_ints(rows, n) and _is_ints(counts, n) and slots.dtype is T.i64 and slots.get_device() == _device and slots.dim() == 1 and slots.is_contiguous()):
+    T, n, m = _types(), rows.numel(), slots.numel()
+    if not (_is_ints(rows, n) and _is_ints(counts, n) and slots.dtype is T.i64 and slots.get_device() == _device and slots.shape == (m,) and slots.is_contiguous()):
         _refuse("mt_kv_reserve")
-    code = (_lib or lib()).mt_kv_reserve(pages.ref, rows.data_ptr(), counts.data_ptr(), n, slots.data_ptr(), slots.numel(), _stream_handle(stream))
+    code = (_lib or lib()).mt_kv_reserve(pages.ref, rows.data_ptr(), counts.data_ptr(), n, slots.data_ptr(), m, _stream_handle(stream))
     if code:
         raise MtError(code, "mt_kv_reserve")
 
@@ -725,7 +725,7 @@ def mt_kv_fork(pages: KvPages, parents, children, copies, stream=None) -> None:
     """Row children[i] becomes what row parents[i] was (int32); copies int32 [n, 3]: what mt_kv_copy has to copy."""
     _types()
     n = parents.numel()
-    if not (_is_ints(parents, n) and _is_ints(children, n) and _is_copies(copies) and copies.shape[0] == n):
+    if not (_is_ints(parents, n) and _is_ints(children, n) and _is_copies(copies, n)):
         _refuse("mt_kv_fork")
     code = (_lib or lib()).mt_kv_fork(pages.ref, parents.data_ptr(), children.data_ptr(), n, copies.data_ptr(), _stream_handle(stream))
     if code:
@@ -746,9 +746,10 @@ def mt_kv_release(pages: KvPages, rows, stream=None) -> None:
 def mt_kv_compact(pages: KvPages, copies, stream=None) -> None:
     """Moves used pages to the front, at most copies.shape[0] of them; copies int32 [n, 3]: what mt_kv_copy has to copy."""
     _types()
-    if not _is_copies(copies):
+    n = copies.numel() // 3
+    if not _is_copies(copies, n):
         _refuse("mt_kv_compact")
-    code = (_lib or lib()).mt_kv_compact(pages.ref, copies.data_ptr(), copies.shape[0], _stream_handle(stream))
+    code = (_lib or lib()).mt_kv_compact(pages.ref, copies.data_ptr(), n, _stream_handle(stream))
     if code:
         raise MtError(code, "mt_kv_compact")
 
@@ -765,9 +766,10 @@ class KvCopier:
 def mt_kv_copy(copier: KvCopier, copies, stream=None) -> None:
     """Copies pages in every cache: copies int32 [n, 3], page from, page to, tokens; -1, -1 is left out."""
     _types()
-    if not _is_copies(copies):
+    n = copies.numel() // 3
+    if not _is_copies(copies, n):
         _refuse("mt_kv_copy")
-    code = (_lib or lib()).mt_kv_copy(copier.array, copier.n, copies.data_ptr(), copies.shape[0], _stream_handle(stream))
+    code = (_lib or lib()).mt_kv_copy(copier.array, copier.n, copies.data_ptr(), n, _stream_handle(stream))
     if code:
         raise MtError(code, "mt_kv_copy")
 

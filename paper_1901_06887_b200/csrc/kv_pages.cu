@@ -5,8 +5,9 @@
 // one that is partly filled, so nothing that a row appends is seen by another.
 //
 // Split.  Bookkeeping is a handful of dependent steps over small integers (who comes first, which pages are free, who gets which, write), so it
-// is one launch of one team: a CTA, or a cluster of eight where there is more to read than a CTA takes quickly.  Free pages are found by a scan of
-// the references: every warp counts its stretch, the counts are added up, every warp lists its stretch.
+// is one launch of one team: a CTA, or a cluster of eight where there is more to read than a CTA takes quickly.  What the steps hand on lies in shared
+// memory where one CTA is the team and it fits (SMALL), else in scratch: every trip to device memory between two steps costs half a microsecond.  Free pages are
+// found by a scan of the references: every warp counts its stretch, the counts are added up, every warp lists its stretch.
 #include "lm_device.cuh"
 #include "lm_host.h"
 
@@ -15,6 +16,8 @@ namespace {
 
 constexpr int kThreads = 1024, kWarps = kThreads / 32;
 constexpr int kTeam = 8;                      // CTAs of a large call
+constexpr int kFew = 4;                       // tokens that a thread adds by itself
+constexpr int kSmall = 1024, kSmallRows = 4096, kSmallList = 4096;            // places, rows and free pages that SMALL holds
 
 __device__ __forceinline__ uint32_t remote_u32(const void* p, uint32_t rank) {
     uint32_t v;
@@ -25,8 +28,30 @@ __device__ __forceinline__ uint32_t remote_u32(const void* p, uint32_t rank) {
 struct Shared {
     int warp_free[kWarps];                    // free pages of each warp's stretch, then those before it in the CTA
     int free, holes;                          // of this CTA
-    long long scan[kWarps];
+    long long scan[2][kWarps];
 };
+
+// What the steps of a call hand on.
+struct SmallHand {
+    int32_t rows[kSmall], other[kSmall], owner[kSmallRows], info[kSmall], list[kSmallList];
+    long long place[2 * kSmall];
+};
+struct Hand {
+    SmallHand* small;
+    const int32_t *rows, *other;              // of the call
+    int32_t *owner, *info;
+    long long* place;
+    int32_t *near, *far;                      // free pages: the first `most_near` of them, the rest
+    int most_near;
+    __device__ __forceinline__ void put(int rank, int page) const {
+        if (rank < most_near) near[rank] = page; else far[rank] = page;
+    }
+};
+// (written by another CTA of the team, perhaps)
+template <bool SMALL, class T>
+__device__ __forceinline__ T fetch(const T* p) { return SMALL ? *p : __ldcg(p); }
+template <bool SMALL>
+__device__ __forceinline__ int free_page(const Hand& h, long long rank) { return rank < h.most_near ? h.near[rank] : __ldcg(h.far + rank); }
 
 struct Team {
     int rank, size, warp, lane;               // warp: of the whole team
@@ -67,10 +92,12 @@ __device__ __forceinline__ uint32_t free_of_four(const int32_t* refs, int at, in
     }
     return m;
 }
-__device__ __forceinline__ void count_free(const Team& t, Shared& s, const int32_t* refs, int n_pages) {
+// (returns the mask of the lane's first four pages, which for_stretch need not read again)
+__device__ __forceinline__ uint32_t count_free(const Team& t, Shared& s, const int32_t* refs, int n_pages) {
     const Stretch x = stretch_of(t, n_pages);
-    int n = 0;
-    for (int at = x.begin + 4 * t.lane; at < x.end; at += 128) n += __popc(free_of_four(refs, at, x.end));
+    const uint32_t first = x.begin + 4 * t.lane < x.end ? free_of_four(refs, x.begin + 4 * t.lane, x.end) : 0;
+    int n = __popc(first);
+    for (int at = x.begin + 128 + 4 * t.lane; at < x.end; at += 128) n += __popc(free_of_four(refs, at, x.end));
 #pragma unroll
     for (int o = 16; o; o >>= 1) n += __shfl_xor_sync(0xffffffffu, n, o);
     if (t.lane == 0) s.warp_free[threadIdx.x >> 5] = n;
@@ -86,6 +113,7 @@ __device__ __forceinline__ void count_free(const Team& t, Shared& s, const int32
         s.warp_free[threadIdx.x] = incl - v;
         if (threadIdx.x == 31) { s.free = incl; s.holes = 0; }
     }
+    return first;
 }
 // (behind a sync of the team) free pages before this CTA's first, and all of them
 __device__ __forceinline__ void total_free(const Team& t, const Shared& s, int& before, int& all) {
@@ -99,12 +127,12 @@ __device__ __forceinline__ void total_free(const Team& t, const Shared& s, int& 
 }
 // f(first page of four, mask of the free ones, number of free pages before them), for this warp's stretch
 template <class F>
-__device__ __forceinline__ void for_stretch(const Team& t, const Shared& s, const int32_t* refs, int n_pages, int before, F f) {
+__device__ __forceinline__ void for_stretch(const Team& t, const Shared& s, const int32_t* refs, int n_pages, uint32_t first, int before, F f) {
     const Stretch x = stretch_of(t, n_pages);
     int run = before + s.warp_free[threadIdx.x >> 5];
     for (int base = x.begin; base < x.end; base += 128) {
         const int at = base + 4 * t.lane;
-        const uint32_t m = at < x.end ? free_of_four(refs, at, x.end) : 0;
+        const uint32_t m = base == x.begin ? first : at < x.end ? free_of_four(refs, at, x.end) : 0;
         const int n = __popc(m);
         int incl = n;
 #pragma unroll
@@ -116,28 +144,36 @@ __device__ __forceinline__ void for_stretch(const Team& t, const Shared& s, cons
         run += __shfl_sync(0xffffffffu, incl, 31);
     }
 }
-__device__ __forceinline__ void list_free(const Team& t, const Shared& s, const int32_t* refs, int n_pages, int before, int32_t* list, int most) {
-    for_stretch(t, s, refs, n_pages, before, [&](int at, uint32_t m, int rank) {
-        for (; m && rank < most; m &= m - 1, ++rank) list[rank] = at + __ffs(m) - 1;
+__device__ __forceinline__ void list_free(const Team& t, const Shared& s, const int32_t* refs, int n_pages, uint32_t first, int before, const Hand& list, int most) {
+    for_stretch(t, s, refs, n_pages, first, before, [&](int at, uint32_t m, int rank) {
+        for (; m && rank < most; m &= m - 1, ++rank) list.put(rank, at + __ffs(m) - 1);
     });
 }
 
-// Sums of the CTA's values before this thread's, and all of them.
-__device__ __forceinline__ long long scan_block(Shared& s, long long v, long long& all) {
+// Sums of the CTA's values before this thread's, and of all, two at a time.
+__device__ __forceinline__ void scan_block(Shared& s, long long (&v)[2], long long (&all)[2]) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    long long incl = v;
+    long long incl[2] = {v[0], v[1]};
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
-        const long long y = __shfl_up_sync(0xffffffffu, incl, d);
-        if (lane >= d) incl += y;
+        const long long y0 = __shfl_up_sync(0xffffffffu, incl[0], d), y1 = __shfl_up_sync(0xffffffffu, incl[1], d);
+        if (lane >= d) { incl[0] += y0; incl[1] += y1; }
     }
-    if (lane == 31) s.scan[warp] = incl;
+    if (lane == 31) { s.scan[0][warp] = incl[0]; s.scan[1][warp] = incl[1]; }
     __syncthreads();
-    long long before = 0;
-    all = 0;
-    for (int w = 0; w < kWarps; ++w) { const long long x = s.scan[w]; if (w < warp) before += x; all += x; }
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        long long of_warps = s.scan[k][lane];
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const long long y = __shfl_up_sync(0xffffffffu, of_warps, d);
+            if (lane >= d) of_warps += y;
+        }
+        const long long before = __shfl_sync(0xffffffffu, of_warps, (warp + 31) & 31);
+        all[k] = __shfl_sync(0xffffffffu, of_warps, 31);
+        v[k] = (warp ? before : 0) + incl[k] - v[k];
+    }
     __syncthreads();
-    return before + incl - v;
 }
 
 struct Params {
@@ -167,38 +203,59 @@ __device__ __forceinline__ void give_back(const Params& p, int page, int i) {
     }
 }
 // The rows of a call: owner[row] is the first place of the call that names it.
-__device__ __forceinline__ void clear_owners(const Params& p, const Team& t, const int32_t* rows) {
-    for (int i = t.thread; i < p.n; i += t.threads) {
-        const int r = rows[i];
-        if (in(r, p.k.n_rows)) p.owner[r] = 0x7fffffff;
+template <bool SMALL>
+__device__ __forceinline__ Hand hand_of(const Params& p, uint8_t* shared) {
+    SmallHand* const s = reinterpret_cast<SmallHand*>(shared);
+    if (SMALL) return {s, s->rows, s->other, s->owner, s->info, s->place, s->list, p.free_list, kSmallList};
+    return {nullptr, p.rows, p.other, p.owner, p.info, p.place, nullptr, p.free_list, 0};
+}
+// owner[row] of the rows of the call: nobody yet.
+template <bool SMALL>
+__device__ __forceinline__ void clear_owners(const Params& p, const Hand& h, const Team& t, bool both) {
+    if (SMALL) {
+        SmallHand* const s = h.small;
+        if ((int)threadIdx.x < p.n) {
+            s->rows[threadIdx.x] = p.rows[threadIdx.x];
+            if (p.other) s->other[threadIdx.x] = p.other[threadIdx.x];
+        }
+        for (int r = threadIdx.x; r < p.k.n_rows; r += kThreads) h.owner[r] = 0x7fffffff;
+    } else {
+        for (int i = t.thread; i < p.n; i += t.threads) {
+            const int r = p.rows[i];
+            if (in(r, p.k.n_rows)) h.owner[r] = 0x7fffffff;
+            const int o = both ? p.other[i] : -1;
+            if (in(o, p.k.n_rows)) h.owner[o] = 0x7fffffff;
+        }
     }
 }
-__device__ __forceinline__ void claim_rows(const Params& p, const Team& t) {
+__device__ __forceinline__ void claim_rows(const Params& p, const Hand& h, const Team& t) {
     for (int i = t.thread; i < p.n; i += t.threads) {
-        const int r = p.rows[i];
-        if (in(r, p.k.n_rows)) atomicMin(p.owner + r, i);
+        const int r = h.rows[i];
+        if (in(r, p.k.n_rows)) atomicMin(h.owner + r, i);
     }
 }
 
+template <bool SMALL>
 __global__ void __launch_bounds__(kThreads) fork_kernel(const Params p) {
+    extern __shared__ __align__(16) uint8_t shared[];
+    const Hand h = hand_of<SMALL>(p, shared);
     __shared__ Shared s;
     const Team t = team_of(p.team);
     const int warps = t.size * kWarps;
     pdl_launch_dependents();
     pdl_wait();
-    clear_owners(p, t, p.rows);
-    clear_owners(p, t, p.other);
-    count_free(t, s, p.k.refs, p.k.n_pages);
+    clear_owners<SMALL>(p, h, t, true);
+    const uint32_t mask = count_free(t, s, p.k.refs, p.k.n_pages);
     t.sync();
-    claim_rows(p, t);
+    claim_rows(p, h, t);
     int before, n_free;
     total_free(t, s, before, n_free);
-    list_free(t, s, p.k.refs, p.k.n_pages, before, p.free_list, p.n);
+    list_free(t, s, p.k.refs, p.k.n_pages, mask, before, h, p.n);
     t.sync();
     // what a pair needs: info = tokens, -1 refused, -2 nothing to do; a parent that is a child too is read before it changes
     for (int i = t.warp; i < p.n; i += warps) {
-        const int child = p.rows[i], parent = p.other[i];
-        bool ok = in(child, p.k.n_rows) && in(parent, p.k.n_rows) && __ldcg(p.owner + child) == i;
+        const int child = h.rows[i], parent = h.other[i];
+        bool ok = in(child, p.k.n_rows) && in(parent, p.k.n_rows) && fetch<SMALL>(h.owner + child) == i;
         int len = 0;
         if (ok) {
             len = p.k.lengths[parent];
@@ -207,7 +264,7 @@ __global__ void __launch_bounds__(kThreads) fork_kernel(const Params p) {
         if (ok) {
             const int pages = pages_of(p, len);
             const int32_t* const from = table_row(p, parent);
-            int32_t* const to = __ldcg(p.owner + parent) != 0x7fffffff ? p.staged + (int64_t)i * p.k.table_width : nullptr;
+            int32_t* const to = fetch<SMALL>(h.owner + parent) != 0x7fffffff ? p.staged + (int64_t)i * p.k.table_width : nullptr;
             bool mine = true;
             for (int c = t.lane; c < pages; c += 32) {
                 const int page = from[c];
@@ -218,37 +275,38 @@ __global__ void __launch_bounds__(kThreads) fork_kernel(const Params p) {
         }
         if (t.lane == 0) {
             if (!ok) raise_status(p.status, MT_ERR_INVALID_ARG, i);
-            p.info[i] = !ok ? -1 : child == parent ? -2 : len;
+            h.info[i] = !ok ? -1 : child == parent ? -2 : len;
         }
     }
     t.sync();
     if (t.rank == 0) {                        // who gets which of the free pages
-        long long run = 0, all;
+        long long run = 0, all[2];
         for (int i0 = 0; i0 < p.n; i0 += kThreads) {
             const int i = i0 + threadIdx.x;
-            const int len = i < p.n ? __ldcg(p.info + i) : -1;
-            const long long at = scan_block(s, len > 0 && (len & (p.k.page_tokens - 1)) ? 1 : 0, all);
-            if (i < p.n) p.place[i] = run + at;
-            run += all;
+            const int len = i < p.n ? fetch<SMALL>(h.info + i) : -1;
+            long long v[2] = {len > 0 && (len & (p.k.page_tokens - 1)) ? 1 : 0, 0};
+            scan_block(s, v, all);
+            if (i < p.n) h.place[i] = run + v[0];
+            run += all[0];
         }
     }
     t.sync();
     for (int i = t.warp; i < p.n; i += warps) {
-        const int child = p.rows[i], parent = p.other[i], len = __ldcg(p.info + i);
+        const int child = h.rows[i], parent = h.other[i], len = fetch<SMALL>(h.info + i);
         const int part = len & (p.k.page_tokens - 1), whole = len >> p.shift;
         int from = -1, fresh = -1;
         bool go = len >= 0;
         if (go && part) {
-            const long long at = __ldcg(p.place + i);
+            const long long at = fetch<SMALL>(h.place + i);
             if (at < n_free) {
-                fresh = __ldcg(p.free_list + at);
+                fresh = free_page<SMALL>(h, at);
             } else {
                 go = false;
                 if (t.lane == 0) raise_status(p.status, MT_ERR_OOM, i);
             }
         }
         if (go) {
-            const int32_t* const src = __ldcg(p.owner + parent) != 0x7fffffff ? p.staged + (int64_t)i * p.k.table_width : table_row(p, parent);
+            const int32_t* const src = fetch<SMALL>(h.owner + parent) != 0x7fffffff ? p.staged + (int64_t)i * p.k.table_width : table_row(p, parent);
             int32_t* const row = table_row(p, child);
             const int was = p.k.lengths[child], old = good_length(p, was) ? pages_of(p, was) : 0;
             if (!good_length(p, was) && t.lane == 0) raise_status(p.status, MT_ERR_INVALID_ARG, i);
@@ -272,29 +330,32 @@ __global__ void __launch_bounds__(kThreads) fork_kernel(const Params p) {
     }
 }
 
+template <bool SMALL>
 __global__ void __launch_bounds__(kThreads) reserve_kernel(const Params p) {
+    extern __shared__ __align__(16) uint8_t shared[];
+    const Hand h = hand_of<SMALL>(p, shared);
     __shared__ Shared s;
     const Team t = team_of(p.team);
     const int warps = t.size * kWarps;
     pdl_launch_dependents();
     pdl_wait();
-    clear_owners(p, t, p.rows);
-    count_free(t, s, p.k.refs, p.k.n_pages);
+    clear_owners<SMALL>(p, h, t, false);
+    const uint32_t mask = count_free(t, s, p.k.refs, p.k.n_pages);
     t.sync();
-    claim_rows(p, t);
+    claim_rows(p, h, t);
     int before, n_free;
     total_free(t, s, before, n_free);
-    list_free(t, s, p.k.refs, p.k.n_pages, before, p.free_list, p.k.n_pages);
     t.sync();
+    int most = p.k.n_pages;                   // free pages that are wanted
     if (t.rank == 0) {                        // place[2 i]: pages of the rows before, place[2 i + 1]: their tokens
-        long long pages = 0, tokens = 0, all;
+        long long pages = 0, tokens = 0, all[2];
         for (int i0 = 0; i0 < p.n; i0 += kThreads) {
             const int i = i0 + threadIdx.x;
             int need = 0, count = 0;
             if (i < p.n) {
-                const int row = p.rows[i];
-                count = p.other[i];
-                bool ok = in(row, p.k.n_rows) && __ldcg(p.owner + row) == i && count >= 0;
+                const int row = h.rows[i];
+                count = h.other[i];
+                bool ok = in(row, p.k.n_rows) && fetch<SMALL>(h.owner + row) == i && count >= 0;
                 int len = 0;
                 if (ok) {
                     len = p.k.lengths[row];
@@ -302,22 +363,24 @@ __global__ void __launch_bounds__(kThreads) reserve_kernel(const Params p) {
                 }
                 if (ok) need = pages_of(p, len + count) - pages_of(p, len);
                 else raise_status(p.status, MT_ERR_INVALID_ARG, i);
-                p.info[i] = ok ? len : -1;
+                h.info[i] = ok ? len : -1;
                 count = max(count, 0);
             }
-            const long long a = scan_block(s, need, all);
-            if (i < p.n) p.place[2 * (int64_t)i] = pages + a;
-            pages += all;
-            const long long b = scan_block(s, count, all);
-            if (i < p.n) p.place[2 * (int64_t)i + 1] = tokens + b;
-            tokens += all;
+            long long v[2] = {need, count};
+            scan_block(s, v, all);
+            if (i < p.n) { h.place[2 * (int64_t)i] = pages + v[0]; h.place[2 * (int64_t)i + 1] = tokens + v[1]; }
+            pages += all[0];
+            tokens += all[1];
         }
         for (int64_t x = tokens + threadIdx.x; x < p.n_slots; x += kThreads) p.slots[x] = -1;
+        if (t.size == 1) most = (int)min(pages, (long long)most);
     }
+    list_free(t, s, p.k.refs, p.k.n_pages, mask, before, h, most);
     t.sync();
-    for (int i = t.warp; i < p.n; i += warps) {
-        const int len = __ldcg(p.info + i), row = p.rows[i], count = max(p.other[i], 0);
-        const long long first = __ldcg(p.place + 2 * (int64_t)i), out = __ldcg(p.place + 2 * (int64_t)i + 1);
+    // Place i, by `size` lanes of which this is `lane`: a warp, or, for a few tokens, a thread.
+    auto place = [&](int i, int lane, int size) {
+        const int len = fetch<SMALL>(h.info + i), row = h.rows[i], count = max(h.other[i], 0);
+        const long long first = fetch<SMALL>(h.place + 2 * (int64_t)i), out = fetch<SMALL>(h.place + 2 * (int64_t)i + 1);
         bool go = len >= 0;
         int had = 0, need = 0;
         if (go) {
@@ -325,40 +388,48 @@ __global__ void __launch_bounds__(kThreads) reserve_kernel(const Params p) {
             need = pages_of(p, len + count) - had;
             if (need > 0 && first + need > n_free) {
                 go = false;
-                if (t.lane == 0) raise_status(p.status, MT_ERR_OOM, i);
+                if (lane == 0) raise_status(p.status, MT_ERR_OOM, i);
             }
         }
         if (go && out + count > p.n_slots) {  // the caller has no room for their slots
             go = false;
-            if (t.lane == 0) raise_status(p.status, MT_ERR_INVALID_ARG, i);
+            if (lane == 0) raise_status(p.status, MT_ERR_INVALID_ARG, i);
         }
+        const int64_t last = go && had > 0 && (len & (p.k.page_tokens - 1)) ? table_row(p, row)[had - 1] : 0;      // the page that is partly filled
         if (go) {
-            for (int c = t.lane; c < need; c += 32) {
-                const int page = __ldcg(p.free_list + first + c);
+            for (int c = lane; c < need; c += size) {
+                const int page = free_page<SMALL>(h, first + c);
                 table_row(p, row)[had + c] = page;
                 p.k.refs[page] = 1;
             }
-            __syncwarp();
-            if (t.lane == 0) p.k.lengths[row] = len + count;
+            if (lane == 0) p.k.lengths[row] = len + count;
         }
-        for (int c = t.lane; c < count && out + c < p.n_slots; c += 32) {
-            const int at = len + c;
-            p.slots[out + c] = go ? ((int64_t)table_row(p, row)[at >> p.shift] << p.shift) + (at & (p.k.page_tokens - 1)) : -1;
+        for (int c = lane; c < count && out + c < p.n_slots; c += size) {
+            const int at = len + c, col = at >> p.shift;
+            const int64_t page = !go ? 0 : col < had ? last : free_page<SMALL>(h, first + col - had);
+            p.slots[out + c] = go ? (page << p.shift) + (at & (p.k.page_tokens - 1)) : -1;
         }
-    }
+    };
+    for (int i = t.thread; i < p.n; i += t.threads)
+        if (h.other[i] <= kFew) place(i, 0, 1);
+    for (int i = t.warp; i < p.n; i += warps)
+        if (h.other[i] > kFew) place(i, t.lane, 32);
 }
 
+template <bool SMALL>
 __global__ void __launch_bounds__(kThreads) release_kernel(const Params p) {
+    extern __shared__ __align__(16) uint8_t shared[];
+    const Hand h = hand_of<SMALL>(p, shared);
     const Team t = team_of(p.team);
     pdl_launch_dependents();
     pdl_wait();
-    clear_owners(p, t, p.rows);
+    clear_owners<SMALL>(p, h, t, false);
     t.sync();
-    claim_rows(p, t);
+    claim_rows(p, h, t);
     t.sync();
     for (int i = t.warp; i < p.n; i += t.size * kWarps) {
-        const int row = p.rows[i];
-        const bool ok = in(row, p.k.n_rows) && __ldcg(p.owner + row) == i;
+        const int row = h.rows[i];
+        const bool ok = in(row, p.k.n_rows) && fetch<SMALL>(h.owner + row) == i;
         const int len = ok ? p.k.lengths[row] : -1;
         if (!ok || !good_length(p, len)) {
             if (t.lane == 0) raise_status(p.status, MT_ERR_INVALID_ARG, i);
@@ -378,13 +449,13 @@ __global__ void __launch_bounds__(kThreads) compact_kernel(const Params p) {
     int32_t *const holes = p.free_list, *const high = p.staged, *const moved = p.owner;
     pdl_launch_dependents();
     pdl_wait();
-    count_free(t, s, p.k.refs, p.k.n_pages);
+    const uint32_t mask = count_free(t, s, p.k.refs, p.k.n_pages);
     t.sync();
     int before, n_free;
     total_free(t, s, before, n_free);
     const int used = p.k.n_pages - n_free;
     int mine = 0;
-    for_stretch(t, s, p.k.refs, p.k.n_pages, before, [&](int at, uint32_t m, int rank) {
+    for_stretch(t, s, p.k.refs, p.k.n_pages, mask, before, [&](int at, uint32_t m, int rank) {
         for (int e = 0; e < 4 && at + e < p.k.n_pages; ++e) {
             const int page = at + e;
             if (page >= used) moved[page] = page;
@@ -432,21 +503,24 @@ __global__ void __launch_bounds__(kThreads) compact_kernel(const Params p) {
 
 // ------------------------------------------------------------------------------------------------ copies
 constexpr int kCopyThreads = 128;
-constexpr int kCachesPerLaunch = 64;
+constexpr int kAhead = 8;                     // vectors of a lane under way
+constexpr int kCachesPerLaunch = 64, kFewCaches = 8;                           // (the block of 64 costs a launch a microsecond on the host)
 struct CopyCache {
     uint8_t* codes[2];                        // keys, values
     uint8_t* params[2];
     int heads, row;                           // bytes of a token's codes
 };
+template <int CACHES>
 struct CopyParams {
     const int32_t* copies;
     int n, n_pages, page_tokens;
     OpStatus status;
-    CopyCache c[kCachesPerLaunch];
+    CopyCache c[CACHES];
 };
-static_assert(sizeof(CopyParams) <= 4096, "");
+static_assert(sizeof(CopyParams<kCachesPerLaunch>) <= 4096, "");
 
-__global__ void __launch_bounds__(kCopyThreads) copy_kernel(const __grid_constant__ CopyParams p) {
+template <int CACHES>
+__global__ void __launch_bounds__(kCopyThreads) copy_kernel(const __grid_constant__ CopyParams<CACHES> p) {
     pdl_launch_dependents();
     pdl_wait();
     const CopyCache& c = p.c[blockIdx.y >> 1];
@@ -466,17 +540,26 @@ __global__ void __launch_bounds__(kCopyThreads) copy_kernel(const __grid_constan
             uint4* const dst = reinterpret_cast<uint4*>(c.codes[kv] + ((int64_t)to * c.heads + h) * head_codes);
             const uint32_t* const ps = reinterpret_cast<const uint32_t*>(c.params[kv] + ((int64_t)from * c.heads + h) * head_params);
             uint32_t* const pd = reinterpret_cast<uint32_t*>(c.params[kv] + ((int64_t)to * c.heads + h) * head_params);
-            for (int v = lane; v < vecs; v += 32) dst[v] = src[v];
+            for (int v0 = lane; v0 < vecs; v0 += 32 * kAhead) {
+                uint4 x[kAhead];
+#pragma unroll
+                for (int k = 0; k < kAhead; ++k) if (v0 + 32 * k < vecs) x[k] = __ldcs(src + v0 + 32 * k);
+#pragma unroll
+                for (int k = 0; k < kAhead; ++k) if (v0 + 32 * k < vecs) __stcs(dst + v0 + 32 * k, x[k]);
+            }
             for (int v = lane; v < tokens; v += 32) pd[v] = ps[v];
         }
     }
 }
 
-cudaError_t launch_team(void (*kernel)(Params), Params& p, int64_t work, cudaStream_t s) {
+// kernels: [0] for a call that is SMALL, [1] for others
+cudaError_t launch_team(void (*const (&kernels)[2])(Params), Params& p, int64_t work, bool small, cudaStream_t s) {
     p.team = work > (1 << 16) ? kTeam : 1;    // words a thread of a single CTA reads: 64
+    small = small && p.team == 1;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)p.team);
     cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = small ? sizeof(SmallHand) : 0;
     cfg.stream = s;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -487,12 +570,18 @@ cudaError_t launch_team(void (*kernel)(Params), Params& p, int64_t work, cudaStr
     cfg.attrs = attr;
     cfg.numAttrs = p.team > 1 ? 2 : 1;
     ++g_kernel_launches;
-    return cudaLaunchKernelEx(&cfg, kernel, p);
+    return cudaLaunchKernelEx(&cfg, kernels[small ? 0 : 1], p);
 }
 
 size_t round_up(size_t x) { return (x + 255) / 256 * 256; }
 
 }  // namespace
+
+cudaError_t configure_kv_pages() {
+    cudaError_t e = cudaFuncSetAttribute(fork_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(SmallHand));
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(reserve_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(SmallHand));
+    return e == cudaSuccess ? cudaFuncSetAttribute(release_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(SmallHand)) : e;
+}
 
 mt_status launch_kv_pages(const KvPagesArgs& a, cudaStream_t s) {
     Params p;
@@ -514,24 +603,35 @@ mt_status launch_kv_pages(const KvPagesArgs& a, cudaStream_t s) {
     p.place = reinterpret_cast<long long*>(w + owner + list + info);
     p.staged = reinterpret_cast<int32_t*>(w + owner + list + info + place);
     const int64_t of_rows = (int64_t)(n * width);
-    const cudaError_t e = fork ? launch_team(fork_kernel, p, (int64_t)pages + 3 * of_rows, s)
-                        : reserve ? launch_team(reserve_kernel, p, 2 * (int64_t)pages, s)
-                        : compact ? launch_team(compact_kernel, p, 2 * (int64_t)pages + (int64_t)(rows * width), s)
-                                  : launch_team(release_kernel, p, of_rows, s);
+    const bool small = a.n <= kSmall && a.k.n_rows <= kSmallRows;
+    void (*const forks[2])(Params) = {fork_kernel<true>, fork_kernel<false>};
+    void (*const reserves[2])(Params) = {reserve_kernel<true>, reserve_kernel<false>};
+    void (*const releases[2])(Params) = {release_kernel<true>, release_kernel<false>};
+    void (*const compacts[2])(Params) = {compact_kernel, compact_kernel};
+    const cudaError_t e = fork ? launch_team(forks, p, (int64_t)pages + 3 * of_rows, small, s)
+                        : reserve ? launch_team(reserves, p, 2 * (int64_t)pages, small, s)
+                        : compact ? launch_team(compacts, p, 2 * (int64_t)pages + (int64_t)(rows * width), false, s)
+                                  : launch_team(releases, p, of_rows, small, s);
     return e == cudaSuccess ? MT_OK : MT_ERR_CUDA;
+}
+
+template <int CACHES>
+static cudaError_t copy_in(const mt_kv_cache* const* caches, int m, const int32_t* copies, int n, const OpStatus& status, cudaStream_t s) {
+    CopyParams<CACHES> p;
+    p.copies = copies; p.n = n; p.n_pages = caches[0]->n_pages; p.page_tokens = caches[0]->page_tokens; p.status = status;
+    for (int i = 0; i < m; ++i) {
+        const mt_kv_cache& c = *caches[i];
+        p.c[i] = {{static_cast<uint8_t*>(c.k_codes), static_cast<uint8_t*>(c.v_codes)},
+                  {static_cast<uint8_t*>(c.k_params), static_cast<uint8_t*>(c.v_params)}, c.kv_heads, c.head_dim / 2};
+    }
+    return launch_pdl(copy_kernel<CACHES>, dim3((unsigned)(n < 4096 ? n : 4096), (unsigned)(2 * m)), dim3(kCopyThreads), 0, s, p);
 }
 
 cudaError_t launch_kv_copy(const mt_kv_cache* const* caches, int n_caches, const int32_t* copies, int n, const OpStatus& status, cudaStream_t s) {
     for (int c0 = 0; c0 < n_caches; c0 += kCachesPerLaunch) {
         const int m = n_caches - c0 < kCachesPerLaunch ? n_caches - c0 : kCachesPerLaunch;
-        CopyParams p;
-        p.copies = copies; p.n = n; p.n_pages = caches[0]->n_pages; p.page_tokens = caches[0]->page_tokens; p.status = status;
-        for (int i = 0; i < m; ++i) {
-            const mt_kv_cache& c = *caches[c0 + i];
-            p.c[i] = {{static_cast<uint8_t*>(c.k_codes), static_cast<uint8_t*>(c.v_codes)},
-                      {static_cast<uint8_t*>(c.k_params), static_cast<uint8_t*>(c.v_params)}, c.kv_heads, c.head_dim / 2};
-        }
-        const cudaError_t e = launch_pdl(copy_kernel, dim3((unsigned)(n < 4096 ? n : 4096), (unsigned)(2 * m)), dim3(kCopyThreads), 0, s, p);
+        const cudaError_t e = m <= kFewCaches ? copy_in<kFewCaches>(caches + c0, m, copies, n, status, s)
+                                              : copy_in<kCachesPerLaunch>(caches + c0, m, copies, n, status, s);
         if (e != cudaSuccess) return e;
         if (n_caches - c0 <= kCachesPerLaunch) break;
     }

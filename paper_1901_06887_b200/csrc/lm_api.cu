@@ -202,6 +202,7 @@ cudaError_t configure_operators() {
     if (e == cudaSuccess) e = configure_token_logprobs();
     if (e == cudaSuccess) e = configure_cross_attention();
     if (e == cudaSuccess) e = configure_token_sample();
+    if (e == cudaSuccess) e = configure_kv_pages();
     return e;
 }
 

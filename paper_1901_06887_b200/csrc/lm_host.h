@@ -127,6 +127,7 @@ struct KvPagesArgs {
     int64_t n_slots;
     OpStatus status;
 };
+cudaError_t configure_kv_pages();
 mt_status launch_kv_pages(const KvPagesArgs& a, cudaStream_t s);
 cudaError_t launch_kv_copy(const mt_kv_cache* const* caches, int n_caches, const int32_t* copies, int n, const OpStatus& status, cudaStream_t s);
 
