@@ -72,6 +72,10 @@ class LanguageTenants:
         a, b = x[..., :half].float(), x[..., half:].float()
         return torch.cat([a * angle.cos() - b * angle.sin(), a * angle.sin() + b * angle.cos()], -1).to(BF16)
 
+    def _look(self, layer, x, ids):
+        """Attention to something else than the text (several_answers.py); nothing here."""
+        return x
+
     def forward(self, tokens, ids, at, slots, attend):
         """Logits fp32 [n, vocab] of n tokens at positions `at`, their keys and values written to `slots`.  attend(layer, q, k, v)
         is the attention: over the packed prompts, or over the cache."""
@@ -82,6 +86,7 @@ class LanguageTenants:
             q, k = self._turn(q, at), self._turn(k, at)
             self.ops.mt_kv_append(l.cache, k, v, slots)
             x = x + self._linear(attend(l, q, k, v).flatten(1), ids, l.out)
+            x = self._look(l, x, ids)
             x = x + self._linear(torch.relu(self._linear(self._norm(x), ids, l.up)), ids, l.down)
         return self._linear(self._norm(x), ids, self.head, torch.float32)
 

@@ -54,14 +54,28 @@ template <> struct Eight<true> {
 };
 
 template <bool FP32, bool NEIGHBOURS>
-__global__ void __launch_bounds__(kThreads) rotate_kernel(const Params p) {
+__global__ void __launch_bounds__(kThreads, 5) rotate_kernel(const Params p) {
     extern __shared__ float table[];          // [tokens][half] cosines, then sines
     const RotateArgs& a = p.a;
     const int t0 = blockIdx.x * p.tokens, n = min(p.tokens, a.n - t0);
     float* const cosines = table;
     float* const sines = table + p.tokens * p.half;
     const int threads = blockDim.x * blockDim.y, me = threadIdx.y * blockDim.x + threadIdx.x;
+    const int u = threadIdx.x;
+    const int first = NEIGHBOURS ? 16 * u : 8 * u, second = NEIGHBOURS ? 16 * u + 8 : p.half + 8 * u;
+    int t = 0, h = threadIdx.y;
+    auto step = [&]() { while (h >= a.heads && t < n) { h -= a.heads; ++t; } };
+    auto load = [&](Eight<FP32>& vx, Eight<FP32>& vy) {
+        if (t >= n) return;
+        const int64_t from = (int64_t)(t0 + t) * a.x_token_stride + (int64_t)h * a.x_head_stride;
+        vx.load(a.x, from + first);
+        vy.load(a.x, from + second);
+    };
+    pdl_launch_dependents();
     pdl_wait();
+    Eight<FP32> vx, vy;                       // the first are under way while the tables are made, each next one while one is turned
+    step();
+    load(vx, vy);
     for (int i = me; i < n * p.half; i += threads) {
         const int t = i / p.half, c = i - t * p.half;
         const int axis = (c >= p.bound[0]) + (c >= p.bound[1]) + (c >= p.bound[2]);
@@ -72,16 +86,8 @@ __global__ void __launch_bounds__(kThreads) rotate_kernel(const Params p) {
         sines[i] = s * p.sign;
     }
     __syncthreads();
-    const int u = threadIdx.x;
-    const int first = NEIGHBOURS ? 16 * u : 8 * u, second = NEIGHBOURS ? 16 * u + 8 : p.half + 8 * u;
-    int t = 0, h = threadIdx.y;
-    while (h >= a.heads && t < n) { h -= a.heads; ++t; }
     while (t < n) {
-        const int64_t from = (int64_t)(t0 + t) * a.x_token_stride + (int64_t)h * a.x_head_stride;
         const int64_t to = (int64_t)(t0 + t) * a.out_token_stride + (int64_t)h * a.out_head_stride;
-        Eight<FP32> vx, vy;
-        vx.load(a.x, from + first);
-        vy.load(a.x, from + second);
         float c[8], s[8], x[8], y[8];
         const float4* const ct = reinterpret_cast<const float4*>(cosines + t * p.half + 8 * u);
         const float4* const st = reinterpret_cast<const float4*>(sines + t * p.half + 8 * u);
@@ -90,6 +96,9 @@ __global__ void __launch_bounds__(kThreads) rotate_kernel(const Params p) {
         s[0] = s0.x; s[1] = s0.y; s[2] = s0.z; s[3] = s0.w; s[4] = s1.x; s[5] = s1.y; s[6] = s1.z; s[7] = s1.w;
         vx.get(x);
         vy.get(y);
+        h += blockDim.y;
+        step();
+        load(vx, vy);
         if (NEIGHBOURS) {                     // x[0], x[1] are pair 0, ..; y[0], y[1] pair 4
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
@@ -107,12 +116,11 @@ __global__ void __launch_bounds__(kThreads) rotate_kernel(const Params p) {
                 y[e] = xa * s[e] + ya * c[e];
             }
         }
-        vx.set(x);
-        vy.set(y);
-        vx.store(a.out, to + first);
-        vy.store(a.out, to + second);
-        h += blockDim.y;
-        while (h >= a.heads && t < n) { h -= a.heads; ++t; }
+        Eight<FP32> out;
+        out.set(x);
+        out.store(a.out, to + first);
+        out.set(y);
+        out.store(a.out, to + second);
     }
     // what is not turned
     if (p.rest > 0) {
