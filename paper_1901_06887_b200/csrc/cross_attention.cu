@@ -11,8 +11,8 @@
 //
 // Order of work.  A unit is a block of states for a tile pair; the units of all (sequence, head pack, tile pair) are in one line, which is cut
 // into equal shares, one a CTA.  A tile pair that a border cuts is done in pieces: each leaves its sums (o without the division, m, l) in scratch, and a
-// second launch joins them.  So one token over a long recording takes all SMs, and ragged batches are even.  Where there are tile pairs enough
-// the borders move to tile pairs and there is no second launch.
+// second launch joins them.  So one token over a long recording takes all SMs.  Where there are tile pairs enough to be even without, they are dealt whole,
+// those with most states first, back and forth over the CTAs, and nothing is joined.
 //
 // Roles (12 warps): warps 0-3 and 4-7 are the softmax of the two tiles, one row per thread; warp 8 copies (TMA), warp 9 issues the matrix
 // instructions, warps 10 and 11 zero the values behind the sequence's last state: their p is zero, but zero times an infinity is NaN.
@@ -26,8 +26,8 @@ namespace {
 constexpr int kThreads = 384;
 constexpr int kMaxSeqs = 512;                 // sequences of one launch
 constexpr float kSlack = 8.f;
-constexpr int kEnough = 8;                    // tile pairs an SM, from which shares end at tile pairs
-constexpr int kUneven = 20;                   // units that the longest such share may have above the mean: what pieces and their joins cost
+constexpr int kEnough = 8;                    // tile pairs an SM, from which they are dealt whole in any case
+constexpr int kUneven = 10;                   // units that a CTA may get above the mean then: what pieces and their joins cost
 constexpr int kJoinThreads = 256;
 
 template <int D> __host__ __device__ constexpr int slots() { return D == 128 ? 4 : 8; }
@@ -35,7 +35,7 @@ template <int D> __host__ __device__ constexpr int operand_bytes() { return kHal
 
 // A share of the line of units, piece by piece.
 struct Walk {
-    int left;                                 // units (of queries that fit in memory a CTA has fewer than 2^31)
+    int left;                                 // units (of queries that fit in memory a CTA has fewer than 2^31); rounds dealt, where tile pairs are whole
     int seq, pack, tile, block;               // where the next one is
 };
 struct Work {
@@ -51,6 +51,8 @@ struct Control {
     unsigned long long longest;
     int start[kMaxSeqs + 1], len[kMaxSeqs], first[kMaxSeqs], states[kMaxSeqs];
     long long before[kMaxSeqs + 1];           // units of the sequences before
+    uint16_t order[kMaxSeqs];                 // sequences by falling number of blocks, and the tile pairs of those before
+    int pairs[kMaxSeqs + 1];
     Walk walk[8];                             // of the softmax warps, while a piece is under way: the registers are needed
     Work work[8];
 };
@@ -78,7 +80,7 @@ struct CrossParams {
     const int32_t *offsets, *ranges;
     int n_seqs, seq0, n_tokens, n_states;
     int q_heads, group, pack, pack_shift;     // pack: heads packed into a tile's rows
-    int whole;                                // shares end at tile pairs: 0 no, 1 yes, 2 if that is even enough
+    int whole;                                // tile pairs are dealt whole: 0 no, 1 yes, 2 if that is even enough
     float c;                                  // |scale| log2(e)
     int negate;                               // scale < 0
     uint16_t* out;
@@ -103,30 +105,43 @@ __device__ __forceinline__ void locate(const Control& s, const CrossParams& p, l
     w.pack = (int)(item / tiles);
     w.tile = (int)(item - (long long)w.pack * tiles);
 }
-// First unit of a CTA's share.
-__device__ __forceinline__ long long share_edge(const Control& s, const CrossParams& p, int cta, bool whole) {
-    const long long total = s.before[p.n_seqs];
-    long long x = share_begin(total, cta, gridDim.x);
-    if (whole && x < total) {
-        Walk w;
-        locate(s, p, x, w);
-        if (w.block > 0) x += blocks_of(s.states[w.seq]) - w.block;
+// The tile pair that a CTA gets in a round: back and forth.
+__device__ __forceinline__ int dealt(int round, int cta) { return round * gridDim.x + ((round & 1) ? gridDim.x - 1 - cta : cta); }
+__device__ __forceinline__ int rank_of(const Control& s, const CrossParams& p, int pair) {
+    int lo = 0, hi = p.n_seqs - 1;            // pairs[r] <= pair < pairs[r + 1]
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (s.pairs[mid] <= pair) lo = mid; else hi = mid - 1;
     }
-    return x;
+    return lo;
 }
 __device__ __forceinline__ Walk begin_share(const Control& s, const CrossParams& p) {
-    const bool whole = s.whole != 0;
-    const long long edge[2] = {share_edge(s, p, blockIdx.x, whole), share_edge(s, p, blockIdx.x + 1, whole)};
     Walk w;
-    w.left = (int)(edge[1] - edge[0]);
-    w.seq = w.pack = w.tile = w.block = 0;
-    if (w.left > 0) locate(s, p, edge[0], w);
+    w.left = w.seq = w.pack = w.tile = w.block = 0;
+    if (s.whole) return w;
+    const long long total = s.before[p.n_seqs], first = share_begin(total, blockIdx.x, gridDim.x);
+    w.left = (int)(share_begin(total, blockIdx.x + 1, gridDim.x) - first);
+    if (w.left > 0) locate(s, p, first, w);
     return w;
 }
 // The next piece of the share.
 __device__ __forceinline__ bool next_piece(const Control& s, const CrossParams& p, Walk& w, Work& k) {
-    if (w.left <= 0) return false;
     const int tokens = 256 >> p.pack_shift, packs = p.q_heads >> p.pack_shift;
+    if (s.whole) {
+        const int pair = dealt(w.left, blockIdx.x);
+        if (pair >= s.pairs[p.n_seqs]) return false;
+        ++w.left;
+        const int rank = rank_of(s, p, pair), seq = s.order[rank], q = pair - s.pairs[rank], tiles = (s.len[seq] + tokens - 1) / tokens;
+        k.seq = seq;
+        k.states = s.states[seq];
+        k.pack = q / tiles;
+        k.t0 = (q - k.pack * tiles) * tokens;
+        k.b0 = 0;
+        k.b1 = k.nb = blocks_of(k.states);
+        k.tiles = k.t0 + tokens / 2 < s.len[seq] ? 2 : 1;
+        return true;
+    }
+    if (w.left <= 0) return false;
     while (w.pack == packs || s.len[w.seq] == 0) { ++w.seq; w.pack = w.tile = w.block = 0; }
     const int len = s.len[w.seq];
     k.seq = w.seq;
@@ -218,10 +233,38 @@ cross_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
         }
         if (lane == 0) { s.before[p.n_seqs] = run; s.whole = p.whole == 1; s.longest = 0; }
     }
-    if (p.whole == 2) {
+    if (p.whole) {
         __syncthreads();
-        for (int i = threadIdx.x; i < gridDim.x; i += kThreads)
-            atomicMax(&s.longest, (unsigned long long)(share_edge(s, p, i + 1, true) - share_edge(s, p, i, true)));
+        for (int i = threadIdx.x; i < p.n_seqs; i += kThreads) {
+            const int n = blocks_of(s.states[i]);
+            int rank = 0;
+            for (int j = 0; j < p.n_seqs; ++j) { const int m = blocks_of(s.states[j]); rank += (m > n || (m == n && j < i)) ? 1 : 0; }
+            s.order[rank] = (uint16_t)i;
+        }
+        __syncthreads();
+        if (warp == 0) {
+            int run = 0;
+            for (int r0 = 0; r0 < p.n_seqs; r0 += 32) {
+                const int r = r0 + lane, v = r < p.n_seqs ? (int)packs * ((s.len[s.order[r]] + tokens - 1) / tokens) : 0;
+                int incl = v;
+#pragma unroll
+                for (int d = 1; d < 32; d <<= 1) {
+                    const int y = __shfl_up_sync(0xffffffffu, incl, d);
+                    if (lane >= d) incl += y;
+                }
+                if (r < p.n_seqs) s.pairs[r] = run + incl - v;
+                run += __shfl_sync(0xffffffffu, incl, 31);
+            }
+            if (lane == 0) s.pairs[p.n_seqs] = run;
+        }
+    }
+    if (p.whole == 2) {                        // the CTA with most
+        __syncthreads();
+        for (int cta = threadIdx.x; cta < gridDim.x; cta += kThreads) {
+            unsigned long long units = 0;
+            for (int round = 0; dealt(round, cta) < s.pairs[p.n_seqs]; ++round) units += blocks_of(s.states[s.order[rank_of(s, p, dealt(round, cta))]]);
+            atomicMax(&s.longest, units);
+        }
         __syncthreads();
         if (threadIdx.x == 0) s.whole = (long long)s.longest <= s.before[p.n_seqs] / gridDim.x + kUneven;
     }
