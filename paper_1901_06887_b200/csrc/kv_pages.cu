@@ -259,7 +259,7 @@ __global__ void __launch_bounds__(kThreads) fork_kernel(const Params p) {
         int len = 0;
         if (ok) {
             len = p.k.lengths[parent];
-            ok = good_length(p, len);
+            ok = good_length(p, len) && good_length(p, p.k.lengths[child]);
         }
         if (ok) {
             const int pages = pages_of(p, len);
@@ -308,8 +308,7 @@ __global__ void __launch_bounds__(kThreads) fork_kernel(const Params p) {
         if (go) {
             const int32_t* const src = fetch<SMALL>(h.owner + parent) != 0x7fffffff ? p.staged + (int64_t)i * p.k.table_width : table_row(p, parent);
             int32_t* const row = table_row(p, child);
-            const int was = p.k.lengths[child], old = good_length(p, was) ? pages_of(p, was) : 0;
-            if (!good_length(p, was) && t.lane == 0) raise_status(p.status, MT_ERR_INVALID_ARG, i);
+            const int old = pages_of(p, p.k.lengths[child]);
             const int now = whole + (part ? 1 : 0);
             for (int c = t.lane; c < max(old, now); c += 32) {
                 if (c < old) give_back(p, row[c], i);

@@ -149,7 +149,7 @@ cudaError_t launch_rotate(const RotateArgs& a, cudaStream_t s) {
     p.sign = a.inverse ? -1.f : 1.f;
     const bool in_place = a.x == a.out && a.x_token_stride == a.out_token_stride && a.x_head_stride == a.out_head_stride;
     p.rest = in_place ? 0 : (a.head_dim - a.rotary_dim) / 8;
-    const dim3 block(p.units, kThreads / p.units), grid((a.n + p.tokens - 1) / p.tokens);
+    const dim3 block(p.units, kThreads / p.units), grid((a.n - 1) / p.tokens + 1);
     const size_t smem = (size_t)p.tokens * p.half * 8;
     if (a.fp32) return a.neighbours ? launch_pdl(rotate_kernel<true, true>, grid, block, smem, s, p) : launch_pdl(rotate_kernel<true, false>, grid, block, smem, s, p);
     return a.neighbours ? launch_pdl(rotate_kernel<false, true>, grid, block, smem, s, p) : launch_pdl(rotate_kernel<false, false>, grid, block, smem, s, p);

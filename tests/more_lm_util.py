@@ -119,7 +119,7 @@ class Book:
         free, taken, copies, errors, changes = self.free(), 0, [], [], []
         for i, (p, c) in enumerate(zip(parents, children)):
             copy = EMPTY
-            ok = self.good(p) and 0 <= c < len(self.lengths) and c not in children[:i] and all(0 <= x < len(self.refs) for x in self.held(p))
+            ok = self.good(p) and self.good(c) and c not in children[:i] and all(0 <= x < len(self.refs) for x in self.held(p))
             if not ok:
                 errors.append((1, i))
             elif p != c:
@@ -134,7 +134,7 @@ class Book:
                     changes.append((i, c, row, self.lengths[p], bool(part)))
                 taken += bool(part)
             copies.append(copy)
-        old = {c: list(self.held(c)) if self.good(c) else [] for _, c, _, _, _ in changes}
+        old = {c: list(self.held(c)) for _, c, _, _, _ in changes}
         for i, c, row, n, part in changes:
             for x in row[: len(row) - part]:
                 self.refs[x] += 1

@@ -98,6 +98,22 @@ def test_a_long_story(n_pages, rows, width, page):
         k.sound()
 
 
+@pytest.mark.parametrize("rows,width,n_pages,many", [(5000, 3, 20000, 1500), (1100, 4, 3000, 1100), (4097, 2, 9000, 40), (300, 900, 40000, 300)])
+def test_large_calls(rows, width, n_pages, many):
+    """More places, rows or table entries than one CTA keeps in shared memory or takes by itself."""
+    rng = random.Random(rows)
+    k = Both(n_pages, 16, rows, width)
+    some = rng.sample(range(rows), many)
+    k.reserve(some, [rng.randint(0, 16 * width) if width < 10 else rng.randint(0, 16 * 80) for _ in some])
+    children = rng.sample(range(rows), many)
+    k.fork([rng.choice(some) for _ in children], children)
+    k.sound()
+    k.reserve(children, [rng.randint(0, 16 * width - k.book.lengths[c]) % 7 for c in children])
+    k.release(children[::2])
+    k.compact(n_pages // 2)
+    k.sound()
+
+
 def test_edges_of_pages():
     """Lengths at and beside the ends of pages."""
     k = Both(30, 16, 8, 4)
@@ -145,7 +161,7 @@ def test_places_that_are_left_out():
     k.book.lengths[5], k.book.lengths[7] = 65, -1               # passes the table; negative
     k.load()
     assert k.reserve([5, 7, 4], [0, 0, 1]) == [(1, 0), (1, 1)]
-    assert k.fork([5, 7], [3, 4]) == [(1, 0), (1, 1)]
+    assert k.fork([5, 7, 0, 0], [3, 4, 7, 5]) == [(1, 0), (1, 1), (1, 2), (1, 3)]
     assert k.release([7, 5]) == [(1, 0), (1, 1)]
 
 
