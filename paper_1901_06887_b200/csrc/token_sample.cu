@@ -7,12 +7,18 @@
 // ones would pass 2^62: sums of them are exact in any order.  (A token below 2^-46 of the likeliest has no mass and is never drawn; all mass lost is
 // below 2^-28 of a row of 2^18.)  The exponential is taken in 64 bits: at fp32's 2^-23 one draw in some hundreds would fall on the other side of a border.
 //
-// The last entry kept.  A histogram, count and mass, of the distance to the maximum over the range where the cut can lie: behind weight
-// (1 - p) W / V all tokens together weigh less than (1 - p) W.  The bin where a limit is reached is put on a list and ranked by counting.  Where it
-// holds too many (long ties, a range of odd shape) it is split by its keys' bits until it does not, or until one value is left, whose ties are taken from
-// the front of the row.
+// The last entry kept.  A histogram, count and mass, of the distance to the maximum over the range where the cut can lie: the tokens whose weight is
+// below (1 - p) / V of the largest weigh less than 1 - p together, and the row at least 1.  The bin where a limit is reached is put on a list and ranked by
+// counting.  Where it holds too many (long ties, a range of odd shape) it is split by its keys' bits until it does not, or until one value is left, whose
+// ties are taken from the front of the row.
 //
-// Split.  A row is cut into parts, one CTA each, that form a cluster; a part into stretches, one a warp.
+// Split.  A row is cut into parts, one CTA each, that form a cluster; a part into stretches, one a warp.  A part that fits stays in shared memory, so that
+// a row is read once; other rows come from L2 again.
+//
+// Cost.  Many rows: the pass of 64-bit exponentials, 30 cycles for a warp's logits on a scheduler, and the first pass at the memory's rate, one behind the
+// other (512 rows of 128 000 in fp32, 178 us, 4.4 times their bytes).  A mixed batch of 64 rows of 128 000 in bf16 takes 58 us: its rows with a limit go three
+// times over their part, the histogram's additions to shared memory take as long as the exponentials, and six barriers of the cluster lie between.  One row of
+// 32 000: 15.5 us, these barriers and the dependent steps between them.
 #include "lm_device.cuh"
 #include "lm_host.h"
 
