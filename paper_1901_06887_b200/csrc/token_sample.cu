@@ -840,7 +840,8 @@ cudaError_t configure_token_sample() {
 mt_status launch_token_sample(const SampleArgs& a, const OpContext& c, cudaStream_t s) {
     Params p;
     p.a = a;
-    // Parts: as many as give every SM its two CTAs (367 rows of 5409 in bf16: 32 us in one, 56 in two).  Rows that are not held then: four parts if that
+    // Parts: as many as give every SM its two CTAs (367 rows of 5409 in bf16: 32 us in one, 56 in two), but eight only where that takes three quarters of the
+    // SMs or less: clusters of eight do not fill the rest (16 rows of 32 000: 21 us in eight, 17 in four; 8 rows 15.7 and 16.1).  Rows that are not held then: four parts if that
     // holds them (107 rows of 73 187 in fp32: 48 us, 61 in two), else at least two, so that no more of them are under way at once than L2 holds (512 rows of
     // 128 000 in fp32: 178 us in two, 200 in one, 193 in four).
     const int vec = a.fp32 ? 4 : 8, most = (a.vocab + 2 * vec - 2) / vec;          // vectors of a row that starts anywhere
@@ -848,6 +849,7 @@ mt_status launch_token_sample(const SampleArgs& a, const OpContext& c, cudaStrea
     auto fits = [&](int parts) { return vecs(parts) * kWarps * 16 <= kHeldBytes; };
     p.parts = 1;
     while (p.parts < kMaxParts && a.vocab / (p.parts * 2) >= kMinPart && ((p.parts == 1 && !fits(1)) || (int64_t)a.n * p.parts * 2 <= 2LL * c.sm_count)) p.parts *= 2;
+    if (p.parts == 8 && 4LL * a.n * 8 > 3LL * c.sm_count) p.parts = 4;
     if (!fits(p.parts) && p.parts < 4 && fits(4)) p.parts = 4;
     p.vecs = vecs(p.parts);
     const bool hold = fits(p.parts);
