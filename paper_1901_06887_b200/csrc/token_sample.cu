@@ -244,13 +244,13 @@ constexpr float kFirst = 8388608.f;
 __device__ __forceinline__ float bin_of(float x, float top, float per) { return fmaf(top - x, per, kFirst); }
 __device__ __forceinline__ int bin_index(float f) { return __float_as_int(f) - 0x4b000000; }
 
-// Adds to shared memory where `on`, without a branch.
+// Adds to shared memory where `on`, without a branch.  (Volatile keeps them between the barriers; without a clobber the table's loads for the next logits may pass.)
 __device__ __forceinline__ void add_if(bool on, uint32_t addr, uint32_t v) {
-    asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.u32 q, %0, 0;\n\t@q red.shared.add.u32 [%1], %2;\n\t}" ::"r"((uint32_t)on), "r"(addr), "r"(v) : "memory");
+    asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.u32 q, %0, 0;\n\t@q red.shared.add.u32 [%1], %2;\n\t}" ::"r"((uint32_t)on), "r"(addr), "r"(v));
 }
 __device__ __forceinline__ uint32_t fetch_add_if(bool on, uint32_t addr, uint32_t v) {
     uint32_t old = 0;
-    asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.u32 q, %1, 0;\n\t@q atom.shared.add.u32 %0, [%2], %3;\n\t}" : "+r"(old) : "r"((uint32_t)on), "r"(addr), "r"(v) : "memory");
+    asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.u32 q, %1, 0;\n\t@q atom.shared.add.u32 %0, [%2], %3;\n\t}" : "+r"(old) : "r"((uint32_t)on), "r"(addr), "r"(v));
     return old;
 }
 
