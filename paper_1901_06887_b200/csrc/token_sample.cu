@@ -186,6 +186,21 @@ __device__ __forceinline__ float element(const void* p, int64_t i) {
     return FP32 ? static_cast<const float*>(p)[i] : bf16_to_f(static_cast<const uint16_t*>(p)[i]);
 }
 
+struct Four { float x[4]; };
+// f(four logits) for a vector: once for fp32, twice, in a loop, for bf16.  (The passes' loops are kept short: unrolled further they miss the instruction cache.)
+template <bool FP32, class F>
+__device__ __forceinline__ void by_fours(uint4 v, F f) {
+    if (FP32) {
+        f(Four{__uint_as_float(v.x), __uint_as_float(v.y), __uint_as_float(v.z), __uint_as_float(v.w)});
+    } else {
+#pragma unroll 1
+        for (int h = 0; h < 2; ++h) {
+            f(Four{bf16_lo(v.x), bf16_hi(v.x), bf16_lo(v.y), bf16_hi(v.y)});
+            v.x = v.z;
+            v.y = v.w;
+        }
+    }
+}
 // Weights as whole numbers, 2^y 2^shift with y = c (x - max).  y = n / 32 + r: 2^(n / 32) comes from a table, 2^r, |r| <= 1/64, from its series to r^4,
 // off by 2^-39.  Adding 2^52 + 2^51 over 32 rounds to parts of 32 and leaves n in the low word; adding 2^52 rounds to a whole number
 // and leaves it there.  Nine operations of 64 bits, which bound the pass; the weight of x = max is exact.  What lies 1000 powers of two and more below the maximum goes
@@ -198,11 +213,9 @@ struct Weights {
     double max, c;
     float top, far;                           // the maximum, and a distance of 1000 powers of two below it
     const double* table;                      // 2^(i / 32) 2^shift, i << 15 taken from the upper word: adding n << 15 to it then multiplies by 2^(n >> 5)
-    __device__ __forceinline__ bool is_far(float x) const { return x - top < far; }
     // with 2^52 in front
-    template <bool CHECK>
     __device__ __forceinline__ u64 raw(float x) const {
-        const bool none = CHECK && is_far(x);
+        const bool none = x - top < far;
         const double d = (double)(none ? top : x) - max;
         const double t = fma(d, c, kMagic), r = fma(d, c, kMagic - t);
         const int n = __double2loint(t);
@@ -214,29 +227,7 @@ struct Weights {
         const int hi = __double2hiint(e) + (n << 15);
         return (u64)__double_as_longlong(fma(p, __hiloint2double(none ? 0 : hi, __double2loint(e)), kTwo52));
     }
-    __device__ __forceinline__ u64 operator()(float x) const { return raw<true>(x) - kWhole; }
-    // of a few: far values are looked for once
-    template <int N>
-    __device__ __forceinline__ void raw_of(const float (&x)[N], u64 (&w)[N]) const {
-        float low = x[0];
-#pragma unroll
-        for (int e = 1; e < N; ++e) low = fminf(low, x[e]);
-        if (is_far(low)) {
-#pragma unroll
-            for (int e = 0; e < N; ++e) w[e] = raw<true>(x[e]);
-        } else {
-#pragma unroll
-            for (int e = 0; e < N; ++e) w[e] = raw<false>(x[e]);
-        }
-    }
-    template <int N>
-    __device__ __forceinline__ u64 sum_of(const float (&x)[N]) const {
-        u64 w[N], sum = 0;
-        raw_of<N>(x, w);
-#pragma unroll
-        for (int e = 0; e < N; ++e) sum += w[e];
-        return sum - N * kWhole;
-    }
+    __device__ __forceinline__ u64 operator()(float x) const { return raw(x) - kWhole; }
 };
 
 // 2^23 and a bin, which rises as the value falls, or more
@@ -304,80 +295,71 @@ __device__ __forceinline__ float max_pass(const Share<FP32, HOLD>& share) {
 
 // The row's mass.
 template <bool FP32, bool HOLD>
-__device__ __forceinline__ u64 sum_pass(const Share<FP32, HOLD>& share, const Weights& weights) {
-    const Share<FP32, HOLD> l = share;
-    const Weights wt = weights;
-    constexpr int N = kVec<FP32>;
+__device__ __forceinline__ u64 sum_pass(const Share<FP32, HOLD>& l, const Weights& wt) {
     u64 mass = 0;
-    uint4 q[2] = {l.get(l.vec0 + l.lane), l.get(l.vec0 + l.lane + 32)};
-    for (int j0 = l.vec0 + l.lane; j0 < l.vec1; j0 += 64) {
+    uint4 q = l.get(l.vec0 + l.lane), next = l.get(l.vec0 + l.lane + 32);
+#pragma unroll 1
+    for (int j = l.vec0 + l.lane; j < l.vec1; j += 32) {
+        const uint4 v = q;
+        q = next;
+        next = l.get(j + 64);
+        by_fours<FP32>(v, [&](const Four& y) {
+            u64 sum = 0;
 #pragma unroll
-        for (int g = 0; g < 2; ++g) {
-            float x[N];
-            decode<FP32>(q[g], x);
-            q[g] = l.get(j0 + 32 * g + 64);
-#pragma unroll
-            for (int e = 0; e < N; e += 4) mass += wt.template sum_of<4>({x[e], x[e + 1], x[e + 2], x[e + 3]});
-        }
+            for (int e = 0; e < 4; ++e) sum += wt.raw(y.x[e]);
+            mass += sum - 4 * kWhole;
+        });
     }
     return mass;
 }
 
 // The row's mass, and the histogram of (count and) mass over bins of the distance to the maximum.
-template <bool FP32, bool HOLD, bool COUNT>
-__device__ __forceinline__ u64 mass_pass(const Share<FP32, HOLD>& share, const Weights& weights, float per, uint32_t counts_at, uint32_t los_at, uint32_t his_at) {
-    const Share<FP32, HOLD> l = share;
-    const Weights wt = weights;
-    constexpr int N = kVec<FP32>;
+template <bool FP32, bool HOLD>
+__device__ __forceinline__ u64 mass_pass(const Share<FP32, HOLD>& l, const Weights& wt, float per, bool count, uint32_t counts_at, uint32_t los_at, uint32_t his_at) {
     u64 mass = 0;
-    uint4 q[2] = {l.get(l.vec0 + l.lane), l.get(l.vec0 + l.lane + 32)};
-    for (int j0 = l.vec0 + l.lane; j0 < l.vec1; j0 += 64) {
+    uint4 q = l.get(l.vec0 + l.lane), next = l.get(l.vec0 + l.lane + 32);
+#pragma unroll 1
+    for (int j = l.vec0 + l.lane; j < l.vec1; j += 32) {
+        const uint4 v = q;
+        q = next;
+        next = l.get(j + 64);
+        by_fours<FP32>(v, [&](const Four& y) {
+            u64 w[4];
+            uint32_t old[4], at[4];
+            bool in[4];
 #pragma unroll
-        for (int g = 0; g < 2; ++g) {
-            float x[N];
-            decode<FP32>(q[g], x);
-            q[g] = l.get(j0 + 32 * g + 64);
+            for (int e = 0; e < 4; ++e) w[e] = wt(y.x[e]);
 #pragma unroll
-            for (int e0 = 0; e0 < N; e0 += 4) {
-                const float y[4] = {x[e0], x[e0 + 1], x[e0 + 2], x[e0 + 3]};
-                u64 w[4];
-                uint32_t old[4], at[4];
-                bool in[4];
-                wt.template raw_of<4>(y, w);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float f = bin_of(y[e], wt.top, per);
-                    in[e] = f < kFirst + kBins;
-                    at[e] = 4 * bin_index(f);
-                    old[e] = fetch_add_if(in[e], los_at + at[e], (uint32_t)w[e]);
-                    if (COUNT) add_if(in[e], counts_at + at[e], 1u);
-                }
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    w[e] -= kWhole;
-                    mass += w[e];
-                    const uint32_t hi = (uint32_t)(w[e] >> 32) + (old[e] + (uint32_t)w[e] < old[e] ? 1u : 0u);
-                    add_if(in[e] && hi > 0, his_at + at[e], hi);
-                }
+            for (int e = 0; e < 4; ++e) {
+                const float f = bin_of(y.x[e], wt.top, per);
+                in[e] = f < kFirst + kBins;
+                at[e] = 4 * bin_index(f);
+                old[e] = fetch_add_if(in[e], los_at + at[e], (uint32_t)w[e]);
+                add_if(in[e] && count, counts_at + at[e], 1u);
             }
-        }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                mass += w[e];
+                const uint32_t hi = (uint32_t)(w[e] >> 32) + (old[e] + (uint32_t)w[e] < old[e] ? 1u : 0u);
+                add_if(in[e] && hi > 0, his_at + at[e], hi);
+            }
+        });
     }
     return mass;
 }
 
 // Counts alone.
 template <bool FP32, bool HOLD>
-__device__ __forceinline__ void count_pass(const Share<FP32, HOLD>& share, float top, float per, uint32_t counts_at) {
-    const Share<FP32, HOLD> l = share;
-    constexpr int N = kVec<FP32>;
+__device__ __forceinline__ void count_pass(const Share<FP32, HOLD>& l, float top, float per, uint32_t counts_at) {
+#pragma unroll 1
     for (int j = l.vec0 + l.lane; j < l.vec1; j += 32) {
-        float x[N];
-        decode<FP32>(l.get(j), x);
+        by_fours<FP32>(l.get(j), [&](const Four& y) {
 #pragma unroll
-        for (int e = 0; e < N; ++e) {
-            const float f = bin_of(x[e], top, per);
-            add_if(f < kFirst + kBins, counts_at + 4 * bin_index(f), 1u);
-        }
+            for (int e = 0; e < 4; ++e) {
+                const float f = bin_of(y.x[e], top, per);
+                add_if(f < kFirst + kBins, counts_at + 4 * bin_index(f), 1u);
+            }
+        });
     }
 }
 
@@ -604,7 +586,7 @@ __global__ void __launch_bounds__(kThreads, CTAS) token_sample_kernel(const Para
         } else {
             // the row's mass and the first histogram in one pass
             if (!by_mass) count_pass(l, top, per, counts_at);
-            else mine = by_count ? mass_pass<FP32, HOLD, true>(l, wt, per, counts_at, los_at, his_at) : mass_pass<FP32, HOLD, false>(l, wt, per, counts_at, los_at, his_at);
+            else mine = mass_pass(l, wt, per, by_count, counts_at, los_at, his_at);
             if (by_mass) {
                 mine = warp_sum_u64(mine);
                 if (lane == 0) s.warp_sum[warp] = mine;
