@@ -463,7 +463,8 @@ mt_status mt_rotate(const mt_rotate_desc* desc_host, const void* x, const int32_
  * All caches of a model (one a layer) go by one of these.  The calls below change it on the device, in stream order, without the host seeing it; they are
  * deterministic: pages are handed out lowest first, in the order of the call.  A shared page is always full, so appending to a row never shows in
  * another.  A row index outside [0, n_rows), one that an earlier place of the same call names, a length that is negative or passes the table, or a page outside
- * the cache: that place of the call is left out (sticky status MT_ERR_INVALID_ARG, its index).  A place for which no free page is left is left out
+ * the cache that would be shared, copied or appended to: that place of the call is left out (sticky status MT_ERR_INVALID_ARG, its index).  A page that is given back although
+ * it lies outside or nobody holds it is passed over, with the same status.  A place for which no free page is left is left out
  * too (MT_ERR_OOM); places behind it that need pages then are as well.  They use scratch, see above.
  * Limits: page_tokens 16, 32, 64, 128 or 256; table_width * page_tokens below 2^31 - 64. */
 typedef struct {
@@ -506,7 +507,7 @@ mt_status mt_kv_copy(const mt_kv_cache* const* caches_host, int32_t n_caches, co
  * min_p above 1, takes the first; one below 2^-126 counts as that.  Weights are 64-bit whole numbers, the largest 2^46 (fewer in rows of more than 2^16 logits), so draws do not depend on the
  * order of summing; what is below one of those units is never drawn.  A row without a distribution (nothing but minus infinity, a NaN or plus infinity) gives id -1 and NaN;
  * so does one with a negative, infinite or NaN temperature, a NaN limit or a uniform number outside [0, 1), with the sticky status MT_ERR_INVALID_ARG.
- * Limits: n at most 2^29; vocab below 2^30. */
+ * Limits: n below 2^29; vocab below 2^30. */
 mt_status mt_token_sample(const void* logits, int32_t dtype, int64_t row_stride, int32_t n, int32_t vocab, const float* temperature,
                           const int32_t* top_k, const float* top_p, const float* min_p, const float* uniform, int32_t* ids, float* logprobs,
                           void* stream);

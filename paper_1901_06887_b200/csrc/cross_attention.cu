@@ -440,7 +440,7 @@ cross_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
         }
     } else {
         // ------------------------------------------------------------------------------------------ softmax, one row per thread
-        // registers move here: 256 threads x 208 + 128 x 88 = the launch's 384 x 168
+        // registers move here: 256 threads x 192 + 128 x 120 = the launch's 384 x 168
         asm volatile("setmaxnreg.inc.sync.aligned.u32 192;");
         const int i = warp >> 2;
         const int r = threadIdx.x & 127;

@@ -199,11 +199,10 @@ __device__ __forceinline__ int pages_of(const Params& p, int len) { return (int)
 __device__ __forceinline__ bool good_length(const Params& p, int len) { return len >= 0 && (int64_t)len <= (int64_t)p.k.table_width << p.shift; }
 __device__ __forceinline__ int32_t* table_row(const Params& p, int row) { return p.k.tables + (int64_t)row * p.k.table_width; }
 __device__ __forceinline__ void give_back(const Params& p, int page, int i) {
-    if (!in(page, p.k.n_pages)) return;
-    if (atomicSub(p.k.refs + page, 1) <= 0) {                  // nobody held it: the table is not the pages'
-        atomicAdd(p.k.refs + page, 1);
-        raise_status(p.status, MT_ERR_INVALID_ARG, i);
-    }
+    const bool there = in(page, p.k.n_pages);
+    const bool held = there && atomicSub(p.k.refs + page, 1) > 0;              // nobody held it: the table is not the pages'
+    if (there && !held) atomicAdd(p.k.refs + page, 1);
+    if (!held) raise_status(p.status, MT_ERR_INVALID_ARG, i);
 }
 // The rows of a call: owner[row] is the first place of the call that names it.
 template <bool SMALL>
@@ -398,6 +397,10 @@ __global__ void __launch_bounds__(kThreads) reserve_kernel(const Params p) {
             if (lane == 0) raise_status(p.status, MT_ERR_INVALID_ARG, i);
         }
         const int64_t last = go && had > 0 && (len & (p.k.page_tokens - 1)) ? table_row(p, row)[had - 1] : 0;      // the page that is partly filled
+        if (go && count > 0 && (uint64_t)last >= (uint64_t)p.k.n_pages) {
+            go = false;
+            if (lane == 0) raise_status(p.status, MT_ERR_INVALID_ARG, i);
+        }
         if (go) {
             for (int c = lane; c < need; c += size) {
                 const int page = free_page<SMALL>(h, first + c);

@@ -476,7 +476,7 @@ mt_status mt_token_sample(const void* logits, int32_t dtype, int64_t row_stride,
                           const int32_t* top_k, const float* top_p, const float* min_p, const float* uniform, int32_t* ids, float* logprobs,
                           void* stream) {
     if (n < 0 || vocab <= 0 || (dtype != MT_BF16 && dtype != MT_FP32)) return MT_ERR_INVALID_ARG;
-    if (n > (1 << 29) || vocab >= (1 << 30) || row_stride < 0 || row_stride >= (int64_t(1) << 36)) return MT_ERR_UNSUPPORTED;
+    if (n >= (1 << 29) || vocab >= (1 << 30) || row_stride < 0 || row_stride >= (int64_t(1) << 36)) return MT_ERR_UNSUPPORTED;
     std::unique_lock<std::mutex> lk;
     OpContext c;
     mt_status st = op_begin(&lk, &c);

@@ -271,7 +271,7 @@ struct Share {
     }
 };
 
-// The passes over a row.  (Inlined into the kernel, although it spills a little: as functions of their own they took 10 % longer.)
+// The passes over a row.  (Inlined into the kernel: as functions of their own they took 10 % longer.)
 
 // The first one: the maximum, NaN if any logit is.
 template <bool FP32, bool HOLD>

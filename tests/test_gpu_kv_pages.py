@@ -177,6 +177,29 @@ def test_pages_outside_the_cache():
     mt.mt_get_async_status()
 
 
+@pytest.mark.parametrize("page", [10, -1, 2 ** 31 - 1])
+def test_a_page_outside_is_neither_appended_to_nor_given_back(page):
+    """The partly filled page of row 0 lies outside, and so does a page that row 1 gives back."""
+    k = Both(10, 16, 4, 3)
+    k.reserve([0, 1, 2], [20, 40, 16])                         # pages 0 1, 2 3 4, 5
+    k.book.tables[0][1] = k.book.tables[1][0] = page
+    k.load()
+    for counts in ([3, 1, 0], [20, 1, 0]):                     # within the page, and past it
+        slots = torch.full((sum(counts),), -9, dtype=torch.int64, device="cuda")
+        mt.mt_kv_reserve(k.pages, i32([0, 1, 2]), i32(counts), slots)
+        assert mt.mt_get_async_status() == (1, 0)
+        n = k.pages.lengths.tolist()[1]
+        assert slots.tolist() == [-1] * counts[0] + [4 * 16 + n - 1 - 32] and k.pages.lengths.tolist() == [20, n, 16, 0]
+    assert k.pages.refs.tolist() == [1] * 6 + [0] * 4
+    copies = torch.empty((1, 3), dtype=torch.int32, device="cuda")
+    mt.mt_kv_fork(k.pages, i32([2]), i32([1]), copies)
+    assert mt.mt_get_async_status() == (1, 0)
+    assert k.pages.refs.tolist() == [1, 1, 1, 0, 0, 2] + [0] * 4 and k.pages.lengths.tolist() == [20, 16, 16, 0]
+    mt.mt_kv_release(k.pages, i32([2, 0]))
+    assert mt.mt_get_async_status() == (1, 1)
+    assert k.pages.refs.tolist() == [0, 1, 1, 0, 0, 1] + [0] * 4 and k.pages.lengths.tolist() == [0, 16, 0, 0]
+
+
 def test_a_page_nobody_holds_is_not_given_back():
     k = Both(10, 16, 3, 3)
     k.reserve([0], [20])
