@@ -16,9 +16,9 @@
 // a row is read once; other rows come from L2 again.
 //
 // Cost.  Many rows: the pass of 64-bit exponentials, 30 cycles for a warp's logits on a scheduler, and the first pass at the memory's rate, one behind the
-// other (512 rows of 128 000 in fp32, 178 us, 4.4 times their bytes).  A mixed batch of 64 rows of 128 000 in bf16 takes 58 us: its rows with a limit go three
+// other (512 rows of 128 000 in fp32, 174 us, 4.3 times their bytes).  A mixed batch of 64 rows of 128 000 in bf16 takes 57 us: its rows with a limit go three
 // times over their part, the histogram's additions to shared memory take as long as the exponentials, and six barriers of the cluster lie between.  One row of
-// 32 000: 15.5 us, these barriers and the dependent steps between them.
+// 32 000: 13.8 us, these barriers and the dependent steps between them.
 #include "lm_device.cuh"
 #include "lm_host.h"
 
@@ -30,9 +30,11 @@ constexpr int kBins = 2 * kThreads;
 constexpr int kFine = 16, kCoarse = kBins / kFine;
 constexpr int kList = kThreads;
 constexpr int kMaxParts = 8;
+constexpr int kAtOnce = 4;                    // parts whose shared memory is read at once
 static_assert(kBins == 2 * kThreads && kCoarse == 64 && kFine == 16 && kMaxParts <= 8, "");
 constexpr int kMinPart = 2048;                // logits of a part, at least
-constexpr int kHeldBytes = 81920;             // of a part that stays in shared memory, at most: two CTAs an SM
+constexpr int kShortPart = 16384;             // and of one that takes an SM by itself, rather
+constexpr int held_bytes(int ctas) { return ctas == 1 ? 196608 : 81920; }      // of a part that stays in shared memory, at most, with so many CTAs an SM
 using u64 = unsigned long long;
 
 struct Params {
@@ -47,7 +49,7 @@ struct Shared {
     uint2 count[kThreads], lo[kThreads], hi[kThreads];       // bins 2 t and 2 t + 1: entries, and mass in two words
     ulonglong2 entry[kList];                                 // the list: (ordered logit, rising as the index falls), weight
     u64 part_entry[kList];                                   // this part's share of it
-    u64 coarse_mass[kCoarse];                 // sixteen bins each
+    alignas(16) u64 coarse_mass[kCoarse];     // sixteen bins each
     alignas(8) uint32_t coarse_count[kCoarse];
     double table[32];
     u64 warp_sum[kWarps], scan[kWarps];
@@ -85,9 +87,15 @@ __device__ __forceinline__ u64 remote_u64(const void* p, uint32_t rank) {
     asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(map_to_cta(smem_u32(p), rank)));
     return v;
 }
+__device__ __forceinline__ ulonglong2 remote_u64x2(const void* p, uint32_t rank) {
+    ulonglong2 v;
+    asm volatile("ld.shared::cluster.v2.u64 {%0, %1}, [%2];" : "=l"(v.x), "=l"(v.y) : "r"(map_to_cta(smem_u32(p), rank)));
+    return v;
+}
+template <int LANES = 32>                     // the sum of so many neighbours
 __device__ __forceinline__ u64 warp_sum_u64(u64 v) {
 #pragma unroll
-    for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    for (int o = LANES / 2; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
     return v;
 }
 template <class T>
@@ -187,13 +195,14 @@ __device__ __forceinline__ float element(const void* p, int64_t i) {
 }
 
 struct Four { float x[4]; };
-// f(four logits) for a vector: once for fp32, twice, in a loop, for bf16.  (The passes' loops are kept short: unrolled further they miss the instruction cache.)
-template <bool FP32, class F>
+// f(four logits) for a vector: once for fp32, twice for bf16, in a loop where there are two CTAs an SM.  (The passes' loops are kept short: unrolled further they miss
+// the instruction cache.  One CTA by itself gains by it: 18 rows of 128 000 38.0 -> 36.5 us.)
+template <bool FP32, int CTAS, class F>
 __device__ __forceinline__ void by_fours(uint4 v, F f) {
     if (FP32) {
         f(Four{__uint_as_float(v.x), __uint_as_float(v.y), __uint_as_float(v.z), __uint_as_float(v.w)});
     } else {
-#pragma unroll 1
+#pragma unroll (CTAS == 1 ? 2 : 1)
         for (int h = 0; h < 2; ++h) {
             f(Four{bf16_lo(v.x), bf16_hi(v.x), bf16_lo(v.y), bf16_hi(v.y)});
             v.x = v.z;
@@ -294,7 +303,7 @@ __device__ __forceinline__ float max_pass(const Share<FP32, HOLD>& share) {
 }
 
 // The row's mass.
-template <bool FP32, bool HOLD>
+template <bool FP32, int CTAS, bool HOLD>
 __device__ __forceinline__ u64 sum_pass(const Share<FP32, HOLD>& l, const Weights& wt) {
     u64 mass = 0;
     uint4 q = l.get(l.vec0 + l.lane), next = l.get(l.vec0 + l.lane + 32);
@@ -303,7 +312,7 @@ __device__ __forceinline__ u64 sum_pass(const Share<FP32, HOLD>& l, const Weight
         const uint4 v = q;
         q = next;
         next = l.get(j + 64);
-        by_fours<FP32>(v, [&](const Four& y) {
+        by_fours<FP32, CTAS>(v, [&](const Four& y) {
             u64 sum = 0;
 #pragma unroll
             for (int e = 0; e < 4; ++e) sum += wt.raw(y.x[e]);
@@ -314,7 +323,7 @@ __device__ __forceinline__ u64 sum_pass(const Share<FP32, HOLD>& l, const Weight
 }
 
 // The row's mass, and the histogram of (count and) mass over bins of the distance to the maximum.
-template <bool FP32, bool HOLD>
+template <bool FP32, int CTAS, bool HOLD>
 __device__ __forceinline__ u64 mass_pass(const Share<FP32, HOLD>& l, const Weights& wt, float per, bool count, uint32_t counts_at, uint32_t los_at, uint32_t his_at) {
     u64 mass = 0;
     uint4 q = l.get(l.vec0 + l.lane), next = l.get(l.vec0 + l.lane + 32);
@@ -323,7 +332,7 @@ __device__ __forceinline__ u64 mass_pass(const Share<FP32, HOLD>& l, const Weigh
         const uint4 v = q;
         q = next;
         next = l.get(j + 64);
-        by_fours<FP32>(v, [&](const Four& y) {
+        by_fours<FP32, CTAS>(v, [&](const Four& y) {
             u64 w[4];
             uint32_t old[4], at[4];
             bool in[4];
@@ -349,11 +358,11 @@ __device__ __forceinline__ u64 mass_pass(const Share<FP32, HOLD>& l, const Weigh
 }
 
 // Counts alone.
-template <bool FP32, bool HOLD>
+template <bool FP32, int CTAS, bool HOLD>
 __device__ __forceinline__ void count_pass(const Share<FP32, HOLD>& l, float top, float per, uint32_t counts_at) {
 #pragma unroll 1
     for (int j = l.vec0 + l.lane; j < l.vec1; j += 32) {
-        by_fours<FP32>(l.get(j), [&](const Four& y) {
+        by_fours<FP32, CTAS>(l.get(j), [&](const Four& y) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const float f = bin_of(y.x[e], top, per);
@@ -415,7 +424,7 @@ __device__ __forceinline__ u64 kept_pass(const Share<FP32, HOLD>& share, const K
     return mass;
 }
 
-// CTAS an SM: two, or, where there are no more than SMs, one, with twice the registers (one row of 32 000: 15.9 against 15.4 us).
+// CTAS an SM: two, or, where there are no more than SMs, one, with twice the registers and more of them held.
 template <bool FP32, bool HOLD, int CTAS>
 __global__ void __launch_bounds__(kThreads, CTAS) token_sample_kernel(const Params p) {
     __shared__ Shared s;
@@ -526,47 +535,79 @@ __global__ void __launch_bounds__(kThreads, CTAS) token_sample_kernel(const Para
             team_sync();
             if (warp == 0) {
                 // a limit is reached among n entries of mass m behind c_before of m_before?  (A target of zero is reached by the first entry, not before it.)
-                auto reached = [&](u64 c_before, u64 m_before, uint32_t n, u64 m) {
-                    const bool was = c_before >= (u64)top_k || m_before >= target, is = c_before + n >= (u64)top_k || m_before + m >= target;
+                auto reached = [&](uint32_t c_before, u64 m_before, uint32_t n, u64 m) {
+                    const bool was = c_before >= (uint32_t)top_k || m_before >= target, is = c_before + n >= (uint32_t)top_k || m_before + m >= target;
                     return (by_count ? n > 0 : m > 0) && is && (!was || (by_count ? c_before == 0 : m_before == 0));
                 };
                 const u64 sum = first && by_mass ? of_parts_u64(s.sum) : 0;
                 uint2 n = make_uint2(0, 0);
                 u64 m0 = 0, m1 = 0;
+                if (parts == 1) {                                  // groups 2 lane and 2 lane + 1
+                    n = *reinterpret_cast<const uint2*>(&s.coarse_count[2 * lane]);
+                    m0 = s.coarse_mass[2 * lane];
+                    m1 = s.coarse_mass[2 * lane + 1];
+                } else {
+#pragma unroll 1
+                    for (int r0 = 0; r0 < parts; r0 += kAtOnce) {
+                        uint2 x[kAtOnce];
+                        ulonglong2 y[kAtOnce];
 #pragma unroll
-                for (int r = 0; r < kMaxParts; ++r) {              // groups 2 lane and 2 lane + 1
-                    if (r >= parts) break;
-                    const uint2 x = parts > 1 ? remote_u32x2(&s.coarse_count[2 * lane], r) : *reinterpret_cast<const uint2*>(&s.coarse_count[2 * lane]);
-                    n.x += x.x;
-                    n.y += x.y;
-                    m0 += parts > 1 ? remote_u64(&s.coarse_mass[2 * lane], r) : s.coarse_mass[2 * lane];
-                    m1 += parts > 1 ? remote_u64(&s.coarse_mass[2 * lane + 1], r) : s.coarse_mass[2 * lane + 1];
+                        for (int r = 0; r < kAtOnce; ++r) {
+                            x[r] = remote_u32x2(&s.coarse_count[2 * lane], (r0 + r) & (parts - 1));
+                            y[r] = remote_u64x2(&s.coarse_mass[2 * lane], (r0 + r) & (parts - 1));
+                        }
+#pragma unroll
+                        for (int r = 0; r < kAtOnce; ++r) {
+                            const bool there = r0 + r < parts;
+                            n.x += there ? x[r].x : 0;
+                            n.y += there ? x[r].y : 0;
+                            m0 += there ? y[r].x : 0;
+                            m1 += there ? y[r].y : 0;
+                        }
+                    }
                 }
                 if (first && by_mass) target = top_p > 0.f ? times(warp_sum_u64(sum), top_p, true) : 0;
-                const u64 c0 = above_count + warp_scan((u64)n.x + n.y, lane) - n.x - n.y, b0 = above_mass + warp_scan(m0 + m1, lane) - m0 - m1;
+                const uint32_t c0 = above_count + warp_scan(n.x + n.y, lane) - n.x - n.y;
+                const u64 b0 = above_mass + warp_scan(m0 + m1, lane) - m0 - m1;
                 const bool in0 = reached(c0, b0, n.x, m0), in1 = reached(c0 + n.x, b0 + m0, n.y, m1);
                 const uint32_t hit = __ballot_sync(0xffffffffu, in0 || in1);
                 int found = -1;
                 if (hit) {
                     const int at = __ffs(hit) - 1, group = __shfl_sync(0xffffffffu, 2 * lane + (in0 ? 0 : 1), at);
-                    const u64 c_group = __shfl_sync(0xffffffffu, in0 ? c0 : c0 + n.x, at), m_group = __shfl_sync(0xffffffffu, in0 ? b0 : b0 + m0, at);
+                    const uint32_t c_group = __shfl_sync(0xffffffffu, in0 ? c0 : c0 + n.x, at);
+                    const u64 m_group = __shfl_sync(0xffffffffu, in0 ? b0 : b0 + m0, at);
                     const int b = group * kFine + lane % kFine;    // of parts lane / 16, + 2, ..
                     uint32_t nb = 0;
                     u64 mb = 0;
+                    if (parts == 1) {
+                        if (lane < kFine) { nb = counts[b]; mb = ((u64)his[b] << 32) + los[b]; }
+                    } else {
+#pragma unroll 1
+                        for (int r0 = 0; r0 < parts; r0 += kAtOnce) {
+                            uint32_t x[kAtOnce / 2][3];
 #pragma unroll
-                    for (int q = 0; q < kMaxParts; q += 2) {
-                        const int of = q + lane / kFine;
-                        if (of >= parts) continue;
-                        nb += parts > 1 ? remote_u32(counts + b, of) : counts[b];
-                        mb += parts > 1 ? ((u64)remote_u32(his + b, of) << 32) + remote_u32(los + b, of) : ((u64)his[b] << 32) + los[b];
+                            for (int q = 0; q < kAtOnce / 2; ++q) {
+                                const int of = (r0 + 2 * q + lane / kFine) & (parts - 1);
+                                x[q][0] = remote_u32(counts + b, of);
+                                x[q][1] = remote_u32(los + b, of);
+                                x[q][2] = remote_u32(his + b, of);
+                            }
+#pragma unroll
+                            for (int q = 0; q < kAtOnce / 2; ++q) {
+                                if (r0 + 2 * q + lane / kFine >= parts) continue;
+                                nb += x[q][0];
+                                mb += ((u64)x[q][2] << 32) + x[q][1];
+                            }
+                        }
                     }
                     nb += __shfl_xor_sync(0xffffffffu, nb, kFine);
                     mb += __shfl_xor_sync(0xffffffffu, mb, kFine);
-                    const u64 before_c = c_group + warp_scan(lane < kFine ? (u64)nb : 0, lane) - nb, before = m_group + warp_scan(lane < kFine ? mb : 0, lane) - mb;
+                    const uint32_t before_c = c_group + warp_scan(lane < kFine ? nb : 0, lane) - nb;
+                    const u64 before = m_group + warp_scan(lane < kFine ? mb : 0, lane) - mb;
                     const uint32_t hits = __ballot_sync(0xffffffffu, lane < kFine && reached(before_c, before, nb, mb));
                     found = group * kFine + __ffs(hits) - 1;
                     if (lane == __ffs(hits) - 1) {
-                        s.above_count = (uint32_t)before_c;
+                        s.above_count = before_c;
                         s.above_mass = before;
                         s.bin_count = nb;
                     }
@@ -585,8 +626,8 @@ __global__ void __launch_bounds__(kThreads, CTAS) token_sample_kernel(const Para
             key_lo = key_hi = ordered(top);
         } else {
             // the row's mass and the first histogram in one pass
-            if (!by_mass) count_pass(l, top, per, counts_at);
-            else mine = mass_pass(l, wt, per, by_count, counts_at, los_at, his_at);
+            if (!by_mass) count_pass<FP32, CTAS>(l, top, per, counts_at);
+            else mine = mass_pass<FP32, CTAS>(l, wt, per, by_count, counts_at, los_at, his_at);
             if (by_mass) {
                 mine = warp_sum_u64(mine);
                 if (lane == 0) s.warp_sum[warp] = mine;
@@ -751,18 +792,18 @@ __global__ void __launch_bounds__(kThreads, CTAS) token_sample_kernel(const Para
     // (a float that lies below the last one kept needs no weight)
     float floor_x = cut == 0 ? -3.402823466e38f : unordered(kept.key);             // (minus infinity never passes: it also stands for what is no token)
     if (least > 0) floor_x = fmaxf(floor_x, (float)(wt.max + ((double)log2f(min_p) - 0.01) / c) - fabsf(top) * 0x1p-20f);
-    mine = all_kept ? sum_pass(l, wt) : kept_pass(l, kept, floor_x);
+    mine = all_kept ? sum_pass<FP32, CTAS>(l, wt) : kept_pass(l, kept, floor_x);
     const u64 stretch = warp_sum_u64(mine);
     if (lane == 0) s.warp_sum[warp] = stretch;
     __syncthreads();
-    const u64 in_warp = lane < kWarps ? s.warp_sum[lane] : 0;
-    u64 before = warp_sum_u64(lane < warp ? in_warp : 0), all = warp_sum_u64(in_warp);
+    const u64 in_warp = s.warp_sum[lane % kWarps];
+    u64 before = warp_sum_u64<kWarps>(lane % kWarps < warp ? in_warp : 0), all = warp_sum_u64<kWarps>(in_warp);
     if (parts > 1) {
         if (t == 0) s.sum = all;
         team_sync();
-        const u64 of_part = of_parts_u64(s.sum);
-        before += warp_sum_u64(lane < part ? of_part : 0);
-        all = warp_sum_u64(of_part);
+        const u64 of_part = lane % kMaxParts < parts ? remote_u64(&s.sum, lane % kMaxParts) : 0;
+        before += warp_sum_u64<kMaxParts>(lane % kMaxParts < part ? of_part : 0);
+        all = warp_sum_u64<kMaxParts>(of_part);
     }
     const u64 at = times(all, u, false);      // below all, since u is below 1
     auto answer = [&](int i) {
@@ -803,38 +844,67 @@ __global__ void __launch_bounds__(kThreads, CTAS) token_sample_kernel(const Para
 }
 
 using Kernel = void (*)(Params);
-template <int CTAS>
-Kernel kernel_of(bool fp32, bool hold) {
-    return fp32 ? (hold ? token_sample_kernel<true, true, CTAS> : token_sample_kernel<true, false, CTAS>)
-                : (hold ? token_sample_kernel<false, true, CTAS> : token_sample_kernel<false, false, CTAS>);
+Kernel kernel_of(bool fp32, bool hold, int ctas) {
+    if (ctas == 1) return fp32 ? token_sample_kernel<true, true, 1> : token_sample_kernel<false, true, 1>;
+    return fp32 ? (hold ? token_sample_kernel<true, true, 2> : token_sample_kernel<true, false, 2>)
+                : (hold ? token_sample_kernel<false, true, 2> : token_sample_kernel<false, false, 2>);
 }
+int g_fit[2][4];                              // clusters of 1, 2, 4 and 8 CTAs that lie beside each other, with one CTA an SM and with two
 
 }  // namespace
 
 cudaError_t configure_token_sample() {
     for (int i = 0; i < 4; ++i) {
-        const cudaError_t e = cudaFuncSetAttribute(i & 2 ? kernel_of<2>(i & 1, true) : kernel_of<1>(i & 1, true), cudaFuncAttributeMaxDynamicSharedMemorySize, kHeldBytes);
+        const int ctas = i / 2 + 1;
+        const cudaError_t e = cudaFuncSetAttribute(kernel_of(i & 1, true, ctas), cudaFuncAttributeMaxDynamicSharedMemorySize, held_bytes(ctas));
         if (e != cudaSuccess) return e;
     }
+    for (int ctas = 1; ctas <= 2; ++ctas)
+        for (int k = 0; k < 4; ++k) {
+            cudaLaunchConfig_t cfg = {};
+            cfg.gridDim = dim3(1u << k);
+            cfg.blockDim = dim3(kThreads);
+            cfg.dynamicSmemBytes = held_bytes(ctas);
+            cudaLaunchAttribute attr;
+            attr.id = cudaLaunchAttributeClusterDimension;
+            attr.val.clusterDim.x = 1u << k;
+            attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+            cfg.attrs = &attr;
+            cfg.numAttrs = 1;
+            const cudaError_t e = cudaOccupancyMaxActiveClusters(&g_fit[ctas - 1][k], kernel_of(true, true, ctas), &cfg);
+            if (e != cudaSuccess) return e;
+        }
     return cudaSuccess;
 }
 
 mt_status launch_token_sample(const SampleArgs& a, const OpContext& c, cudaStream_t s) {
     Params p;
     p.a = a;
-    // Parts: as many as give every SM its two CTAs (367 rows of 5409 in bf16: 32 us in one, 56 in two), but eight only where that takes three quarters of the
-    // SMs or less: clusters of eight do not fill the rest (16 rows of 32 000: 21 us in eight, 17 in four; 8 rows 15.7 and 16.1).  Rows that are not held then: four parts if that
-    // holds them (107 rows of 73 187 in fp32: 48 us, 61 in two), else at least two, so that no more of them are under way at once than L2 holds (512 rows of
-    // 128 000 in fp32: 178 us in two, 200 in one, 193 in four).
     const int vec = a.fp32 ? 4 : 8, most = (a.vocab + 2 * vec - 2) / vec;          // vectors of a row that starts anywhere
     auto vecs = [&](int parts) { return (most + parts * kWarps - 1) / (parts * kWarps); };
-    auto fits = [&](int parts) { return vecs(parts) * kWarps * 16 <= kHeldBytes; };
-    p.parts = 1;
-    while (p.parts < kMaxParts && a.vocab / (p.parts * 2) >= kMinPart && ((p.parts == 1 && !fits(1)) || (int64_t)a.n * p.parts * 2 <= 2LL * c.sm_count)) p.parts *= 2;
-    if (p.parts == 8 && 4LL * a.n * 8 > 3LL * c.sm_count) p.parts = 4;
-    if (!fits(p.parts) && p.parts < 4 && fits(4)) p.parts = 4;
+    auto fits = [&](int parts, int ctas) { return (int64_t)vecs(parts) * kWarps * 16 <= held_bytes(ctas); };
+    // Parts: as many as make clusters that all lie beside each other, held, with one CTA an SM: then they spread over the SMs, and a thread has more registers (15 rows of
+    // 128 000 in bf16: 22 us in eight parts, 33 in four, 16 rows 50 and 37, for clusters of eight do not fill the SMs; 64 rows of 32 000: 21 in two, 23 in four with two CTAs an
+    // SM; 74 rows 23, 27 and 29; 146 rows of 16 000: 20 in one part, 24 in two).  Where that leaves long parts, two CTAs an SM, of different rows, do better, if they fill the SMs
+    // and are held (64 rows of 128 000: 56 us in four parts, 72 in two with one CTA an SM; 33 rows 42 and 46; 18 rows, which do not fill them, 42 and 37).
+    auto most_parts = [&](int ctas) {
+        int k = 3;
+        while (k >= 0 && !(a.n <= g_fit[ctas - 1][k] && (k == 0 || a.vocab >> k >= kMinPart) && fits(1 << k, ctas))) --k;
+        return k;
+    };
+    const int one = most_parts(1), two = most_parts(2);
+    const int ctas = one >= 0 && (a.vocab >> one <= kShortPart || two < 0 || a.n << two <= c.sm_count) ? 1 : 2;
+    int k = ctas == 1 ? one : two;
+    // More rows, with two CTAs an SM: as few parts as can be held (107 rows of 73 187 in fp32: 48 us in four, 61 in two).  Rows that are not held: as many as lie beside each other,
+    // at least two, so that no more of them are under way at once than L2 holds (512 rows of 128 000 in fp32: 174 us in two, 200 in one, 193 in four).
+    if (k < 0) {
+        for (k = 0; k < 2 && !fits(1 << k, 2);) ++k;
+        if (!fits(1 << k, 2))
+            for (k = 3; k > 1 && a.n > g_fit[1][k];) --k;
+    }
+    p.parts = 1 << k;
     p.vecs = vecs(p.parts);
-    const bool hold = fits(p.parts);
+    const bool hold = fits(p.parts, ctas);
     p.shift = 46;
     while (p.shift > 0 && ((int64_t)a.vocab << p.shift) > (1ll << 62)) --p.shift;
     cudaLaunchConfig_t cfg = {};
@@ -851,7 +921,7 @@ mt_status launch_token_sample(const SampleArgs& a, const OpContext& c, cudaStrea
     cfg.attrs = attr;
     cfg.numAttrs = p.parts > 1 ? 2 : 1;
     ++g_kernel_launches;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, cfg.gridDim.x <= (unsigned)c.sm_count ? kernel_of<1>(a.fp32, hold) : kernel_of<2>(a.fp32, hold), p);
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel_of(a.fp32, hold, ctas), p);
     return e == cudaSuccess ? MT_OK : MT_ERR_CUDA;
 }
 

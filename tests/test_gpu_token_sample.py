@@ -101,6 +101,36 @@ def test_rows(n, dtype):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("v", [9000, 40000, 130001])
+@pytest.mark.parametrize("n", [13, 16, 33, 38, 74, 76, 148, 150, 298])
+def test_a_row_does_not_depend_on_the_others(n, v, dtype):
+    """Rows in more or fewer parts, held or not, one CTA an SM or two: the same tokens."""
+    x, u, g = random_logits(n, v, dtype, n + v)
+    kw = arrays(n, dict(temperature=0.9, min_p=0.0))
+    kw["top_p"] = torch.where(torch.rand(n, generator=g, device="cuda") < 0.6, torch.rand(n, generator=g, device="cuda"), 1.0)
+    kw["top_k"] = (torch.rand(n, generator=g, device="cuda") * 300).int()
+    init()
+    ids, logprobs = draw(x, u, **kw)
+    check(x[:3], u[:3].contiguous(), **{k: w[:3].contiguous() for k, w in kw.items()})
+    for i in range(0, n, 7):
+        some = draw(x[i:i + 7], u[i:i + 7].contiguous(), **{k: w[i:i + 7].contiguous() for k, w in kw.items()})
+        assert (ids[i:i + 7] == some[0]).all() and (logprobs[i:i + 7] == some[1]).all()
+
+
+def test_rows_of_half_a_billion():
+    """Sizes in bytes pass 32 bits; many rows that are one (row stride 0)."""
+    v, n = (1 << 29) + 3, 300
+    x = torch.full((1, v), -float("inf"), device="cuda")
+    at = [0, 5, 1 << 28, v - 1]
+    x[0, at] = 0.0
+    u = f32([0.0, 0.2, 0.25, 0.49, 0.5, 0.7, 0.75, 1.0 - 2.0 ** -24] * 38)[:n]
+    init()
+    ids, logprobs = draw(x.expand(n, v), u)
+    assert (ids == np.array([at[int(4 * w)] for w in u.tolist()])).all()
+    assert np.abs(logprobs + math.log(4)).max() <= sample_bound(-math.log(4))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("v", [5, 1001, 30011])
 def test_strides_and_alignment(v, dtype):
     """Rows at any element, and neighbours that must not be read as logits."""
