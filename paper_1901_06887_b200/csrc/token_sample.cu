@@ -16,7 +16,7 @@
 // a row is read once; other rows come from L2 again.
 //
 // Cost.  Many rows: the pass of 64-bit exponentials, 30 cycles for a warp's logits on a scheduler, and the first pass at the memory's rate, one behind the
-// other (512 rows of 128 000 in fp32, 174 us, 4.3 times their bytes).  A mixed batch of 64 rows of 128 000 in bf16 takes 57 us: its rows with a limit go three
+// other (512 rows of 128 000 in fp32, 174 us, 4.3 times their bytes).  A mixed batch of 64 rows of 128 000 in bf16 takes 50 us: its rows with a limit go three
 // times over their part, the histogram's additions to shared memory take as long as the exponentials, and six barriers of the cluster lie between.  One row of
 // 32 000: 13.8 us, these barriers and the dependent steps between them.
 #include "lm_device.cuh"
@@ -28,7 +28,7 @@ namespace {
 constexpr int kThreads = 512, kWarps = kThreads / 32;
 constexpr int kBins = 2 * kThreads;
 constexpr int kFine = 16, kCoarse = kBins / kFine;
-constexpr int kList = kThreads;
+constexpr int kList = kThreads, kSome = 32;
 constexpr int kMaxParts = 8;
 constexpr int kAtOnce = 4;                    // parts whose shared memory is read at once
 static_assert(kBins == 2 * kThreads && kCoarse == 64 && kFine == 16 && kMaxParts <= 8, "");
@@ -761,29 +761,58 @@ __global__ void __launch_bounds__(kThreads, CTAS) token_sample_kernel(const Para
                 const u64 x = parts > 1 ? remote_u64(&s.part_entry[t - first], from) : s.part_entry[t];
                 s.entry[t] = make_ulonglong2(x, by_mass ? wt(unordered((uint32_t)(x >> 32))) : 0);
             }
+            if (t == 0) s.found = 0;
             __syncthreads();
-            // what stands before an entry, counted and weighed by 1 to 32 threads; the last entry kept is the largest at which a limit is reached
-            int each = 1;
-            while (each < 32 && n * each * 2 <= kThreads) each *= 2;
-            const int i = t / each;
-            u64 own = i < n ? s.entry[i].x : ~0ull, mass = 0;
-            uint32_t rank = 0;
+            // Of m entries the last that is kept: the largest at which a limit is reached, or zero; next: the smallest at which none is.  What stands before an entry is counted and
+            // weighed by 1 to 32 threads.
+            auto last_kept = [&](int m, auto entry, u64& next) {
+                int each = 1;
+                while (each < 32 && m * each * 2 <= kThreads) each *= 2;
+                const int i = t / each;
+                const u64 own = i < m ? entry(i) : 0;
+                u64 mass = 0;
+                uint32_t rank = 0;
 #pragma unroll 4
-            for (int j = t & (each - 1); j < n; j += each) {
-                const ulonglong2 o = s.entry[j];
-                if (o.x >= own) { ++rank; mass += o.y; }
+                for (int j = t & (each - 1); j < n; j += each) {
+                    const ulonglong2 o = s.entry[j];
+                    if (o.x >= own) { ++rank; mass += o.y; }
+                }
+                for (int o = each / 2; o; o >>= 1) { rank += __shfl_xor_sync(0xffffffffu, rank, o); mass += __shfl_xor_sync(0xffffffffu, mass, o); }
+                const bool is = (u64)above_count + rank >= (u64)top_k || above_mass + mass >= target;
+                u64 last = i < m && is ? own : 0;
+                next = i < m && !is ? own : ~0ull;
+#pragma unroll
+                for (int o = 16; o; o >>= 1) {
+                    const u64 x = __shfl_xor_sync(0xffffffffu, last, o), y = __shfl_xor_sync(0xffffffffu, next, o);
+                    last = max(last, x);
+                    next = min(next, y);
+                }
+                if (lane == 0) { s.scan[warp] = last; s.warp_sum[warp] = next; }
+                __syncthreads();
+                last = s.scan[lane % kWarps];
+                next = s.warp_sum[lane % kWarps];
+#pragma unroll
+                for (int o = kWarps / 2; o; o >>= 1) {
+                    const u64 x = __shfl_xor_sync(0xffffffffu, last, o), y = __shfl_xor_sync(0xffffffffu, next, o);
+                    last = max(last, x);
+                    next = min(next, y);
+                }
+                __syncthreads();
+                return last;
+            };
+            // A long list: some entries from all over it first, then those between the two of them where the cut lies (18 rows of 128 000 in bf16: 46 -> 38 us).
+            u64 next;
+            if (n <= 3 * kSome) {
+                cut = last_kept(n, [&](int i) { return s.entry[i].x; }, next);
+            } else {
+                cut = last_kept(kSome, [&](int i) { return s.entry[i * n / kSome].x; }, next);
+                u64* const between = reinterpret_cast<u64*>(s.count);              // (nobody reads the bins any more)
+                const u64 x = t < n ? s.entry[t].x : 0;
+                if (x > cut && x < next) between[atomicAdd(&s.found, 1)] = x;
+                __syncthreads();
+                const int m = s.found;
+                if (m > 0) cut = max(cut, last_kept(m, [&](int i) { return between[i]; }, next));
             }
-            for (int o = each / 2; o; o >>= 1) { rank += __shfl_xor_sync(0xffffffffu, rank, o); mass += __shfl_xor_sync(0xffffffffu, mass, o); }
-            if (i >= n || !((u64)above_count + rank >= (u64)top_k || above_mass + mass >= target)) own = 0;
-#pragma unroll
-            for (int o = 16; o; o >>= 1) { const u64 y = __shfl_xor_sync(0xffffffffu, own, o); own = y > own ? y : own; }
-            if (lane == 0) s.scan[warp] = own;
-            __syncthreads();
-            cut = lane < kWarps ? s.scan[lane] : 0;
-#pragma unroll
-            for (int o = kWarps / 2; o; o >>= 1) { const u64 y = __shfl_xor_sync(0xffffffffu, cut, o); cut = y > cut ? y : cut; }
-            cut = __shfl_sync(0xffffffffu, cut, 0);
-            __syncthreads();
         }
     }
 
@@ -886,7 +915,7 @@ mt_status launch_token_sample(const SampleArgs& a, const OpContext& c, cudaStrea
     // Parts: as many as make clusters that all lie beside each other, held, with one CTA an SM: then they spread over the SMs, and a thread has more registers (15 rows of
     // 128 000 in bf16: 22 us in eight parts, 33 in four, 16 rows 50 and 37, for clusters of eight do not fill the SMs; 64 rows of 32 000: 21 in two, 23 in four with two CTAs an
     // SM; 74 rows 23, 27 and 29; 146 rows of 16 000: 20 in one part, 24 in two).  Where that leaves long parts, two CTAs an SM, of different rows, do better, if they fill the SMs
-    // and are held (64 rows of 128 000: 56 us in four parts, 72 in two with one CTA an SM; 33 rows 42 and 46; 18 rows, which do not fill them, 42 and 37).
+    // and are held (before the list was ranked in two steps: 64 rows of 128 000 56 us in four parts, 72 in two with one CTA an SM; 33 rows 42 and 46; 18 rows, which do not fill them, 42 and 37).
     auto most_parts = [&](int ctas) {
         int k = 3;
         while (k >= 0 && !(a.n <= g_fit[ctas - 1][k] && (k == 0 || a.vocab >> k >= kMinPart) && fits(1 << k, ctas))) --k;
