@@ -28,13 +28,14 @@ namespace {
 constexpr int kThreads = 512, kWarps = kThreads / 32;
 constexpr int kBins = 2 * kThreads;
 constexpr int kFine = 16, kCoarse = kBins / kFine;
-constexpr int kList = kThreads, kSome = 32;
+constexpr int kList = 2 * kThreads, kSome = 32;
 constexpr int kMaxParts = 8;
 constexpr int kAtOnce = 4;                    // parts whose shared memory is read at once
+static_assert(kList * 8 <= 3 * kThreads * sizeof(uint2), "the list over the bins");
 static_assert(kBins == 2 * kThreads && kCoarse == 64 && kFine == 16 && kMaxParts <= 8, "");
 constexpr int kMinPart = 2048;                // logits of a part, at least
 constexpr int kShortPart = 16384;             // and of one that takes an SM by itself, rather
-constexpr int held_bytes(int ctas) { return ctas == 1 ? 196608 : 81920; }      // of a part that stays in shared memory, at most, with so many CTAs an SM
+constexpr int held_bytes(int ctas) { return ctas == 1 ? 193792 : 77056; }      // of a part that stays in shared memory, at most, with so many CTAs an SM
 using u64 = unsigned long long;
 
 struct Params {
@@ -46,7 +47,7 @@ struct Params {
 
 struct Shared {
     uint4 edge[3];                            // the row's first and last vector with minus infinity outside it, and nothing but that
-    uint2 count[kThreads], lo[kThreads], hi[kThreads];       // bins 2 t and 2 t + 1: entries, and mass in two words
+    uint2 count[kThreads], lo[kThreads], hi[kThreads];       // bins 2 t and 2 t + 1: entries, and mass in two words; then a part of the list
     ulonglong2 entry[kList];                                 // the list: (ordered logit, rising as the index falls), weight
     u64 part_entry[kList];                                   // this part's share of it
     alignas(16) u64 coarse_mass[kCoarse];     // sixteen bins each
@@ -751,15 +752,18 @@ __global__ void __launch_bounds__(kThreads, CTAS) token_sample_kernel(const Para
         } else if (!none) {                   // a list
             const int n = (int)n_in;
             const int upto = warp_scan(in_part, lane);
-            int from = 0, first = 0;          // entry t: of which part, and that part's first
+#pragma unroll 1
+            for (int i0 = 0; i0 < n; i0 += kThreads) {
+                const int i = i0 + t;
+                int from = 0, first = 0;      // entry i: of which part, and that part's first
 #pragma unroll
-            for (int r = 0; r < kMaxParts - 1; ++r) {
-                const int end = __shfl_sync(0xffffffffu, upto, r);
-                if (r + 1 < parts && t >= end) { from = r + 1; first = end; }
-            }
-            if (t < n) {
-                const u64 x = parts > 1 ? remote_u64(&s.part_entry[t - first], from) : s.part_entry[t];
-                s.entry[t] = make_ulonglong2(x, by_mass ? wt(unordered((uint32_t)(x >> 32))) : 0);
+                for (int r = 0; r < kMaxParts - 1; ++r) {
+                    const int end = __shfl_sync(0xffffffffu, upto, r);
+                    if (r + 1 < parts && i >= end) { from = r + 1; first = end; }
+                }
+                if (i >= n) continue;
+                const u64 x = parts > 1 ? remote_u64(&s.part_entry[i - first], from) : s.part_entry[i];
+                s.entry[i] = make_ulonglong2(x, by_mass ? wt(unordered((uint32_t)(x >> 32))) : 0);
             }
             if (t == 0) s.found = 0;
             __syncthreads();
@@ -768,19 +772,24 @@ __global__ void __launch_bounds__(kThreads, CTAS) token_sample_kernel(const Para
             auto last_kept = [&](int m, auto entry, u64& next) {
                 int each = 1;
                 while (each < 32 && m * each * 2 <= kThreads) each *= 2;
-                const int i = t / each;
-                const u64 own = i < m ? entry(i) : 0;
-                u64 mass = 0;
-                uint32_t rank = 0;
+                u64 last = 0;
+                next = ~0ull;
+#pragma unroll 1
+                for (int i0 = 0; i0 < m; i0 += kThreads / each) {
+                    const int i = i0 + t / each;
+                    const u64 own = i < m ? entry(i) : 0;
+                    u64 mass = 0;
+                    uint32_t rank = 0;
 #pragma unroll 4
-                for (int j = t & (each - 1); j < n; j += each) {
-                    const ulonglong2 o = s.entry[j];
-                    if (o.x >= own) { ++rank; mass += o.y; }
+                    for (int j = t & (each - 1); j < n; j += each) {
+                        const ulonglong2 o = s.entry[j];
+                        if (o.x >= own) { ++rank; mass += o.y; }
+                    }
+                    for (int o = each / 2; o; o >>= 1) { rank += __shfl_xor_sync(0xffffffffu, rank, o); mass += __shfl_xor_sync(0xffffffffu, mass, o); }
+                    const bool is = (u64)above_count + rank >= (u64)top_k || above_mass + mass >= target;
+                    if (i < m && is) last = max(last, own);
+                    if (i < m && !is) next = min(next, own);
                 }
-                for (int o = each / 2; o; o >>= 1) { rank += __shfl_xor_sync(0xffffffffu, rank, o); mass += __shfl_xor_sync(0xffffffffu, mass, o); }
-                const bool is = (u64)above_count + rank >= (u64)top_k || above_mass + mass >= target;
-                u64 last = i < m && is ? own : 0;
-                next = i < m && !is ? own : ~0ull;
 #pragma unroll
                 for (int o = 16; o; o >>= 1) {
                     const u64 x = __shfl_xor_sync(0xffffffffu, last, o), y = __shfl_xor_sync(0xffffffffu, next, o);
@@ -807,8 +816,10 @@ __global__ void __launch_bounds__(kThreads, CTAS) token_sample_kernel(const Para
             } else {
                 cut = last_kept(kSome, [&](int i) { return s.entry[i * n / kSome].x; }, next);
                 u64* const between = reinterpret_cast<u64*>(s.count);              // (nobody reads the bins any more)
-                const u64 x = t < n ? s.entry[t].x : 0;
-                if (x > cut && x < next) between[atomicAdd(&s.found, 1)] = x;
+                for (int i = t; i < n; i += kThreads) {
+                    const u64 x = s.entry[i].x;
+                    if (x > cut && x < next) between[atomicAdd(&s.found, 1)] = x;
+                }
                 __syncthreads();
                 const int m = s.found;
                 if (m > 0) cut = max(cut, last_kept(m, [&](int i) { return between[i]; }, next));

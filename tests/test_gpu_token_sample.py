@@ -117,6 +117,21 @@ def test_a_row_does_not_depend_on_the_others(n, v, dtype):
         assert (ids[i:i + 7] == some[0]).all() and (logprobs[i:i + 7] == some[1]).all()
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("m", [90, 97, 400, 512, 513, 1000, 1024, 1025, 2000])
+def test_many_near_the_cut(m, dtype):
+    """m logits that differ by little (bf16: not at all) and the cut among them."""
+    n, v = 5, 20000
+    x, u, g = random_logits(n, v, dtype, m, spread=0.5)
+    for i in range(n):
+        at = torch.randperm(v, generator=g, device="cuda")[:m]
+        x[i, at] = (9.0 + 1e-4 * torch.rand(m, generator=g, device="cuda")).to(dtype)
+    check(x, u, **arrays(n, dict(top_k=m // 3)))
+    kw = arrays(n, dict(temperature=0.9, top_k=m - 1))
+    kw["top_p"] = torch.rand(n, generator=g, device="cuda")
+    check(x, u, **kw)
+
+
 def test_rows_of_half_a_billion():
     """Sizes in bytes pass 32 bits; many rows that are one (row stride 0)."""
     v, n = (1 << 29) + 3, 300
