@@ -532,22 +532,25 @@ mt_status ensure_resident(const std::vector<int>& ids, const std::vector<int>& r
     std::vector<Load> loads;
     std::vector<int> evicted;
     mt_status result = MT_OK;
+    uint64_t youngest = 0;                       // batch that may have read a victim's bytes
     for (size_t i = 0; i < ids.size(); ++i) {
         HostModel& hm = g.models[ids[i]];
         size_t off = 0;
+        const size_t so_far = evicted.size();
         const WeightCache::Result r = g.cache.acquire(ids[i], hm.block_bytes, tick, &off, &evicted);
+        // (at once: a victim may be one of `ids` itself and come back further on, as used by the batch being prepared)
+        for (size_t e = so_far; e < evicted.size(); ++e)
+            if (g.models[evicted[e]].last_batch > youngest) youngest = g.models[evicted[e]].last_batch;
         if (r == WeightCache::kNoRoom) { result = MT_ERR_OOM; break; }
         if (r == WeightCache::kLoaded) { loads.push_back({ids[i], off}); g.request_misses += reqs[i]; }
         else g.request_hits += reqs[i];
         hm.last_batch = g.batch_no + 1;          // the batch being prepared
     }
-    uint64_t youngest = 0;
     for (int e : evicted) {
         TableUpdate u;
         memset(&u, 0, sizeof u);
         u.id = e; u.alive = 2;
         launch_table_update(u, s);
-        if (g.models[e].last_batch > youngest) youngest = g.models[e].last_batch;
     }
     if (!loads.empty()) {
         if (youngest > g.synced_batch && youngest <= g.batch_no)
