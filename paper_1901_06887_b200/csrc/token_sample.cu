@@ -454,6 +454,7 @@ __global__ void __launch_bounds__(kThreads, CTAS) token_sample_kernel(const Para
     if (temperature == 0.f || min_p > 1.f) { top_k = 1; min_p = 0.f; }
     temperature = temperature == 0.f ? 1.f : fmaxf(temperature, 0x1p-126f);
     if (top_k <= 0 || top_k > a.vocab) top_k = a.vocab;
+    top_p = fmaxf(top_p, 0.f);                // (what is below zero asks for the first entry, as zero does; the histogram's range is made of 1 - top_p)
 
     // --- the maximum
     const double c = 1.4426950408889634074 / (double)temperature;
