@@ -4,8 +4,9 @@
 // keeps a front part, so what passes all of them is a front part too, up to a last entry (key, index).  The drawn token is the first, in index order, at
 // which the kept mass exceeds u times all of it.
 // A border between two tokens must not depend on the order of summing, so weights are whole numbers, w_i 2^s rounded, s = 46 or less where a row of
-// ones would pass 2^62: sums of them are exact in any order.  (A token below 2^-46 of the likeliest has no mass and is never drawn; all mass lost is
-// below 2^-28 of a row of 2^18.)  The exponential is taken in 64 bits: at fp32's 2^-23 one draw in some hundreds would fall on the other side of a border.
+// ones would pass 2^62: sums of them are exact in any order.  (A token below half a unit, 2^-s, of the likeliest has no mass and is never drawn; of a
+// row of V at most V / 2 units are lost or won by rounding: 2^-31 of it for 2^16 logits, 2^-27 for 2^18, 2^-23 for 2^20.)  The exponential is taken in 64 bits:
+// at fp32's 2^-23 one draw in some hundreds would fall on the other side of a border.
 //
 // The last entry kept.  A histogram, count and mass, of the distance to the maximum over the range where the cut can lie: the tokens whose weight is
 // below (1 - p) / V of the largest weigh less than 1 - p together, and the row at least 1.  The bin where a limit is reached is put on a list and ranked by
@@ -505,7 +506,7 @@ __global__ void __launch_bounds__(kThreads, CTAS) token_sample_kernel(const Para
     if (by_count || by_mass) {
         u64 target = ~0ull;                   // mass at which top-p is reached
         float range = (float)p.shift + 2.f;   // in powers of two below the maximum
-        if (by_mass) range = fminf(range, log2f((float)a.vocab / fmaxf(1.f - top_p, 1e-7f)) + 1.f);
+        if (by_mass) range = fminf(range, log2f((float)a.vocab / (1.f - top_p)) + 1.f);
         const float per = fminf((float)wt.c * ((float)(kBins - 1) / range), 3.402823466e38f);
         uint32_t* const counts = reinterpret_cast<uint32_t*>(s.count);
         uint32_t* const los = reinterpret_cast<uint32_t*>(s.lo);
@@ -947,7 +948,7 @@ mt_status launch_token_sample(const SampleArgs& a, const OpContext& c, cudaStrea
     p.vecs = vecs(p.parts);
     const bool hold = fits(p.parts, ctas);
     p.shift = 46;
-    while (p.shift > 0 && ((int64_t)a.vocab << p.shift) > (1ll << 62)) --p.shift;
+    while (a.vocab > 1ll << (62 - p.shift)) --p.shift;          // (a vocabulary below 2^30 leaves 32 at least)
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)((int64_t)a.n * p.parts));
     cfg.blockDim = dim3(kThreads);

@@ -1,4 +1,6 @@
 """mt_token_sample at the ends of what its arguments may be."""
+from fractions import Fraction
+
 import numpy as np
 import pytest
 import torch
@@ -23,3 +25,46 @@ def test_top_p_far_below_zero(p, v, dtype):
     assert (check(x, u, **arrays(n, dict(top_p=p))) == first).all()
     assert (check(x, u, **arrays(n, dict(top_p=p, top_k=3, temperature=0.7))) == first).all()
     assert mt.mt_get_async_status() == (0, -1)
+
+
+LARGE = [65536, 131071, 131072, 152064, 262144, 262145, 300000, 1 << 20]
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("v", LARGE)
+@pytest.mark.parametrize("n", [1, 5, 300])
+def test_equal_logits_of_large_vocabularies(n, v, dtype):
+    """Every token weighs as much as the likeliest: the row's mass is the largest there is.  Weights and sums of them are exact, so are the tokens."""
+    init()
+    x = torch.full((1, v), 1.25, dtype=dtype, device="cuda").expand(n, v)
+    u = (torch.arange(n, device="cuda") + 0.75) / n
+    for p in (1.0, 0.5, 0.777, 0.99):
+        share = Fraction(float(np.float32(p)))
+        kept = -(-share.numerator * v // share.denominator)
+        ids, logprobs = draw(x, u, **arrays(n, dict(top_p=p)))
+        assert ids.tolist() == [int(Fraction(w) * kept) for w in u.tolist()], p
+        assert np.abs(logprobs + np.log(kept)).max() <= sample_bound(np.log(kept)), p
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("v", LARGE)
+def test_flat_rows_of_large_vocabularies(v, dtype):
+    """A high temperature: masses near the largest, weights of all sizes.  (The sum is off by half a unit a weight, 2^-43 of a weight of most: far less than the bound.)"""
+    n = 3
+    x, u, _ = random_logits(n, v, dtype, v)
+    for kw in (dict(), dict(top_p=0.9), dict(top_k=v // 2), dict(top_k=v // 3, top_p=0.6, min_p=0.3)):
+        check(x, u, **arrays(n, dict(temperature=10.0, **kw)))
+
+
+@pytest.mark.parametrize("v", [262144, 300000])
+def test_rows_of_large_vocabularies_do_not_depend_on_the_others(v):
+    """Held in parts, or read twice: the same tokens."""
+    init()
+    n = 160
+    x, u, g = random_logits(n, v, BF16, 5)
+    kw = arrays(n, dict(temperature=6.0))
+    kw["top_p"] = torch.where(torch.rand(n, generator=g, device="cuda") < 0.6, torch.rand(n, generator=g, device="cuda"), 1.0)
+    ids, logprobs = draw(x, u, **kw)
+    for i in range(0, n, 37):
+        some = draw(x[i:i + 3], u[i:i + 3].contiguous(), **{k: w[i:i + 3].contiguous() for k, w in kw.items()})
+        assert (ids[i:i + 3] == some[0]).all() and (logprobs[i:i + 3] == some[1]).all()
