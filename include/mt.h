@@ -184,11 +184,16 @@ mt_status mt_get_cache_stats(mt_cache_stats* out, int32_t reset);
 
 /* The cache's policy by itself - first-fit arena, least-recently-used eviction on a clock the caller makes up - for
  * tests without a GPU.  access: result 0 = hit, 1 = placed (ids evicted to make room in evicted_out, at most
- * evicted_cap of them, their number in *n_evicted_out), -1 = does not fit beside the blocks touched at `tick`. */
+ * evicted_cap of them, their number in *n_evicted_out), -1 = does not fit beside the blocks touched at `tick`.
+ * read: the batch being prepared reads a resident block; batch: it has been enqueued (they count from 1), or, with finished != 0, all of them are
+ * known to have finished; wait: the batch that what is written into the arena after the last access has to wait for (0: none). */
 mt_status mt_cache_sim_create(size_t capacity_bytes, void** sim_out);
 mt_status mt_cache_sim_access(void* sim, int32_t id, size_t bytes, uint64_t tick, int32_t* result_out, int64_t* offset_out,
                               int32_t* evicted_out, int32_t evicted_cap, int32_t* n_evicted_out);
 mt_status mt_cache_sim_release(void* sim, int32_t id);
+mt_status mt_cache_sim_read(void* sim, int32_t id);
+mt_status mt_cache_sim_batch(void* sim, int32_t finished);
+mt_status mt_cache_sim_wait(void* sim, uint64_t* batch_out);
 mt_status mt_cache_sim_stats(void* sim, mt_cache_stats* out);
 mt_status mt_cache_sim_destroy(void* sim);
 

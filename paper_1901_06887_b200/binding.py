@@ -25,7 +25,7 @@ EXPORTS = ["mt_init", "mt_shutdown", "mt_register_model", "mt_infer", "mt_infer_
            "mt_get_async_status", "mt_status_string", "mt_debug_last_bucketing", "mt_set_kernel_timing",
            "mt_get_kernel_times", "mt_bucket_noalloc", "mt_debug_wait_timeout", "mt_debug_launch_count", "mt_debug_set_option", "mt_debug_empty_launches", "mt_debug_item_cost",
            "mt_debug_schedule_balance", "mt_set_cache_bytes", "mt_prefetch", "mt_get_cache_stats", "mt_cache_sim_create",
-           "mt_cache_sim_access", "mt_cache_sim_release", "mt_cache_sim_stats", "mt_cache_sim_destroy", "mt_output_elems", "mt_input_elems",
+           "mt_cache_sim_access", "mt_cache_sim_release", "mt_cache_sim_read", "mt_cache_sim_batch", "mt_cache_sim_wait", "mt_cache_sim_stats", "mt_cache_sim_destroy", "mt_output_elems", "mt_input_elems",
            "mt_prompt_attention", "mt_kv_append", "mt_kv_read", "mt_kv_attention", "mt_quant_packed_bytes", "mt_quant_pack",
            "mt_quant_linear", "mt_token_logprobs", "mt_cross_attention", "mt_rotate", "mt_kv_reserve", "mt_kv_fork", "mt_kv_release",
            "mt_kv_compact", "mt_kv_copy", "mt_token_sample"]
@@ -113,6 +113,9 @@ def lib() -> ctypes.CDLL:
         l.mt_cache_sim_access.argtypes = [vp, i32, ctypes.c_size_t, ctypes.c_uint64, ctypes.POINTER(i32),
                                           ctypes.POINTER(ctypes.c_int64), ctypes.POINTER(i32), i32, ctypes.POINTER(i32)]
         l.mt_cache_sim_release.argtypes = [vp, i32]
+        l.mt_cache_sim_read.argtypes = [vp, i32]
+        l.mt_cache_sim_batch.argtypes = [vp, i32]
+        l.mt_cache_sim_wait.argtypes = [vp, ctypes.POINTER(ctypes.c_uint64)]
         l.mt_cache_sim_stats.argtypes = [vp, ctypes.POINTER(CacheStats)]
         l.mt_cache_sim_destroy.argtypes = [vp]
         l.mt_debug_item_cost.argtypes = [i32, i32, i32, ctypes.POINTER(ctypes.c_double)]
@@ -313,6 +316,23 @@ def mt_cache_sim_access(sim, model_id: int, nbytes: int, tick: int):
 
 def mt_cache_sim_release(sim, model_id: int) -> None:
     _check(lib().mt_cache_sim_release(sim, int(model_id)), "mt_cache_sim_release")
+
+
+def mt_cache_sim_read(sim, model_id: int) -> None:
+    """The batch being prepared reads a resident block."""
+    _check(lib().mt_cache_sim_read(sim, int(model_id)), "mt_cache_sim_read")
+
+
+def mt_cache_sim_batch(sim, finished: bool = False) -> None:
+    """The batch being prepared has been enqueued; or all of them are known to have finished."""
+    _check(lib().mt_cache_sim_batch(sim, int(bool(finished))), "mt_cache_sim_batch")
+
+
+def mt_cache_sim_wait(sim) -> int:
+    """The batch that what is written into the arena after the last access has to wait for (0: none)."""
+    b = ctypes.c_uint64(0)
+    _check(lib().mt_cache_sim_wait(sim, ctypes.byref(b)), "mt_cache_sim_wait")
+    return int(b.value)
 
 
 def mt_cache_sim_stats(sim) -> dict:

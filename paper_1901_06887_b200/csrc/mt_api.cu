@@ -38,7 +38,6 @@ struct HostModel {
     size_t block_bytes = 0;
     void* host_image = nullptr;
     std::vector<size_t> w_off, b_off;      // per layer: offsets of weights and bias inside the block
-    uint64_t last_batch = 0;               // number of the last batch that may have read the block
     cudaEvent_t ready = nullptr;           // asynchronous registration: the block's copies and re-layout have finished
 };
 
@@ -165,8 +164,6 @@ struct Ctx {
     uint8_t* arena = nullptr;
     WeightCache cache;
     cudaStream_t load_stream = nullptr;
-    uint64_t batch_no = 0;                              // batches enqueued so far (with the cache on)
-    uint64_t synced_batch = 0;                          // batches up to this one are known to have finished
     uint64_t cache_tick = 0;                            // logical clock of the eviction policy
     static constexpr int kBatchEvents = 8;
     cudaEvent_t batch_done[kBatchEvents] = {nullptr};   // batch b's kernels have finished: batch_done[b % kBatchEvents]
@@ -532,19 +529,15 @@ mt_status ensure_resident(const std::vector<int>& ids, const std::vector<int>& r
     std::vector<Load> loads;
     std::vector<int> evicted;
     mt_status result = MT_OK;
-    uint64_t youngest = 0;                       // batch that may have read a victim's bytes
+    uint64_t last_reader = 0;                    // batch that may have read a victim's bytes
     for (size_t i = 0; i < ids.size(); ++i) {
         HostModel& hm = g.models[ids[i]];
         size_t off = 0;
-        const size_t so_far = evicted.size();
-        const WeightCache::Result r = g.cache.acquire(ids[i], hm.block_bytes, tick, &off, &evicted);
-        // (at once: a victim may be one of `ids` itself and come back further on, as used by the batch being prepared)
-        for (size_t e = so_far; e < evicted.size(); ++e)
-            if (g.models[evicted[e]].last_batch > youngest) youngest = g.models[evicted[e]].last_batch;
+        const WeightCache::Result r = g.cache.acquire(ids[i], hm.block_bytes, tick, &off, &evicted, nullptr, &last_reader);
         if (r == WeightCache::kNoRoom) { result = MT_ERR_OOM; break; }
         if (r == WeightCache::kLoaded) { loads.push_back({ids[i], off}); g.request_misses += reqs[i]; }
         else g.request_hits += reqs[i];
-        hm.last_batch = g.batch_no + 1;          // the batch being prepared
+        g.cache.reads(ids[i]);
     }
     for (int e : evicted) {
         TableUpdate u;
@@ -553,8 +546,8 @@ mt_status ensure_resident(const std::vector<int>& ids, const std::vector<int>& r
         launch_table_update(u, s);
     }
     if (!loads.empty()) {
-        if (youngest > g.synced_batch && youngest <= g.batch_no)
-            CU_OK(cudaStreamWaitEvent(g.load_stream, g.batch_done[youngest % Ctx::kBatchEvents], 0));
+        if (g.cache.in_flight(last_reader))
+            CU_OK(cudaStreamWaitEvent(g.load_stream, g.batch_done[last_reader % Ctx::kBatchEvents], 0));
         for (const Load& l : loads) {
             const HostModel& hm = g.models[l.id];
             CU_OK(cudaMemcpyAsync(g.arena + l.off, hm.host_image, hm.block_bytes, cudaMemcpyHostToDevice, g.load_stream));
@@ -584,19 +577,17 @@ void tenant_set_of(const int32_t* ids_host, int n, std::vector<int>* ids, std::v
 }
 
 // Book-keeping around one batch when the cache is on: the batch number is the clock of "who may still be reading
-// which block"; a batch whose ids live on the device may read any resident block.
+// which block" (see WeightCache); a batch whose ids live on the device may read any resident block.
 void cache_begin_batch(bool ids_unknown) {
     if (!g.cache_bytes) return;
     if (ids_unknown) {
         g.cache.touch_all(++g.cache_tick);
-        for (int t = 0; t < g.T; ++t)
-            if (g.models[t].alive && g.cache.resident(t)) g.models[t].last_batch = g.batch_no + 1;
+        g.cache.reads_all();
     }
 }
 mt_status cache_end_batch(cudaStream_t s) {
     if (!g.cache_bytes) return MT_OK;
-    g.batch_no += 1;
-    CU_OK(cudaEventRecord(g.batch_done[g.batch_no % Ctx::kBatchEvents], s));
+    CU_OK(cudaEventRecord(g.batch_done[g.cache.enqueued() % Ctx::kBatchEvents], s));
     return MT_OK;
 }
 
@@ -1053,7 +1044,6 @@ mt_status adopt_model(int id, const std::vector<HostLayer>& hl, uint8_t* block, 
     hm.host_image = host_image;
     hm.w_off = w_off;
     hm.b_off = b_off;
-    hm.last_batch = 0;
     if (hm.ready && hm.ready != ready) cudaEventDestroy(hm.ready);
     hm.ready = ready;
     g.live += 1;
@@ -1099,18 +1089,15 @@ mt_status register_async(const mt_layer_desc* layers, const std::vector<HostLaye
     std::vector<int> evicted;
     if (g.cache_bytes) {
         size_t off = 0;
-        const WeightCache::Result got = g.cache.acquire(id, total, ++g.cache_tick, &off, &evicted);
+        uint64_t last_reader = 0;
+        const WeightCache::Result got = g.cache.acquire(id, total, ++g.cache_tick, &off, &evicted, nullptr, &last_reader);
         block = g.arena + off;
         // the victims' bytes may still be read by batches in flight; their table entries flip at the next flush
         // (also when no room could be made in the end: what was evicted on the way stays evicted)
-        uint64_t youngest = 0;
-        for (int v : evicted) {
-            g.pending_ops.push_back({v, 2});
-            if (g.models[v].last_batch > youngest) youngest = g.models[v].last_batch;
-        }
+        for (int v : evicted) g.pending_ops.push_back({v, 2});
         if (got == WeightCache::kNoRoom) return MT_ERR_OOM;
-        if (youngest > g.synced_batch && youngest <= g.batch_no)
-            CU_OK(cudaStreamWaitEvent(g.load_stream, g.batch_done[youngest % Ctx::kBatchEvents], 0));
+        if (g.cache.in_flight(last_reader))
+            CU_OK(cudaStreamWaitEvent(g.load_stream, g.batch_done[last_reader % Ctx::kBatchEvents], 0));
     } else {
         CU_OK(cudaMalloc(&block, total));
     }
@@ -1237,7 +1224,7 @@ mt_status mt_shutdown(void) {
     for (cudaEvent_t& ev : g.batch_done)
         if (ev) { cudaEventDestroy(ev); ev = nullptr; }
     if (g.loads_done) { cudaEventDestroy(g.loads_done); g.loads_done = nullptr; }
-    g.batch_no = g.synced_batch = g.cache_tick = 0;
+    g.cache_tick = 0;
     g.request_hits = g.request_misses = 0;
     free_workspace();
     cudaFree(g.d_models); g.d_models = nullptr;
@@ -1319,7 +1306,7 @@ mt_status mt_register_model(const mt_layer_desc* layers, int32_t n_layers, int32
         size_t off = 0;
         const WeightCache::Result got = g.cache.acquire(id, total, ++g.cache_tick, &off, &evicted);
         CU_OK(cudaDeviceSynchronize());
-        g.synced_batch = g.batch_no;
+        g.cache.finished();
         for (int v : evicted) {     // also when no room could be made in the end: what was evicted on the way stays evicted
             const int32_t two = 2;
             CU_OK(cudaMemcpy(g.d_brief + v, &two, sizeof two, cudaMemcpyHostToDevice));
@@ -1408,7 +1395,7 @@ mt_status mt_release(int32_t model_id) {
     const int32_t dead = 0;
     CU_OK(cudaMemcpy(g.d_brief + model_id, &dead, sizeof dead, cudaMemcpyHostToDevice));
     HostModel& hm = g.models[model_id];
-    g.synced_batch = g.batch_no;
+    g.cache.finished();
     if (g.cache_bytes) g.cache.release(model_id);
     if (hm.host_image) { cudaFreeHost(hm.host_image); hm.host_image = nullptr; }
     cudaFree(hm.dev_block);
@@ -1566,7 +1553,7 @@ mt_status mt_set_cache_bytes(size_t device_bytes) {
     if (!g.loads_done) CU_OK(cudaEventCreateWithFlags(&g.loads_done, cudaEventDisableTiming));
     g.cache.reset(cap);
     g.cache_bytes = cap;
-    g.batch_no = g.synced_batch = g.cache_tick = 0;
+    g.cache_tick = 0;
     g.request_hits = g.request_misses = 0;
     return MT_OK;
 }
@@ -1602,7 +1589,10 @@ mt_status mt_get_cache_stats(mt_cache_stats* out, int32_t reset) {
 }
 
 // The eviction policy by itself, on a made-up clock (host code only: usable without a GPU).
-struct CacheSim { mt::WeightCache c; };
+struct CacheSim {
+    mt::WeightCache c;
+    uint64_t last_reader = 0;                    // of what the last access evicted
+};
 mt_status mt_cache_sim_create(size_t capacity_bytes, void** sim_out) {
     if (!sim_out) return MT_ERR_INVALID_ARG;
     CacheSim* s = new CacheSim();
@@ -1615,7 +1605,9 @@ mt_status mt_cache_sim_access(void* sim, int32_t id, size_t bytes, uint64_t tick
     if (!sim || !result_out) return MT_ERR_INVALID_ARG;
     std::vector<int> ev;
     size_t off = 0;
-    const mt::WeightCache::Result r = static_cast<CacheSim*>(sim)->c.acquire(id, bytes, tick, &off, &ev);
+    CacheSim& s = *static_cast<CacheSim*>(sim);
+    s.last_reader = 0;
+    const mt::WeightCache::Result r = s.c.acquire(id, bytes, tick, &off, &ev, nullptr, &s.last_reader);
     *result_out = (int32_t)r;
     if (offset_out) *offset_out = r == mt::WeightCache::kNoRoom ? -1 : (int64_t)off;
     if (n_evicted_out) *n_evicted_out = (int32_t)ev.size();
@@ -1625,6 +1617,23 @@ mt_status mt_cache_sim_access(void* sim, int32_t id, size_t bytes, uint64_t tick
 mt_status mt_cache_sim_release(void* sim, int32_t id) {
     if (!sim) return MT_ERR_INVALID_ARG;
     static_cast<CacheSim*>(sim)->c.release(id);
+    return MT_OK;
+}
+mt_status mt_cache_sim_read(void* sim, int32_t id) {
+    if (!sim || !static_cast<CacheSim*>(sim)->c.resident(id)) return MT_ERR_INVALID_ARG;
+    static_cast<CacheSim*>(sim)->c.reads(id);
+    return MT_OK;
+}
+mt_status mt_cache_sim_batch(void* sim, int32_t finished) {
+    if (!sim) return MT_ERR_INVALID_ARG;
+    if (finished) static_cast<CacheSim*>(sim)->c.finished();
+    else static_cast<CacheSim*>(sim)->c.enqueued();
+    return MT_OK;
+}
+mt_status mt_cache_sim_wait(void* sim, uint64_t* batch_out) {
+    if (!sim || !batch_out) return MT_ERR_INVALID_ARG;
+    CacheSim& s = *static_cast<CacheSim*>(sim);
+    *batch_out = s.c.in_flight(s.last_reader) ? s.last_reader : 0;
     return MT_OK;
 }
 mt_status mt_cache_sim_stats(void* sim, mt_cache_stats* out) {

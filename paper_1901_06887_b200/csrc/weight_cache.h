@@ -5,6 +5,9 @@
 // memory the PCIe link stops being the bottleneck.  This class is that cache's bookkeeping: a fixed arena of device
 // bytes, a first-fit free list with coalescing, and least-recently-used eviction driven by a logical clock that the
 // caller supplies (one tick per batch), so the policy can be tested with a made-up clock and no GPU.
+//
+// It also knows which batch may have read a block last.  Batches are numbered as they are enqueued, and finish in that order; what is
+// written over an evicted block has to wait for its last reader.
 #pragma once
 
 #include <stddef.h>
@@ -21,6 +24,7 @@ public:
     struct Entry {
         size_t off = 0, size = 0;
         uint64_t last_use = 0;
+        uint64_t last_batch = 0;             // that may have read it, or is to be enqueued next and will
     };
     struct Stats {
         uint64_t hits = 0, misses = 0, evictions = 0, bytes_loaded = 0;
@@ -35,6 +39,7 @@ public:
         live_.clear();
         stats_ = Stats();
         resident_bytes_ = 0;
+        batches_ = finished_ = 0;
     }
     size_t capacity() const { return capacity_; }
     size_t resident_bytes() const { return resident_bytes_; }
@@ -46,13 +51,25 @@ public:
         return it == live_.end() ? nullptr : &it->second;
     }
 
+    // The batch that is being prepared reads block `id` / any resident block.
+    void reads(int id) { live_[id].last_batch = batches_ + 1; }
+    void reads_all() {
+        for (auto& kv : live_) kv.second.last_batch = batches_ + 1;
+    }
+    // It has been enqueued: its number.
+    uint64_t enqueued() { return ++batches_; }
+    // All batches so far are known to have finished.
+    void finished() { finished_ = batches_; }
+    bool in_flight(uint64_t batch) const { return batch > finished_; }
+
     // Make block `id` of `size` bytes resident at time `tick`.  A resident block is a hit (its clock is refreshed).
     // Otherwise room is made by evicting least-recently-used blocks whose last use is OLDER than `tick` - blocks
     // touched at `tick` itself belong to the batch being prepared and stay - and the ids evicted are appended to
     // *evicted (each with the time of its last use in *evicted_last_use, when given).  kNoRoom: the block does not
-    // fit beside what the current tick holds (blocks evicted on the way stay evicted).
+    // fit beside what the current tick holds (blocks evicted on the way stay evicted).  *last_reader is raised to the youngest enqueued batch
+    // that may have read a block evicted (at least that: a batch that a block was made ready for may never have been enqueued).
     Result acquire(int id, size_t size, uint64_t tick, size_t* off_out, std::vector<int>* evicted,
-                   std::vector<uint64_t>* evicted_last_use = nullptr) {
+                   std::vector<uint64_t>* evicted_last_use = nullptr, uint64_t* last_reader = nullptr) {
         auto it = live_.find(id);
         if (it != live_.end()) {
             it->second.last_use = tick;
@@ -74,6 +91,7 @@ public:
             if (victim < 0) return kNoRoom;
             if (evicted) evicted->push_back(victim);
             if (evicted_last_use) evicted_last_use->push_back(oldest);
+            if (last_reader) *last_reader = std::max(*last_reader, std::min(live_[victim].last_batch, batches_));
             drop(victim);
             ++stats_.evictions;
         }
@@ -141,6 +159,7 @@ private:
     }
 
     size_t capacity_ = 0, align_ = 1024, resident_bytes_ = 0;
+    uint64_t batches_ = 0, finished_ = 0;
     std::map<size_t, size_t> free_;        // offset -> length
     std::map<int, Entry> live_;
     Stats stats_;
