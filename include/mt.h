@@ -186,7 +186,7 @@ mt_status mt_get_cache_stats(mt_cache_stats* out, int32_t reset);
  * tests without a GPU.  access: result 0 = hit, 1 = placed (ids evicted to make room in evicted_out, at most
  * evicted_cap of them, their number in *n_evicted_out), -1 = does not fit beside the blocks touched at `tick`.
  * read: the batch being prepared reads a resident block; batch: it has been enqueued (they count from 1), or, with finished != 0, all of them are
- * known to have finished; wait: the batch that what is written into the arena after the last access has to wait for (0: none). */
+ * known to have finished; wait: the batch that what is now written into the arena has to wait for (0: none; asking is waiting). */
 mt_status mt_cache_sim_create(size_t capacity_bytes, void** sim_out);
 mt_status mt_cache_sim_access(void* sim, int32_t id, size_t bytes, uint64_t tick, int32_t* result_out, int64_t* offset_out,
                               int32_t* evicted_out, int32_t evicted_cap, int32_t* n_evicted_out);

@@ -329,7 +329,7 @@ def mt_cache_sim_batch(sim, finished: bool = False) -> None:
 
 
 def mt_cache_sim_wait(sim) -> int:
-    """The batch that what is written into the arena after the last access has to wait for (0: none)."""
+    """The batch that what is now written into the arena has to wait for (0: none); asking is waiting."""
     b = ctypes.c_uint64(0)
     _check(lib().mt_cache_sim_wait(sim, ctypes.byref(b)), "mt_cache_sim_wait")
     return int(b.value)

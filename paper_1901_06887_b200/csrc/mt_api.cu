@@ -516,7 +516,7 @@ mt_status flush_tables(cudaStream_t s) {
 // requests of ids[i] in the batch, for the request-level hit count).  Blocks that are missing are copied from their
 // pinned host images on the load stream, into free arena space or over least-recently-used blocks; `s` waits for the
 // copies, then the device tables are switched by small kernels on `s`.  A victim's bytes may still be read by
-// batches in flight, so the copies wait for the youngest batch that could have used one.  MT_ERR_OOM: the set does
+// batches in flight, so the copies (this call's, or those of a later call that takes the bytes) wait for the youngest batch that could have used one.  MT_ERR_OOM: the set does
 // not fit the cache (nothing of this batch has been enqueued; tenants evicted on the way stay evicted).
 mt_status ensure_resident(const std::vector<int>& ids, const std::vector<int>& reqs, cudaStream_t s) {
     if (!g.cache_bytes || ids.empty()) return MT_OK;
@@ -529,11 +529,10 @@ mt_status ensure_resident(const std::vector<int>& ids, const std::vector<int>& r
     std::vector<Load> loads;
     std::vector<int> evicted;
     mt_status result = MT_OK;
-    uint64_t last_reader = 0;                    // batch that may have read a victim's bytes
     for (size_t i = 0; i < ids.size(); ++i) {
         HostModel& hm = g.models[ids[i]];
         size_t off = 0;
-        const WeightCache::Result r = g.cache.acquire(ids[i], hm.block_bytes, tick, &off, &evicted, nullptr, &last_reader);
+        const WeightCache::Result r = g.cache.acquire(ids[i], hm.block_bytes, tick, &off, &evicted);
         if (r == WeightCache::kNoRoom) { result = MT_ERR_OOM; break; }
         if (r == WeightCache::kLoaded) { loads.push_back({ids[i], off}); g.request_misses += reqs[i]; }
         else g.request_hits += reqs[i];
@@ -546,8 +545,8 @@ mt_status ensure_resident(const std::vector<int>& ids, const std::vector<int>& r
         launch_table_update(u, s);
     }
     if (!loads.empty()) {
-        if (g.cache.in_flight(last_reader))
-            CU_OK(cudaStreamWaitEvent(g.load_stream, g.batch_done[last_reader % Ctx::kBatchEvents], 0));
+        if (const uint64_t batch = g.cache.wait_for())
+            CU_OK(cudaStreamWaitEvent(g.load_stream, g.batch_done[batch % Ctx::kBatchEvents], 0));
         for (const Load& l : loads) {
             const HostModel& hm = g.models[l.id];
             CU_OK(cudaMemcpyAsync(g.arena + l.off, hm.host_image, hm.block_bytes, cudaMemcpyHostToDevice, g.load_stream));
@@ -1089,15 +1088,14 @@ mt_status register_async(const mt_layer_desc* layers, const std::vector<HostLaye
     std::vector<int> evicted;
     if (g.cache_bytes) {
         size_t off = 0;
-        uint64_t last_reader = 0;
-        const WeightCache::Result got = g.cache.acquire(id, total, ++g.cache_tick, &off, &evicted, nullptr, &last_reader);
+        const WeightCache::Result got = g.cache.acquire(id, total, ++g.cache_tick, &off, &evicted);
         block = g.arena + off;
         // the victims' bytes may still be read by batches in flight; their table entries flip at the next flush
         // (also when no room could be made in the end: what was evicted on the way stays evicted)
         for (int v : evicted) g.pending_ops.push_back({v, 2});
         if (got == WeightCache::kNoRoom) return MT_ERR_OOM;
-        if (g.cache.in_flight(last_reader))
-            CU_OK(cudaStreamWaitEvent(g.load_stream, g.batch_done[last_reader % Ctx::kBatchEvents], 0));
+        if (const uint64_t batch = g.cache.wait_for())
+            CU_OK(cudaStreamWaitEvent(g.load_stream, g.batch_done[batch % Ctx::kBatchEvents], 0));
     } else {
         CU_OK(cudaMalloc(&block, total));
     }
@@ -1589,10 +1587,7 @@ mt_status mt_get_cache_stats(mt_cache_stats* out, int32_t reset) {
 }
 
 // The eviction policy by itself, on a made-up clock (host code only: usable without a GPU).
-struct CacheSim {
-    mt::WeightCache c;
-    uint64_t last_reader = 0;                    // of what the last access evicted
-};
+struct CacheSim { mt::WeightCache c; };
 mt_status mt_cache_sim_create(size_t capacity_bytes, void** sim_out) {
     if (!sim_out) return MT_ERR_INVALID_ARG;
     CacheSim* s = new CacheSim();
@@ -1605,9 +1600,7 @@ mt_status mt_cache_sim_access(void* sim, int32_t id, size_t bytes, uint64_t tick
     if (!sim || !result_out) return MT_ERR_INVALID_ARG;
     std::vector<int> ev;
     size_t off = 0;
-    CacheSim& s = *static_cast<CacheSim*>(sim);
-    s.last_reader = 0;
-    const mt::WeightCache::Result r = s.c.acquire(id, bytes, tick, &off, &ev, nullptr, &s.last_reader);
+    const mt::WeightCache::Result r = static_cast<CacheSim*>(sim)->c.acquire(id, bytes, tick, &off, &ev);
     *result_out = (int32_t)r;
     if (offset_out) *offset_out = r == mt::WeightCache::kNoRoom ? -1 : (int64_t)off;
     if (n_evicted_out) *n_evicted_out = (int32_t)ev.size();
@@ -1632,8 +1625,7 @@ mt_status mt_cache_sim_batch(void* sim, int32_t finished) {
 }
 mt_status mt_cache_sim_wait(void* sim, uint64_t* batch_out) {
     if (!sim || !batch_out) return MT_ERR_INVALID_ARG;
-    CacheSim& s = *static_cast<CacheSim*>(sim);
-    *batch_out = s.c.in_flight(s.last_reader) ? s.last_reader : 0;
+    *batch_out = static_cast<CacheSim*>(sim)->c.wait_for();
     return MT_OK;
 }
 mt_status mt_cache_sim_stats(void* sim, mt_cache_stats* out) {

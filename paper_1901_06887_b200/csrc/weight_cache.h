@@ -7,7 +7,8 @@
 // caller supplies (one tick per batch), so the policy can be tested with a made-up clock and no GPU.
 //
 // It also knows which batch may have read a block last.  Batches are numbered as they are enqueued, and finish in that order; what is
-// written over an evicted block has to wait for its last reader.
+// written over an evicted block has to wait for its last reader.  Bytes that are free again may be taken by a later call, so the wait is owed
+// until something is written, whichever call evicted.
 #pragma once
 
 #include <stddef.h>
@@ -39,7 +40,7 @@ public:
         live_.clear();
         stats_ = Stats();
         resident_bytes_ = 0;
-        batches_ = finished_ = 0;
+        batches_ = finished_ = owed_ = 0;
     }
     size_t capacity() const { return capacity_; }
     size_t resident_bytes() const { return resident_bytes_; }
@@ -60,16 +61,21 @@ public:
     uint64_t enqueued() { return ++batches_; }
     // All batches so far are known to have finished.
     void finished() { finished_ = batches_; }
-    bool in_flight(uint64_t batch) const { return batch > finished_; }
+    // The caller is about to write into the arena: the batch that has to finish before (0: none).  Asking is waiting.
+    uint64_t wait_for() {
+        const uint64_t batch = owed_ > finished_ ? owed_ : 0;
+        owed_ = 0;
+        return batch;
+    }
 
     // Make block `id` of `size` bytes resident at time `tick`.  A resident block is a hit (its clock is refreshed).
     // Otherwise room is made by evicting least-recently-used blocks whose last use is OLDER than `tick` - blocks
     // touched at `tick` itself belong to the batch being prepared and stay - and the ids evicted are appended to
     // *evicted (each with the time of its last use in *evicted_last_use, when given).  kNoRoom: the block does not
-    // fit beside what the current tick holds (blocks evicted on the way stay evicted).  *last_reader is raised to the youngest enqueued batch
-    // that may have read a block evicted (at least that: a batch that a block was made ready for may never have been enqueued).
+    // fit beside what the current tick holds (blocks evicted on the way stay evicted).  What is owed for a block evicted is the
+    // youngest enqueued batch that may have read it (at most that: the batch that a block was made ready for may never have been enqueued).
     Result acquire(int id, size_t size, uint64_t tick, size_t* off_out, std::vector<int>* evicted,
-                   std::vector<uint64_t>* evicted_last_use = nullptr, uint64_t* last_reader = nullptr) {
+                   std::vector<uint64_t>* evicted_last_use = nullptr) {
         auto it = live_.find(id);
         if (it != live_.end()) {
             it->second.last_use = tick;
@@ -91,7 +97,7 @@ public:
             if (victim < 0) return kNoRoom;
             if (evicted) evicted->push_back(victim);
             if (evicted_last_use) evicted_last_use->push_back(oldest);
-            if (last_reader) *last_reader = std::max(*last_reader, std::min(live_[victim].last_batch, batches_));
+            owed_ = std::max(owed_, std::min(live_[victim].last_batch, batches_));
             drop(victim);
             ++stats_.evictions;
         }
@@ -159,7 +165,7 @@ private:
     }
 
     size_t capacity_ = 0, align_ = 1024, resident_bytes_ = 0;
-    uint64_t batches_ = 0, finished_ = 0;
+    uint64_t batches_ = 0, finished_ = 0, owed_ = 0;
     std::map<size_t, size_t> free_;        // offset -> length
     std::map<int, Entry> live_;
     Stats stats_;

@@ -76,3 +76,33 @@ def test_what_is_not_resident_is_not_read(w):
     with pytest.raises(mt.MtError) as e:
         mt.mt_cache_sim_read(w.sim, 7)
     assert e.value.code == 1
+
+
+def test_a_wait_is_owed_until_something_is_written(w):
+    """A call displaces a block, then finds no room after all and writes nothing; the bytes go to a later call, which displaces nobody."""
+    w.batch(0, 1)                                    # batch 1
+    w.batch(1)                                       # batch 2
+    assert w.prepare(1, 2, 3) == [(0, []), (1, [0]), (-1, [])]
+    mt.mt_cache_sim_release(w.sim, 2)                # (its copy never began)
+    assert w.prepare(4) == [(1, [])]
+    assert w.wait() == 1
+    assert w.wait() == 0                             # what has been waited for is not waited for again
+
+
+def test_a_block_too_large_after_all(w):
+    """Everything is displaced on the way, and still no room: no load of that call, but of the next ones."""
+    w.batch(0)
+    w.batch(1)                                       # batch 2
+    assert w.prepare(1) == [(0, [])]
+    w.tick += 1
+    mt.mt_cache_sim_access(w.sim, 1, 4 * KB, w.tick)                                     # block 1 is of the call that is prepared
+    assert mt.mt_cache_sim_access(w.sim, 2, 8 * KB, w.tick)[::2] == (-1, [0])
+    assert w.prepare(3) == [(1, [])] and w.wait() == 1
+    assert w.prepare(4)[0][1] == [1] and w.wait() == 2
+
+
+def test_a_victim_that_comes_back_in_the_same_call(w):
+    w.batch(0, 1)                                    # batch 1
+    w.batch(1)                                       # batch 2: block 0 is the oldest
+    assert w.prepare(2, 0) == [(1, [0]), (1, [1])]   # 0 goes, and comes back over 1
+    assert w.wait() == 2
