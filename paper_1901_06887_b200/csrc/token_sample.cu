@@ -215,19 +215,19 @@ __device__ __forceinline__ void by_fours(uint4 v, F f) {
 // Weights as whole numbers, 2^y 2^shift with y = c (x - max).  y = n / 32 + r: 2^(n / 32) comes from a table, 2^r, |r| <= 1/64, from its series to r^4,
 // off by 2^-39.  Adding 2^52 + 2^51 over 32 rounds to parts of 32 and leaves n in the low word; adding 2^52 rounds to a whole number
 // and leaves it there.  Nine operations of 64 bits, which bound the pass; the weight of x = max is exact.  What lies 1000 powers of two and more below the maximum goes
-// through as the maximum, so that n stays small, and gets a factor next to zero.
+// through as that, so that n stays small, and gets a factor next to zero.
 constexpr u64 kWhole = 0x4330000000000000ull;          // 2^52
 // (in constant memory they are operands where they stand; as literals two moves each)
 __constant__ double kMagic = 211106232532992.0, kTwo52 = 4503599627370496.0;
 __constant__ double kSeries[4] = {6.9314718055994530e-1, 2.4022650695910071e-1, 5.5504108664821579e-2, 9.6181291076284771e-3};    // ln(2)^i / i!
 struct Weights {
     double max, c;
-    float top, far;                           // the maximum, and a distance of 1000 powers of two below it
+    float half_top, least;                    // half the maximum; the least logit that counts: 1000 powers of two below the maximum, if it is a number
     const double* table;                      // 2^(i / 32) 2^shift, i << 15 taken from the upper word: adding n << 15 to it then multiplies by 2^(n >> 5)
     // with 2^52 in front
     __device__ __forceinline__ u64 raw(float x) const {
-        const bool none = x - top < far;
-        const double d = (double)(none ? top : x) - max;
+        const bool none = x < least;
+        const double d = (double)(none ? least : x) - max;
         const double t = fma(d, c, kMagic), r = fma(d, c, kMagic - t);
         const int n = __double2loint(t);
         double p = fma(r, kSeries[3], kSeries[2]);
@@ -241,9 +241,9 @@ struct Weights {
     __device__ __forceinline__ u64 operator()(float x) const { return raw(x) - kWhole; }
 };
 
-// 2^23 and a bin, which rises as the value falls, or more
+// 2^23 and a bin, which rises as the value falls, or more.  (By half the distance to the maximum: the whole one may pass the largest number.)
 constexpr float kFirst = 8388608.f;
-__device__ __forceinline__ float bin_of(float x, float top, float per) { return fmaf(top - x, per, kFirst); }
+__device__ __forceinline__ float bin_of(float x, float half_top, float per) { return fmaf(fmaf(x, -0.5f, half_top), per, kFirst); }
 __device__ __forceinline__ int bin_index(float f) { return __float_as_int(f) - 0x4b000000; }
 
 // Adds to shared memory where `on`, without a branch.  (Volatile keeps them between the barriers; without a clobber the table's loads for the next logits may pass.)
@@ -342,7 +342,7 @@ __device__ __forceinline__ u64 mass_pass(const Share<FP32, HOLD>& l, const Weigh
             for (int e = 0; e < 4; ++e) w[e] = wt(y.x[e]);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const float f = bin_of(y.x[e], wt.top, per);
+                const float f = bin_of(y.x[e], wt.half_top, per);
                 in[e] = f < kFirst + kBins;
                 at[e] = 4 * bin_index(f);
                 old[e] = fetch_add_if(in[e], los_at + at[e], (uint32_t)w[e]);
@@ -361,13 +361,13 @@ __device__ __forceinline__ u64 mass_pass(const Share<FP32, HOLD>& l, const Weigh
 
 // Counts alone.
 template <bool FP32, int CTAS, bool HOLD>
-__device__ __forceinline__ void count_pass(const Share<FP32, HOLD>& l, float top, float per, uint32_t counts_at) {
+__device__ __forceinline__ void count_pass(const Share<FP32, HOLD>& l, float half_top, float per, uint32_t counts_at) {
 #pragma unroll 1
     for (int j = l.vec0 + l.lane; j < l.vec1; j += 32) {
         by_fours<FP32, CTAS>(l.get(j), [&](const Four& y) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const float f = bin_of(y.x[e], top, per);
+                const float f = bin_of(y.x[e], half_top, per);
                 add_if(f < kFirst + kBins, counts_at + 4 * bin_index(f), 1u);
             }
         });
@@ -467,7 +467,6 @@ __global__ void __launch_bounds__(kThreads, CTAS) token_sample_kernel(const Para
     }
     Weights wt;
     wt.c = c;
-    wt.far = -(float)fmin(1000.0 / c, 3.402823466e38);
     wt.table = s.table;
     u64 mine = 0;
     float m = -INFINITY;                      // NaN if any is
@@ -498,7 +497,8 @@ __global__ void __launch_bounds__(kThreads, CTAS) token_sample_kernel(const Para
         return;
     }
     wt.max = top;
-    wt.top = top;
+    wt.half_top = 0.5f * top;
+    wt.least = __double2float_ru(fmax((double)top - 1000.0 / c, -3.4028234663852886e38));     // (the lowest number: minus infinity lies below it)
     const u64 least = min_p > 0.f ? (u64)ceil((double)min_p * scale) : 0;
 
     // --- the last entry kept: all, unless a limit is reached.  An entry is (ordered logit, ~index): the larger comes first.
@@ -507,7 +507,7 @@ __global__ void __launch_bounds__(kThreads, CTAS) token_sample_kernel(const Para
         u64 target = ~0ull;                   // mass at which top-p is reached
         float range = (float)p.shift + 2.f;   // in powers of two below the maximum
         if (by_mass) range = fminf(range, log2f((float)a.vocab / (1.f - top_p)) + 1.f);
-        const float per = fminf((float)wt.c * ((float)(kBins - 1) / range), 3.402823466e38f);
+        const float per = fminf((float)wt.c * ((float)(2 * kBins - 2) / range), 3.402823466e38f);
         uint32_t* const counts = reinterpret_cast<uint32_t*>(s.count);
         uint32_t* const los = reinterpret_cast<uint32_t*>(s.lo);
         uint32_t* const his = reinterpret_cast<uint32_t*>(s.hi);
@@ -629,7 +629,7 @@ __global__ void __launch_bounds__(kThreads, CTAS) token_sample_kernel(const Para
             key_lo = key_hi = ordered(top);
         } else {
             // the row's mass and the first histogram in one pass
-            if (!by_mass) count_pass<FP32, CTAS>(l, top, per, counts_at);
+            if (!by_mass) count_pass<FP32, CTAS>(l, wt.half_top, per, counts_at);
             else mine = mass_pass<FP32, CTAS>(l, wt, per, by_count, counts_at, los_at, his_at);
             if (by_mass) {
                 mine = warp_sum_u64(mine);
@@ -647,7 +647,7 @@ __global__ void __launch_bounds__(kThreads, CTAS) token_sample_kernel(const Para
         // the entries of the bin, or of the keys in question: how many, and the first kList of each part put down
         int in_part = 0;
         auto collect = [&]() {
-            for_passing(l, [&](float x) { return bin_of(x, top, per) == bin1; }, [&](float x, int i, bool there) {
+            for_passing(l, [&](float x) { return bin_of(x, wt.half_top, per) == bin1; }, [&](float x, int i, bool there) {
                 const uint32_t key = ordered(x);
                 if (!there || key < key_lo || key > key_hi) return;
                 const int at = atomicAdd(&s.n_list, 1);
@@ -660,7 +660,7 @@ __global__ void __launch_bounds__(kThreads, CTAS) token_sample_kernel(const Para
         if (!ties && !none) n_in = collect();
         if (!ties && !none && n_in > (uint32_t)kList) {       // too many: on by the bits of the bin's keys
             uint32_t lo = 0xffffffffu, hi = 0;
-            for_passing(l, [&](float x) { return bin_of(x, top, per) == bin1; }, [&](float x, int, bool) {
+            for_passing(l, [&](float x) { return bin_of(x, wt.half_top, per) == bin1; }, [&](float x, int, bool) {
                 const uint32_t key = ordered(x);
                 lo = min(lo, key);
                 hi = max(hi, key);
@@ -684,7 +684,7 @@ __global__ void __launch_bounds__(kThreads, CTAS) token_sample_kernel(const Para
                 while ((key_hi - key_lo) >> down >= (uint32_t)kBins) ++down;
                 s.count[t] = s.lo[t] = s.hi[t] = make_uint2(0, 0);
                 __syncthreads();
-                for_passing(l, [&](float x) { return bin_of(x, top, per) == bin1; }, [&](float x, int, bool there) {
+                for_passing(l, [&](float x) { return bin_of(x, wt.half_top, per) == bin1; }, [&](float x, int, bool there) {
                     const uint32_t key = ordered(x);
                     if (there && key >= key_lo && key <= key_hi) into_bin((int)((key_hi - key) >> down), by_mass ? wt(x) : 0);
                 });
@@ -833,7 +833,7 @@ __global__ void __launch_bounds__(kThreads, CTAS) token_sample_kernel(const Para
     const Kept kept = {wt, least, (uint32_t)(cut >> 32), (int)~(uint32_t)cut};
     // (a float that lies below the last one kept needs no weight)
     float floor_x = cut == 0 ? -3.402823466e38f : unordered(kept.key);             // (minus infinity never passes: it also stands for what is no token)
-    if (least > 0) floor_x = fmaxf(floor_x, (float)(wt.max + ((double)log2f(min_p) - 0.01) / c) - fabsf(top) * 0x1p-20f);
+    if (least > 0) floor_x = fmaxf(floor_x, (float)(wt.max + ((double)log2f(min_p) - 0.01) / c) - fabsf(2.f * wt.half_top) * 0x1p-20f);
     mine = all_kept ? sum_pass<FP32, CTAS>(l, wt) : kept_pass(l, kept, floor_x);
     const u64 stretch = warp_sum_u64(mine);
     if (lane == 0) s.warp_sum[warp] = stretch;

@@ -68,3 +68,18 @@ def test_rows_of_large_vocabularies_do_not_depend_on_the_others(v):
     for i in range(0, n, 37):
         some = draw(x[i:i + 3], u[i:i + 3].contiguous(), **{k: w[i:i + 3].contiguous() for k, w in kw.items()})
         assert (ids[i:i + 3] == some[0]).all() and (logprobs[i:i + 3] == some[1]).all()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("v", [3, 700, 40000])
+@pytest.mark.parametrize("t", [1e35, 1e36, 5e37, 1e38, 3.4e38])
+def test_logits_further_apart_than_the_largest_number(t, v, dtype):
+    """Temperatures at which the lowest numbers weigh something beside the largest; minus infinity never does."""
+    n = 8
+    _, u, g = random_logits(n, v, F32, v)
+    x = (3.38e38 * (2 * torch.rand((n, v), generator=g, device="cuda") - 1)).to(dtype)
+    x[:, 0], x[:, -1] = torch.finfo(dtype).max, torch.finfo(dtype).min
+    x[1::2, 1] = -float("inf")
+    x[3, 2:] = -float("inf")
+    for kw in (dict(), dict(top_k=max(2, v // 3)), dict(top_p=0.6), dict(min_p=0.2), dict(top_k=max(2, v // 2), top_p=0.9, min_p=0.01)):
+        check(x, u, **arrays(n, dict(temperature=t, **kw)))
