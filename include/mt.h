@@ -320,8 +320,8 @@ mt_status mt_bucket_noalloc(const int32_t* model_ids, int32_t n, int32_t n_model
  * instances of one graph must not overlap); it is used again for other graphs when the graph and its instances are gone.
  * All scratch goes away with mt_shutdown, after which a graph with such a call must not be replayed.
  *
- * Refusals: MT_ERR_INVALID_ARG null pointer, negative size, unknown type, misaligned pointer, a scale of attention that, times
- * log2(e), is not finite; MT_ERR_UNSUPPORTED a size or stride outside what the kernels take; nothing is enqueued then.  A count of zero is
+ * Refusals: MT_ERR_INVALID_ARG null pointer, negative size, unknown type, misaligned pointer, a scale that is not
+ * finite; MT_ERR_UNSUPPORTED a size or stride outside what the kernels take; nothing is enqueued then.  A count of zero is
  * a no-op.  What only the device can see (an id, page, slot, length or offset out of range) never faults: the rows
  * concerned are NaN (or left out, where rows are written to a cache), and the sticky status of mt_get_async_status is
  * MT_ERR_BAD_MODEL_ID (ids), MT_ERR_INVALID_ARG or MT_ERR_OOM (pages), with the smallest index concerned of the first such call

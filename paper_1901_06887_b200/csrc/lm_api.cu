@@ -54,8 +54,6 @@ struct OutsideCaptures {
 };
 
 bool misaligned(const void* p, uintptr_t to = 16) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) != 0; }
-// (the kernels take powers of two of scores times scale log2(e))
-bool bad_scale(float s) { return !std::isfinite(s * 1.44269504088896341f); }
 bool bad_stride(int64_t s, int64_t least) { return s < least || (s & 7) != 0 || s >= (int64_t(1) << 36); }
 
 mt_status to_status(cudaError_t e) {
@@ -214,7 +212,7 @@ extern "C" {
 
 mt_status mt_prompt_attention(const mt_prompt_desc* d, const void* q, const void* k, const void* v, const int32_t* offsets,
                               void* out, void* stream) {
-    if (!d || d->n_tokens < 0 || d->n_seqs < 0 || d->q_heads <= 0 || d->kv_heads <= 0 || bad_scale(d->scale)) return MT_ERR_INVALID_ARG;
+    if (!d || d->n_tokens < 0 || d->n_seqs < 0 || d->q_heads <= 0 || d->kv_heads <= 0 || !std::isfinite(d->scale)) return MT_ERR_INVALID_ARG;
     if (!(d->head_dim == 64 || d->head_dim == 128) || d->q_heads % d->kv_heads || d->q_heads > 65535) return MT_ERR_UNSUPPORTED;
     if (d->n_tokens > (1 << 30)) return MT_ERR_UNSUPPORTED;
     const int64_t hd = d->head_dim;
@@ -270,7 +268,7 @@ mt_status mt_kv_attention(const mt_kv_cache* cache, const void* q, int64_t q_seq
                           float scale, void* out, void* stream) {
     mt_status st = check_cache(cache);
     if (st != MT_OK) return st;
-    if (n_seqs < 0 || q_heads <= 0 || table_width < 0 || bad_scale(scale)) return MT_ERR_INVALID_ARG;
+    if (n_seqs < 0 || q_heads <= 0 || table_width < 0 || !std::isfinite(scale)) return MT_ERR_INVALID_ARG;
     if (q_heads % cache->kv_heads || q_heads / cache->kv_heads > 16) return MT_ERR_UNSUPPORTED;
     if ((int64_t)n_seqs * cache->kv_heads >= (1 << 20) || (int64_t)table_width * cache->page_tokens > INT_MAX - 64) return MT_ERR_UNSUPPORTED;
     if (bad_stride(q_seq_stride, 0) || bad_stride(q_head_stride, 0)) return MT_ERR_UNSUPPORTED;
@@ -361,7 +359,7 @@ mt_status mt_token_logprobs(const void* logits, int32_t dtype, int64_t row_strid
 
 mt_status mt_cross_attention(const mt_cross_desc* d, const void* q, const void* k, const void* v, const int32_t* offsets,
                              const int32_t* ranges, void* out, void* stream) {
-    if (!d || d->n_tokens < 0 || d->n_states < 0 || d->n_seqs < 0 || d->q_heads <= 0 || d->kv_heads <= 0 || bad_scale(d->scale)) return MT_ERR_INVALID_ARG;
+    if (!d || d->n_tokens < 0 || d->n_states < 0 || d->n_seqs < 0 || d->q_heads <= 0 || d->kv_heads <= 0 || !std::isfinite(d->scale)) return MT_ERR_INVALID_ARG;
     if (!(d->head_dim == 64 || d->head_dim == 128) || d->q_heads % d->kv_heads || d->q_heads > 65535) return MT_ERR_UNSUPPORTED;
     if (d->n_tokens > (1 << 30) || d->n_states > (1 << 30)) return MT_ERR_UNSUPPORTED;
     const int64_t hd = d->head_dim;
