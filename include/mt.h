@@ -436,7 +436,8 @@ mt_status mt_token_logprobs(const void* logits, int32_t dtype, int64_t row_strid
  * rows outside every sequence are not written.  A sequence without states gives zeros.  A sequence whose offsets or range break this is not computed
  * (its rows are left as they were; sticky status, index of the sequence).  Scores and sums are fp32; the probabilities are rounded to bf16 before they
  * meet v.  States outside a sequence's range never show, whatever they hold.  (An infinity of v in a state that IS seen may come out as NaN.)
- * May report MT_ERR_TIMEOUT and uses scratch, see above.  Limits as mt_prompt_attention; n_tokens and n_states at most 2^30. */
+ * May report MT_ERR_TIMEOUT and uses scratch, see above.  Limits as mt_prompt_attention; n_tokens and n_states at most 2^30; a scale that is not finite when
+ * multiplied by log2(e), beyond 2.35e38, is refused too (MT_ERR_INVALID_ARG), and one nearer to zero than 6.9e-31 counts as that. */
 typedef struct {
     int32_t n_tokens, n_states, n_seqs, q_heads, kv_heads, head_dim;
     float scale;

@@ -359,7 +359,8 @@ mt_status mt_token_logprobs(const void* logits, int32_t dtype, int64_t row_strid
 
 mt_status mt_cross_attention(const mt_cross_desc* d, const void* q, const void* k, const void* v, const int32_t* offsets,
                              const int32_t* ranges, void* out, void* stream) {
-    if (!d || d->n_tokens < 0 || d->n_states < 0 || d->n_seqs < 0 || d->q_heads <= 0 || d->kv_heads <= 0 || !std::isfinite(d->scale)) return MT_ERR_INVALID_ARG;
+    if (!d || d->n_tokens < 0 || d->n_states < 0 || d->n_seqs < 0 || d->q_heads <= 0 || d->kv_heads <= 0) return MT_ERR_INVALID_ARG;
+    if (!std::isfinite(d->scale * 1.44269504088896341f)) return MT_ERR_INVALID_ARG;         // (powers of two are taken of scores times that)
     if (!(d->head_dim == 64 || d->head_dim == 128) || d->q_heads % d->kv_heads || d->q_heads > 65535) return MT_ERR_UNSUPPORTED;
     if (d->n_tokens > (1 << 30) || d->n_states > (1 << 30)) return MT_ERR_UNSUPPORTED;
     const int64_t hd = d->head_dim;
