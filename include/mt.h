@@ -201,7 +201,7 @@ mt_status mt_cache_sim_destroy(void* sim);
  * *status_out is MT_OK, MT_ERR_BAD_MODEL_ID or MT_ERR_NOT_RESIDENT (with the smallest offending arrival index of the
  * first such batch in *bad_request_index_out, else -1), MT_ERR_TIMEOUT, or, where no batch had an error, that of the first
  * call of an operator of the language-model tenants (below) that had one, MT_ERR_INVALID_ARG, MT_ERR_BAD_MODEL_ID or MT_ERR_OOM
- * (no free page) with the smallest index of that call's sequences, tokens or rows concerned.  Either out pointer may be NULL. */
+ * (no free page), with the smallest index of that call's sequences, tokens or rows concerned and what went wrong there.  Either out pointer may be NULL. */
 mt_status mt_get_async_status(void* stream, int32_t* status_out, int32_t* bad_request_index_out);
 
 const char* mt_status_string(mt_status s);

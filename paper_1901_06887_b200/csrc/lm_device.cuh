@@ -16,11 +16,11 @@ __device__ __forceinline__ float bf16_to_f(uint16_t b) { return __uint_as_float(
 __device__ __forceinline__ uint16_t f_to_bf16(float x) { return static_cast<uint16_t>(pack_bf16x2(x, 0.f)); }
 __device__ __forceinline__ float nan_f() { return __int_as_float(0x7fffffff); }
 
-// Sticky status: the first call that went wrong, and the smallest index of that call.  One number, so that code and index are always
-// those of one error (their kinds differ: row, token, sequence).
+// Sticky status: the first call that went wrong, and the smallest index of that call, whatever went wrong there.  One number, so that code and
+// index are always those of one error (their kinds differ: row, token, sequence).
 __device__ __forceinline__ void raise_status(const OpStatus& s, int code, int index) {
     atomicMin(reinterpret_cast<unsigned long long*>(s.word + ST_OP),
-              (unsigned long long)s.call << 36 | (unsigned long long)code << 32 | (uint32_t)index);
+              (unsigned long long)s.call << 36 | (unsigned long long)(uint32_t)index << 4 | (uint32_t)code);
 }
 
 __device__ __forceinline__ float warp_max(float x) {

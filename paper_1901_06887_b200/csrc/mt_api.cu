@@ -1651,8 +1651,8 @@ mt_status mt_get_async_status(void* stream, int32_t* status_out, int32_t* bad_re
     CU_OK(cudaMemcpy(w, g.d_status, sizeof w, cudaMemcpyDeviceToHost));
     int32_t code = w[ST_CODE], index = w[ST_BAD_INDEX] == INT_MAX ? -1 : w[ST_BAD_INDEX];
     if (code == MT_OK && (w[ST_OP] != -1 || w[ST_OP + 1] != -1)) {
-        code = w[ST_OP + 1] & 15;
-        index = w[ST_OP];
+        code = w[ST_OP] & 15;
+        index = (int32_t)((uint32_t)w[ST_OP] >> 4 | (uint32_t)w[ST_OP + 1] << 28);
     }
     if (status_out) *status_out = code;
     if (bad_request_index_out) *bad_request_index_out = index;
