@@ -418,7 +418,8 @@ _MOST = 0x7fffffff       # of sizes: C's int32, which ctypes would cut larger nu
 
 
 def _place(t) -> int:
-    """Where the tensors of a cache or a bank have to be: on the context's device (a cache may be put together before there is one)."""
+    """Where the tensors of a cache, a bank or a book of pages have to be: on the context's device.  (They may be put together before there is one, or
+    outlive one; each call asks again.)"""
     return t.get_device() if _device is None else _device
 
 
@@ -465,7 +466,7 @@ class KvCache:
             if not (c.dtype is T.u8 and p.dtype is T.bf16 and c.is_cuda and pages <= _MOST and heads <= _MOST and c.get_device() == p.get_device() == at and c.is_contiguous() and p.is_contiguous() and
                     tuple(c.shape) == (pages, heads, page, half) and tuple(p.shape) == (pages, heads, page, 2)):
                 _refuse("KvCache", False)
-        self.tensors = (k_codes, k_params, v_codes, v_params)
+        self.tensors, self.device = (k_codes, k_params, v_codes, v_params), at
         self.heads, self.dim = heads, 2 * half
         self.desc = KvCacheDesc(pages, page, heads, 2 * half, *[x.data_ptr() for x in self.tensors])
         self.ref = ctypes.byref(self.desc)
@@ -491,7 +492,7 @@ def mt_kv_append(cache: KvCache, k, v, slots, stream=None) -> None:
     except ValueError:
         _refuse("mt_kv_append")
     if not (k.dtype is T.bf16 and v.dtype is T.bf16 and slots.dtype is T.i64 and
-            k.get_device() == v.get_device() == slots.get_device() == _device and
+            k.get_device() == v.get_device() == slots.get_device() == cache.device == _device and
             v.shape == shape and h == cache.heads and d == cache.dim and slots.dim() == 1 and slots.numel() == n and slots.is_contiguous() and
             (n == 0 or k2 == v2 == 1) and n <= _MOST):
         _refuse("mt_kv_append")
@@ -508,7 +509,7 @@ def mt_kv_read(cache: KvCache, slots, k_out, v_out, stream=None) -> None:
     except ValueError:
         _refuse("mt_kv_read")
     if not (k_out.dtype is T.bf16 and v_out.dtype is T.bf16 and slots.dtype is T.i64 and slots.dim() == 1 and slots.numel() == n and
-            k_out.get_device() == v_out.get_device() == slots.get_device() == _device and v_out.shape == shape and h == cache.heads and d == cache.dim and
+            k_out.get_device() == v_out.get_device() == slots.get_device() == cache.device == _device and v_out.shape == shape and h == cache.heads and d == cache.dim and
             k_out.is_contiguous() and v_out.is_contiguous() and slots.is_contiguous() and n <= _MOST):
         _refuse("mt_kv_read")
     code = (_lib or lib()).mt_kv_read(cache.ref, slots.data_ptr(), n, k_out.data_ptr(), v_out.data_ptr(), _stream_handle(stream))
@@ -527,7 +528,7 @@ def mt_kv_attention(cache: KvCache, q, tables, lengths, out, scale: Optional[flo
     except ValueError:
         _refuse("mt_kv_attention")
     if not (q.dtype is T.bf16 and out.dtype is T.bf16 and tables.dtype is T.i32 and lengths.dtype is T.i32 and
-            q.get_device() == out.get_device() == tables.get_device() == lengths.get_device() == _device and d == cache.dim and out.shape == shape and rows == n and lengths.dim() == 1 and
+            q.get_device() == out.get_device() == tables.get_device() == lengths.get_device() == cache.device == _device and d == cache.dim and out.shape == shape and rows == n and lengths.dim() == 1 and
             lengths.numel() == n and out.is_contiguous() and tables.is_contiguous() and lengths.is_contiguous() and (n == 0 or q2 == 1) and
             n <= _MOST and hq <= _MOST and width <= _MOST):
         _refuse("mt_kv_attention")
@@ -582,7 +583,7 @@ class QuantBank:
         with torch.cuda.stream(stream):
             self.packed = torch.empty((t, mt_quant_packed_bytes(k, n, group)), dtype=torch.uint8, device=codes.device)
         mt_quant_pack(codes, scales, self.packed, stream)
-        self.bias, self.in_features, self.out_features = bias, k, n
+        self.bias, self.in_features, self.out_features, self.device = bias, k, n, codes.get_device()
         self.desc = QuantBankDesc(t, k, n, group, self.packed.data_ptr(), _ptr(bias))
         self.ref = ctypes.byref(self.desc)
 
@@ -599,7 +600,7 @@ def mt_quant_linear(x, ids, bank: QuantBank, y, stream=None) -> None:
         _refuse("mt_quant_linear")
     wide = y.dtype is T.f32
     if not (x.dtype is T.bf16 and ids.dtype is T.i32 and (wide or y.dtype is T.bf16) and
-            x.get_device() == ids.get_device() == y.get_device() == _device and
+            x.get_device() == ids.get_device() == y.get_device() == bank.device == _device and
             k == bank.in_features and rows == n and out == bank.out_features and ids.dim() == 1 and ids.numel() == n and
             ids.is_contiguous() and (n == 0 or (x1 == 1 and (y1 == 1 or out == 1))) and n <= _MOST):
         _refuse("mt_quant_linear")
@@ -711,7 +712,7 @@ class KvPages:
                 lengths.dim() == 1 and lengths.numel() == tables.shape[0] and refs.is_contiguous() and tables.is_contiguous() and
                 lengths.is_contiguous() and max(refs.numel(), *tables.shape) <= _MOST and 0 <= page_tokens <= _MOST):
             _refuse("KvPages", False)
-        self.refs, self.tables, self.lengths, self.page_tokens = refs, tables, lengths, page_tokens
+        self.refs, self.tables, self.lengths, self.page_tokens, self.device = refs, tables, lengths, page_tokens, at
         self.desc = KvPagesDesc(refs.numel(), page_tokens, *tables.shape, refs.data_ptr(), tables.data_ptr(), lengths.data_ptr())
         self.ref = ctypes.byref(self.desc)
 
@@ -734,7 +735,7 @@ def _is_copies(t, n: int) -> bool:
 def mt_kv_reserve(pages: KvPages, rows, counts, slots, stream=None) -> None:
     """Room for counts[i] more tokens in row rows[i] (int32); slots int64 (at least sum(counts)): where they go, for mt_kv_append."""
     T, n, m = _types(), rows.numel(), slots.numel()
-    if not (_is_ints(rows, n) and _is_ints(counts, n) and slots.dtype is T.i64 and slots.get_device() == _device and slots.shape == (m,) and slots.is_contiguous()):
+    if not (pages.device == _device and _is_ints(rows, n) and _is_ints(counts, n) and slots.dtype is T.i64 and slots.get_device() == _device and slots.shape == (m,) and slots.is_contiguous()):
         _refuse("mt_kv_reserve")
     code = (_lib or lib()).mt_kv_reserve(pages.ref, rows.data_ptr(), counts.data_ptr(), n, slots.data_ptr(), m, _stream_handle(stream))
     if code:
@@ -745,7 +746,7 @@ def mt_kv_fork(pages: KvPages, parents, children, copies, stream=None) -> None:
     """Row children[i] becomes what row parents[i] was (int32); copies int32 [n, 3]: what mt_kv_copy has to copy."""
     _types()
     n = parents.numel()
-    if not (_is_ints(parents, n) and _is_ints(children, n) and _is_copies(copies, n)):
+    if not (pages.device == _device and _is_ints(parents, n) and _is_ints(children, n) and _is_copies(copies, n)):
         _refuse("mt_kv_fork")
     code = (_lib or lib()).mt_kv_fork(pages.ref, parents.data_ptr(), children.data_ptr(), n, copies.data_ptr(), _stream_handle(stream))
     if code:
@@ -756,7 +757,7 @@ def mt_kv_release(pages: KvPages, rows, stream=None) -> None:
     """Gives the pages of rows (int32) back; their lengths become 0."""
     _types()
     n = rows.numel()
-    if not _is_ints(rows, n):
+    if not (pages.device == _device and _is_ints(rows, n)):
         _refuse("mt_kv_release")
     code = (_lib or lib()).mt_kv_release(pages.ref, rows.data_ptr(), n, _stream_handle(stream))
     if code:
@@ -767,7 +768,7 @@ def mt_kv_compact(pages: KvPages, copies, stream=None) -> None:
     """Moves used pages to the front, at most copies.shape[0] of them; copies int32 [n, 3]: what mt_kv_copy has to copy."""
     _types()
     n = copies.numel() // 3
-    if not _is_copies(copies, n):
+    if not (pages.device == _device and _is_copies(copies, n)):
         _refuse("mt_kv_compact")
     code = (_lib or lib()).mt_kv_compact(pages.ref, copies.data_ptr(), n, _stream_handle(stream))
     if code:
@@ -781,13 +782,14 @@ class KvCopier:
         self.caches = list(caches)
         self.array = (ctypes.POINTER(KvCacheDesc) * len(self.caches))(*[ctypes.pointer(c.desc) for c in self.caches])
         self.n = len(self.caches)
+        self.devices = {c.device for c in self.caches}
 
 
 def mt_kv_copy(copier: KvCopier, copies, stream=None) -> None:
     """Copies pages in every cache: copies int32 [n, 3], page from, page to, tokens; -1, -1 is left out."""
     _types()
     n = copies.numel() // 3
-    if not _is_copies(copies, n):
+    if not (_is_copies(copies, n) and copier.devices <= {_device}):
         _refuse("mt_kv_copy")
     code = (_lib or lib()).mt_kv_copy(copier.array, copier.n, copies.data_ptr(), n, _stream_handle(stream))
     if code:
