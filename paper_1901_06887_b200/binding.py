@@ -685,7 +685,7 @@ def mt_rotate(x, positions, frequencies, out, sections: Optional[Sequence[int]] 
     except ValueError:
         _refuse("mt_rotate")
     half = frequencies.numel()
-    axes = 1 if positions.dim() == 1 else positions.shape[-1]
+    axes = positions.shape[1] if positions.dim() == 2 else 1
     cut = (half,) if sections is None else tuple(sections)
     if not ((wide or x.dtype is T.bf16) and out.dtype is x.dtype and positions.dtype is T.i32 and frequencies.dtype is T.f32 and
             x.get_device() == out.get_device() == positions.get_device() == frequencies.get_device() == _device and out.shape == shape and
