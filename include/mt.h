@@ -472,7 +472,7 @@ mt_status mt_rotate(const mt_rotate_desc* desc_host, const void* x, const int32_
  * the cache that would be shared, copied or appended to: that place of the call is left out (sticky status MT_ERR_INVALID_ARG, its index).  A page that is given back although
  * it lies outside or nobody holds it is passed over, with the same status.  A place for which no free page is left is left out
  * too (MT_ERR_OOM); places behind it that need pages then are as well.  They use scratch, see above.
- * Limits: page_tokens 16, 32, 64, 128 or 256; table_width * page_tokens below 2^31 - 64. */
+ * Limits: page_tokens 16, 32, 64, 128 or 256; table_width * page_tokens below 2^31 - 64; n_rows, and the places (n) of a call, at most 2^30. */
 typedef struct {
     int32_t n_pages, page_tokens, n_rows, table_width;
     int32_t *refs, *tables, *lengths;
@@ -500,7 +500,7 @@ mt_status mt_kv_compact(const mt_kv_pages* pages_host, int32_t* copies, int32_t 
 
 /* Copies the first tokens' rows of pages, codes and parameters of keys and values, in each of n_caches caches with the same n_pages and page_tokens: copies int32
  * [n][3], page from, page to, tokens; -1, -1 is left out.  Anything else outside the cache, or a number of tokens outside [0, page_tokens], is left out and sets the
- * sticky status.  No page may be copied to twice, or be copied from and to. */
+ * sticky status.  No page may be copied to twice, or be copied from and to.  n is at most 2^30. */
 mt_status mt_kv_copy(const mt_kv_cache* const* caches_host, int32_t n_caches, const int32_t* copies, int32_t n, void* stream);
 
 /* Draws a token from each of n rows of `vocab` logits (bf16 or fp32 by dtype, row_stride elements apart, any alignment of whole elements).

@@ -71,10 +71,11 @@ mt_status check_cache(const mt_kv_cache* c) {
     return MT_OK;
 }
 
-mt_status check_pages(const mt_kv_pages* p) {
-    if (!p || p->n_pages < 0 || p->n_rows < 0 || p->table_width < 0) return MT_ERR_INVALID_ARG;
+constexpr int kMostPlaces = 1 << 30;          // of a call, and rows: the kernels step past the last one by as many as work at once
+mt_status check_pages(const mt_kv_pages* p, int32_t n) {
+    if (!p || p->n_pages < 0 || p->n_rows < 0 || p->table_width < 0 || n < 0) return MT_ERR_INVALID_ARG;
     if (p->page_tokens < 16 || p->page_tokens > 256 || (p->page_tokens & (p->page_tokens - 1))) return MT_ERR_UNSUPPORTED;
-    if (p->n_pages > INT_MAX - 256 || (int64_t)p->table_width * p->page_tokens > INT_MAX - 64) return MT_ERR_UNSUPPORTED;
+    if (n > kMostPlaces || p->n_rows > kMostPlaces || p->n_pages > INT_MAX - 256 || (int64_t)p->table_width * p->page_tokens > INT_MAX - 64) return MT_ERR_UNSUPPORTED;
     if ((p->n_pages > 0 && !p->refs) || (p->n_rows > 0 && (!p->lengths || (p->table_width > 0 && !p->tables)))) return MT_ERR_INVALID_ARG;
     if (misaligned(p->refs) || misaligned(p->tables, 4) || misaligned(p->lengths, 4)) return MT_ERR_INVALID_ARG;
     return MT_OK;
@@ -411,9 +412,9 @@ mt_status mt_rotate(const mt_rotate_desc* d, const void* x, const int32_t* posit
 }
 
 mt_status mt_kv_reserve(const mt_kv_pages* pages, const int32_t* rows, const int32_t* counts, int32_t n, int64_t* slots, int64_t n_slots, void* stream) {
-    mt_status st = check_pages(pages);
+    mt_status st = check_pages(pages, n);
     if (st != MT_OK) return st;
-    if (n < 0 || n_slots < 0) return MT_ERR_INVALID_ARG;
+    if (n_slots < 0) return MT_ERR_INVALID_ARG;
     std::unique_lock<std::mutex> lk;
     OpContext c;
     st = op_begin(&lk, &c);
@@ -423,9 +424,8 @@ mt_status mt_kv_reserve(const mt_kv_pages* pages, const int32_t* rows, const int
 }
 
 mt_status mt_kv_fork(const mt_kv_pages* pages, const int32_t* parents, const int32_t* children, int32_t n, int32_t* copies, void* stream) {
-    mt_status st = check_pages(pages);
+    mt_status st = check_pages(pages, n);
     if (st != MT_OK) return st;
-    if (n < 0) return MT_ERR_INVALID_ARG;
     std::unique_lock<std::mutex> lk;
     OpContext c;
     st = op_begin(&lk, &c);
@@ -435,9 +435,8 @@ mt_status mt_kv_fork(const mt_kv_pages* pages, const int32_t* parents, const int
 }
 
 mt_status mt_kv_release(const mt_kv_pages* pages, const int32_t* rows, int32_t n, void* stream) {
-    mt_status st = check_pages(pages);
+    mt_status st = check_pages(pages, n);
     if (st != MT_OK) return st;
-    if (n < 0) return MT_ERR_INVALID_ARG;
     std::unique_lock<std::mutex> lk;
     OpContext c;
     st = op_begin(&lk, &c);
@@ -447,9 +446,8 @@ mt_status mt_kv_release(const mt_kv_pages* pages, const int32_t* rows, int32_t n
 }
 
 mt_status mt_kv_compact(const mt_kv_pages* pages, int32_t* copies, int32_t n, void* stream) {
-    mt_status st = check_pages(pages);
+    mt_status st = check_pages(pages, n);
     if (st != MT_OK) return st;
-    if (n < 0) return MT_ERR_INVALID_ARG;
     std::unique_lock<std::mutex> lk;
     OpContext c;
     st = op_begin(&lk, &c);
@@ -460,6 +458,7 @@ mt_status mt_kv_compact(const mt_kv_pages* pages, int32_t* copies, int32_t n, vo
 
 mt_status mt_kv_copy(const mt_kv_cache* const* caches, int32_t n_caches, const int32_t* copies, int32_t n, void* stream) {
     if (n_caches < 0 || n < 0 || (n_caches > 0 && !caches)) return MT_ERR_INVALID_ARG;
+    if (n > kMostPlaces) return MT_ERR_UNSUPPORTED;
     for (int i = 0; i < n_caches; ++i) {
         const mt_status st = check_cache(caches[i]);
         if (st != MT_OK) return st;
