@@ -722,7 +722,6 @@ __global__ void __launch_bounds__(kThreads, CTAS) token_sample_kernel(const Para
             if (t == 0) s.found = -1;
             __syncthreads();
             const uint32_t in_warp = lane < kWarps ? s.warp_a[lane] : 0;
-            if (t == 0) s.ties = 0;
             const uint32_t in_part = __reduce_add_sync(0xffffffffu, in_warp);
             if (t == 0) s.ties = in_part;
             team_sync();
