@@ -449,7 +449,7 @@ __global__ void __launch_bounds__(kThreads, CTAS) token_sample_kernel(const Para
 
     // --- what the row asks for
     float temperature = a.temperature ? a.temperature[row_i] : 1.f, top_p = a.top_p ? a.top_p[row_i] : 1.f, min_p = a.min_p ? a.min_p[row_i] : 0.f;
-    const float u = a.uniform[row_i];
+    const float u = a.uniform[row_i] + 0.f;   // (minus zero is zero)
     int top_k = a.top_k ? a.top_k[row_i] : 0;
     const bool refused = !(temperature >= 0.f && temperature < INFINITY) || top_p != top_p || min_p != min_p || !(u >= 0.f && u < 1.f);
     if (temperature == 0.f || min_p > 1.f) { top_k = 1; min_p = 0.f; }

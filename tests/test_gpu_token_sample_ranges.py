@@ -83,3 +83,21 @@ def test_logits_further_apart_than_the_largest_number(t, v, dtype):
     x[3, 2:] = -float("inf")
     for kw in (dict(), dict(top_k=max(2, v // 3)), dict(top_p=0.6), dict(min_p=0.2), dict(top_k=max(2, v // 2), top_p=0.9, min_p=0.01)):
         check(x, u, **arrays(n, dict(temperature=t, **kw)))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("v", [7, 3000, 90000])
+def test_minus_zero(v, dtype):
+    """The same as zero, in every argument that may be zero."""
+    init()
+    x, u, _ = random_logits(6, v, dtype, 13)
+    u.zero_()
+    for kw in (dict(), dict(top_p=0.8), dict(top_k=5, min_p=0.01)):
+        plus, minus = draw(x, u, **arrays(6, kw)), draw(x, -u, **arrays(6, kw))
+        assert (plus[0] == minus[0]).all() and (plus[1] == minus[1]).all() and (plus[0] >= 0).all()
+        check(x, -u, **arrays(6, kw))
+    u += 0.4
+    for name in ("temperature", "top_p", "min_p"):
+        plus, minus = draw(x, u, **arrays(6, {name: 0.0})), draw(x, u, **arrays(6, {name: -0.0}))
+        assert (plus[0] == minus[0]).all() and (plus[1] == minus[1]).all()
+    assert mt.mt_get_async_status() == (0, -1)
