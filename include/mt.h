@@ -510,8 +510,8 @@ mt_status mt_kv_copy(const mt_kv_cache* const* caches_host, int32_t n_caches, co
  *   min_p > 0    w_i >= min_p
  * and the first in any case.  ids[i] is the first token, in the order of the vocabulary, at which the sum of kept w exceeds uniform[i] (in [0, 1)) times all of it;
  * logprobs[i] its log probability among the kept (may be NULL).  temperature, top_k, top_p, min_p and uniform are arrays of n; NULL: 1, none, none, none.  Temperature 0, or a
- * min_p above 1, takes the first; one below 2^-126 counts as that.  Weights are 64-bit whole numbers, the largest 2^46 (fewer in rows of more than 2^16 logits), so draws do not depend on the
- * order of summing; what is below one of those units is never drawn.  A row without a distribution (nothing but minus infinity, a NaN or plus infinity) gives id -1 and NaN;
+ * min_p above 1, takes the first; one below 2^-126 counts as that.  Weights are 64-bit whole numbers, the largest 2^46, or, for more than 2^16 logits, the power of two with which vocab
+ * such weights add up to 2^62 at most (2^42 for 2^20), so draws do not depend on the order of summing; what is below half of one of those units is never drawn.  A row without a distribution (nothing but minus infinity, a NaN or plus infinity) gives id -1 and NaN;
  * so does one with a negative, infinite or NaN temperature, a NaN limit or a uniform number outside [0, 1), with the sticky status MT_ERR_INVALID_ARG.
  * Limits: n below 2^29; vocab below 2^30. */
 mt_status mt_token_sample(const void* logits, int32_t dtype, int64_t row_stride, int32_t n, int32_t vocab, const float* temperature,

@@ -11,13 +11,16 @@
 //
 // Order of work.  A unit is a block of states for a tile pair; the units of all (sequence, head pack, tile pair) are in one line, which is cut
 // into equal shares, one a CTA.  A tile pair that a border cuts is done in pieces: each leaves its sums (o without the division, m, l) in scratch, and a
-// second launch joins them.  So one token over a long recording takes all SMs.  Where there are tile pairs enough to be even without, they are dealt whole,
-// those with most states first, back and forth over the CTAs, and nothing is joined.
+// second launch joins them.  So one token over a long recording takes all SMs.  Many tile pairs are dealt whole, those with most states first, back and
+// forth over the CTAs, and nothing is joined: from one an SM on where that leaves no CTA far above the mean, from eight on in any case.  (Nothing asks
+// there whether it is even: one source far longer than the others is then one CTA's.  1000 sources of 128 states take 218 us, one of 24 000 by itself 49, all
+// together 518; 64 tokens each, 16 / 4 heads of 128.)
 //
-// Cost.  One token of 64 answers to 16 sources of 577 to 4000 states, 32 / 8 heads of 128: 38 us for 116 MB, of which some 18 are fixed (set-up, the first
-// loads, the join); four times the sources take 102.  16 prompts of 1 to 700 tokens over 49 to 2305 states: 101 us, tensor pipe and exponentials half
-// busy each, as in the prompt kernel.  11 001 queries over 4500 to 6000 states, 16 heads of 64: 323 us, exponentials 75 % of the time at the 1.6 GHz that the
-// power cap leaves.  (A part of them by a polynomial on the multiply-add units: 330 to 373.)
+// Cost.  One token of 64 answers to 16 sources of 577 to 4000 states, 32 / 8 heads of 128: 37 us for 116 MB, of which some 18 are fixed (set-up, the first
+// loads, the join); four times the sources take 102.  Groups that are no power of two stream their states once for each share of the largest one that divides
+// them: 24 / 8 heads 82 us, 40 / 8 127.  16 prompts of 1 to 700 tokens over 49 to 2305 states: 110 us, tensor
+// pipe and exponentials half busy each, as in the prompt kernel.  11 001 queries over 4500 to 6000 states, 16 heads of 64: 330 to 338 us, exponentials 75 % of
+// the time at the 1.6 GHz that the power cap leaves.  (A part of them by a polynomial on the multiply-add units: 330 to 373 where all of them by the exponential unit took 323.)
 //
 // Roles (12 warps): warps 0-3 and 4-7 are the softmax of the two tiles, one row per thread; warp 8 copies (TMA), warp 9 issues the matrix
 // instructions, warps 10 and 11 zero the values behind the sequence's last state: their p is zero, but zero times an infinity is NaN.

@@ -9,8 +9,9 @@
 // memory where one CTA is the team and it fits (SMALL), else in scratch: every trip to device memory between two steps costs half a microsecond.  Free pages are
 // found by a scan of the references: every warp counts its stretch, the counts are added up, every warp lists its stretch.
 //
-// Cost.  Bookkeeping is latency: 64 rows of some 30 pages are forked in 10.4, given a token each in 7.5 and released in 5.8 us (8 rows of a small model: 6.6, 6.2,
-// 3.1).  Copies are bytes: 254 MB in and out in 41 us, 6.2 TB/s.
+// Cost.  Bookkeeping is latency: one call behind the other, 64 rows of some 30 pages are forked and released in 13.1 and given a token each in 5.4 us (8 rows of a
+// small model: 7.7 and 5.1).  Copies are bytes: 254 MB in and out in 41 us, 6.2 TB/s; many pages of 1, 2, 4 or 8 heads of 128 at 6.5 to 6.7 (a warp takes a head:
+// pages of fewer than four heads leave warps idle, which other CTAs make up for).
 #include "lm_device.cuh"
 #include "lm_host.h"
 

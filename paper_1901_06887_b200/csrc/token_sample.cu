@@ -6,7 +6,7 @@
 // A border between two tokens must not depend on the order of summing, so weights are whole numbers, w_i 2^s rounded, s = 46 or less where a row of
 // ones would pass 2^62: sums of them are exact in any order.  (A token below half a unit, 2^-s, of the likeliest has no mass and is never drawn; of a
 // row of V at most V / 2 units are lost or won by rounding: 2^-31 of it for 2^16 logits, 2^-27 for 2^18, 2^-23 for 2^20.)  The exponential is taken in 64 bits:
-// at fp32's 2^-23 one draw in some hundreds would fall on the other side of a border.
+// with fp32 arguments one draw in ten thousand of a row of 128 000 would fall on the other side of a border, and sums of fp32 would add to that.
 //
 // The last entry kept.  A histogram, count and mass, of the distance to the maximum over the range where the cut can lie: the tokens whose weight is
 // below (1 - p) / V of the largest weigh less than 1 - p together, and the row at least 1.  The bin where a limit is reached is put on a list and ranked by
@@ -16,10 +16,11 @@
 // Split.  A row is cut into parts, one CTA each, that form a cluster; a part into stretches, one a warp.  A part that fits stays in shared memory, so that
 // a row is read once; other rows come from L2 again.
 //
-// Cost.  Many rows: the pass of 64-bit exponentials, 30 cycles for a warp's logits on a scheduler, and the first pass at the memory's rate, one behind the
-// other (512 rows of 128 000 in fp32, 174 us, 4.3 times their bytes).  A mixed batch of 64 rows of 128 000 in bf16 takes 50 us: its rows with a limit go three
-// times over their part, the histogram's additions to shared memory take as long as the exponentials, and six barriers of the cluster lie between.  One row of
-// 32 000: 13.8 us, these barriers and the dependent steps between them.
+// Cost.  Many rows: the first pass and the pass of 64-bit exponentials, one behind the other: 512 rows of 128 000 in fp32, whose bytes are 40 us, take 170, of which
+// 55 without the weights.  (The other 115 are some 55 cycles of a scheduler for a warp's logits, the last of 3.5 waves of clusters counted whole; nine 64-bit
+// operations and a conversion are 30 by themselves.)  A mixed batch of 64 rows of 128 000 in bf16 takes 48 us, all of them without a limit 24, with top-k 27, with
+// top-p 56: rows with a limit go three times over their part, the histogram's additions to shared memory take as long as the exponentials, and five barriers
+// of the cluster lie between.  One row of 32 000: 13.6 us, these barriers and the dependent steps between them; 6.2 without a limit.
 #include "lm_device.cuh"
 #include "lm_host.h"
 
